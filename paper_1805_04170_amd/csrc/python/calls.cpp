@@ -1,4 +1,4 @@
-// The layer, flatten and retile calls as a Python extension module: arguments go from Python objects straight into the call's
+// The layer, flatten, retile and token calls as a Python extension module: arguments go from Python objects straight into the call's
 // C arguments.  A training step of a small chain is six calls with 27 shard lists between them; through ctypes they took
 // 44 us of host time, as long as the GPU needs for half the kernels, and so 12 us.
 //
@@ -10,6 +10,7 @@
 #include <Python.h>
 #include <cstring>
 #include "tensor_tiling.h"
+#include "tensor_tiling_tokens.h"
 
 namespace {
 
@@ -62,6 +63,20 @@ struct Args {
         const int v = PyObject_IsTrue(o);
         if (v < 0) fail();
         return v > 0;
+    }
+    float real()
+    {
+        PyObject *o = next();
+        if (!o) return 0.0f;
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) fail();
+        return (float)v;
+    }
+    // a device buffer: an object with a data_ptr(), an address, or None (NULL)
+    template <typename T = void> T *buffer()
+    {
+        PyObject *o = next();
+        return !o || o == Py_None ? nullptr : reinterpret_cast<T *>((uintptr_t)pointer_of(o));
     }
     // bytes of a ctypes object, valid until the call is over
     const void *bytes_of(PyObject *o, Py_ssize_t least)
@@ -296,6 +311,125 @@ PyObject *retile(PyObject *, PyObject *const *args, Py_ssize_t n)
     return finish(g, [&] { return fn(dst, B, in(src), A, k, rows, cols, eb, stream); });
 }
 
+// embed_forward(address, tokens, vocab, width, k, dtype, tW, tX, id_dtype, ids, scale, W, X, stream): tt_embed_forward
+PyObject *embed_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 14);
+    auto fn = g.address<decltype(&tt_embed_forward)>();
+    const int64_t tokens = g.i64(), vocab = g.i64(), width = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tW = g.tiling(), tX = g.tiling();
+    const int idt = g.i32();
+    const void *ids = g.buffer();
+    const float scale = g.real();
+    void *w[kMaxShards], *x[kMaxShards];
+    void **W = g.shards(w), **X = g.shards(x);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(tokens, vocab, width, k, dt, tW, tX, idt, ids, scale, in(W), X, stream); });
+}
+
+// embed_backward(address, tokens, vocab, width, k, dtype, tdX, tdW, id_dtype, ids, scale, dX, dW, workspace, stream): tt_embed_backward
+PyObject *embed_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 15);
+    auto fn = g.address<decltype(&tt_embed_backward)>();
+    const int64_t tokens = g.i64(), vocab = g.i64(), width = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tW = g.tiling();
+    const int idt = g.i32();
+    const void *ids = g.buffer();
+    const float scale = g.real();
+    void *dx[kMaxShards], *dw[kMaxShards];
+    void **dX = g.shards(dx), **dW = g.shards(dw);
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    return finish(g, [&] { return fn(tokens, vocab, width, k, dt, tX, tW, idt, ids, scale, in(dX), dW, ws, bytes, stream); });
+}
+
+// policy_loss(address, policy, tokens, vocab, k, dtype, tX, tdX, X, id_dtype, actions, old_logp, ref_logp, advantage, weight, loss,
+// logp, dX, workspace, stream): tt_policy_loss
+PyObject *policy_loss(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 20);
+    auto fn = g.address<decltype(&tt_policy_loss)>();
+    PyObject *o = g.next();
+    const tt_policy *policy = o ? static_cast<const tt_policy *>(g.bytes_of(o, sizeof(tt_policy))) : nullptr;
+    const int64_t tokens = g.i64(), vocab = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tdX = g.tiling();
+    void *x[kMaxShards], *dx[kMaxShards];
+    void **X = g.shards(x);
+    const int idt = g.i32();
+    const void *actions = g.buffer();
+    const float *old_logp = g.buffer<float>(), *ref_logp = g.buffer<float>(), *advantage = g.buffer<float>(), *weight = g.buffer<float>();
+    float *loss = g.buffer<float>(), *logp = g.buffer<float>();
+    void **dX = g.shards(dx);
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    return finish(g, [&] {
+        return fn(policy, tokens, vocab, k, dt, tX, tdX, in(X), idt, actions, old_logp, ref_logp, advantage, weight, loss, logp, dX, ws, bytes, stream);
+    });
+}
+
+// token_logp(address, tokens, vocab, k, dtype, tX, scale, X, id_dtype, ids, logp, workspace, stream): tt_token_logp
+PyObject *token_logp(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 13);
+    auto fn = g.address<decltype(&tt_token_logp)>();
+    const int64_t tokens = g.i64(), vocab = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling();
+    const float scale = g.real();
+    void *x[kMaxShards];
+    void **X = g.shards(x);
+    const int idt = g.i32();
+    const void *ids = g.buffer();
+    float *logp = g.buffer<float>();
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    return finish(g, [&] { return fn(tokens, vocab, k, dt, tX, scale, in(X), idt, ids, logp, ws, bytes, stream); });
+}
+
+// pack8(address, rows, cols, k, dtype, t, a, b, c, stream): tt_pack8 (X, Q, S) and tt_unpack8 (Q, S, X), whose shard lists are
+// arrays of pointers alike
+PyObject *pack8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 10);
+    typedef tt_status (*Fn)(int64_t, int64_t, int, int, tt_tiling, void *const *, void *const *, void *const *, void *);
+    auto fn = g.address<Fn>();
+    const int64_t rows = g.i64(), cols = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling t = g.tiling();
+    void *a[kMaxShards], *b[kMaxShards], *c[kMaxShards];
+    void **A = g.shards(a), **B = g.shards(b), **C = g.shards(c);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(rows, cols, k, dt, t, A, B, C, stream); });
+}
+
+// backward_packed(address, layer, batch, k, dtype, tX, tW, tY, tdY, tdX, forms_dgrad, forms_wgrad, XQ, XS, W, YQ, YS, dY, dX, dW,
+// workspace, stream): tt_fc_backward_packed
+PyObject *backward_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 22);
+    auto fn = g.address<decltype(&tt_fc_backward_packed)>();
+    const tt_layer *lay = g.layer();
+    const int64_t batch = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tW = g.tiling(), tY = g.tiling(), tdY = g.tiling(), tdX = g.tiling();
+    uint8_t fdb[TT_MAX_K], fwb[TT_MAX_K];
+    void *xq[kMaxShards], *xs[kMaxShards], *w[kMaxShards], *yq[kMaxShards], *ys[kMaxShards], *dy[kMaxShards], *dx[kMaxShards], *dw[kMaxShards];
+    const uint8_t *fd = g.forms(fdb), *fw = g.forms(fwb);
+    void **XQ = g.shards(xq), **XS = g.shards(xs), **W = g.shards(w), **YQ = g.shards(yq), **YS = g.shards(ys), **dY = g.shards(dy);
+    void **dX = g.shards(dx), **dW = g.shards(dw);
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    const auto i8 = [](void **p) { return reinterpret_cast<const int8_t *const *>(p); };
+    const auto u8 = [](void **p) { return reinterpret_cast<const uint8_t *const *>(p); };
+    return finish(g, [&] {
+        return fn(lay, batch, k, dt, tX, tW, tY, tdY, tdX, fd, fw, i8(XQ), u8(XS), in(W), i8(YQ), u8(YS), in(dY), dX, dW, ws, bytes, stream);
+    });
+}
+
 // converters(tiling, forms, dtype): what the binding uses for arguments that are no plain strings
 PyObject *converters(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -317,7 +451,9 @@ template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)> PyMethodDef
 }
 
 PyMethodDef g_methods[] = {method_def<forward>("forward"), method_def<forward_static>("forward_static"), method_def<backward>("backward"),
-                           method_def<flatten>("flatten"), method_def<retile>("retile"), method_def<converters>("converters"),
+                           method_def<flatten>("flatten"), method_def<retile>("retile"), method_def<embed_forward>("embed_forward"), method_def<embed_backward>("embed_backward"),
+                           method_def<policy_loss>("policy_loss"), method_def<token_logp>("token_logp"), method_def<pack8>("pack8"),
+                           method_def<backward_packed>("backward_packed"), method_def<converters>("converters"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,106 @@
+// Wave-wide operations (64 lanes) of the token operators' kernels, and what those kernels share: reductions over a wave or a
+// workgroup, 16-byte vectors at any element's alignment, bf16 values.  The host emulation build takes its stand-ins of the
+// wave-wide operations from emu_wave.h.
+#pragma once
+#include <cstdint>
+#include "tt_device.h"
+#include "tt_bf16.h"
+#ifdef TT_HOST_EMULATION
+#include "emu_wave.h"
+#else
+namespace tt {
+namespace wave {
+
+__device__ __forceinline__ uint32_t lane() { return threadIdx.x & 63u; }
+__device__ __forceinline__ float shfl_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
+__device__ __forceinline__ uint32_t shfl_xor(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask, 64); }
+__device__ __forceinline__ uint32_t shfl_up(uint32_t v, int by) { return (uint32_t)__shfl_up((int)v, by, 64); }
+__device__ __forceinline__ uint32_t read_lane(uint32_t v, int from) { return (uint32_t)__builtin_amdgcn_readlane((int)v, from); }
+__device__ __forceinline__ uint64_t ballot(bool p) { return __ballot(p); }
+// integer counter in LDS (the order of additions does not matter)
+__device__ __forceinline__ void lds_add(uint32_t *p, uint32_t v) { atomicAdd(p, v); }
+// LDS accesses of the wave's lanes before this are done, and those after it not begun
+__device__ __forceinline__ void fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+// 2^x (1 ulp; what lies below 2^-126 is 0)
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+} // namespace wave
+} // namespace tt
+#endif
+
+namespace tt {
+
+// a value that all lanes of a wave hold, in a scalar register
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v = fmaxf(v, wave::shfl_xor(v, m));
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v += wave::shfl_xor(v, m);
+    return v;
+}
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v)
+{
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v += wave::shfl_xor(v, m);
+    return v;
+}
+
+// ---- 16-byte vectors that begin at any element: rows of odd length begin anywhere, and the memory system takes a 16-byte
+// access at any address (the compiler splits it where a target does not)
+template <int ALIGN> struct Vec16;
+template <> struct Vec16<2> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Vec16<4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> __device__ __forceinline__ u32x4 load16(const T *p)
+{
+    const typename Vec16<sizeof(T)>::type v = *reinterpret_cast<const typename Vec16<sizeof(T)>::type *>(p);
+    return u32x4{v.x, v.y, v.z, v.w};
+}
+template <typename T> __device__ __forceinline__ void store16(T *p, u32x4 v)
+{
+    *reinterpret_cast<typename Vec16<sizeof(T)>::type *>(p) = v;
+}
+
+// ---- element types: bf16 travels as its 16 bits
+__device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+__device__ __forceinline__ float to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ float to_float(float v) { return v; }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ uint16_t from_float<uint16_t>(float v) { return (uint16_t)f32_to_bf16_bits(v); }
+
+// a 16-byte vector as 4 or 8 floats, and back (round to nearest even)
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
+__device__ __forceinline__ void unpack16(u32x4 v, float (&f)[8], uint16_t)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(v[i]); f[2 * i + 1] = bf16_hi(v[i]); }
+}
+__device__ __forceinline__ void unpack16(u32x4 v, float (&f)[4], float)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+}
+__device__ __forceinline__ u32x4 pack16(const float (&f)[8], uint16_t)
+{
+    return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+}
+__device__ __forceinline__ u32x4 pack16(const float (&f)[4], float)
+{
+    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+}
+
+} // namespace tt

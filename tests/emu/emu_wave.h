@@ -1,0 +1,43 @@
+// Host stand-ins for the wave-wide operations of csrc/tt_wave.h, in lock step (emu_lockstep.h): every lane that has not ended
+// takes part, as on the device where all 64 are active.
+#pragma once
+#ifndef TT_EMU_LOCKSTEP
+#error "the token operators' kernels read what other lanes wrote: lock-step emulation only"
+#endif
+
+namespace tt {
+namespace wave {
+
+inline uint32_t lane() { return threadIdx.x & 63u; }
+
+// each lane gives a word and gets the word of lane from(lane)
+template <class F> inline uint32_t exchange(int kind, uint32_t v, F &&from)
+{
+    emu::WaveState &w = emu::my_wave();
+    const int l = emu::lane();
+    std::memcpy(&w.fa[l], &v, 4);
+    emu::wave_collective(kind, [](emu::WaveState &s) { std::memcpy(s.fb, s.fa, sizeof(s.fa)); });
+    uint32_t r;
+    std::memcpy(&r, &w.fb[from(l)], 4);
+    return r;
+}
+inline uint32_t shfl_xor(uint32_t v, int mask) { return exchange(10, v, [&](int l) { return l ^ mask; }); }
+inline float shfl_xor(float v, int mask) { return __uint_as_float(shfl_xor(__float_as_uint(v), mask)); }
+inline uint32_t shfl_up(uint32_t v, int by) { return exchange(11, v, [&](int l) { return l >= by ? l - by : l; }); }
+inline uint32_t read_lane(uint32_t v, int from) { return exchange(12, v, [&](int) { return from; }); }
+inline uint64_t ballot(bool p)
+{
+    uint64_t m = 0;
+    emu::WaveState &w = emu::my_wave();
+    const int l = emu::lane();
+    w.fa[l] = p ? 1.0f : 0.0f;
+    emu::wave_collective(13, [](emu::WaveState &s) { std::memcpy(s.fb, s.fa, sizeof(s.fa)); });
+    for (int i = 0; i < emu::kWave; ++i) m |= (uint64_t)(w.fb[i] != 0.0f) << i;
+    return m;
+}
+inline void lds_add(uint32_t *p, uint32_t v) { *p += v; }
+inline void fence() { emu::wave_sync(); }
+inline float exp2_fast(float x) { return std::exp2(x); }
+
+} // namespace wave
+} // namespace tt

@@ -1,0 +1,435 @@
+"""The token operators (embedding and its gradient, policy loss, activations in 8 bits) against their plain 64-bit forms.
+
+Bounds, from the arithmetic the kernels are said to do (eps = 2^-24, half a step of fp32 next to 1; a bf16 result adds half a step
+of bf16, which has 8 significant bits: 2^-8 of its value):
+  embedding            one fp32 product: eps |z|
+  table gradient       n fp32 additions and one product: (n + 1) eps sum |terms|
+  log probabilities    statistics in fp32.  The logits' factor and each exponent are rounded (2 eps of the distance from the
+                       maximum: |logp| + log V covers it), the sum is one of chains of at most 256 additions and a tree over them,
+                       the logarithm is good to a step: 4 eps (2 |logp| + 2 log V + 160)
+  loss                 the terms' derivatives times that, and 64 eps of the sum of magnitudes
+  logits' gradient     the derivative's error from the log probability's, and the softmax's relative one, eps-wise as above
+  8-bit form           exact
+"""
+import ctypes
+import math
+import mmap
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1805_04170_amd as tt
+from oracle import layers as ly
+from oracle import tiling as tl
+from oracle import tokens as tk
+from synthetic import bf16_bits_to_f64, normal_f32, to_bf16_bits
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+EPS = 2.0 ** -24
+GUARD = "end"       # host runs: which side of a buffer the inaccessible page lies on
+_libc = None
+
+
+def _guarded(nbytes):
+    """host memory whose neighbour page (behind it, or in front of it) cannot be touched"""
+    global _libc
+    _libc = _libc or ctypes.CDLL(None, use_errno=True)
+    page = mmap.PAGESIZE
+    body = max(page, -(-nbytes // page) * page)
+    m = mmap.mmap(-1, body + 2 * page)
+    raw = torch.frombuffer(m, dtype=torch.uint8)
+    base = raw.data_ptr()
+    for at in (base, base + page + body):
+        assert _libc.mprotect(ctypes.c_void_p(at), ctypes.c_size_t(page), 0) == 0
+    lo = page + (body - nbytes if GUARD == "end" else 0)
+    return raw[lo:lo + nbytes]
+
+
+def empty(shape, dtype, skew=0):
+    """a buffer full of 0x5a bytes; skew: elements by which it is off a 256-byte boundary (device runs)"""
+    e = torch.empty(0, dtype=dtype).element_size()
+    n = int(np.prod(shape))
+    if DEV == "cpu":
+        raw = _guarded(n * e)
+    else:
+        raw = torch.empty(max(1, (n + skew) * e), dtype=torch.uint8, device=DEV)[skew * e:]
+    raw.fill_(0x5a)
+    if n == 0:
+        return torch.empty(shape, dtype=dtype, device=DEV)
+    return raw[:n * e].view(dtype).view(shape)
+
+
+def up(a, skew=0):
+    """numpy array to the device; uint16 travels as bf16"""
+    t = torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).view(torch.bfloat16) if a.dtype == np.uint16 else torch.from_numpy(np.ascontiguousarray(a))
+    out = empty(tuple(t.shape), t.dtype, skew)
+    out.copy_(t)
+    return out
+
+
+def down(t):
+    return bf16_bits_to_f64(t.cpu().contiguous().view(torch.int16).numpy().view(np.uint16)) if t.dtype == torch.bfloat16 else t.cpu().numpy()
+
+
+def stored(a, dt):
+    """what a tensor of type dt holds of the values: (array to upload, the same in 64 bits)"""
+    a = a.astype(np.float32)
+    if dt == "bf16":
+        bits = to_bf16_bits(a)
+        return bits, bf16_bits_to_f64(bits)
+    return a, a.astype(np.float64)
+
+
+def shards(a, t, skew=0):
+    return [up(s, skew) for s in tl.tile(a, t)]
+
+
+def outputs(rows, cols, t, dt, skew=0):
+    sr, sc = tl.shard_shape(rows, cols, t)
+    return [empty((sr, sc), torch.bfloat16 if dt == "bf16" else torch.float32, skew) for _ in range(1 << len(t))]
+
+
+def full(sh, t, rows, cols):
+    return tl.untile([down(s) for s in sh], t, rows, cols)
+
+
+def workspace(nbytes):
+    return empty((max(256, nbytes),), torch.uint8)
+
+
+def out_eps(dt):
+    return 2.0 ** -8 if dt == "bf16" else 0.0
+
+
+def check(got, want, bound, what):
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (what, np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+def ids_of(values, idt):
+    return up(np.asarray(values, dtype=np.int32 if idt == "i32" else np.int64))
+
+
+# --------------------------------------------------------------- embedding
+
+def run_embed(T, V, D, dt, tW="", tX="", idt="i64", seed=1, ids=None, scale=None, skew=0):
+    rng = np.random.default_rng(seed)
+    k = len(tW)
+    scale = math.sqrt(D) if scale is None else scale
+    if ids is None:
+        ids = np.minimum((np.exp(rng.random(T) * math.log(V + 1)) - 1).astype(np.int64), V - 1)
+        ids = np.where(rng.random(T) < 0.1, -1, ids)
+    W, Wf = stored(normal_f32(seed, 0, (V, D), 0.5), dt)
+    G, Gf = stored(normal_f32(seed, 1, (T, D), 0.5), dt)
+    d_ids = ids_of(ids, idt)
+    Xs = outputs(T, D, tX, dt, skew)
+    tt.tt_embed_forward(T, V, D, k, dt, tW, tX, d_ids, scale, shards(W, tW, skew), Xs)
+    s32 = float(np.float32(scale))
+    want = tk.embed_forward(Wf, ids, s32)
+    check(full(Xs, tX, T, D), want, (EPS + out_eps(dt) * (1 + EPS)) * np.abs(want), "X")
+    dWs = outputs(V, D, tW, dt, skew)
+    ws = workspace(tt.tt_embed_workspace_bytes(T, V, D, k, dt, tX, tW))
+    Gs = shards(G, tX, skew)
+    tt.tt_embed_backward(T, V, D, k, dt, tX, tW, d_ids, scale, Gs, dWs, ws)
+    want, mag, n = tk.embed_backward(Gf, ids, V, s32)
+    err = (n[:, None] + 1) * EPS * mag
+    check(full(dWs, tW, V, D), want, err + out_eps(dt) * (np.abs(want) + err), "dW")
+    again = outputs(V, D, tW, dt, skew)
+    ws.fill_(0xa5)
+    tt.tt_embed_backward(T, V, D, k, dt, tX, tW, d_ids, scale, Gs, again, ws)
+    for a, b in zip(dWs, again):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,D", [(1, 1, 1), (1, 5, 8), (7, 40, 33), (65, 300, 64), (130, 17, 250), (257, 1031, 72)])
+def test_embedding(T, V, D, dt):
+    run_embed(T, V, D, dt, seed=T)
+
+
+@pytest.mark.parametrize("tW,tX", [("R", "C"), ("C", "r"), ("r", "R"), ("RC", "CR"), ("rC", "Cr"), ("CC", "RR"), ("RCr", "CCC")])
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 24), ("bf16", 40)])
+def test_embedding_tiled(tW, tX, dt, D):
+    run_embed(48, 96, D, dt, tW, tX, "i32", seed=len(tW) + D)
+
+
+@pytest.mark.parametrize("what", ["one", "none", "two", "huge", "long_runs"])
+def test_embedding_token_patterns(what):
+    T, V = 300, 50
+    rng = np.random.default_rng(4)
+    ids = {"one": np.full(T, 49), "none": np.full(T, -1), "two": np.where(np.arange(T) % 2 == 0, 3, 4),
+           "huge": np.where(np.arange(T) % 3 == 0, 2 ** 62, np.where(np.arange(T) % 3 == 1, -2 ** 62, V)),
+           "long_runs": np.sort(rng.integers(0, 4, T))[::-1].copy()}[what].astype(np.int64)
+    run_embed(T, V, 20, "f32", ids=ids)
+
+
+def test_embedding_skewed_buffers():
+    run_embed(33, 70, 48, "bf16", seed=8, skew=1)
+    run_embed(34, 70, 48, "f32", "C", "R", seed=9, skew=3)
+
+
+def test_embedding_without_tokens_is_a_gradient_of_zeros():
+    dW = [empty((6, 5), torch.float32)]
+    ws = workspace(tt.tt_embed_workspace_bytes(0, 6, 5, 0, "f32", "", ""))
+    none = empty((1,), torch.int64)
+    tt.tt_embed_backward(0, 6, 5, 0, "f32", "", "", none, 1.0, [empty((1, 5), torch.float32)], dW, ws)
+    assert not down(dW[0]).any()
+
+
+# ------------------------------------------------------------- policy loss
+
+def policy_inputs(T, V, dt, seed, scale, kl, masked):
+    rng = np.random.default_rng(seed)
+    raw, x = stored(normal_f32(seed, 0, (T, V), 2.0), dt)
+    a = rng.integers(0, V, T)
+    w = np.full(T, 1.0 / T, dtype=np.float32)
+    if masked:
+        def put(rows, cols, v):
+            raw[rows, cols] = to_bf16_bits(np.full(1, v, np.float32))[0] if dt == "bf16" else v
+            x[rows, cols] = v
+        put(slice(None), slice(V - V // 7, None), -np.inf)
+        a = rng.integers(0, max(1, V - V // 7), T)
+        for t in range(T):
+            if t % 5 == 1:
+                w[t] = 0
+                put(t, slice(None), [np.nan, np.inf, -np.inf, 1.0][t % 4])
+            if t % 7 == 3:
+                put(t, slice(None), -np.inf)
+            if t % 11 == 6:
+                a[t] = V if t % 2 else -1
+            if t % 13 == 8:     # one logit left, and it is the action's
+                keep = x[t, a[t]]
+                if 0 <= a[t] < V and np.isfinite(keep):
+                    put(t, slice(None), -np.inf)
+                    put(t, int(a[t]), keep)
+    logp = tk.token_logp(np.where(np.isnan(x) | (x == np.inf), 0.0, x), a, scale)
+    # ratios that stay away from where the clip begins, on both sides of it
+    old = (logp - rng.choice([-0.5, -0.1, 0.0, 0.05, 0.4], T)).astype(np.float32)
+    ref = (logp + rng.normal(0, 0.3, T)).astype(np.float32)
+    adv = rng.normal(0, 1, T).astype(np.float32)
+    adv[::9] = 0
+    return raw, x, a, old, ref, adv, w
+
+
+def logp_bound(logp, V):
+    return 4 * EPS * (2 * np.abs(logp) + 2 * math.log(V + 1) + 160)
+
+
+def run_policy(T, V, dt, tX="", tG="", idt="i64", seed=1, scale=1.0, kl=0.05, masked=False, with_dx=True, skew=0, clip=(0.2, 0.25)):
+    k = len(tX)
+    scale = float(np.float32(scale))
+    raw, x, a, old, ref, adv, w = policy_inputs(T, V, dt, seed, scale, kl, masked)
+    p = tt.policy(clip_low=clip[0], clip_high=clip[1], kl=kl, scale=scale)
+    lo, hi, klf = (float(np.float32(v)) for v in (clip[0], clip[1], kl))
+    loss, logp = empty((1,), torch.float32), empty((T,), torch.float32)
+    Xs, dX = shards(raw, tX, skew), outputs(T, V, tG, dt, skew) if with_dx else None
+    ws = workspace(tt.tt_policy_workspace_bytes(T, V, k, dt, tX, tG if with_dx else None))
+    args = (up(old), up(ref) if kl else None, up(adv), up(w))
+    d_a = ids_of(a, idt)
+    tt.tt_policy_loss(p, T, V, k, dt, tX, tG, Xs, d_a, *args, loss, logp, dX, ws)
+    want_loss, want_logp, want_dX, d = tk.policy_loss(x, a, old.astype(float), ref.astype(float), adv.astype(float), w.astype(float), scale, lo, hi, klf)
+    live = np.array([tk.counts(x[t], a[t], w[t]) for t in range(T)])
+    lb = np.where(live, logp_bound(want_logp, V), 0)
+    check(down(logp), want_logp, lb, "logp")
+    # dL/dlogp moves by (|ratio adv| + kl exp(ref - logp)) times the log probability's error; L itself by |dL/dlogp| times it
+    ratio = np.exp(np.where(live, want_logp - old, 0))
+    kle = klf * np.exp(np.where(live, ref - want_logp, 0)) if kl else 0 * ratio
+    slope = np.abs(ratio * adv) + kle
+    size = np.abs(ratio * adv) + kle * 2 + klf * np.abs(np.where(live, ref - want_logp, 0))
+    wl = np.where(live, w, 0)
+    check(down(loss)[0], want_loss, np.sum(wl * (slope * (lb + 16 * EPS) + 64 * EPS * size)), "loss")
+    if with_dx:
+        d_err = slope * (lb + 16 * EPS)
+        z = np.where(np.isfinite(x) & live[:, None], scale * x, -np.inf)
+        top = np.where(live, np.max(z, axis=1, initial=-1e30), 0)
+        with np.errstate(invalid="ignore", divide="ignore"):
+            away = np.where(np.isfinite(z), top[:, None] - z, 0)
+            ls = np.where(live[:, None], z - top[:, None], -np.inf)
+            prob = np.exp(ls) / np.maximum(np.sum(np.exp(ls), axis=1, keepdims=True), 1e-300)
+        p_rel = 4 * EPS * (2 * away + 2 * math.log(V + 1) + 160)
+        hot = np.zeros((T, V))
+        hot[np.arange(T)[live], a[live]] = 1
+        err = wl[:, None] * scale * (d_err[:, None] * (hot + prob) + np.abs(d)[:, None] * (prob * p_rel + 8 * EPS * hot)) + 1e-37
+        check(full(dX, tG, T, V), want_dX, np.where(live[:, None], err + out_eps(dt) * (np.abs(want_dX) + err), 0), "dX")
+        again, loss2, logp2 = outputs(T, V, tG, dt, skew), empty((1,), torch.float32), empty((T,), torch.float32)
+        ws.fill_(0xa5)
+        tt.tt_policy_loss(p, T, V, k, dt, tX, tG, Xs, d_a, *args, loss2, logp2, again, ws)
+        for u, v in zip([loss, logp] + dX, [loss2, logp2] + again):
+            assert torch.equal(u.view(torch.uint8), v.view(torch.uint8))
+    return loss, logp
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V", [(1, 1), (1, 2), (3, 7), (5, 64), (33, 1000), (4, 2051), (2, 8200)])
+def test_policy_loss(T, V, dt):
+    run_policy(T, V, dt, seed=T + V)
+
+
+@pytest.mark.parametrize("tX,tG", [("C", "R"), ("R", "C"), ("r", "C"), ("CC", "RC"), ("CR", "rr"), ("rC", "Cr"), ("CCC", "RRC")])
+@pytest.mark.parametrize("dt,V", [("bf16", 512), ("f32", 328), ("bf16", 104)])
+def test_policy_loss_tiled(tX, tG, dt, V):
+    run_policy(24, V, dt, tX, tG, "i32", seed=len(tX), masked=True, scale=0.7)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,kl", [(40, 50, 0.0), (60, 333, 0.05), (30, 1031, 0.3)])
+def test_policy_loss_masked(T, V, kl, dt):
+    run_policy(T, V, dt, seed=V, kl=kl, masked=True, scale=1.3)
+
+
+def test_policy_loss_without_gradient_and_log_probabilities_alone():
+    _, logp = run_policy(21, 300, "bf16", masked=False, with_dx=False)
+    raw, x, a, *_ = policy_inputs(21, 300, "bf16", 1, 1.0, 0.05, False)
+    out = empty((21,), torch.float32)
+    ws = workspace(tt.tt_policy_workspace_bytes(21, 300, 0, "bf16", ""))
+    tt.tt_token_logp(21, 300, 0, "bf16", "", 1.0, shards(raw, ""), ids_of(a, "i64"), out, ws)
+    assert torch.equal(out, logp)
+
+
+def run_logp(T, V, dt, tX="", seed=3, scale=1.0):
+    rng = np.random.default_rng(seed)
+    raw, x = stored(normal_f32(seed, 0, (T, V), 2.0), dt)
+    a = rng.integers(-1, V + 1, T)
+    out = empty((T,), torch.float32)
+    ws = workspace(tt.tt_policy_workspace_bytes(T, V, len(tX), dt, tX))
+    tt.tt_token_logp(T, V, len(tX), dt, tX, scale, shards(raw, tX), ids_of(a, "i32"), out, ws)
+    want = tk.token_logp(x, a, float(np.float32(scale)))
+    check(down(out), want, np.where((a >= 0) & (a < V), logp_bound(want, V), 0), "logp")
+
+
+@pytest.mark.parametrize("T,V,dt,tX", [(1, 1, "f32", ""), (1, 4099, "bf16", ""), (3, 9000, "f32", ""), (8, 640, "bf16", "CC"), (6, 36, "bf16", "CR"), (4, 20, "f32", "CCr")])
+def test_token_logp(T, V, dt, tX):
+    run_logp(T, V, dt, tX, scale=0.8)
+
+
+def test_policy_rows_that_count_show_their_nan():
+    x = np.zeros((4, 40), np.float32)
+    x[0, 3], x[1, 5], x[2, :] = np.nan, np.inf, np.nan
+    one = np.ones(4, np.float32)
+    loss, logp = empty((1,), torch.float32), empty((4,), torch.float32)
+    dX, ws = outputs(4, 40, "", "f32"), workspace(tt.tt_policy_workspace_bytes(4, 40, 0, "f32", "", ""))
+    tt.tt_policy_loss(tt.policy(), 4, 40, 0, "f32", "", "", shards(x, ""), ids_of([0] * 4, "i64"), up(0 * one), None, up(one), up(one), loss, logp, dX, ws)
+    assert np.isnan(down(loss)).all()
+    assert np.isnan(down(logp)[:3]).all() and abs(down(logp)[3] + math.log(40)) < 1e-5
+    assert np.isnan(down(dX[0])[:3]).all() and np.isfinite(down(dX[0])[3]).all()
+
+
+def test_policy_loss_of_no_tokens_is_zero():
+    loss = empty((1,), torch.float32)
+    none = empty((1,), torch.float32)
+    tt.tt_policy_loss(tt.policy(), 0, 40, 0, "f32", "", "", [none], empty((1,), torch.int64), none, None, none, none, loss, none, [none], workspace(256))
+    assert down(loss)[0] == 0
+
+
+# ------------------------------------------------ activations in 8 bits
+
+def run_pack(rows, cols, dt, t="", seed=1, values=None, skew=0):
+    k = len(t)
+    a = normal_f32(seed, 0, (rows, cols), 1.0) * np.exp(normal_f32(seed, 1, (1, cols), 2.0)) if values is None else values
+    raw, x = stored(a, dt)
+    sr, sc = tl.shard_shape(rows, cols, t)
+    n = 1 << k
+    Q, S = [empty((sr, sc), torch.int8) for _ in range(n)], [empty((sr, -(-sc // 32)), torch.uint8) for _ in range(n)]
+    tt.tt_pack8(rows, cols, k, dt, t, shards(raw, t, skew), Q, S)
+    X = outputs(rows, cols, t, dt, skew)
+    tt.tt_unpack8(rows, cols, k, dt, t, Q, S, X)
+    for s, xs in enumerate(tl.tile(x, t)):
+        q, e = tk.pack8(xs)
+        assert np.array_equal(down(S[s]), e), s
+        assert np.array_equal(down(Q[s]), q), s
+        v = tk.unpack8(q, e)
+        got = down(X[s])
+        assert np.array_equal(got, v, equal_nan=True), s
+        fine = np.isfinite(v)
+        assert np.array_equal(np.sign(v[fine]), np.sign(xs[fine]))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 16), (3, 31), (5, 33), (7, 64), (2, 200), (9, 47)])
+def test_pack8(rows, cols, dt):
+    run_pack(rows, cols, dt, seed=cols)
+
+
+@pytest.mark.parametrize("t", ["R", "C", "r", "RC", "CCr"])
+def test_pack8_tiled(t):
+    run_pack(16, 96, "bf16", t)
+    run_pack(16, 88, "f32", t)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_pack8_values_at_the_edges(dt):
+    tiny, big = 1e-45, 3.3e38
+    rows = [[127.0, 126.5, 0.5, -0.5, 1.5, 2.5, 0.4, -0.4, 1e-30], [127.00001, 1, -1, 0.2], [255, 254, 253, -127.5], [128, 64.5, 63.5], [0] * 5, [-0.0, 0.0],
+            [tiny, 2 * tiny, -tiny], [big, -big, 1, tiny], [np.nan, 1, 2], [np.inf, 1], [1, -np.inf], [2.0 ** -120, 2.0 ** -126, 2.0 ** -119.3],
+            [1.984375], [1.98438], [1.9843], [63.5 * 2.0 ** 121]]
+    a = np.zeros((len(rows), 40), np.float32)
+    for i, r in enumerate(rows):
+        a[i, :len(r)] = r
+        a[i, 39] = 3.0
+    run_pack(len(rows), 40, dt, values=a)
+
+
+def test_pack8_skewed_buffers():
+    run_pack(6, 70, "bf16", skew=1)
+    run_pack(6, 70, "f32", skew=3)
+
+
+def run_packed_backward(b, ni, no, dt, relu, tX, tW, tY, tdY, tdX, fd=None, fw=None, with_dx=True, seed=1, nan=False):
+    k = len(tX)
+    lay = tt.layer("fc", "relu" if relu else "none", ni, no)
+    pack = lambda a, t: [tk.pack8(s) for s in tl.tile(a, t)]  # noqa: E731
+    value = lambda ps, t, r, c: tl.untile([tk.unpack8(*p) for p in ps], t, r, c)  # noqa: E731
+    Y = normal_f32(seed, 1, (b, no), 1.0)
+    if nan:
+        Y[1, 3] = np.inf
+    X8, Y8 = pack(stored(normal_f32(seed, 0, (b, ni), 1.0), dt)[1], tX), pack(stored(Y, dt)[1], tY)
+    W, Wf = stored(normal_f32(seed, 2, (ni, no), 0.1), dt)
+    dY, dYf = stored(normal_f32(seed, 3, (b, no), 1.0), dt)
+    dX, dW = outputs(b, ni, tdX, dt) if with_dx else None, outputs(ni, no, tW, dt)
+    ws = workspace(tt.tt_fc_packed_workspace_bytes(lay, b, k, dt, tX, tW, tY, tdY, tdX, fd, fw, with_dx))
+    lists = [[up(p[i]) for p in ps] for ps in (X8, Y8) for i in (0, 1)]
+    Ws, dYs = shards(W, tW), shards(dY, tdY)
+    tt.tt_fc_backward_packed(lay, b, k, dt, tX, tW, tY, tdY, tdX, fd, fw, lists[0], lists[1], Ws, lists[2] if relu else None, lists[3] if relu else None,
+                             dYs, dX, dW, ws)
+    Xv, Yv = value(X8, tX, b, ni), value(Y8, tY, b, no)
+    with np.errstate(invalid="ignore"):
+        G = dYf * (Yv > 0) if relu else dYf
+    rel = 1e-4 if dt == "bf16" else 1e-5        # the shard products' own bounds
+    if with_dx:
+        want = G @ Wf.T
+        check(full(dX, tdX, b, ni), want, rel * ly.abs_product(G, Wf.T) + 2 * out_eps(dt) * np.abs(want), "dX")
+    want = Xv.T @ G
+    check(full(dW, tW, ni, no), want, rel * ly.abs_product(Xv.T, G) + 2 * out_eps(dt) * np.abs(want), "dW")
+    # and the 16-bit pass on the unpacked activations, bit for bit
+    def unpacked(q, s, r, c, t):
+        out = outputs(r, c, t, dt)
+        tt.tt_unpack8(r, c, k, dt, t, q, s, out)
+        return out
+    Xu, Yu = unpacked(lists[0], lists[1], b, ni, tX), unpacked(lists[2], lists[3], b, no, tY)
+    dX2, dW2 = outputs(b, ni, tdX, dt) if with_dx else None, outputs(ni, no, tW, dt)
+    ws2 = workspace(tt.tt_fc_workspace_bytes(lay, b, k, dt, tt.TT_OP_DGRAD, tX, tW, tY, tdY, tdX, fd, fw, with_dx))
+    tt.tt_fc_backward(lay, b, k, dt, tX, tW, tY, tdY, tdX, fd, fw, Xu, Ws, Yu, dYs, dX2, dW2, ws2)
+    for u, v in zip((dX or []) + dW, (dX2 or []) + dW2):
+        assert torch.equal(u.view(torch.uint8), v.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("relu", [True, False])
+def test_packed_backward_untiled(dt, relu):
+    run_packed_backward(24, 48, 40, dt, relu, "", "", "", "", "")
+    run_packed_backward(5, 17, 9, dt, relu, "", "", "", "", "", with_dx=False)
+
+
+@pytest.mark.parametrize("t", [("R", "r", "R", "R", "R"), ("r", "C", "C", "C", "R"), ("C", "R", "r", "R", "C"), ("CC", "RR", "CR", "RC", "Cr"),
+                               ("CCC", "RRR", "CCr", "CCr", "CCC")])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_packed_backward_tiled(t, dt):
+    run_packed_backward(16, 64, 72 if len(t[0]) < 3 else 64, dt, True, *t, seed=len(t[0]))
+
+
+def test_packed_backward_gates_out_what_is_not_a_number():
+    run_packed_backward(8, 32, 64, "bf16", True, "", "", "", "", "", nan=True)
+    run_packed_backward(8, 32, 64, "bf16", True, "R", "r", "C", "R", "R", nan=True)
