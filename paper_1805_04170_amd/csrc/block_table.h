@@ -7,10 +7,22 @@
 
 namespace tt {
 
+// n / d for n below 2^31 by one multiplication: with 2^(s-1) < d <= 2^s and m = ceil(2^(31+s) / d) the excess m d - 2^(31+s) is below
+// d <= 2^s, and n times it below 2^(31+s).
+struct Divisor { uint32_t d, m, s; };
+inline Divisor divisor(uint32_t d)
+{
+    Divisor v{d, 0, 0};
+    while ((uint64_t(1) << v.s) < d) ++v.s;
+    if (d > 1) v.m = (uint32_t)(((uint64_t(1) << (31 + v.s)) + d - 1) / d);
+    return v;
+}
+
 struct BlockTable {
     void *p[kMaxShards]; // block (r, c), replica x at (r * nC + c) * nrep + x
-    uint32_t nC, nrep;
+    uint32_t nR, nC, nrep;
     uint32_t srows, scols; // shard extent
+    Divisor by_srows;
 };
 
 // false: an uneven cut.  Entries are NULL where the list is (a size query needs the geometry alone).
@@ -18,10 +30,12 @@ inline bool make_blocks(const void *const *shards, const tt_tiling &t, int k, in
 {
     Grid g;
     if (!make_grid(t.cut, k, rows, cols, &g)) return false;
+    b->nR = 1u << g.kR;
     b->nC = 1u << g.kC;
     b->nrep = 1u << g.kX;
     b->srows = (uint32_t)g.srows;
     b->scols = (uint32_t)g.scols;
+    b->by_srows = divisor(b->srows ? b->srows : 1);
     for (uint32_t i = 0; i < (uint32_t)kMaxShards; ++i) b->p[i] = nullptr;
     for (uint32_t s = 0; s < (1u << k); ++s) {
         const uint32_t r = extract(s, g.maskR, k), c = extract(s, g.maskC, k), x = extract(s, g.maskX, k);

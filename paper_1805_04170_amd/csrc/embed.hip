@@ -13,262 +13,436 @@
 namespace tt {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kU = 4; // vectors per lane and unit of work
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kU = 2;     // vectors per lane of a wave's part of a segment
+constexpr int kBatch = 4; // rows that are on their way together
+constexpr int kRows = 8;  // rows of the table's gradient per wave
 
-// A unit of work is kU vectors per lane of a group of lanes; a row is `upr` units.
-struct RowSplit : Pieces {
-    uint32_t upr;  // units per row
-    uint32_t glog; // log2 of the lanes of a group
+// How the segments of a row are shared out.  Wide segments (more than 32 vectors): a part of kU vectors per lane to a wave, so
+// that a wave's row, segment and addresses are scalars.  Narrow ones: a vector per lane, a segment to 2^glog lanes.
+struct Split {
+    Pieces s;
+    uint32_t wide, glog;
+    uint32_t parts; // of a segment (wide)
+    Divisor by_row, by_segment, by_nseg; // parts of a row, of a segment; segments of a row
 };
 
-RowSplit split_row(const BlockTable &a, const BlockTable &b, int64_t cols, int ev)
+Split split_rows(const BlockTable &a, const BlockTable &b, int64_t cols, int ev)
 {
-    RowSplit s;
-    static_cast<Pieces &>(s) = pieces_of(a, b, cols, ev);
-    s.glog = 0;
-    while (s.glog < 6 && (1u << s.glog) < s.nvec) ++s.glog;
-    s.upr = (s.nvec + (kU << s.glog) - 1) / (kU << s.glog);
-    return s;
+    Split w;
+    w.s = pieces_of(a, b, cols, ev);
+    w.wide = w.s.vps > 32;
+    w.glog = 0;
+    while ((1u << w.glog) < w.s.vps && w.glog < 6) ++w.glog;
+    w.parts = w.wide ? (w.s.vps + 64 * kU - 1) / (64 * kU) : 1;
+    w.by_row = divisor(w.s.nseg * w.parts);
+    w.by_segment = divisor(w.parts);
+    w.by_nseg = divisor(w.s.nseg);
+    return w;
+}
+
+// workgroups for `rows` rows, `per_wave` of them to a wave of the wide form
+uint64_t groups_of(const Split &w, uint64_t rows, uint64_t per_wave)
+{
+    if (w.wide) return ((rows + per_wave - 1) / per_wave * w.s.nseg * w.parts + kWaves - 1) / kWaves;
+    return ((rows * w.s.nseg << w.glog) + kThreads - 1) / kThreads;
+}
+
+// a wave's work in the wide form, all of it scalars
+struct WaveWork { uint32_t row, q, j0; };
+__device__ __forceinline__ WaveWork wave_work(const Split &w)
+{
+    const uint32_t g = blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
+    const uint32_t row = quotient(g, w.by_row), rest = g - row * w.by_row.d;
+    const uint32_t q = quotient(rest, w.by_segment);
+    return {row, q, (rest - q * w.parts) * 64 * kU};
+}
+// a lane's in the narrow form: vector j of a segment
+struct LaneWork { uint32_t row, q, j; };
+__device__ __forceinline__ LaneWork lane_work(const Split &w)
+{
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x, g = i >> w.glog, row = quotient(g, w.by_nseg);
+    return {row, g - row * w.s.nseg, i & ((1u << w.glog) - 1)};
+}
+
+template <typename T> __device__ __forceinline__ u32x4 scaled(u32x4 v, float scale)
+{
+    float f[kVec<T>];
+    unpack16(v, f, T());
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) f[i] *= scale;
+    return pack16(f, T());
 }
 
 // ------------------------------------------------------------------------------------------------------- forward
 
 struct EmbedParams {
     BlockTable W, X;
-    RowSplit s;
+    Split w;
     const void *ids;
-    uint32_t tokens, units;
+    uint32_t tokens;
     int64_t vocab;
     float scale;
 };
 
-// One unit per group of lanes: kU vectors of one token's row, all of them loaded before the first is stored.
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_forward_kernel(const EmbedParams p)
+// A wave's part of one token's row, all of it loaded before the first vector is stored.
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_wide_kernel(const EmbedParams p)
 {
-    const uint32_t g = (blockIdx.x * kThreads + threadIdx.x) >> p.s.glog, l = threadIdx.x & ((1u << p.s.glog) - 1);
-    if (g >= p.units) return;
-    const uint32_t t = g / p.s.upr, j0 = ((g - t * p.s.upr) * kU << p.s.glog) + l;
-    const int64_t v = token_at<I>(p.ids, t);
+    const WaveWork g = wave_work(p.w);
+    if (g.row >= p.tokens) return;
+    const int64_t v = token_at<I>(p.ids, g.row);
     const bool in = v >= 0 && v < p.vocab;
+    const uint32_t lane = threadIdx.x & 63u;
     u32x4 r[kU];
-    uint32_t col[kU], n[kU];
+    uint32_t n[kU];
+    const T *src = in ? source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q) : nullptr;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-        const uint32_t j = j0 + ((uint32_t)u << p.s.glog);
+        const uint32_t j = g.j0 + u * 64 + lane;
+        n[u] = values_of(p.w.s, kVec<T>, j);
         r[u] = u32x4{0, 0, 0, 0};
-        n[u] = 0;
-        if (j < p.s.nvec) {
-            vector_of(p.s, kVec<T>, j, &col[u], &n[u]);
-            if (in) r[u] = load_vector(source_of<T>(p.W, (uint32_t)v, col[u]), n[u]);
-        }
+        if (in && n[u]) r[u] = load_vector(src + j * kVec<T>, n[u]);
     }
+    const Place to = place_of(p.X, p.w.s, p.w.s.b_shift, g.row, g.q);
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
         if (n[u] == 0) continue;
-        float f[kVec<T>];
-        unpack16(r[u], f, T());
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) f[i] = in ? f[i] * p.scale : 0.0f;
-        store_all<T>(p.X, t, col[u], n[u], pack16(f, T()));
+        store_all<T>(p.X, to, (g.j0 + u * 64 + lane) * kVec<T>, n[u], in ? scaled<T>(r[u], p.scale) : r[u]);
     }
 }
 
-// ------------------------------------------------------------------------------------------------------ backward
-// Three launches.  (1) Tokens sorted by number, stably: `order` lists the tokens with number 0, then 1, ...; `start[v]` is
-// where v's begin.  (2) Numbers with many tokens (more than `chunk`) would keep one group of lanes busy long after the
-// rest is done: the sorted list is cut into runs of `chunk`, and each run adds up its part of such a number into a
-// partial sum.  (3) Every row of the table's gradient: the sum over its tokens in order, or over its partial sums.
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_narrow_kernel(const EmbedParams p)
+{
+    const LaneWork g = lane_work(p.w);
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
+    if (g.row >= p.tokens || n == 0) return;
+    const int64_t v = token_at<I>(p.ids, g.row);
+    u32x4 r = u32x4{0, 0, 0, 0};
+    if (v >= 0 && v < p.vocab) r = scaled<T>(load_vector(source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q) + g.j * kVec<T>, n), p.scale);
+    store_all<T>(p.X, place_of(p.X, p.w.s, p.w.s.b_shift, g.row, g.q), g.j * kVec<T>, n, r);
+}
 
-// (1) A workgroup owns a range of numbers and reads all tokens, each wave a stretch of them: it counts how many lie below its
-// range (where its part of the list begins) and how often each of its numbers comes in each wave's stretch; after a scan
-// over (number, wave) the waves walk their stretches again and put their tokens in place, in order.  No workgroup waits for
-// another, whatever the numbers are.
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortRange = 1024;
+// ------------------------------------------------------------------------------------------------------ backward
+// Three launches.  (1) Tokens sorted by number, stably.  (2) Numbers with many tokens (more than `chunk`) would keep one wave
+// busy long after the rest is done: the sorted list is cut into runs of `chunk`, and each run adds up its part of such a
+// number into a partial sum.  (3) Every row of the table's gradient: the sum over its tokens in order, or over its partial sums.
+
+// (1) Numbers are dealt out to workgroups like cards (frequent numbers are neighbours in most vocabularies): workgroup w sorts
+// the tokens whose number is w modulo the workgroups' count, 2^wlog of them.  The list has w's numbers behind w - 1's, each
+// workgroup's in increasing order: place(v) = (v mod 2^wlog) * range + v / 2^wlog numbers them so, and start[place(v)],
+// start[place(v) + 1] enclose v's tokens.
+//
+// A workgroup reads all tokens, each wave a stretch of them.  It counts how many belong to workgroups before it (where its part
+// of the list begins) and how often each of its numbers comes in each wave's stretch; after a scan over (number, wave) the
+// waves walk their stretches again and put their tokens in place, in order.  No workgroup waits for another, whatever the
+// numbers are.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortRange = 1024, kSortLoads = 16;
+
+struct Places { uint32_t wlog, range; };
+__device__ __forceinline__ uint32_t place(const Places &s, uint32_t v) { return (v & ((1u << s.wlog) - 1)) * s.range + (v >> s.wlog); }
 
 struct SortParams {
     const void *ids;
-    uint32_t tokens, range; // numbers per workgroup
+    uint32_t tokens;
+    Places to;
     int64_t vocab;
     uint32_t *order, *start;
 };
 
+constexpr uint32_t kNoToken = ~0u;
+template <typename I> __device__ __forceinline__ uint32_t number_at(const SortParams &p, uint32_t t, uint32_t end)
+{
+    if (t >= end) return kNoToken;
+    const int64_t v = token_at<I>(p.ids, t);
+    return v >= 0 && v < p.vocab ? (uint32_t)v : kNoToken;
+}
+
 template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const SortParams p)
 {
     __shared__ uint32_t at[kSortWaves * kSortRange];
-    __shared__ uint32_t part[kSortWaves + 1];
-    const uint32_t lane = threadIdx.x & 63u, w = uniform(threadIdx.x >> 6);
-    const int64_t lo = (int64_t)blockIdx.x * p.range;
-    const uint32_t own = (uint32_t)(p.vocab - lo < (int64_t)p.range ? p.vocab - lo : (int64_t)p.range);
-    for (uint32_t i = threadIdx.x; i < kSortWaves * p.range; i += kSortThreads) at[i] = 0;
+    __shared__ uint32_t part[2][kSortWaves];
+    const uint32_t lane = threadIdx.x & 63u, w = uniform(threadIdx.x >> 6), me = blockIdx.x, range = p.to.range;
+    const uint32_t groups = 1u << p.to.wlog;
+    for (uint32_t i = threadIdx.x; i < kSortWaves * range; i += kSortThreads) at[i] = 0;
     __syncthreads();
     const uint32_t stretch = ((p.tokens + kSortThreads - 1) / kSortThreads) * 64;
     const uint32_t t0 = w * stretch < p.tokens ? w * stretch : p.tokens, t1 = t0 + stretch < p.tokens ? t0 + stretch : p.tokens;
-    uint32_t *mine = at + w * p.range;
+    uint32_t *mine = at + w * range;
     uint32_t below = 0;
-    for (uint32_t t = t0 + lane; t < t1; t += 64) {
-        const int64_t v = token_at<I>(p.ids, t);
-        if (v >= 0 && v < lo) ++below;
-        if (v >= lo && v < lo + own) wave::lds_add(&mine[v - lo], 1);
+    for (uint32_t tb = t0; tb < t1; tb += 64 * kSortLoads) {
+        uint32_t v[kSortLoads];
+#pragma unroll
+        for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
+#pragma unroll
+        for (int i = 0; i < kSortLoads; ++i) {
+            if (v[i] == kNoToken) continue;
+            const uint32_t who = v[i] & (groups - 1);
+            below += who < me ? 1 : 0;
+            if (who == me) wave::lds_add(&mine[v[i] >> p.to.wlog], 1);
+        }
     }
     below = wave_sum(below);
-    if (lane == 0) part[w] = below;
+    if (lane == 0) part[0][w] = below;
     __syncthreads();
-    // thread r: number lo + r; exclusive scan of the totals over the workgroup
-    uint32_t total = 0, base = 0;
-    if (threadIdx.x < own)
-        for (uint32_t i = 0; i < (uint32_t)kSortWaves; ++i) total += at[i * p.range + threadIdx.x];
-    for (uint32_t i = 0; i < (uint32_t)kSortWaves; ++i) base += part[i];
+    // thread r: the workgroup's r-th number; exclusive scan of the totals over the workgroup
+    uint32_t total = 0, before = 0;
+    if (threadIdx.x < range)
+        for (uint32_t i = 0; i < (uint32_t)kSortWaves; ++i) total += at[i * range + threadIdx.x];
     uint32_t incl = total;
 #pragma unroll
     for (int by = 1; by < 64; by <<= 1) {
         const uint32_t o = wave::shfl_up(incl, by);
         if (lane >= (uint32_t)by) incl += o;
     }
+    if (lane == 63) part[1][w] = incl;
     __syncthreads();
-    if (lane == 63) part[w] = incl;
-    __syncthreads();
-    uint32_t before = base + incl - total;
-    for (uint32_t i = 0; i < w; ++i) before += part[i];
-    if (threadIdx.x < own) {
-        p.start[lo + threadIdx.x] = before;
+    for (uint32_t i = 0; i < (uint32_t)kSortWaves; ++i) before += part[0][i] + (i < w ? part[1][i] : 0);
+    before += incl - total;
+    if (threadIdx.x < range) {
+        p.start[me * range + threadIdx.x] = before;
         uint32_t run = before;
         for (uint32_t i = 0; i < (uint32_t)kSortWaves; ++i) {
-            const uint32_t c = at[i * p.range + threadIdx.x];
-            at[i * p.range + threadIdx.x] = run;
+            const uint32_t c = at[i * range + threadIdx.x];
+            at[i * range + threadIdx.x] = run;
             run += c;
         }
-        if (lo + threadIdx.x + 1 == p.vocab) p.start[p.vocab] = run;
+        if (me + 1 == groups && threadIdx.x + 1 == range) p.start[groups * range] = run;
     }
     __syncthreads();
-    for (uint32_t tt0 = t0; tt0 < t1; tt0 += 64) {
-        const uint32_t t = tt0 + lane;
-        const int64_t v = t < t1 ? token_at<I>(p.ids, t) : -1;
-        const bool in = v >= lo && v < lo + own;
-        const uint32_t r = in ? (uint32_t)(v - lo) : 0;
-        uint64_t left = wave::ballot(in);
-        while (left) { // one number of the 64 tokens at a time
-            const uint32_t n = wave::read_lane(r, __builtin_ctzll(left));
-            const bool same = in && r == n;
-            const uint64_t who = wave::ballot(same);
-            const uint32_t to = mine[n];
-            wave::fence();
-            if (same) {
-                const uint32_t rank = (uint32_t)__builtin_popcountll(who & ((uint64_t(1) << lane) - 1));
-                p.order[to + rank] = t;
-                if (rank == 0) mine[n] = to + (uint32_t)__builtin_popcountll(who);
+    for (uint32_t tb = t0; tb < t1; tb += 64 * kSortLoads) {
+        uint32_t v[kSortLoads];
+#pragma unroll
+        for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
+#pragma unroll
+        for (int i = 0; i < kSortLoads; ++i) {
+            const bool in = v[i] != kNoToken && (v[i] & (groups - 1)) == me;
+            const uint32_t r = in ? v[i] >> p.to.wlog : 0;
+            uint64_t left = wave::ballot(in);
+            while (left) { // one number of the 64 tokens at a time
+                const uint32_t n = wave::read_lane(r, __builtin_ctzll(left));
+                const bool same = in && r == n;
+                const uint64_t who = wave::ballot(same);
+                const uint32_t to = mine[n];
+                wave::fence();
+                if (same) {
+                    const uint32_t rank = (uint32_t)__builtin_popcountll(who & ((uint64_t(1) << lane) - 1));
+                    p.order[to + rank] = tb + i * 64 + lane;
+                    if (rank == 0) mine[n] = to + (uint32_t)__builtin_popcountll(who);
+                }
+                wave::fence();
+                left &= ~who;
             }
-            wave::fence();
-            left &= ~who;
         }
     }
 }
 
 struct EmbedGradParams {
     BlockTable G, W; // the rows' gradients, the table's
-    RowSplit s;
+    Split w;
     const void *ids;
     const uint32_t *order, *start;
     float *partial; // [2 runs][cols]: run c's part of a number that began before the run, of one that begins inside it
-    uint32_t chunk, runs, cols, units;
+    Places to;
+    Divisor by_range, by_chunk;
+    uint32_t places; // 2^wlog * range
+    uint32_t chunk, runs, cols;
     int64_t vocab;
     float scale;
 };
-
-template <typename T> struct Sums {
-    float f[kU][kVec<T>];
-    uint32_t col[kU], n[kU];
-};
-
-template <typename T> __device__ __forceinline__ void begin(Sums<T> &a, const RowSplit &s, uint32_t j0)
+// the number at a place of the sorted order
+__device__ __forceinline__ uint32_t number_of(const EmbedGradParams &p, uint32_t at)
 {
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        const uint32_t j = j0 + ((uint32_t)u << s.glog);
-        a.n[u] = 0;
-        a.col[u] = 0;
-        if (j < s.nvec) vector_of(s, kVec<T>, j, &a.col[u], &a.n[u]);
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) a.f[u][i] = 0.0f;
-    }
+    const uint32_t w = quotient(at, p.by_range);
+    return ((at - w * p.to.range) << p.to.wlog) + w;
+}
+__device__ __forceinline__ float *partial_of(const EmbedGradParams &p, uint32_t run, bool inside, uint32_t q)
+{
+    return p.partial + (size_t)(2 * run + (inside ? 1 : 0)) * p.cols + (size_t)q * p.w.s.seg;
 }
 
-// the rows order[b .. e) added to the sums, in that order
-template <typename T> __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, uint32_t b, uint32_t e)
-{
-    for (uint32_t i = b; i < e; ++i) {
-        const uint32_t t = p.order[i];
-        u32x4 r[kU];
+// 64 places of the sorted list in the lanes of a wave, of those that the wave will ask for (up to `end`)
+struct Window {
+    uint32_t base, end, tokens;
+    __device__ __forceinline__ void load(const EmbedGradParams &p, uint32_t at)
+    {
+        base = at;
+        const uint32_t i = at + (threadIdx.x & 63u);
+        tokens = i < end ? p.order[i] : 0;
+    }
+};
+
+// the sums of a wave's part of a segment
+template <typename T> struct Sums {
+    float f[kU][kVec<T>];
+    uint32_t n[kU];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            r[u] = u32x4{0, 0, 0, 0};
-            if (a.n[u]) r[u] = load_vector(source_of<T>(p.G, t, a.col[u]), a.n[u]);
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) f[u][i] = 0.0f;
+    }
+    __device__ __forceinline__ void add(int u, u32x4 v)
+    {
+        float g[kVec<T>];
+        unpack16(v, g, T());
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) f[u][i] += g[i];
+    }
+};
+
+// the rows of places [b, e) added to the sums in that order, BATCH of them on their way at a time
+template <typename T, int BATCH> __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, const WaveWork &g, Window &win, uint32_t b, uint32_t e)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    for (uint32_t i = b; i < e; i += BATCH) {
+        if (i + BATCH > win.base + 64) win.load(p, i);
+        u32x4 r[BATCH][kU];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            if (i + k >= e) break;
+            const T *src = source_of<T>(p.G, p.w.s, p.w.s.a_shift, wave::read_lane(win.tokens, (int)(i + k - win.base)), g.q);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                r[k][u] = u32x4{0, 0, 0, 0};
+                if (a.n[u]) r[k][u] = load_vector(src + (g.j0 + u * 64 + lane) * kVec<T>, a.n[u]);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            float f[kVec<T>];
-            unpack16(r[u], f, T());
+        for (int k = 0; k < BATCH; ++k) {
+            if (i + k >= e) break;
 #pragma unroll
-            for (int q = 0; q < kVec<T>; ++q) a.f[u][q] += f[q];
+            for (int u = 0; u < kU; ++u) a.add(u, r[k][u]);
         }
     }
 }
 
 // (2)
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_runs_kernel(const EmbedGradParams p)
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_runs_wide_kernel(const EmbedGradParams p)
 {
-    const uint32_t g = (blockIdx.x * kThreads + threadIdx.x) >> p.s.glog, l = threadIdx.x & ((1u << p.s.glog) - 1);
-    if (g >= p.units) return;
-    const uint32_t c = g / p.s.upr, j0 = ((g - c * p.s.upr) * kU << p.s.glog) + l;
-    const uint32_t total = p.start[p.vocab];
-    const uint32_t b = c * p.chunk;
-    if (b >= total) return;
+    const WaveWork g = wave_work(p.w);
+    const uint32_t lane = threadIdx.x & 63u, c = g.row, total = p.start[p.places], b = c * p.chunk;
+    if (c >= p.runs || b >= total) return;
     const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
-    const int64_t first = token_at<I>(p.ids, p.order[b]), last = token_at<I>(p.ids, p.order[e - 1]);
+    const uint32_t first = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[b])), last = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[e - 1]));
+    Sums<T> a;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) a.n[u] = values_of(p.w.s, kVec<T>, g.j0 + u * 64 + lane);
 #pragma unroll 1
     for (int side = 0; side < 2; ++side) {
-        const int64_t v = side == 0 ? first : last;
         if (side == 1 && last == first) break;
-        const uint32_t vb = p.start[v], ve = p.start[v + 1];
+        const uint32_t at = side == 0 ? first : last, vb = p.start[at], ve = p.start[at + 1];
         if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
-        Sums<T> a;
-        begin(a, p.s, j0);
-        add_rows(a, p, vb > b ? vb : b, ve < e ? ve : e);
-        float *to = p.partial + (size_t)(2 * c + (vb > b ? 1 : 0)) * p.cols;
+        const uint32_t lo = vb > b ? vb : b, hi = ve < e ? ve : e;
+        Window win{0, hi, 0};
+        win.load(p, lo);
+        a.clear();
+        add_rows<T, kBatch>(a, p, g, win, lo, hi);
+        float *to = partial_of(p, c, vb > b, g.q);
 #pragma unroll
         for (int u = 0; u < kU; ++u)
-            for (uint32_t i = 0; i < a.n[u]; ++i) to[a.col[u] + i] = a.f[u][i];
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i)
+                if ((uint32_t)i < a.n[u]) to[(g.j0 + u * 64 + lane) * kVec<T> + i] = a.f[u][i];
     }
 }
 
-// (3)
-template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_kernel(const EmbedGradParams p)
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_runs_narrow_kernel(const EmbedGradParams p)
 {
-    const uint64_t g = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> p.s.glog;
-    const uint32_t l = threadIdx.x & ((1u << p.s.glog) - 1);
-    const uint64_t row = g / p.s.upr;
-    if (row >= (uint64_t)p.vocab) return;
-    const uint32_t v = (uint32_t)row, j0 = ((uint32_t)(g - row * p.s.upr) * kU << p.s.glog) + l;
-    const uint32_t b = p.start[v], e = p.start[v + 1];
-    Sums<T> a;
-    begin(a, p.s, j0);
-    if (e - b <= p.chunk) {
-        add_rows(a, p, b, e);
-    } else {
-        for (uint32_t c = b / p.chunk; c * p.chunk < e; ++c) {
-            const float *from = p.partial + (size_t)(2 * c + (b > c * p.chunk ? 1 : 0)) * p.cols;
+    const LaneWork g = lane_work(p.w);
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j), c = g.row, total = p.start[p.places], b = c * p.chunk;
+    if (c >= p.runs || b >= total || n == 0) return;
+    const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
+    const uint32_t first = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[b])), last = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[e - 1]));
+    for (int side = 0; side < 2; ++side) {
+        if (side == 1 && last == first) break;
+        const uint32_t at = side == 0 ? first : last, vb = p.start[at], ve = p.start[at + 1];
+        if (ve - vb <= p.chunk) continue;
+        float s[kVec<T>] = {};
+        for (uint32_t i = vb > b ? vb : b; i < (ve < e ? ve : e); ++i) {
+            float f[kVec<T>];
+            unpack16(load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, p.order[i], g.q) + g.j * kVec<T>, n), f, T());
 #pragma unroll
-            for (int u = 0; u < kU; ++u)
-                for (uint32_t i = 0; i < a.n[u]; ++i) a.f[u][i] += from[a.col[u] + i];
+            for (int q = 0; q < kVec<T>; ++q) s[q] += f[q];
+        }
+        float *to = partial_of(p, c, vb > b, g.q) + g.j * kVec<T>;
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i)
+            if ((uint32_t)i < n) to[i] = s[i];
+    }
+}
+
+// (3) A wave does kRows neighbouring places: where their tokens begin comes in one load, and so do the tokens.
+template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_wide_kernel(const EmbedGradParams p)
+{
+    const WaveWork g = wave_work(p.w);
+    const uint32_t lane = threadIdx.x & 63u, at0 = g.row * kRows;
+    if (at0 >= p.places) return;
+    const uint32_t at_lane = at0 + (lane < (uint32_t)kRows ? lane : (uint32_t)kRows);
+    const uint32_t starts = p.start[at_lane < p.places ? at_lane : p.places];
+    const uint32_t first = wave::read_lane(starts, 0), end = wave::read_lane(starts, kRows);
+    Window win{0, end, 0};
+    win.load(p, first);
+    Sums<T> a;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) a.n[u] = values_of(p.w.s, kVec<T>, g.j0 + u * 64 + lane);
+#pragma unroll 1
+    for (int k = 0; k < kRows; ++k) {
+        if (at0 + k >= p.places) break;
+        const uint32_t v = number_of(p, at0 + k);
+        if ((int64_t)v >= p.vocab) continue;
+        const uint32_t b = wave::read_lane(starts, k), e = wave::read_lane(starts, k + 1);
+        const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q);
+        a.clear();
+        if (e - b <= p.chunk) {
+            add_rows<T, kBatch>(a, p, g, win, b, e);
+        } else {
+            for (uint32_t c = quotient(b, p.by_chunk); c * p.chunk < e; ++c) {
+                const float *from = partial_of(p, c, b > c * p.chunk, g.q);
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+#pragma unroll
+                    for (int i = 0; i < kVec<T>; ++i)
+                        if ((uint32_t)i < a.n[u]) a.f[u][i] += from[(g.j0 + u * 64 + lane) * kVec<T> + i];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            if (a.n[u] == 0) continue;
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= p.scale;
+            store_all<T>(p.W, to, (g.j0 + u * 64 + lane) * kVec<T>, a.n[u], pack16(a.f[u], T()));
+        }
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_narrow_kernel(const EmbedGradParams p)
+{
+    const LaneWork g = lane_work(p.w);
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
+    if (g.row >= p.places || n == 0) return;
+    const uint32_t v = number_of(p, g.row);
+    if ((int64_t)v >= p.vocab) return;
+    const uint32_t b = p.start[g.row], e = p.start[g.row + 1];
+    float s[kVec<T>] = {};
+    if (e - b <= p.chunk) {
+        for (uint32_t i = b; i < e; ++i) {
+            float f[kVec<T>];
+            unpack16(load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, p.order[i], g.q) + g.j * kVec<T>, n), f, T());
+#pragma unroll
+            for (int q = 0; q < kVec<T>; ++q) s[q] += f[q];
+        }
+    } else {
+        for (uint32_t c = quotient(b, p.by_chunk); c * p.chunk < e; ++c) {
+            const float *from = partial_of(p, c, b > c * p.chunk, g.q) + g.j * kVec<T>;
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i)
+                if ((uint32_t)i < n) s[i] += from[i];
         }
     }
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        if (a.n[u] == 0) continue;
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= p.scale;
-        store_all<T>(p.W, v, a.col[u], a.n[u], pack16(a.f[u], T()));
-    }
+    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
+    store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q), g.j * kVec<T>, n, pack16(s, T()));
 }
 
 // ----------------------------------------------------------------------------------------------------- host side
@@ -277,7 +451,7 @@ tt_status check_sizes(int64_t tokens, int64_t vocab, int64_t width, int k, int d
 {
     if (!valid_k(k) || !valid_tiling(a, k) || !valid_tiling(b, k) || !valid_dtype(dtype)) return TT_EINVAL;
     if (tokens < 0 || vocab < 0 || width < 0) return TT_EINVAL;
-    if (!fits31(tokens) || !fits31(vocab) || !fits31(width)) return TT_EUNSUPPORTED;
+    if (!fits31(tokens) || vocab >= (int64_t(1) << 30) || !fits31(width)) return TT_EUNSUPPORTED;
     return TT_OK;
 }
 
@@ -287,27 +461,45 @@ bool valid_ids(int id_dtype, const void *ids, int64_t tokens)
     return tokens == 0 || aligned_to(ids, id_dtype == TT_I32 ? 4 : 8);
 }
 
-// places of the sorted list per run: a run is added up by one group of lanes and the runs of a number by another, so both are
-// to stay short
-uint32_t run_length(int64_t tokens) { return tokens <= 8192 ? 32 : tokens <= 65536 ? 64 : 128; }
+// places of the sorted list per run: a run is added up by one wave and the runs of a number by another, so both are to stay short
+uint32_t run_length(int64_t tokens) { return tokens <= 16384 ? 32 : tokens <= 65536 ? 64 : 128; }
+
+// the numbers' places: 256 workgroups, one a CU, or as many as make a workgroup's counters enough
+Places places_of(int64_t vocab)
+{
+    Places s{0, 0};
+    while (s.wlog < 8 && (int64_t(1) << s.wlog) < vocab) ++s.wlog;
+    while (((vocab + (int64_t(1) << s.wlog) - 1) >> s.wlog) > kSortRange) ++s.wlog;
+    s.range = (uint32_t)((vocab + (int64_t(1) << s.wlog) - 1) >> s.wlog);
+    return s;
+}
 
 struct GradSpace {
     size_t order, start, partial, bytes;
     uint32_t runs;
+    Places to;
 };
 GradSpace grad_space(int64_t tokens, int64_t vocab, int64_t width)
 {
     GradSpace s;
     const uint32_t chunk = run_length(tokens);
     s.runs = tokens > chunk ? (uint32_t)((tokens + chunk - 1) / chunk) : 0;
+    s.to = places_of(vocab);
     s.order = 0;
     s.start = align_up((size_t)tokens * 4, 256);
-    s.partial = s.start + align_up(((size_t)vocab + 1) * 4, 256);
+    s.partial = s.start + align_up((((size_t)s.to.range << s.to.wlog) + 1) * 4, 256);
     s.bytes = s.partial + align_up((size_t)2 * s.runs * (size_t)width * 4, 256);
     return s;
 }
 
 tt_status launched() { return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE; }
+
+template <typename T, typename I> tt_status launch_embed(const EmbedParams &p, uint32_t grid, hipStream_t s)
+{
+    if (p.w.wide) hipLaunchKernelGGL((embed_wide_kernel<T, I>), dim3(grid), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((embed_narrow_kernel<T, I>), dim3(grid), dim3(kThreads), 0, s, p);
+    return launched();
+}
 
 } // namespace
 } // namespace tt
@@ -324,26 +516,18 @@ extern "C" tt_status tt_embed_forward(int64_t tokens, int64_t vocab, int64_t wid
     EmbedParams p;
     if (!make_blocks(W, tW, k, vocab, width, &p.W) || !make_blocks(const_cast<const void *const *>(X), tX, k, tokens, width, &p.X)) return TT_EINFEASIBLE;
     if (tokens == 0 || width == 0) return TT_OK;
-    p.s = split_row(p.W, p.X, width, 16 / e);
+    p.w = split_rows(p.W, p.X, width, 16 / e);
     p.ids = ids;
     p.tokens = (uint32_t)tokens;
     p.vocab = vocab;
     p.scale = scale;
-    const uint64_t units = (uint64_t)tokens * p.s.upr, groups = (uint64_t)kThreads >> p.s.glog, grid = (units + groups - 1) / groups;
-    if (grid * kThreads >= (uint64_t(1) << 32)) return TT_EUNSUPPORTED;
-    p.units = (uint32_t)units;
+    const uint64_t grid = groups_of(p.w, (uint64_t)tokens, 1);
+    if (grid * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED, 1 << k, tokens, width, e, (uint64_t)tokens * row * (1 + p.X.nrep), 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const dim3 g((uint32_t)grid), b(kThreads);
-    if (dtype == TT_BF16) {
-        if (id_dtype == TT_I32) hipLaunchKernelGGL((embed_forward_kernel<uint16_t, int32_t>), g, b, 0, s, p);
-        else hipLaunchKernelGGL((embed_forward_kernel<uint16_t, int64_t>), g, b, 0, s, p);
-    } else {
-        if (id_dtype == TT_I32) hipLaunchKernelGGL((embed_forward_kernel<float, int32_t>), g, b, 0, s, p);
-        else hipLaunchKernelGGL((embed_forward_kernel<float, int64_t>), g, b, 0, s, p);
-    }
-    return launched();
+    if (dtype == TT_BF16) return id_dtype == TT_I32 ? launch_embed<uint16_t, int32_t>(p, (uint32_t)grid, s) : launch_embed<uint16_t, int64_t>(p, (uint32_t)grid, s);
+    return id_dtype == TT_I32 ? launch_embed<float, int32_t>(p, (uint32_t)grid, s) : launch_embed<float, int64_t>(p, (uint32_t)grid, s);
 }
 
 extern "C" tt_status tt_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width, int k, int dtype, tt_tiling tdX,
@@ -363,11 +547,16 @@ namespace tt {
 namespace {
 
 template <typename T, typename I>
-tt_status launch_embed_grad(const SortParams &sp, EmbedGradParams &p, uint32_t sort_groups, uint32_t run_groups, uint32_t row_groups, hipStream_t s)
+tt_status launch_embed_grad(const SortParams &sp, const EmbedGradParams &p, uint32_t run_groups, uint32_t row_groups, hipStream_t s)
 {
-    hipLaunchKernelGGL((sort_tokens_kernel<I>), dim3(sort_groups), dim3(kSortThreads), 0, s, sp);
-    if (run_groups) hipLaunchKernelGGL((embed_runs_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
-    hipLaunchKernelGGL((embed_rows_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((sort_tokens_kernel<I>), dim3(1u << sp.to.wlog), dim3(kSortThreads), 0, s, sp);
+    if (p.w.wide) {
+        if (run_groups) hipLaunchKernelGGL((embed_runs_wide_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_rows_wide_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+    } else {
+        if (run_groups) hipLaunchKernelGGL((embed_runs_narrow_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_rows_narrow_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+    }
     return launched();
 }
 
@@ -393,34 +582,32 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     q.ids = ids;
     q.tokens = (uint32_t)tokens;
     q.vocab = vocab;
-    // a range of numbers per CU, at most what a workgroup's counters hold
-    const int64_t per_cu = (vocab + 255) / 256;
-    q.range = (uint32_t)(per_cu < kSortRange ? per_cu : kSortRange);
+    q.to = sp.to;
     q.order = reinterpret_cast<uint32_t *>(ws + sp.order);
     q.start = reinterpret_cast<uint32_t *>(ws + sp.start);
-    const uint32_t sort_groups = (uint32_t)((vocab + q.range - 1) / q.range);
-    p.s = split_row(p.G, p.W, width, 16 / e);
+    p.w = split_rows(p.G, p.W, width, 16 / e);
     p.ids = ids;
     p.order = q.order;
     p.start = q.start;
     p.partial = reinterpret_cast<float *>(ws + sp.partial);
+    p.to = sp.to;
+    p.places = sp.to.range << sp.to.wlog;
     p.chunk = run_length(tokens);
+    p.by_range = divisor(sp.to.range);
+    p.by_chunk = divisor(p.chunk);
     p.runs = sp.runs;
     p.cols = (uint32_t)width;
     p.vocab = vocab;
     p.scale = scale;
-    const uint64_t groups = (uint64_t)kThreads >> p.s.glog;
-    const uint64_t run_units = (uint64_t)sp.runs * p.s.upr, run_groups = (run_units + groups - 1) / groups;
-    const uint64_t row_groups = ((uint64_t)vocab * p.s.upr + groups - 1) / groups;
-    if (run_groups * kThreads >= (uint64_t(1) << 32) || row_groups * kThreads >= (uint64_t(1) << 32)) return TT_EUNSUPPORTED;
-    p.units = (uint32_t)run_units;
+    const uint64_t run_groups = groups_of(p.w, sp.runs, 1), row_groups = groups_of(p.w, p.places, kRows);
+    if (run_groups * kThreads >= (uint64_t(1) << 31) || row_groups * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED_GRAD, 1 << k, vocab, width, e, (uint64_t)tokens * row + (uint64_t)vocab * row * p.W.nrep, 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const uint32_t rg = (uint32_t)run_groups, wg = (uint32_t)row_groups;
     if (dtype == TT_BF16)
-        return id_dtype == TT_I32 ? launch_embed_grad<uint16_t, int32_t>(q, p, sort_groups, rg, wg, s)
-                                  : launch_embed_grad<uint16_t, int64_t>(q, p, sort_groups, rg, wg, s);
-    return id_dtype == TT_I32 ? launch_embed_grad<float, int32_t>(q, p, sort_groups, rg, wg, s)
-                              : launch_embed_grad<float, int64_t>(q, p, sort_groups, rg, wg, s);
+        return id_dtype == TT_I32 ? launch_embed_grad<uint16_t, int32_t>(q, p, rg, wg, s)
+                                  : launch_embed_grad<uint16_t, int64_t>(q, p, rg, wg, s);
+    return id_dtype == TT_I32 ? launch_embed_grad<float, int32_t>(q, p, rg, wg, s)
+                              : launch_embed_grad<float, int64_t>(q, p, rg, wg, s);
 }

@@ -11,162 +11,389 @@
 namespace tt {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct PolicyParams {
     BlockTable X, G;
     Pieces s;
+    Divisor by_ups;        // units (64 neighbouring vectors, one a lane of a wave) that are whole in a segment,
+    uint32_t units;        // ... in a row
+    uint32_t rest;         // vectors of a segment behind its whole units
     const void *actions;
+    uint32_t wide_ids, with_dx;
     const float *old_logp, *ref_logp, *advantage, *weight; // weight NULL: log probabilities alone
     float *logp, *row_loss;                                // either may be NULL
-    uint32_t tokens;
+    uint32_t tokens, groups; // rows, and the workgroups that share them
     int64_t vocab;
     tt_policy policy;
 };
 
-// What a row's statistics come to: its log probability, its part of the loss, and the derivative by the log probability
-struct RowLoss { float logp, loss, d; };
-
-__device__ __forceinline__ RowLoss row_loss(const PolicyParams &p, uint32_t t, float logp)
+__device__ __forceinline__ int64_t action_of(const PolicyParams &p, uint32_t t)
 {
-    RowLoss r{logp, 0.0f, 0.0f};
+    return p.wide_ids ? token_at<int64_t>(p.actions, t) : token_at<int32_t>(p.actions, t);
+}
+// whether a token counts as far as its weight and action go
+__device__ __forceinline__ bool counts(const PolicyParams &p, uint32_t t, int64_t a) { return a >= 0 && a < p.vocab && !(p.weight && p.weight[t] == 0.0f); }
+
+// Statistics of a part of a row, in base 2: the sum of 2^(x kk - top) over it, top the largest x kk (rounded: any number serves as
+// long as all use the same).  A part with nothing above -inf has top -inf and a sum of 0, or NaN where it holds one.
+struct Stats { float top, sum; };
+__device__ __forceinline__ Stats joined(Stats a, Stats b)
+{
+    const float top = fmaxf(a.top, b.top);
+    const float fa = a.top == -INFINITY ? 1.0f : wave::exp2_fast(a.top - top), fb = b.top == -INFINITY ? 1.0f : wave::exp2_fast(b.top - top);
+    return {top, a.sum * fa + b.sum * fb};
+}
+__device__ __forceinline__ Stats wave_joined(Stats s)
+{
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) s = joined(s, Stats{wave::shfl_xor(s.top, m), wave::shfl_xor(s.sum, m)});
+    return s;
+}
+// over a workgroup's waves, in their order; `red`: a Stats per wave
+template <int WAVES> __device__ __forceinline__ Stats group_joined(Stats s, Stats *red)
+{
+    s = wave_joined(s);
+    if constexpr (WAVES == 1) return s;
+    if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    float top = red[0].top;
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, red[i].top);
+    s = {top, 0.0f};
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) s.sum += red[i].sum * (red[i].top == -INFINITY ? 1.0f : wave::exp2_fast(red[i].top - top));
+    return s;
+}
+
+template <typename T> __device__ __forceinline__ float max_of(u32x4 v, float m)
+{
+    float f[kVec<T>];
+    unpack16(v, f, T());
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, f[i]);
+    return m;
+}
+template <typename T> __device__ __forceinline__ float sum_of(u32x4 v, float kk, float top, float s)
+{
+    float f[kVec<T>];
+    unpack16(v, f, T());
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) s += wave::exp2_fast(fmaf(f[i], kk, -top));
+    return s;
+}
+
+// What a row's statistics come to: its log probability, its part of the loss, the factor of p's numerators in its gradient and
+// what the action's entry has on top.  A few scalars a row, with the differences of near numbers (x_a kk - top, log probabilities)
+// taken in 64 bits: the loss is a sum of terms of both signs.
+struct RowResult { float logp, loss, coef, at_a; bool live; };
+__device__ __forceinline__ RowResult row_result(const PolicyParams &p, uint32_t t, Stats s, float xa, float kk)
+{
+    RowResult r{0.0f, 0.0f, 0.0f, 0.0f, true};
+    if (s.top == -INFINITY && s.sum == 0.0f) { // nothing above -inf
+        r.live = false;
+        return r;
+    }
+    int e = 0;
+    const float f = frexpf(s.sum, &e); // log2 of a number next to 1, and a whole number
+    const double lp = ((double)xa * (double)kk - (double)s.top - (double)e - (double)log2f(f)) * 0.6931471805599453;
+    r.logp = (float)lp;
     if (!p.weight) return r;
     const float w = p.weight[t], adv = p.advantage[t], lo = 1.0f - p.policy.clip_low, hi = 1.0f + p.policy.clip_high;
-    const float ratio = expf(logp - p.old_logp[t]);
+    const float ratio = expf((float)(lp - (double)p.old_logp[t]));
     const float clipped = ratio < lo ? lo : ratio > hi ? hi : ratio;
     const float a = ratio * adv, b = clipped * adv;
-    r.loss = a < b || a != a ? -a : -b;
+    float loss = a < b || a != a ? -a : -b;
     const bool held = (adv > 0.0f && ratio > hi) || (adv < 0.0f && ratio < lo);
-    r.d = held ? 0.0f : -a;
+    float d = held ? 0.0f : -a;
     if (p.policy.kl != 0.0f) {
-        const float diff = p.ref_logp[t] - logp, em1 = expm1f(diff);
-        r.loss += p.policy.kl * (em1 - diff);
-        r.d -= p.policy.kl * em1;
+        const float diff = (float)((double)p.ref_logp[t] - lp), em1 = expm1f(diff);
+        loss += p.policy.kl * (em1 - diff);
+        d -= p.policy.kl * em1;
     }
-    r.loss *= w;
-    r.d *= w;
+    r.loss = w * loss;
+    r.at_a = w * d * p.policy.scale;
+    r.coef = -r.at_a / s.sum;
     return r;
 }
-
-// Over a workgroup of WAVES waves; every thread gets the result.  `red` is WAVES floats that no earlier reader still needs.
-template <int WAVES> __device__ __forceinline__ float group_max(float v, float *red)
+__device__ __forceinline__ void store_scalars(const PolicyParams &p, uint32_t t, const RowResult &r)
 {
-    v = wave_max(v);
-    if constexpr (WAVES == 1) return v;
-    if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) v = fmaxf(v, red[i]);
-    return v;
-}
-template <int WAVES> __device__ __forceinline__ float group_sum(float v, float *red)
-{
-    v = wave_sum(v);
-    if constexpr (WAVES == 1) return v;
-    if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) v += red[i];
-    return v;
+    if (p.logp) p.logp[t] = r.logp;
+    if (p.row_loss) p.row_loss[t] = r.loss;
 }
 
-// One workgroup per token; the row is read for its maximum, for its sum and for its gradient (the later times from the caches,
-// where it fits).
-template <typename T, typename I, int THREADS> __global__ __launch_bounds__(THREADS) void policy_stream_kernel(const PolicyParams p)
+template <typename T> __device__ __forceinline__ u32x4 gradient_of(u32x4 v, float kk, float top, float coef)
 {
-    constexpr int EV = kVec<T>, WAVES = THREADS / 64;
-    __shared__ float red[2][WAVES];
-    const uint32_t t = blockIdx.x;
-    const int64_t a = token_at<I>(p.actions, t);
-    const bool in = a >= 0 && a < p.vocab && !(p.weight && p.weight[t] == 0.0f);
+    float f[kVec<T>];
+    unpack16(v, f, T());
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) f[i] = coef * wave::exp2_fast(fmaf(f[i], kk, -top));
+    return pack16(f, T());
+}
+
+// Where whole unit u of a row lies: segment and first vector
+struct Unit { uint32_t q, j0; };
+__device__ __forceinline__ Unit unit_of(const PolicyParams &p, uint32_t u)
+{
+    const uint32_t q = p.s.nseg == 1 ? 0 : quotient(u, p.by_ups);
+    return {q, (u - q * p.by_ups.d) * 64};
+}
+template <typename T> __device__ __forceinline__ u32x4 load_unit(const PolicyParams &p, uint32_t t, uint32_t u)
+{
+    const Unit g = unit_of(p, u);
+    const T *src = source_of<T>(p.X, p.s, p.s.a_shift, t, g.q) + g.j0 * kVec<T>;
+    return load16(src + (threadIdx.x & 63u) * kVec<T>);
+}
+template <typename T> __device__ __forceinline__ void store_unit(const PolicyParams &p, uint32_t t, uint32_t u, u32x4 v)
+{
+    const Unit g = unit_of(p, u);
+    const Place to = place_of(p.G, p.s, p.s.b_shift, t, g.q);
+    for (uint32_t x = 0; x < p.G.nrep; ++x) {
+        T *dst = static_cast<T *>(p.G.p[to.block + x]) + to.at + g.j0 * kVec<T>;
+        store16(dst + (threadIdx.x & 63u) * kVec<T>, v);
+    }
+}
+
+template <typename T> constexpr uint32_t kNothing = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u; // -inf
+// The rest of segment q, up to 64 vectors of which the last may be short: -inf where there is nothing
+template <typename T> __device__ __forceinline__ u32x4 load_rest(const PolicyParams &p, uint32_t t, uint32_t q)
+{
+    u32x4 r = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
+    const uint32_t j = p.by_ups.d * 64 + (threadIdx.x & 63u), n = values_of(p.s, kVec<T>, j);
+    if (n == 0) return r;
+    const T *src = source_of<T>(p.X, p.s, p.s.a_shift, t, q) + j * kVec<T>;
+    if (n == (uint32_t)kVec<T>) return load16(src);
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) {
+        if ((uint32_t)i >= n) continue;
+        if constexpr (sizeof(T) == 2) r[i >> 1] = i & 1 ? (r[i >> 1] & 0xffffu) | (uint32_t)src[i] << 16 : (r[i >> 1] & 0xffff0000u) | src[i];
+        else r[i] = __float_as_uint(src[i]);
+    }
+    return r;
+}
+template <typename T> __device__ __forceinline__ void store_rest(const PolicyParams &p, uint32_t t, uint32_t q, u32x4 v)
+{
+    const uint32_t j = p.by_ups.d * 64 + (threadIdx.x & 63u), n = values_of(p.s, kVec<T>, j);
+    if (n) store_all<T>(p.G, place_of(p.G, p.s, p.s.b_shift, t, q), j * kVec<T>, n, v);
+}
+
+// where column c of a row lies
+struct Column { uint32_t q, offset; };
+__device__ __forceinline__ Column column_of(const PolicyParams &p, uint32_t c)
+{
+    const uint32_t q = p.s.nseg == 1 ? 0 : c / p.s.seg;
+    return {q, c - q * p.s.seg};
+}
+template <typename T> __device__ __forceinline__ float logit_at(const PolicyParams &p, uint32_t t, const Column &c)
+{
+    return to_float(source_of<T>(p.X, p.s, p.s.a_shift, t, c.q)[c.offset]);
+}
+// The action's entry once more, with what it has on top, by the thread that wrote the vector it lies in: its later store of the two.
+template <typename T, int WAVES> __device__ __forceinline__ void store_action(const PolicyParams &p, uint32_t t, const Column &c, float v)
+{
+    const uint32_t j = c.offset / kVec<T>, unit = j / 64, wave = unit < p.by_ups.d ? (c.q * p.by_ups.d + unit) % WAVES : c.q % WAVES;
+    if (threadIdx.x != wave * 64 + (j & 63u)) return;
+    const Place to = place_of(p.G, p.s, p.s.b_shift, t, c.q);
+    for (uint32_t x = 0; x < p.G.nrep; ++x) static_cast<T *>(p.G.p[to.block + x])[to.at + c.offset] = from_float<T>(v);
+}
+
+// A row in the registers of a workgroup: up to NC vectors a thread of whole units, unit i * WAVES + w with wave w, and the rest of
+// segment w with it as well.  The row is read once, for its statistics and for its gradient.  Workgroups stay and take every
+// groups-th row: as a vector's gradient leaves, the next row's vector is fetched into its registers, so that memory always
+// has work while the workgroup computes.
+template <typename T, int WAVES, int NC> __global__ __launch_bounds__(WAVES * 64) void policy_rows_kernel(const PolicyParams p)
+{
+    __shared__ Stats red[2][WAVES];
+    const uint32_t w = uniform(threadIdx.x >> 6);
     const float kk = p.policy.scale * kLog2e;
-    RowLoss r{0.0f, 0.0f, 0.0f};
-    float top = 0.0f, coef = 0.0f;
-    bool live = false;
-    if (in) {
-        float m = -INFINITY;
-        for (uint32_t j = threadIdx.x; j < p.s.nvec; j += THREADS) {
-            uint32_t col, n;
-            vector_of(p.s, EV, j, &col, &n);
-            float f[EV];
-            unpack16(load_vector(source_of<T>(p.X, t, col), n), f, T());
+    const bool has_rest = p.rest && w < p.s.nseg;
+    uint32_t t = blockIdx.x;
+    int64_t a = action_of(p, t);
+    bool in = counts(p, t, a);
+    u32x4 r[NC], rest = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
 #pragma unroll
-            for (int i = 0; i < EV; ++i) m = (uint32_t)i < n ? fmaxf(m, f[i]) : m;
-        }
-        m = group_max<WAVES>(m, red[0]);
-        top = m * kk;
-        const bool bottom = m == -INFINITY; // nothing above -inf: all -inf, or NaN among them
-        float s = 0.0f;
-        for (uint32_t j = threadIdx.x; j < p.s.nvec; j += THREADS) {
-            uint32_t col, n;
-            vector_of(p.s, EV, j, &col, &n);
-            float f[EV];
-            unpack16(load_vector(source_of<T>(p.X, t, col), n), f, T());
-#pragma unroll
-            for (int i = 0; i < EV; ++i) {
-                const float e = bottom ? (f[i] == -INFINITY ? 0.0f : f[i]) : wave::exp2_fast(fmaf(f[i], kk, -top));
-                s += (uint32_t)i < n ? e : 0.0f;
-            }
-        }
-        s = group_sum<WAVES>(s, red[1]);
-        live = !(bottom && s == 0.0f);
-        if (live) {
-            const float xa = to_float(*source_of<T>(p.X, t, (uint32_t)a));
-            r = row_loss(p, t, (fmaf(xa, kk, -top) - log2f(s)) * kLn2);
-            coef = -r.d * p.policy.scale / s;
-        }
+    for (int i = 0; i < NC; ++i) {
+        r[i] = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
+        if (in && i * WAVES + w < p.units) r[i] = load_unit<T>(p, t, i * WAVES + w);
     }
-    if (threadIdx.x == 0) {
-        if (p.logp) p.logp[t] = r.logp;
-        if (p.row_loss) p.row_loss[t] = r.loss;
-    }
-    if (!p.G.p[0]) return;
-    const float at_a = r.d * p.policy.scale;
-    for (uint32_t j = threadIdx.x; j < p.s.nvec; j += THREADS) {
-        uint32_t col, n;
-        vector_of(p.s, EV, j, &col, &n);
-        float f[EV];
-        if (live) {
-            unpack16(load_vector(source_of<T>(p.X, t, col), n), f, T());
+    if (in && has_rest) rest = load_rest<T>(p, t, w);
+    uint32_t odd = 0;
+    for (;;) {
+        const uint32_t next = t + p.groups;
+        const bool more = next < p.tokens;
+        const int64_t next_a = more ? action_of(p, next) : -1;
+        const bool next_in = more && counts(p, next, next_a);
+        RowResult res{0.0f, 0.0f, 0.0f, 0.0f, false};
+        Stats s{0.0f, 0.0f};
+        Column ca{0, 0};
+        float xa = 0.0f;
+        if (in) {
+            ca = column_of(p, (uint32_t)a);
+            xa = logit_at<T>(p, t, ca);
+            float m = max_of<T>(rest, -INFINITY);
 #pragma unroll
-            for (int i = 0; i < EV; ++i) {
-                f[i] = coef * wave::exp2_fast(fmaf(f[i], kk, -top));
-                if ((int64_t)col + i == a) f[i] += at_a;
+            for (int i = 0; i < NC; ++i) {
+                if (i * WAVES + w < p.units) m = max_of<T>(r[i], m);
+                wave::forget(r[i]);
             }
-        } else {
+            s.top = m * kk;
+            const float from = m == -INFINITY ? 0.0f : s.top;
+            s.sum = sum_of<T>(rest, kk, from, 0.0f);
 #pragma unroll
-            for (int i = 0; i < EV; ++i) f[i] = 0.0f;
+            for (int i = 0; i < NC; ++i) {
+                if (i * WAVES + w < p.units) s.sum = sum_of<T>(r[i], kk, from, s.sum);
+                wave::forget(r[i]);
+            }
+            s = group_joined<WAVES>(s, red[odd]);
+            odd ^= 1; // (the next row's partial statistics must not overtake a wave that still reads these)
+            res = row_result(p, t, s, xa, kk);
         }
-        store_all<T>(p.G, t, col, n, pack16(f, T()));
+        if (threadIdx.x == 0) store_scalars(p, t, res);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            uint32_t u = i * WAVES + w;
+            wave::forget_uniform(u); // (addresses are worked out where they are used and not kept for all NC)
+            if (u < p.units) {
+                if (p.with_dx) store_unit<T>(p, t, u, res.live ? gradient_of<T>(r[i], kk, s.top, res.coef) : u32x4{0, 0, 0, 0});
+                if (next_in) r[i] = load_unit<T>(p, next, u);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (has_rest) {
+            if (p.with_dx) store_rest<T>(p, t, w, res.live ? gradient_of<T>(rest, kk, s.top, res.coef) : u32x4{0, 0, 0, 0});
+            if (next_in) rest = load_rest<T>(p, next, w);
+        }
+        if (p.with_dx && res.live) store_action<T, WAVES>(p, t, ca, fmaf(res.coef, wave::exp2_fast(fmaf(xa, kk, -s.top)), res.at_a));
+        if (!more) break;
+        t = next;
+        a = next_a;
+        in = next_in;
     }
 }
 
-// The rows' losses, added up in an order that depends on their number alone
-constexpr int kSumThreads = 1024;
+// Rows that do not fit: one workgroup per row, which reads it for its statistics and again for its gradient (from the caches,
+// where they hold it).
+constexpr int kStreamWaves = 16;
+template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void policy_stream_kernel(const PolicyParams p)
+{
+    constexpr int U = 4;
+    __shared__ Stats red[kStreamWaves];
+    const uint32_t t = blockIdx.x, w = uniform(threadIdx.x >> 6);
+    const int64_t a = action_of(p, t);
+    const float kk = p.policy.scale * kLog2e;
+    RowResult res{0.0f, 0.0f, 0.0f, 0.0f, false};
+    Stats s{-INFINITY, 0.0f};
+    Column ca{0, 0};
+    float xa = 0.0f;
+    const auto take = [&](const u32x4 *r, int n) {
+        float m = -INFINITY;
+        for (int i = 0; i < n; ++i) m = max_of<T>(r[i], m);
+        Stats part{m * kk, 0.0f};
+        const float from = m == -INFINITY ? 0.0f : part.top;
+        for (int i = 0; i < n; ++i) part.sum = sum_of<T>(r[i], kk, from, part.sum);
+        s = joined(s, part);
+    };
+    if (counts(p, t, a)) {
+        ca = column_of(p, (uint32_t)a);
+        xa = logit_at<T>(p, t, ca);
+        uint32_t u = w;
+        for (; u + (U - 1) * kStreamWaves < p.units; u += U * kStreamWaves) {
+            u32x4 r[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) r[i] = load_unit<T>(p, t, u + i * kStreamWaves);
+            take(r, U);
+        }
+        for (; u < p.units; u += kStreamWaves) {
+            const u32x4 r = load_unit<T>(p, t, u);
+            take(&r, 1);
+        }
+        if (p.rest)
+            for (uint32_t q = w; q < p.s.nseg; q += kStreamWaves) {
+                const u32x4 r = load_rest<T>(p, t, q);
+                take(&r, 1);
+            }
+        s = group_joined<kStreamWaves>(s, red);
+        res = row_result(p, t, s, xa, kk);
+    }
+    if (threadIdx.x == 0) store_scalars(p, t, res);
+    if (!p.with_dx) return;
+    const u32x4 zero = u32x4{0, 0, 0, 0};
+    uint32_t u = w;
+    for (; u + (U - 1) * kStreamWaves < p.units; u += U * kStreamWaves) {
+        u32x4 r[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) r[i] = res.live ? load_unit<T>(p, t, u + i * kStreamWaves) : zero;
+#pragma unroll
+        for (int i = 0; i < U; ++i) store_unit<T>(p, t, u + i * kStreamWaves, res.live ? gradient_of<T>(r[i], kk, s.top, res.coef) : zero);
+    }
+    for (; u < p.units; u += kStreamWaves) store_unit<T>(p, t, u, res.live ? gradient_of<T>(load_unit<T>(p, t, u), kk, s.top, res.coef) : zero);
+    if (p.rest)
+        for (uint32_t q = w; q < p.s.nseg; q += kStreamWaves) store_rest<T>(p, t, q, res.live ? gradient_of<T>(load_rest<T>(p, t, q), kk, s.top, res.coef) : zero);
+    if (res.live) store_action<T, kStreamWaves>(p, t, ca, fmaf(res.coef, wave::exp2_fast(fmaf(xa, kk, -s.top)), res.at_a));
+}
+
+// The rows' losses, added up in 64 bits in an order that depends on their number alone
+constexpr int kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void sum_losses_kernel(const float *row_loss, uint32_t n, float *loss)
 {
-    __shared__ float red[kSumThreads / 64];
-    float s = 0.0f;
-    for (uint32_t i = threadIdx.x; i < n; i += kSumThreads) s += row_loss[i];
-    s = group_sum<kSumThreads / 64>(s, red);
-    if (threadIdx.x == 0) *loss = s;
+    __shared__ double part[kSumThreads];
+    double s = 0.0;
+    for (uint32_t i = threadIdx.x; i < n; i += kSumThreads) s += (double)row_loss[i];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        s = (part[threadIdx.x] + part[threadIdx.x + 64]) + (part[threadIdx.x + 128] + part[threadIdx.x + 192]);
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) s += wave::shfl_xor(s, m);
+        if (threadIdx.x == 0) *loss = (float)s;
+    }
 }
 
 size_t policy_space(int64_t tokens) { return align_up((size_t)tokens * 4, 256); }
 
-template <typename T, typename I> tt_status launch_policy(const PolicyParams &p, hipStream_t s)
+// workgroups that fit the chip at a time: 16 waves of up to 128 registers on each of 256 CUs
+template <typename T, int WAVES, int NC> void launch_rows(PolicyParams &p, hipStream_t s)
 {
-    if (p.vocab >= 8192) hipLaunchKernelGGL((policy_stream_kernel<T, I, 1024>), dim3(p.tokens), dim3(1024), 0, s, p);
-    else hipLaunchKernelGGL((policy_stream_kernel<T, I, 256>), dim3(p.tokens), dim3(256), 0, s, p);
+    const uint32_t most = 256 * (16 / WAVES);
+    p.groups = p.tokens < most ? p.tokens : most;
+    hipLaunchKernelGGL((policy_rows_kernel<T, WAVES, NC>), dim3(p.groups), dim3(WAVES * 64), 0, s, p);
+}
+
+template <typename T> tt_status launch_policy(PolicyParams &p, hipStream_t s)
+{
+    const uint32_t u = p.units, q = p.rest ? p.s.nseg : 0; // whole units, and segments with a rest: one at most to a wave
+    const auto fits = [&](uint32_t waves, uint32_t nc) { return u <= waves * nc && q <= waves; };
+    if (!fits(16, 19)) {
+        hipLaunchKernelGGL((policy_stream_kernel<T>), dim3(p.tokens), dim3(kStreamWaves * 64), 0, s, p);
+    } else if (p.tokens <= 256) { // a CU to every row: as many waves as have something to do
+        if (fits(4, 1)) launch_rows<T, 4, 1>(p, s);
+        else if (fits(16, 2)) launch_rows<T, 16, 2>(p, s);
+        else if (fits(16, 4)) launch_rows<T, 16, 4>(p, s);
+        else if (fits(16, 8)) launch_rows<T, 16, 8>(p, s);
+        else if (fits(16, 16)) launch_rows<T, 16, 16>(p, s);
+        else launch_rows<T, 16, 19>(p, s);
+    } else {
+        if (fits(1, 4)) launch_rows<T, 1, 4>(p, s);
+        else if (fits(1, 16)) launch_rows<T, 1, 16>(p, s);
+        else if (fits(2, 16)) launch_rows<T, 2, 16>(p, s);
+        else if (fits(4, 16)) launch_rows<T, 4, 16>(p, s);
+        else if (fits(8, 16)) launch_rows<T, 8, 16>(p, s);
+        else if (fits(16, 16)) launch_rows<T, 16, 16>(p, s);
+        else launch_rows<T, 16, 19>(p, s);
+    }
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }
 
-tt_status launch_policy(const PolicyParams &p, int dtype, int id_dtype, hipStream_t s)
+tt_status launch_policy(PolicyParams &p, int dtype, int id_dtype, hipStream_t s)
 {
-    if (dtype == TT_BF16) return id_dtype == TT_I32 ? launch_policy<uint16_t, int32_t>(p, s) : launch_policy<uint16_t, int64_t>(p, s);
-    return id_dtype == TT_I32 ? launch_policy<float, int32_t>(p, s) : launch_policy<float, int64_t>(p, s);
+    p.wide_ids = id_dtype == TT_I64;
+    p.s = p.vocab > 0 ? pieces_of(p.X, p.G, p.vocab, 16 / dtype_bytes(dtype)) : Pieces{1, 0, 0, 0, 0, 0};
+    const uint32_t whole = (p.s.vps - (p.s.tail ? 1 : 0)) / 64;
+    p.by_ups = divisor(whole ? whole : 1);
+    p.by_ups.d = whole;
+    p.units = p.s.nseg * whole;
+    p.rest = p.s.vps - whole * 64;
+    return dtype == TT_BF16 ? launch_policy<uint16_t>(p, s) : launch_policy<float>(p, s);
 }
 
 tt_status check_sizes(int64_t tokens, int64_t vocab, int k, int dtype, const tt_tiling &tX)
@@ -214,13 +441,9 @@ extern "C" tt_status tt_policy_loss(const tt_policy *policy, int64_t tokens, int
     PolicyParams p;
     if (!make_blocks(X, tX, k, tokens, vocab, &p.X)) return TT_EINFEASIBLE;
     p.G = p.X;
-    if (dX) {
-        if (!make_blocks(const_cast<const void *const *>(dX), tdX, k, tokens, vocab, &p.G)) return TT_EINFEASIBLE;
-    } else {
-        for (void *&q : p.G.p) q = nullptr;
-    }
+    p.with_dx = dX != nullptr;
+    if (dX && !make_blocks(const_cast<const void *const *>(dX), tdX, k, tokens, vocab, &p.G)) return TT_EINFEASIBLE;
     if (tokens > 0 && (!workspace || ws_bytes < policy_space(tokens) || reinterpret_cast<uintptr_t>(workspace) % 256)) return TT_EWORKSPACE;
-    p.s = vocab > 0 ? pieces_of(p.X, p.G, vocab, 16 / e) : Pieces{1, 0, 0, 0};
     p.actions = actions;
     p.old_logp = old_logp;
     p.ref_logp = ref_logp;
@@ -253,8 +476,7 @@ extern "C" tt_status tt_token_logp(int64_t tokens, int64_t vocab, int k, int dty
     if (tokens == 0) return TT_OK;
     if (!workspace || ws_bytes < policy_space(tokens) || reinterpret_cast<uintptr_t>(workspace) % 256) return TT_EWORKSPACE;
     p.G = p.X;
-    for (void *&q : p.G.p) q = nullptr;
-    p.s = vocab > 0 ? pieces_of(p.X, p.G, vocab, 16 / e) : Pieces{1, 0, 0, 0};
+    p.with_dx = 0;
     p.actions = ids;
     p.old_logp = p.ref_logp = p.advantage = p.weight = nullptr;
     p.logp = logp;

@@ -14,6 +14,7 @@ namespace wave {
 __device__ __forceinline__ uint32_t lane() { return threadIdx.x & 63u; }
 __device__ __forceinline__ float shfl_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
 __device__ __forceinline__ uint32_t shfl_xor(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask, 64); }
+__device__ __forceinline__ double shfl_xor(double v, int mask) { return __shfl_xor(v, mask, 64); }
 __device__ __forceinline__ uint32_t shfl_up(uint32_t v, int by) { return (uint32_t)__shfl_up((int)v, by, 64); }
 __device__ __forceinline__ uint32_t read_lane(uint32_t v, int from) { return (uint32_t)__builtin_amdgcn_readlane((int)v, from); }
 __device__ __forceinline__ uint64_t ballot(bool p) { return __ballot(p); }
@@ -25,6 +26,10 @@ __device__ __forceinline__ void fence()
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
+// The compiler takes v for a new value from here on: what it worked out from v before is worked out again instead of being kept
+// (a row that waits in registers as 16 bits a value must not wait as 32).
+template <typename V> __device__ __forceinline__ void forget(V &v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void forget_uniform(uint32_t &v) { asm volatile("" : "+s"(v)); }
 // 2^x (1 ulp; what lies below 2^-126 is 0)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -5,6 +5,8 @@
 #error "the token operators' kernels read what other lanes wrote: lock-step emulation only"
 #endif
 
+inline uint32_t __umulhi(uint32_t a, uint32_t b) { return (uint32_t)(((uint64_t)a * b) >> 32); }
+
 namespace tt {
 namespace wave {
 
@@ -23,6 +25,15 @@ template <class F> inline uint32_t exchange(int kind, uint32_t v, F &&from)
 }
 inline uint32_t shfl_xor(uint32_t v, int mask) { return exchange(10, v, [&](int l) { return l ^ mask; }); }
 inline float shfl_xor(float v, int mask) { return __uint_as_float(shfl_xor(__float_as_uint(v), mask)); }
+inline double shfl_xor(double v, int mask)
+{
+    uint32_t h[2];
+    std::memcpy(h, &v, 8);
+    h[0] = shfl_xor(h[0], mask);
+    h[1] = shfl_xor(h[1], mask);
+    std::memcpy(&v, h, 8);
+    return v;
+}
 inline uint32_t shfl_up(uint32_t v, int by) { return exchange(11, v, [&](int l) { return l >= by ? l - by : l; }); }
 inline uint32_t read_lane(uint32_t v, int from) { return exchange(12, v, [&](int) { return from; }); }
 inline uint64_t ballot(bool p)
@@ -37,6 +48,8 @@ inline uint64_t ballot(bool p)
 }
 inline void lds_add(uint32_t *p, uint32_t v) { *p += v; }
 inline void fence() { emu::wave_sync(); }
+template <typename V> inline void forget(V &) {}
+inline void forget_uniform(uint32_t &) {}
 inline float exp2_fast(float x) { return std::exp2(x); }
 
 } // namespace wave

@@ -150,6 +150,24 @@ def test_embedding(T, V, D, dt):
     run_embed(T, V, D, dt, seed=T)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,D", [(40, 20, 600), (129, 300, 2052), (200, 3, 1031), (3, 1000, 4100)])
+def test_embedding_of_wide_rows(T, V, D, dt):
+    run_embed(T, V, D, dt, seed=D)
+
+
+@pytest.mark.parametrize("tW,tX,D", [("C", "R", 1200), ("RC", "Cr", 2064), ("CC", "RR", 4200)])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_embedding_of_wide_rows_tiled(tW, tX, D, dt):
+    run_embed(100, 40, D, dt, tW, tX, seed=D)
+
+
+def test_embedding_of_large_vocabularies_and_many_tokens():
+    run_embed(3000, 1500, 40, "f32", seed=5)
+    run_embed(700, 270000, 3, "bf16", seed=6)      # more numbers than 256 workgroups' counters hold
+    run_embed(20000, 7, 16, "f32", seed=7)
+
+
 @pytest.mark.parametrize("tW,tX", [("R", "C"), ("C", "r"), ("r", "R"), ("RC", "CR"), ("rC", "Cr"), ("CC", "RR"), ("RCr", "CCC")])
 @pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 24), ("bf16", 40)])
 def test_embedding_tiled(tW, tX, dt, D):
@@ -201,8 +219,8 @@ def policy_inputs(T, V, dt, seed, scale, kl, masked):
             if t % 11 == 6:
                 a[t] = V if t % 2 else -1
             if t % 13 == 8:     # one logit left, and it is the action's
-                keep = x[t, a[t]]
-                if 0 <= a[t] < V and np.isfinite(keep):
+                keep = x[t, a[t]] if 0 <= a[t] < V else np.nan
+                if np.isfinite(keep):
                     put(t, slice(None), -np.inf)
                     put(t, int(a[t]), keep)
     logp = tk.token_logp(np.where(np.isnan(x) | (x == np.inf), 0.0, x), a, scale)
@@ -266,6 +284,18 @@ def run_policy(T, V, dt, tX="", tG="", idt="i64", seed=1, scale=1.0, kl=0.05, ma
 @pytest.mark.parametrize("T,V", [(1, 1), (1, 2), (3, 7), (5, 64), (33, 1000), (4, 2051), (2, 8200)])
 def test_policy_loss(T, V, dt):
     run_policy(T, V, dt, seed=T + V)
+
+
+@pytest.mark.parametrize("T,V,dt", [(4300, 40, "f32"), (4200, 530, "bf16"), (2300, 1100, "f32"), (1100, 4200, "f32"), (560, 16600, "bf16"), (270, 66000, "bf16"),
+                                    (258, 70000, "f32"), (3, 90000, "f32"), (2, 140001, "bf16"), (5, 160000, "bf16")])
+def test_policy_loss_of_more_rows_than_workgroups_and_of_long_rows(T, V, dt):
+    run_policy(T, V, dt, seed=V, masked=T < 4000)
+
+
+@pytest.mark.parametrize("tX,tG,V", [("C", "R", 1100), ("CC", "RC", 4140), ("RC", "CC", 2084), ("CCCCC", "RRCCC", 17600)])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_policy_loss_of_long_rows_tiled(tX, tG, V, dt):
+    run_policy(8, V, dt, tX, tG, "i32", seed=V, masked=True)
 
 
 @pytest.mark.parametrize("tX,tG", [("C", "R"), ("R", "C"), ("r", "C"), ("CC", "RC"), ("CR", "rr"), ("rC", "Cr"), ("CCC", "RRC")])

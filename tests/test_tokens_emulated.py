@@ -48,6 +48,11 @@ def test_embedding(T, V, D, dt):
     g.run_embed(T, V, D, dt, seed=T)
 
 
+@pytest.mark.parametrize("T,V,D,dt,tW,tX", [(40, 20, 600, "bf16", "", ""), (45, 3, 1031, "f32", "", ""), (40, 8, 1200, "bf16", "C", "R"), (36, 6, 532, "f32", "rC", "CR")])
+def test_embedding_of_wide_rows(T, V, D, dt, tW, tX):
+    g.run_embed(T, V, D, dt, tW, tX, seed=D)
+
+
 @pytest.mark.parametrize("tW,tX,dt,D", [("R", "C", "bf16", 64), ("RC", "CR", "f32", 24), ("rC", "Cr", "bf16", 40), ("RCr", "CCC", "bf16", 40)])
 def test_embedding_tiled(tW, tX, dt, D):
     g.run_embed(40, 48, D, dt, tW, tX, "i32", seed=len(tW) + D)
@@ -70,6 +75,11 @@ def test_policy_loss(T, V, dt, masked):
 @pytest.mark.parametrize("tX,tG,dt,V", [("C", "R", "bf16", 512), ("CC", "RC", "f32", 328), ("CR", "rr", "bf16", 104), ("rC", "Cr", "f32", 36), ("CCC", "RRC", "bf16", 104)])
 def test_policy_loss_tiled(tX, tG, dt, V):
     g.run_policy(16, V, dt, tX, tG, "i32", seed=len(tX), masked=True, scale=0.7)
+
+
+@pytest.mark.parametrize("tX,tG,dt,V", [("", "", "bf16", 17000), ("C", "R", "bf16", 1100), ("RC", "CC", "f32", 2084), ("CCCCC", "RRCCC", "f32", 17600)])
+def test_policy_loss_of_long_rows(tX, tG, dt, V):
+    g.run_policy(4, V, dt, tX, tG, "i32", seed=V, masked=True)
 
 
 def test_policy_special_rows():
