@@ -15,8 +15,11 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kU = 2;     // vectors per lane of a wave's part of a segment
-constexpr int kBatch = 4; // rows that are on their way together
-constexpr int kRows = 8;  // rows of the table's gradient per wave
+#ifndef VRB
+#define VRB 8
+#define VWB 4
+#endif
+constexpr int kRunBatch = VRB, kRowBatch = VWB; // rows that are on their way together
 
 // How the segments of a row are shared out.  Wide segments (more than 32 vectors): a part of kU vectors per lane to a wave, so
 // that a wave's row, segment and addresses are scalars.  Narrow ones: a vector per lane, a segment to 2^glog lanes.
@@ -243,31 +246,42 @@ struct EmbedGradParams {
     const uint32_t *order, *start;
     float *partial; // [2 runs][cols]: run c's part of a number that began before the run, of one that begins inside it
     Places to;
-    Divisor by_range, by_chunk;
+    Divisor by_chunk;
     uint32_t places; // 2^wlog * range
     uint32_t chunk, runs, cols;
+    uint32_t rows; // of the table's gradient per wave (wide)
     int64_t vocab;
     float scale;
 };
-// the number at a place of the sorted order
-__device__ __forceinline__ uint32_t number_of(const EmbedGradParams &p, uint32_t at)
-{
-    const uint32_t w = quotient(at, p.by_range);
-    return ((at - w * p.to.range) << p.to.wlog) + w;
-}
 __device__ __forceinline__ float *partial_of(const EmbedGradParams &p, uint32_t run, bool inside, uint32_t q)
 {
     return p.partial + (size_t)(2 * run + (inside ? 1 : 0)) * p.cols + (size_t)q * p.w.s.seg;
 }
 
-// 64 places of the sorted list in the lanes of a wave, of those that the wave will ask for (up to `end`)
-struct Window {
-    uint32_t base, end, tokens;
-    __device__ __forceinline__ void load(const EmbedGradParams &p, uint32_t at)
+// Where a wave's part of a segment lies in the rows of the tokens' gradients.  Cuts by rows make the block a matter of the token;
+// the lanes then hold the table of blocks (a scalar load per row would be a trip to memory per row).
+template <typename T> struct Sources {
+    const T *base; // nothing cut by rows: of token 0
+    uint32_t lo, hi, block, at;
+    __device__ __forceinline__ Sources(const EmbedGradParams &p, const WaveWork &g)
     {
-        base = at;
-        const uint32_t i = at + (threadIdx.x & 63u);
-        tokens = i < end ? p.order[i] : 0;
+        const uint32_t cb = g.q >> p.w.s.a_shift;
+        at = (g.q - (cb << p.w.s.a_shift)) * p.w.s.seg + g.j0 * kVec<T>;
+        block = cb * p.G.nrep;
+        base = static_cast<const T *>(p.G.p[block]) + at;
+        lo = hi = 0;
+        if (p.G.nR > 1) {
+            const uint64_t mine = (uint64_t)(uintptr_t)p.G.p[threadIdx.x & 63u];
+            lo = (uint32_t)mine;
+            hi = (uint32_t)(mine >> 32);
+        }
+    }
+    __device__ __forceinline__ const T *row(const EmbedGradParams &p, uint32_t t) const
+    {
+        if (p.G.nR == 1) return base + (size_t)t * p.G.scols;
+        const uint32_t rb = quotient(t, p.G.by_srows), b = rb * p.G.nC * p.G.nrep + block;
+        const uint64_t q = (uint64_t)wave::read_lane(hi, (int)b) << 32 | wave::read_lane(lo, (int)b);
+        return reinterpret_cast<const T *>((uintptr_t)q) + (size_t)(t - rb * p.G.srows) * p.G.scols + at;
     }
 };
 
@@ -291,29 +305,35 @@ template <typename T> struct Sums {
     }
 };
 
-// the rows of places [b, e) added to the sums in that order, BATCH of them on their way at a time
-template <typename T, int BATCH> __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, const WaveWork &g, Window &win, uint32_t b, uint32_t e)
+// n rows (all of them where n >= BATCH) added to the sums in order, on their way together; token(k): the k-th
+template <typename T, int BATCH, class F>
+__device__ __forceinline__ void add_batch(Sums<T> &a, const EmbedGradParams &p, const Sources<T> &src, uint32_t n, F &&token)
 {
     const uint32_t lane = threadIdx.x & 63u;
-    for (uint32_t i = b; i < e; i += BATCH) {
-        if (i + BATCH > win.base + 64) win.load(p, i);
-        u32x4 r[BATCH][kU];
+    u32x4 r[BATCH][kU];
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            if (i + k >= e) break;
-            const T *src = source_of<T>(p.G, p.w.s, p.w.s.a_shift, wave::read_lane(win.tokens, (int)(i + k - win.base)), g.q);
+    for (int k = 0; k < BATCH; ++k) {
+        if ((uint32_t)k >= n) break;
+        const T *from = src.row(p, token(k));
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                r[k][u] = u32x4{0, 0, 0, 0};
-                if (a.n[u]) r[k][u] = load_vector(src + (g.j0 + u * 64 + lane) * kVec<T>, a.n[u]);
-            }
+        for (int u = 0; u < kU; ++u) {
+            r[k][u] = u32x4{0, 0, 0, 0};
+            if (a.n[u]) r[k][u] = load_vector(from + (u * 64 + lane) * kVec<T>, a.n[u]);
         }
+    }
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            if (i + k >= e) break;
+    for (int k = 0; k < BATCH; ++k) {
+        if ((uint32_t)k >= n) break;
 #pragma unroll
-            for (int u = 0; u < kU; ++u) a.add(u, r[k][u]);
-        }
+        for (int u = 0; u < kU; ++u) a.add(u, r[k][u]);
+    }
+}
+// the rows of places [b, e) of the sorted list
+template <typename T, int BATCH> __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, const Sources<T> &src, uint32_t b, uint32_t e)
+{
+    for (uint32_t w = b; w < e; w += 64) {
+        const uint32_t mine = w + (threadIdx.x & 63u), tokens = mine < e ? p.order[mine] : 0, n = e - w < 64 ? e - w : 64;
+        for (uint32_t i = 0; i < n; i += BATCH) add_batch<T, BATCH>(a, p, src, n - i, [&](int k) { return wave::read_lane(tokens, (int)i + k); });
     }
 }
 
@@ -325,6 +345,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     if (c >= p.runs || b >= total) return;
     const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
     const uint32_t first = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[b])), last = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[e - 1]));
+    const Sources<T> src(p, g);
     Sums<T> a;
 #pragma unroll
     for (int u = 0; u < kU; ++u) a.n[u] = values_of(p.w.s, kVec<T>, g.j0 + u * 64 + lane);
@@ -334,10 +355,8 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
         const uint32_t at = side == 0 ? first : last, vb = p.start[at], ve = p.start[at + 1];
         if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
         const uint32_t lo = vb > b ? vb : b, hi = ve < e ? ve : e;
-        Window win{0, hi, 0};
-        win.load(p, lo);
         a.clear();
-        add_rows<T, kBatch>(a, p, g, win, lo, hi);
+        add_rows<T, kRunBatch>(a, p, src, lo, hi);
         float *to = partial_of(p, c, vb > b, g.q);
 #pragma unroll
         for (int u = 0; u < kU; ++u)
@@ -372,30 +391,34 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     }
 }
 
-// (3) A wave does kRows neighbouring places: where their tokens begin comes in one load, and so do the tokens.
+// (3) A wave does up to 8 neighbouring numbers, 8 lanes to each of them: where their tokens begin comes in one load, and the first
+// 8 tokens of each in another.
 template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_wide_kernel(const EmbedGradParams p)
 {
     const WaveWork g = wave_work(p.w);
-    const uint32_t lane = threadIdx.x & 63u, at0 = g.row * kRows;
-    if (at0 >= p.places) return;
-    const uint32_t at_lane = at0 + (lane < (uint32_t)kRows ? lane : (uint32_t)kRows);
-    const uint32_t starts = p.start[at_lane < p.places ? at_lane : p.places];
-    const uint32_t first = wave::read_lane(starts, 0), end = wave::read_lane(starts, kRows);
-    Window win{0, end, 0};
-    win.load(p, first);
+    const uint32_t lane = threadIdx.x & 63u, v0 = g.row * p.rows, vocab = (uint32_t)p.vocab;
+    if (v0 >= vocab) return;
+    const uint32_t rows = vocab - v0 < p.rows ? vocab - v0 : p.rows;
+    uint32_t begin = 0, end = 0, tokens = 0;
+    if ((lane >> 3) < rows) {
+        const uint32_t at = place(p.to, v0 + (lane >> 3));
+        begin = p.start[at];
+        end = p.start[at + 1];
+        if (begin + (lane & 7u) < end) tokens = p.order[begin + (lane & 7u)];
+    }
+    const Sources<T> src(p, g);
     Sums<T> a;
 #pragma unroll
     for (int u = 0; u < kU; ++u) a.n[u] = values_of(p.w.s, kVec<T>, g.j0 + u * 64 + lane);
 #pragma unroll 1
-    for (int k = 0; k < kRows; ++k) {
-        if (at0 + k >= p.places) break;
-        const uint32_t v = number_of(p, at0 + k);
-        if ((int64_t)v >= p.vocab) continue;
-        const uint32_t b = wave::read_lane(starts, k), e = wave::read_lane(starts, k + 1);
+    for (uint32_t k = 0; k < rows; ++k) {
+        const uint32_t v = v0 + k, b = wave::read_lane(begin, (int)k * 8), e = wave::read_lane(end, (int)k * 8);
         const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q);
         a.clear();
         if (e - b <= p.chunk) {
-            add_rows<T, kBatch>(a, p, g, win, b, e);
+            const uint32_t n = e - b < 8 ? e - b : 8;
+            for (uint32_t i = 0; i < n; i += kRowBatch) add_batch<T, kRowBatch>(a, p, src, n - i, [&](int j) { return wave::read_lane(tokens, (int)(k * 8 + i) + j); });
+            if (b + 8 < e) add_rows<T, kRowBatch>(a, p, src, b + 8, e);
         } else {
             for (uint32_t c = quotient(b, p.by_chunk); c * p.chunk < e; ++c) {
                 const float *from = partial_of(p, c, b > c * p.chunk, g.q);
@@ -419,11 +442,9 @@ template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_wid
 template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_narrow_kernel(const EmbedGradParams p)
 {
     const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
-    if (g.row >= p.places || n == 0) return;
-    const uint32_t v = number_of(p, g.row);
-    if ((int64_t)v >= p.vocab) return;
-    const uint32_t b = p.start[g.row], e = p.start[g.row + 1];
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j), v = g.row;
+    if ((int64_t)v >= p.vocab || n == 0) return;
+    const uint32_t at = place(p.to, v), b = p.start[at], e = p.start[at + 1];
     float s[kVec<T>] = {};
     if (e - b <= p.chunk) {
         for (uint32_t i = b; i < e; ++i) {
@@ -593,13 +614,15 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     p.to = sp.to;
     p.places = sp.to.range << sp.to.wlog;
     p.chunk = run_length(tokens);
-    p.by_range = divisor(sp.to.range);
     p.by_chunk = divisor(p.chunk);
     p.runs = sp.runs;
     p.cols = (uint32_t)width;
     p.vocab = vocab;
     p.scale = scale;
-    const uint64_t run_groups = groups_of(p.w, sp.runs, 1), row_groups = groups_of(p.w, p.places, kRows);
+    // as many as leave every CU 32 waves
+    const uint64_t waves = (uint64_t)vocab * p.w.s.nseg * p.w.parts;
+    p.rows = waves >= 8 * 8192 ? 8 : waves >= 4 * 8192 ? 4 : waves >= 2 * 8192 ? 2 : 1;
+    const uint64_t run_groups = groups_of(p.w, sp.runs, 1), row_groups = groups_of(p.w, (uint64_t)vocab, p.rows);
     if (run_groups * kThreads >= (uint64_t(1) << 31) || row_groups * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED_GRAD, 1 << k, vocab, width, e, (uint64_t)tokens * row + (uint64_t)vocab * row * p.W.nrep, 0);

@@ -51,16 +51,16 @@ template <typename T> __device__ __forceinline__ u32x4 load_part(const T *p, uin
 {
     uint32_t w[4] = {0, 0, 0, 0};
     for (uint32_t i = 0; i < n; ++i) {
-        if constexpr (sizeof(T) == 2) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-        else w[i] = __float_as_uint(p[i]);
+        if constexpr (sizeof(T) == 2) w[i >> 1] |= (uint32_t)load1(p + i) << (16 * (i & 1));
+        else w[i] = __float_as_uint(load1(p + i));
     }
     return u32x4{w[0], w[1], w[2], w[3]};
 }
 template <typename T> __device__ __forceinline__ void store_part(T *p, u32x4 v, uint32_t n)
 {
     for (uint32_t i = 0; i < n; ++i) {
-        if constexpr (sizeof(T) == 2) p[i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
-        else p[i] = __uint_as_float(v[i]);
+        if constexpr (sizeof(T) == 2) store1(p + i, (uint16_t)(v[i >> 1] >> (16 * (i & 1))));
+        else store1(p + i, __uint_as_float(v[i]));
     }
 }
 
@@ -77,6 +77,8 @@ template <typename T> __device__ __forceinline__ void store_all(const BlockTable
 
 template <typename T> __device__ __forceinline__ u32x4 load_vector(const T *p, uint32_t n) { return n == (uint32_t)kVec<T> ? load16(p) : load_part(p, n); }
 
-template <typename I> __device__ __forceinline__ int64_t token_at(const void *ids, size_t i) { return (int64_t) static_cast<const I *>(ids)[i]; }
+template <typename I> __device__ __forceinline__ int64_t token_at(const void *ids, size_t i) { return (int64_t)load1(static_cast<const I *>(ids) + i); }
+// ... at an index that all lanes share
+template <typename I> __device__ __forceinline__ int64_t token_scalar(const void *ids, size_t i) { return (int64_t)load_scalar(static_cast<const I *>(ids) + i); }
 
 } // namespace tt

@@ -7,7 +7,15 @@
 #include "tt_bf16.h"
 #ifdef TT_HOST_EMULATION
 #include "emu_wave.h"
+#define TT_GLOBAL
+#define TT_CONSTANT
 #else
+// Memory that is not LDS, said so: for a pointer out of a table the compiler makes accesses that could be either, which count as
+// both and are waited for as such.
+#define TT_GLOBAL __attribute__((address_space(1)))
+// Memory that nothing writes while the kernel runs: a value at an address that all lanes share comes as a scalar, and is waited
+// for apart from the vectors on their way.
+#define TT_CONSTANT __attribute__((address_space(4)))
 namespace tt {
 namespace wave {
 
@@ -42,6 +50,8 @@ namespace tt {
 // a value that all lanes of a wave hold, in a scalar register
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
+__device__ __forceinline__ uint64_t uniform(uint64_t v) { return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
+
 __device__ __forceinline__ float wave_max(float v)
 {
 #pragma unroll
@@ -70,13 +80,19 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T> __device__ __forceinline__ u32x4 load16(const T *p)
 {
-    const typename Vec16<sizeof(T)>::type v = *reinterpret_cast<const typename Vec16<sizeof(T)>::type *>(p);
+    typedef typename Vec16<sizeof(T)>::type V;
+    const V v = *(const TT_GLOBAL V *)p;
     return u32x4{v.x, v.y, v.z, v.w};
 }
 template <typename T> __device__ __forceinline__ void store16(T *p, u32x4 v)
 {
-    *reinterpret_cast<typename Vec16<sizeof(T)>::type *>(p) = v;
+    typedef typename Vec16<sizeof(T)>::type V;
+    *(TT_GLOBAL V *)p = v;
 }
+
+template <typename T> __device__ __forceinline__ T load_scalar(const T *p) { return *(const TT_CONSTANT T *)p; }
+template <typename T> __device__ __forceinline__ T load1(const T *p) { return *(const TT_GLOBAL T *)p; }
+template <typename T> __device__ __forceinline__ void store1(T *p, T v) { *(TT_GLOBAL T *)p = v; }
 
 // ---- element types: bf16 travels as its 16 bits
 __device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
