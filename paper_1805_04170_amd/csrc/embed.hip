@@ -15,11 +15,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kU = 2;     // vectors per lane of a wave's part of a segment
-#ifndef VRB
-#define VRB 8
-#define VWB 4
-#endif
-constexpr int kRunBatch = VRB, kRowBatch = VWB; // rows that are on their way together
+constexpr int kRunBatch = 8, kRowBatch = 4, kPartials = 4; // rows, or partial sums, that are on their way together
 
 // How the segments of a row are shared out.  Wide segments (more than 32 vectors): a part of kU vectors per lane to a wave, so
 // that a wave's row, segment and addresses are scalars.  Narrow ones: a vector per lane, a segment to 2^glog lanes.
@@ -44,10 +40,10 @@ Split split_rows(const BlockTable &a, const BlockTable &b, int64_t cols, int ev)
     return w;
 }
 
-// workgroups for `rows` rows, `per_wave` of them to a wave of the wide form
-uint64_t groups_of(const Split &w, uint64_t rows, uint64_t per_wave)
+// workgroups for `rows` rows
+uint64_t groups_of(const Split &w, uint64_t rows)
 {
-    if (w.wide) return ((rows + per_wave - 1) / per_wave * w.s.nseg * w.parts + kWaves - 1) / kWaves;
+    if (w.wide) return (rows * w.s.nseg * w.parts + kWaves - 1) / kWaves;
     return ((rows * w.s.nseg << w.glog) + kThreads - 1) / kThreads;
 }
 
@@ -67,6 +63,40 @@ __device__ __forceinline__ LaneWork lane_work(const Split &w)
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x, g = i >> w.glog, row = quotient(g, w.by_nseg);
     return {row, g - row * w.s.nseg, i & ((1u << w.glog) - 1)};
 }
+
+// A wave's vectors of a segment, one per lane and u.  Every lane loads whole vectors, so that no load depends on a lane: a
+// segment's last vector, where it is short, is the values that end with the segment (those in front of its own are its
+// neighbour's too), lanes past the end take it as well; `own` says how many of a vector's last values are the lane's to store.
+template <typename T> struct Columns {
+    uint32_t col[kU], own[kU];
+    __device__ __forceinline__ Columns(const Pieces &s, uint32_t j0)
+    {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const uint32_t j = j0 + u * 64 + (threadIdx.x & 63u), last = s.seg - kVec<T>;
+            own[u] = values_of(s, kVec<T>, j);
+            col[u] = j * kVec<T> < last ? j * kVec<T> : last;
+        }
+    }
+    // into every replica of a segment that begins at `to`
+    __device__ __forceinline__ void store(const BlockTable &b, const Place &to, int u, u32x4 v) const
+    {
+        if (own[u] == 0) return;
+        for (uint32_t x = 0; x < b.nrep; ++x) {
+            T *dst = static_cast<T *>(b.p[to.block + x]) + to.at + col[u];
+            if (own[u] == (uint32_t)kVec<T>) {
+                store16(dst, v);
+                continue;
+            }
+#pragma unroll
+            for (int i = 1; i < kVec<T>; ++i) {
+                if ((uint32_t)i < kVec<T> - own[u]) continue;
+                if constexpr (sizeof(T) == 2) store1(dst + i, (uint16_t)(v[i >> 1] >> (16 * (i & 1))));
+                else store1(dst + i, __uint_as_float(v[i]));
+            }
+        }
+    }
+};
 
 template <typename T> __device__ __forceinline__ u32x4 scaled(u32x4 v, float scale)
 {
@@ -93,25 +123,21 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 {
     const WaveWork g = wave_work(p.w);
     if (g.row >= p.tokens) return;
-    const int64_t v = token_at<I>(p.ids, g.row);
-    const bool in = v >= 0 && v < p.vocab;
-    const uint32_t lane = threadIdx.x & 63u;
-    u32x4 r[kU];
-    uint32_t n[kU];
-    const T *src = in ? source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q) : nullptr;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        const uint32_t j = g.j0 + u * 64 + lane;
-        n[u] = values_of(p.w.s, kVec<T>, j);
-        r[u] = u32x4{0, 0, 0, 0};
-        if (in && n[u]) r[u] = load_vector(src + j * kVec<T>, n[u]);
-    }
+    const int64_t v = token_scalar<I>(p.ids, g.row);
+    const Columns<T> c(p.w.s, g.j0);
     const Place to = place_of(p.X, p.w.s, p.w.s.b_shift, g.row, g.q);
+    u32x4 r[kU];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        if (n[u] == 0) continue;
-        store_all<T>(p.X, to, (g.j0 + u * 64 + lane) * kVec<T>, n[u], in ? scaled<T>(r[u], p.scale) : r[u]);
+    for (int u = 0; u < kU; ++u) r[u] = u32x4{0, 0, 0, 0};
+    if (v >= 0 && v < p.vocab) {
+        const T *src = source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) r[u] = load16(src + c.col[u]);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) r[u] = scaled<T>(r[u], p.scale);
     }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) c.store(p.X, to, u, r[u]);
 }
 
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_narrow_kernel(const EmbedParams p)
@@ -249,7 +275,7 @@ struct EmbedGradParams {
     Divisor by_chunk;
     uint32_t places; // 2^wlog * range
     uint32_t chunk, runs, cols;
-    uint32_t rows; // of the table's gradient per wave (wide)
+    uint32_t rows, apart; // of the table's gradient per wave, and how far they lie from each other (wide)
     int64_t vocab;
     float scale;
 };
@@ -258,7 +284,7 @@ __device__ __forceinline__ float *partial_of(const EmbedGradParams &p, uint32_t 
     return p.partial + (size_t)(2 * run + (inside ? 1 : 0)) * p.cols + (size_t)q * p.w.s.seg;
 }
 
-// Where a wave's part of a segment lies in the rows of the tokens' gradients.  Cuts by rows make the block a matter of the token;
+// Where a wave's segment lies in the rows of the tokens' gradients.  Cuts by rows make the block a matter of the token;
 // the lanes then hold the table of blocks (a scalar load per row would be a trip to memory per row).
 template <typename T> struct Sources {
     const T *base; // nothing cut by rows: of token 0
@@ -266,7 +292,7 @@ template <typename T> struct Sources {
     __device__ __forceinline__ Sources(const EmbedGradParams &p, const WaveWork &g)
     {
         const uint32_t cb = g.q >> p.w.s.a_shift;
-        at = (g.q - (cb << p.w.s.a_shift)) * p.w.s.seg + g.j0 * kVec<T>;
+        at = (g.q - (cb << p.w.s.a_shift)) * p.w.s.seg;
         block = cb * p.G.nrep;
         base = static_cast<const T *>(p.G.p[block]) + at;
         lo = hi = 0;
@@ -288,7 +314,6 @@ template <typename T> struct Sources {
 // the sums of a wave's part of a segment
 template <typename T> struct Sums {
     float f[kU][kVec<T>];
-    uint32_t n[kU];
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
@@ -305,21 +330,17 @@ template <typename T> struct Sums {
     }
 };
 
-// n rows (all of them where n >= BATCH) added to the sums in order, on their way together; token(k): the k-th
+// n rows (all BATCH of them where n is larger) added to the sums in order, on their way together; token(k): the k-th
 template <typename T, int BATCH, class F>
-__device__ __forceinline__ void add_batch(Sums<T> &a, const EmbedGradParams &p, const Sources<T> &src, uint32_t n, F &&token)
+__device__ __forceinline__ void add_batch(Sums<T> &a, const EmbedGradParams &p, const Sources<T> &src, const Columns<T> &c, uint32_t n, F &&token)
 {
-    const uint32_t lane = threadIdx.x & 63u;
     u32x4 r[BATCH][kU];
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
         if ((uint32_t)k >= n) break;
         const T *from = src.row(p, token(k));
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            r[k][u] = u32x4{0, 0, 0, 0};
-            if (a.n[u]) r[k][u] = load_vector(from + (u * 64 + lane) * kVec<T>, a.n[u]);
-        }
+        for (int u = 0; u < kU; ++u) r[k][u] = load16(from + c.col[u]);
     }
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
@@ -329,11 +350,12 @@ __device__ __forceinline__ void add_batch(Sums<T> &a, const EmbedGradParams &p, 
     }
 }
 // the rows of places [b, e) of the sorted list
-template <typename T, int BATCH> __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, const Sources<T> &src, uint32_t b, uint32_t e)
+template <typename T, int BATCH>
+__device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, const Sources<T> &src, const Columns<T> &c, uint32_t b, uint32_t e)
 {
     for (uint32_t w = b; w < e; w += 64) {
         const uint32_t mine = w + (threadIdx.x & 63u), tokens = mine < e ? p.order[mine] : 0, n = e - w < 64 ? e - w : 64;
-        for (uint32_t i = 0; i < n; i += BATCH) add_batch<T, BATCH>(a, p, src, n - i, [&](int k) { return wave::read_lane(tokens, (int)i + k); });
+        for (uint32_t i = 0; i < n; i += BATCH) add_batch<T, BATCH>(a, p, src, c, n - i, [&](int k) { return wave::read_lane(tokens, (int)i + k); });
     }
 }
 
@@ -341,28 +363,27 @@ template <typename T, int BATCH> __device__ __forceinline__ void add_rows(Sums<T
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_runs_wide_kernel(const EmbedGradParams p)
 {
     const WaveWork g = wave_work(p.w);
-    const uint32_t lane = threadIdx.x & 63u, c = g.row, total = p.start[p.places], b = c * p.chunk;
-    if (c >= p.runs || b >= total) return;
+    const uint32_t run = g.row, total = load_scalar(p.start + p.places), b = run * p.chunk;
+    if (run >= p.runs || b >= total) return;
     const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
-    const uint32_t first = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[b])), last = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[e - 1]));
+    const uint32_t first = place(p.to, (uint32_t)token_scalar<I>(p.ids, load_scalar(p.order + b)));
+    const uint32_t last = place(p.to, (uint32_t)token_scalar<I>(p.ids, load_scalar(p.order + e - 1)));
     const Sources<T> src(p, g);
-    Sums<T> a;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) a.n[u] = values_of(p.w.s, kVec<T>, g.j0 + u * 64 + lane);
+    const Columns<T> c(p.w.s, g.j0);
 #pragma unroll 1
     for (int side = 0; side < 2; ++side) {
         if (side == 1 && last == first) break;
-        const uint32_t at = side == 0 ? first : last, vb = p.start[at], ve = p.start[at + 1];
+        const uint32_t at = side == 0 ? first : last, vb = load_scalar(p.start + at), ve = load_scalar(p.start + at + 1);
         if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
-        const uint32_t lo = vb > b ? vb : b, hi = ve < e ? ve : e;
+        Sums<T> a;
         a.clear();
-        add_rows<T, kRunBatch>(a, p, src, lo, hi);
-        float *to = partial_of(p, c, vb > b, g.q);
+        add_rows<T, kRunBatch>(a, p, src, c, vb > b ? vb : b, ve < e ? ve : e);
+        float *to = partial_of(p, run, vb > b, g.q);
 #pragma unroll
         for (int u = 0; u < kU; ++u)
 #pragma unroll
-            for (int i = 0; i < kVec<T>; ++i)
-                if ((uint32_t)i < a.n[u]) to[(g.j0 + u * 64 + lane) * kVec<T> + i] = a.f[u][i];
+            for (int i = 0; i < kVec<T>; i += 4)
+                store16(to + c.col[u] + i, u32x4{__float_as_uint(a.f[u][i]), __float_as_uint(a.f[u][i + 1]), __float_as_uint(a.f[u][i + 2]), __float_as_uint(a.f[u][i + 3])});
     }
 }
 
@@ -391,51 +412,83 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     }
 }
 
-// (3) A wave does up to 8 neighbouring numbers, 8 lanes to each of them: where their tokens begin comes in one load, and the first
-// 8 tokens of each in another.
-template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_wide_kernel(const EmbedGradParams p)
+// (3) The first waves, one per run, look for a number with many tokens whose first one lies in their run (there is one at most)
+// and add up its partial sums.  The others do p.rows numbers each, 8 lanes to each of them: where their tokens begin comes in one
+// load, and the first 8 tokens of each in another.  The numbers lie p.apart from each other: the frequent ones, which
+// neighbour each other in most vocabularies, go to different waves.
+template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, const EmbedGradParams &p, const Columns<T> &c, uint32_t v, uint32_t q)
 {
-    const WaveWork g = wave_work(p.w);
-    const uint32_t lane = threadIdx.x & 63u, v0 = g.row * p.rows, vocab = (uint32_t)p.vocab;
-    if (v0 >= vocab) return;
-    const uint32_t rows = vocab - v0 < p.rows ? vocab - v0 : p.rows;
-    uint32_t begin = 0, end = 0, tokens = 0;
-    if ((lane >> 3) < rows) {
-        const uint32_t at = place(p.to, v0 + (lane >> 3));
-        begin = p.start[at];
-        end = p.start[at + 1];
-        if (begin + (lane & 7u) < end) tokens = p.order[begin + (lane & 7u)];
-    }
-    const Sources<T> src(p, g);
-    Sums<T> a;
+    const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, q);
 #pragma unroll
-    for (int u = 0; u < kU; ++u) a.n[u] = values_of(p.w.s, kVec<T>, g.j0 + u * 64 + lane);
-#pragma unroll 1
-    for (uint32_t k = 0; k < rows; ++k) {
-        const uint32_t v = v0 + k, b = wave::read_lane(begin, (int)k * 8), e = wave::read_lane(end, (int)k * 8);
-        const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q);
+    for (int u = 0; u < kU; ++u) {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= p.scale;
+        c.store(p.W, to, u, pack16(a.f[u], T()));
+    }
+}
+
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_rows_wide_kernel(const EmbedGradParams p)
+{
+    constexpr int kPartials = 4; // on their way together
+    const WaveWork g = wave_work(p.w);
+    const uint32_t lane = threadIdx.x & 63u, vocab = (uint32_t)p.vocab;
+    const Columns<T> c(p.w.s, g.j0);
+    Sums<T> a;
+    if (g.row < p.runs) {
+        const uint32_t total = load_scalar(p.start + p.places), lo = g.row * p.chunk;
+        if (lo >= total) return;
+        const uint32_t hi = lo + p.chunk < total ? lo + p.chunk : total, v = (uint32_t)token_scalar<I>(p.ids, load_scalar(p.order + hi - 1));
+        const uint32_t at = place(p.to, v), b = load_scalar(p.start + at), e = load_scalar(p.start + at + 1);
+        if (b < lo || e - b <= p.chunk) return;
         a.clear();
-        if (e - b <= p.chunk) {
-            const uint32_t n = e - b < 8 ? e - b : 8;
-            for (uint32_t i = 0; i < n; i += kRowBatch) add_batch<T, kRowBatch>(a, p, src, n - i, [&](int j) { return wave::read_lane(tokens, (int)(k * 8 + i) + j); });
-            if (b + 8 < e) add_rows<T, kRowBatch>(a, p, src, b + 8, e);
-        } else {
-            for (uint32_t c = quotient(b, p.by_chunk); c * p.chunk < e; ++c) {
-                const float *from = partial_of(p, c, b > c * p.chunk, g.q);
+        const uint32_t last = quotient(e - 1, p.by_chunk);
+        for (uint32_t run = g.row; run <= last; run += kPartials) {
+            u32x4 r[kPartials][kU][kVec<T> / 4];
+#pragma unroll
+            for (int k = 0; k < kPartials; ++k) {
+                if (run + k > last) break;
+                const float *from = partial_of(p, run + k, b > (run + k) * p.chunk, g.q);
 #pragma unroll
                 for (int u = 0; u < kU; ++u)
 #pragma unroll
-                    for (int i = 0; i < kVec<T>; ++i)
-                        if ((uint32_t)i < a.n[u]) a.f[u][i] += from[(g.j0 + u * 64 + lane) * kVec<T> + i];
+                    for (int i = 0; i < kVec<T> / 4; ++i) r[k][u][i] = load16(from + c.col[u] + 4 * i);
+            }
+#pragma unroll
+            for (int k = 0; k < kPartials; ++k) {
+                if (run + k > last) break;
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+#pragma unroll
+                    for (int i = 0; i < kVec<T>; ++i) a.f[u][i] += __uint_as_float(r[k][u][i / 4][i % 4]);
             }
         }
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            if (a.n[u] == 0) continue;
-#pragma unroll
-            for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= p.scale;
-            store_all<T>(p.W, to, (g.j0 + u * 64 + lane) * kVec<T>, a.n[u], pack16(a.f[u], T()));
+        finish_row(a, p, c, v, g.q);
+        return;
+    }
+    const uint32_t v0 = g.row - p.runs;
+    if (v0 >= p.apart) return;
+    uint32_t begin = 0, end = 0, tokens = 0;
+    {
+        const uint32_t k = lane >> 3, v = v0 + k * p.apart;
+        if (k < p.rows && v < vocab) {
+            const uint32_t at = place(p.to, v);
+            begin = p.start[at];
+            end = p.start[at + 1];
+            if (begin + (lane & 7u) < end) tokens = p.order[begin + (lane & 7u)];
         }
+    }
+    const Sources<T> src(p, g);
+#pragma unroll 1
+    for (uint32_t k = 0; k < p.rows; ++k) {
+        const uint32_t v = v0 + k * p.apart, b = wave::read_lane(begin, (int)k * 8), e = wave::read_lane(end, (int)k * 8);
+        if (v >= vocab) break;
+        if (e - b > p.chunk) continue;
+        a.clear();
+        const uint32_t n = e - b < 8 ? e - b : 8;
+        for (uint32_t i = 0; i < n; i += kRowBatch)
+            add_batch<T, kRowBatch>(a, p, src, c, n - i, [&](int j) { return wave::read_lane(tokens, (int)(k * 8 + i) + j); });
+        if (b + 8 < e) add_rows<T, kRowBatch>(a, p, src, c, b + 8, e);
+        finish_row(a, p, c, v, g.q);
     }
 }
 
@@ -542,7 +595,7 @@ extern "C" tt_status tt_embed_forward(int64_t tokens, int64_t vocab, int64_t wid
     p.tokens = (uint32_t)tokens;
     p.vocab = vocab;
     p.scale = scale;
-    const uint64_t grid = groups_of(p.w, (uint64_t)tokens, 1);
+    const uint64_t grid = groups_of(p.w, (uint64_t)tokens);
     if (grid * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED, 1 << k, tokens, width, e, (uint64_t)tokens * row * (1 + p.X.nrep), 0);
@@ -573,7 +626,7 @@ tt_status launch_embed_grad(const SortParams &sp, const EmbedGradParams &p, uint
     hipLaunchKernelGGL((sort_tokens_kernel<I>), dim3(1u << sp.to.wlog), dim3(kSortThreads), 0, s, sp);
     if (p.w.wide) {
         if (run_groups) hipLaunchKernelGGL((embed_runs_wide_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
-        hipLaunchKernelGGL((embed_rows_wide_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_rows_wide_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
     } else {
         if (run_groups) hipLaunchKernelGGL((embed_runs_narrow_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
         hipLaunchKernelGGL((embed_rows_narrow_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
@@ -622,7 +675,8 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     // as many as leave every CU 32 waves
     const uint64_t waves = (uint64_t)vocab * p.w.s.nseg * p.w.parts;
     p.rows = waves >= 8 * 8192 ? 8 : waves >= 4 * 8192 ? 4 : waves >= 2 * 8192 ? 2 : 1;
-    const uint64_t run_groups = groups_of(p.w, sp.runs, 1), row_groups = groups_of(p.w, (uint64_t)vocab, p.rows);
+    p.apart = (uint32_t)((vocab + p.rows - 1) / p.rows);
+    const uint64_t run_groups = groups_of(p.w, sp.runs), row_groups = groups_of(p.w, p.w.wide ? (uint64_t)sp.runs + p.apart : (uint64_t)vocab);
     if (run_groups * kThreads >= (uint64_t(1) << 31) || row_groups * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED_GRAD, 1 << k, vocab, width, e, (uint64_t)tokens * row + (uint64_t)vocab * row * p.W.nrep, 0);
