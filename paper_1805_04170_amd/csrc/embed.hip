@@ -78,14 +78,15 @@ template <typename T> struct Columns {
             col[u] = j * kVec<T> < last ? j * kVec<T> : last;
         }
     }
-    // into every replica of a segment that begins at `to`
-    __device__ __forceinline__ void store(const BlockTable &b, const Place &to, int u, u32x4 v) const
+    // into every replica of a segment that begins at `to`; ONCE: store16_once
+    template <bool ONCE> __device__ __forceinline__ void store(const BlockTable &b, const Place &to, int u, u32x4 v) const
     {
         if (own[u] == 0) return;
         for (uint32_t x = 0; x < b.nrep; ++x) {
             T *dst = static_cast<T *>(b.p[to.block + x]) + to.at + col[u];
             if (own[u] == (uint32_t)kVec<T>) {
-                store16(dst, v);
+                if constexpr (ONCE) store16_once(dst, v);
+                else store16(dst, v);
                 continue;
             }
 #pragma unroll
@@ -137,7 +138,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
         for (int u = 0; u < kU; ++u) r[u] = scaled<T>(r[u], p.scale);
     }
 #pragma unroll
-    for (int u = 0; u < kU; ++u) c.store(p.X, to, u, r[u]);
+    for (int u = 0; u < kU; ++u) c.template store<true>(p.X, to, u, r[u]);
 }
 
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_narrow_kernel(const EmbedParams p)
@@ -152,9 +153,10 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 }
 
 // ------------------------------------------------------------------------------------------------------ backward
-// Three launches.  (1) Tokens sorted by number, stably.  (2) Numbers with many tokens (more than `chunk`) would keep one wave
-// busy long after the rest is done: the sorted list is cut into runs of `chunk`, and each run adds up its part of such a
-// number into a partial sum.  (3) Every row of the table's gradient: the sum over its tokens in order, or over its partial sums.
+// Three launches.  (1) Tokens sorted by number, stably.  (2) Every row of the table's gradient: the sum over its tokens in order.
+// Numbers with many tokens (more than `chunk`) would keep one wave busy long after the rest is done: the sorted list is cut into
+// runs of `chunk`, and in the same launch each run adds up its part of such a number into a partial sum.  (3) The rows of
+// those numbers: the sums over their partial sums.
 
 // (1) Numbers are dealt out to workgroups like cards (frequent numbers are neighbours in most vocabularies): workgroup w sorts
 // the tokens whose number is w modulo the workgroups' count, 2^wlog of them.  The list has w's numbers behind w - 1's, each
@@ -197,9 +199,8 @@ template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_token
     const uint32_t stretch = ((p.tokens + kSortThreads - 1) / kSortThreads) * 64;
     const uint32_t t0 = w * stretch < p.tokens ? w * stretch : p.tokens, t1 = t0 + stretch < p.tokens ? t0 + stretch : p.tokens;
     uint32_t *mine = at + w * range;
-    uint32_t below = 0;
+    uint32_t below = 0, v[kSortLoads];
     for (uint32_t tb = t0; tb < t1; tb += 64 * kSortLoads) {
-        uint32_t v[kSortLoads];
 #pragma unroll
         for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
 #pragma unroll
@@ -239,9 +240,10 @@ template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_token
     }
     __syncthreads();
     for (uint32_t tb = t0; tb < t1; tb += 64 * kSortLoads) {
-        uint32_t v[kSortLoads];
+        if (stretch > 64 * kSortLoads) { // (otherwise they are still here)
 #pragma unroll
-        for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
+            for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
+        }
 #pragma unroll
         for (int i = 0; i < kSortLoads; ++i) {
             const bool in = v[i] != kNoToken && (v[i] & (groups - 1)) == me;
@@ -359,62 +361,18 @@ __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, c
     }
 }
 
-// (2)
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_runs_wide_kernel(const EmbedGradParams p)
+// What a run has to do with numbers of many tokens: it may end one at its first place and begin one at its last.
+struct Run { uint32_t b, e, first, last; bool any; };
+template <typename I> __device__ __forceinline__ Run run_of(const EmbedGradParams &p, uint32_t run)
 {
-    const WaveWork g = wave_work(p.w);
-    const uint32_t run = g.row, total = load_scalar(p.start + p.places), b = run * p.chunk;
-    if (run >= p.runs || b >= total) return;
+    const uint32_t total = p.start[p.places], b = run * p.chunk;
+    if (b >= total) return {0, 0, 0, 0, false};
     const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
-    const uint32_t first = place(p.to, (uint32_t)token_scalar<I>(p.ids, load_scalar(p.order + b)));
-    const uint32_t last = place(p.to, (uint32_t)token_scalar<I>(p.ids, load_scalar(p.order + e - 1)));
-    const Sources<T> src(p, g);
-    const Columns<T> c(p.w.s, g.j0);
-#pragma unroll 1
-    for (int side = 0; side < 2; ++side) {
-        if (side == 1 && last == first) break;
-        const uint32_t at = side == 0 ? first : last, vb = load_scalar(p.start + at), ve = load_scalar(p.start + at + 1);
-        if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
-        Sums<T> a;
-        a.clear();
-        add_rows<T, kRunBatch>(a, p, src, c, vb > b ? vb : b, ve < e ? ve : e);
-        float *to = partial_of(p, run, vb > b, g.q);
-#pragma unroll
-        for (int u = 0; u < kU; ++u)
-#pragma unroll
-            for (int i = 0; i < kVec<T>; i += 4)
-                store16(to + c.col[u] + i, u32x4{__float_as_uint(a.f[u][i]), __float_as_uint(a.f[u][i + 1]), __float_as_uint(a.f[u][i + 2]), __float_as_uint(a.f[u][i + 3])});
-    }
+    return {b, e, (uint32_t)token_at<I>(p.ids, p.order[b]), (uint32_t)token_at<I>(p.ids, p.order[e - 1]), true};
 }
 
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_runs_narrow_kernel(const EmbedGradParams p)
-{
-    const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j), c = g.row, total = p.start[p.places], b = c * p.chunk;
-    if (c >= p.runs || b >= total || n == 0) return;
-    const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
-    const uint32_t first = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[b])), last = place(p.to, (uint32_t)token_at<I>(p.ids, p.order[e - 1]));
-    for (int side = 0; side < 2; ++side) {
-        if (side == 1 && last == first) break;
-        const uint32_t at = side == 0 ? first : last, vb = p.start[at], ve = p.start[at + 1];
-        if (ve - vb <= p.chunk) continue;
-        float s[kVec<T>] = {};
-        for (uint32_t i = vb > b ? vb : b; i < (ve < e ? ve : e); ++i) {
-            float f[kVec<T>];
-            unpack16(load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, p.order[i], g.q) + g.j * kVec<T>, n), f, T());
-#pragma unroll
-            for (int q = 0; q < kVec<T>; ++q) s[q] += f[q];
-        }
-        float *to = partial_of(p, c, vb > b, g.q) + g.j * kVec<T>;
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i)
-            if ((uint32_t)i < n) to[i] = s[i];
-    }
-}
-
-// (3) The first waves, one per run, look for a number with many tokens whose first one lies in their run (there is one at most)
-// and add up its partial sums.  The others do p.rows numbers each, 8 lanes to each of them: where their tokens begin comes in one
-// load, and the first 8 tokens of each in another.  The numbers lie p.apart from each other: the frequent ones, which
+// (2) The first waves take a run each.  The others do p.rows numbers each, 8 lanes to each of them: where their tokens begin comes
+// in one load, and the first 8 tokens of each in another.  The numbers lie p.apart from each other: the frequent ones, which
 // neighbour each other in most vocabularies, go to different waves.
 template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, const EmbedGradParams &p, const Columns<T> &c, uint32_t v, uint32_t q)
 {
@@ -423,46 +381,34 @@ template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, con
     for (int u = 0; u < kU; ++u) {
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= p.scale;
-        c.store(p.W, to, u, pack16(a.f[u], T()));
+        c.template store<false>(p.W, to, u, pack16(a.f[u], T()));
     }
 }
 
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_rows_wide_kernel(const EmbedGradParams p)
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_sums_wide_kernel(const EmbedGradParams p)
 {
-    constexpr int kPartials = 4; // on their way together
     const WaveWork g = wave_work(p.w);
     const uint32_t lane = threadIdx.x & 63u, vocab = (uint32_t)p.vocab;
     const Columns<T> c(p.w.s, g.j0);
+    const Sources<T> src(p, g);
     Sums<T> a;
     if (g.row < p.runs) {
-        const uint32_t total = load_scalar(p.start + p.places), lo = g.row * p.chunk;
-        if (lo >= total) return;
-        const uint32_t hi = lo + p.chunk < total ? lo + p.chunk : total, v = (uint32_t)token_scalar<I>(p.ids, load_scalar(p.order + hi - 1));
-        const uint32_t at = place(p.to, v), b = load_scalar(p.start + at), e = load_scalar(p.start + at + 1);
-        if (b < lo || e - b <= p.chunk) return;
-        a.clear();
-        const uint32_t last = quotient(e - 1, p.by_chunk);
-        for (uint32_t run = g.row; run <= last; run += kPartials) {
-            u32x4 r[kPartials][kU][kVec<T> / 4];
+        const Run r = run_of<I>(p, g.row);
+        if (!r.any) return;
+#pragma unroll 1
+        for (int side = 0; side < 2; ++side) {
+            if (side == 1 && r.last == r.first) break;
+            const uint32_t at = uniform(place(p.to, side == 0 ? r.first : r.last)), vb = load_scalar(p.start + at), ve = load_scalar(p.start + at + 1);
+            if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
+            a.clear();
+            add_rows<T, kRunBatch>(a, p, src, c, vb > r.b ? vb : r.b, ve < r.e ? ve : r.e);
+            float *to = partial_of(p, g.row, vb > r.b, g.q);
 #pragma unroll
-            for (int k = 0; k < kPartials; ++k) {
-                if (run + k > last) break;
-                const float *from = partial_of(p, run + k, b > (run + k) * p.chunk, g.q);
+            for (int u = 0; u < kU; ++u)
 #pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int i = 0; i < kVec<T> / 4; ++i) r[k][u][i] = load16(from + c.col[u] + 4 * i);
-            }
-#pragma unroll
-            for (int k = 0; k < kPartials; ++k) {
-                if (run + k > last) break;
-#pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int i = 0; i < kVec<T>; ++i) a.f[u][i] += __uint_as_float(r[k][u][i / 4][i % 4]);
-            }
+                for (int i = 0; i < kVec<T>; i += 4)
+                    store16(to + c.col[u] + i, u32x4{__float_as_uint(a.f[u][i]), __float_as_uint(a.f[u][i + 1]), __float_as_uint(a.f[u][i + 2]), __float_as_uint(a.f[u][i + 3])});
         }
-        finish_row(a, p, c, v, g.q);
         return;
     }
     const uint32_t v0 = g.row - p.runs;
@@ -477,12 +423,17 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
             if (begin + (lane & 7u) < end) tokens = p.order[begin + (lane & 7u)];
         }
     }
-    const Sources<T> src(p, g);
 #pragma unroll 1
     for (uint32_t k = 0; k < p.rows; ++k) {
         const uint32_t v = v0 + k * p.apart, b = wave::read_lane(begin, (int)k * 8), e = wave::read_lane(end, (int)k * 8);
         if (v >= vocab) break;
-        if (e - b > p.chunk) continue;
+        if (e - b > p.chunk) continue; // (3)
+        if (e == b) { // most rows
+            const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) c.template store<false>(p.W, to, u, u32x4{0, 0, 0, 0});
+            continue;
+        }
         a.clear();
         const uint32_t n = e - b < 8 ? e - b : 8;
         for (uint32_t i = 0; i < n; i += kRowBatch)
@@ -492,31 +443,133 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     }
 }
 
-template <typename T> __global__ __launch_bounds__(kThreads) void embed_rows_narrow_kernel(const EmbedGradParams p)
+// the rows of places [b, e) of the sorted list, a vector of each, kRunBatch of them on their way together
+template <typename T> __device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, uint32_t n, uint32_t b, uint32_t e)
 {
-    const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j), v = g.row;
-    if ((int64_t)v >= p.vocab || n == 0) return;
-    const uint32_t at = place(p.to, v), b = p.start[at], e = p.start[at + 1];
-    float s[kVec<T>] = {};
-    if (e - b <= p.chunk) {
-        for (uint32_t i = b; i < e; ++i) {
+    for (uint32_t i = b; i < e; i += kRunBatch) {
+        uint32_t t[kRunBatch];
+        u32x4 r[kRunBatch];
+#pragma unroll
+        for (int k = 0; k < kRunBatch; ++k) t[k] = p.order[i + k < e ? i + k : e - 1];
+#pragma unroll
+        for (int k = 0; k < kRunBatch; ++k) r[k] = load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, t[k], g.q) + g.j * kVec<T>, n);
+#pragma unroll
+        for (int k = 0; k < kRunBatch; ++k) {
             float f[kVec<T>];
-            unpack16(load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, p.order[i], g.q) + g.j * kVec<T>, n), f, T());
+            unpack16(r[k], f, T());
 #pragma unroll
-            for (int q = 0; q < kVec<T>; ++q) s[q] += f[q];
-        }
-    } else {
-        for (uint32_t c = quotient(b, p.by_chunk); c * p.chunk < e; ++c) {
-            const float *from = partial_of(p, c, b > c * p.chunk, g.q) + g.j * kVec<T>;
-#pragma unroll
-            for (int i = 0; i < kVec<T>; ++i)
-                if ((uint32_t)i < n) s[i] += from[i];
+            for (int q = 0; q < kVec<T>; ++q) s[q] = i + k < e ? s[q] + f[q] : s[q];
         }
     }
+}
+
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_sums_narrow_kernel(const EmbedGradParams p)
+{
+    const LaneWork g = lane_work(p.w);
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
+    if (n == 0) return;
+    if (g.row < p.runs) {
+        const Run r = run_of<I>(p, g.row);
+        if (!r.any) return;
+        for (int side = 0; side < 2; ++side) {
+            if (side == 1 && r.last == r.first) break;
+            const uint32_t at = place(p.to, side == 0 ? r.first : r.last), vb = p.start[at], ve = p.start[at + 1];
+            if (ve - vb <= p.chunk) continue;
+            float s[kVec<T>] = {};
+            add_vectors<T>(s, p, g, n, vb > r.b ? vb : r.b, ve < r.e ? ve : r.e);
+            float *to = partial_of(p, g.row, vb > r.b, g.q) + g.j * kVec<T>;
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i)
+                if ((uint32_t)i < n) to[i] = s[i];
+        }
+        return;
+    }
+    const uint32_t v = g.row - p.runs;
+    if ((int64_t)v >= p.vocab) return;
+    const uint32_t at = place(p.to, v), b = p.start[at], e = p.start[at + 1];
+    if (e - b > p.chunk) return; // (3)
+    float s[kVec<T>] = {};
+    add_vectors<T>(s, p, g, n, b, e);
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
     store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q), g.j * kVec<T>, n, pack16(s, T()));
+}
+
+// (3) A wave per run and part (a group of lanes per run and segment) looks for a number of many tokens whose first one lies in its
+// run; there is one at most, the run's last.
+struct Long { uint32_t v, last; bool any; };
+template <typename I> __device__ __forceinline__ Long long_of(const EmbedGradParams &p, uint32_t run)
+{
+    const Run r = run_of<I>(p, run);
+    if (!r.any) return {0, 0, false};
+    const uint32_t at = place(p.to, r.last), b = p.start[at], e = p.start[at + 1];
+    return {r.last, quotient(e - 1, p.by_chunk), b >= r.b && e - b > p.chunk};
+}
+// (the first of its partial sums counts as begun inside the run unless it is the run's first place)
+__device__ __forceinline__ const float *partial_in(const EmbedGradParams &p, uint32_t run, uint32_t first_run, bool inside, uint32_t q)
+{
+    return partial_of(p, run, run == first_run && inside, q);
+}
+
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_wide_kernel(const EmbedGradParams p)
+{
+    const WaveWork g = wave_work(p.w);
+    if (g.row >= p.runs) return;
+    const Long w = long_of<I>(p, g.row);
+    if (!w.any) return;
+    const uint32_t v = uniform(w.v), last = uniform(w.last);
+    const bool inside = load_scalar(p.start + place(p.to, v)) > g.row * p.chunk;
+    const Columns<T> c(p.w.s, g.j0);
+    Sums<T> a;
+    a.clear();
+    for (uint32_t run = g.row; run <= last; run += kPartials) {
+        u32x4 r[kPartials][kU][kVec<T> / 4];
+#pragma unroll
+        for (int k = 0; k < kPartials; ++k) {
+            if (run + k > last) break;
+            const float *from = partial_in(p, run + k, g.row, inside, g.q);
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int i = 0; i < kVec<T> / 4; ++i) r[k][u][i] = load16(from + c.col[u] + 4 * i);
+        }
+#pragma unroll
+        for (int k = 0; k < kPartials; ++k) {
+            if (run + k > last) break;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int i = 0; i < kVec<T>; ++i) a.f[u][i] += __uint_as_float(r[k][u][i / 4][i % 4]);
+        }
+    }
+    finish_row(a, p, c, v, g.q);
+}
+
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_narrow_kernel(const EmbedGradParams p)
+{
+    const LaneWork g = lane_work(p.w);
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
+    if (g.row >= p.runs || n == 0) return;
+    const Long w = long_of<I>(p, g.row);
+    if (!w.any) return;
+    const bool inside = p.start[place(p.to, w.v)] > g.row * p.chunk;
+    float s[kVec<T>] = {};
+    for (uint32_t run = g.row; run <= w.last; run += kPartials) {
+        float f[kPartials][kVec<T>];
+#pragma unroll
+        for (int k = 0; k < kPartials; ++k) {
+            const float *from = partial_in(p, run + k < w.last ? run + k : w.last, g.row, inside, g.q) + g.j * kVec<T>;
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) f[k][i] = (uint32_t)i < n ? load1(from + i) : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < kPartials; ++k)
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) s[i] = run + k <= w.last ? s[i] + f[k][i] : s[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
+    store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, w.v, g.q), g.j * kVec<T>, n, pack16(s, T()));
 }
 
 // ----------------------------------------------------------------------------------------------------- host side
@@ -625,11 +678,11 @@ tt_status launch_embed_grad(const SortParams &sp, const EmbedGradParams &p, uint
 {
     hipLaunchKernelGGL((sort_tokens_kernel<I>), dim3(1u << sp.to.wlog), dim3(kSortThreads), 0, s, sp);
     if (p.w.wide) {
-        if (run_groups) hipLaunchKernelGGL((embed_runs_wide_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
-        hipLaunchKernelGGL((embed_rows_wide_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_sums_wide_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        if (run_groups) hipLaunchKernelGGL((embed_join_wide_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
     } else {
-        if (run_groups) hipLaunchKernelGGL((embed_runs_narrow_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
-        hipLaunchKernelGGL((embed_rows_narrow_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_sums_narrow_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        if (run_groups) hipLaunchKernelGGL((embed_join_narrow_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
     }
     return launched();
 }
@@ -676,7 +729,7 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     const uint64_t waves = (uint64_t)vocab * p.w.s.nseg * p.w.parts;
     p.rows = waves >= 8 * 8192 ? 8 : waves >= 4 * 8192 ? 4 : waves >= 2 * 8192 ? 2 : 1;
     p.apart = (uint32_t)((vocab + p.rows - 1) / p.rows);
-    const uint64_t run_groups = groups_of(p.w, sp.runs), row_groups = groups_of(p.w, p.w.wide ? (uint64_t)sp.runs + p.apart : (uint64_t)vocab);
+    const uint64_t run_groups = groups_of(p.w, sp.runs), row_groups = groups_of(p.w, (uint64_t)sp.runs + (p.w.wide ? p.apart : (uint64_t)vocab));
     if (run_groups * kThreads >= (uint64_t(1) << 31) || row_groups * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED_GRAD, 1 << k, vocab, width, e, (uint64_t)tokens * row + (uint64_t)vocab * row * p.W.nrep, 0);

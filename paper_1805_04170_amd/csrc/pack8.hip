@@ -7,9 +7,7 @@
 #include <cstdint>
 #include <cstring>
 #include "launch_util.h"
-#include "block_table.h"
-#include "tensor_tiling_tokens.h"
-#include "tt_wave.h"
+#include "tiled_rows.h"
 
 namespace tt {
 namespace {
@@ -20,8 +18,10 @@ struct PackParams {
     void *X[kMaxShards];
     int8_t *Q[kMaxShards];
     uint8_t *S[kMaxShards];
-    uint32_t rows, cols, bpr; // of a shard; blocks per row
-    uint64_t units;           // half blocks per shard
+    uint32_t rows, cols; // of a shard
+    Divisor by_bpr;      // blocks per row
+    uint32_t narrow;     // blocks are counted in 31 bits
+    uint64_t units;      // half blocks per shard
 };
 
 // 2^-e of a block from the exponent byte e + 127, and the byte from the largest magnitude's bits
@@ -33,108 +33,169 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top)
     return top >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
 }
 
-// Two lanes a block, 16 values each (for the values a row does not have: zeros).
+// Where half a block lies: 16 values of a row (n of them are there)
+struct Half { uint64_t block; size_t at; uint32_t n; };
+__device__ __forceinline__ Half half_of(const PackParams &p, uint64_t u)
+{
+    const uint64_t blk = u >> 1;
+    const uint32_t row = p.narrow ? quotient((uint32_t)blk, p.by_bpr) : (uint32_t)(blk / p.by_bpr.d), b = (uint32_t)(blk - (uint64_t)row * p.by_bpr.d);
+    const uint32_t col = b * kBlock + ((uint32_t)u & 1u) * 16;
+    return {blk, (size_t)row * p.cols + col, u >= p.units || col >= p.cols ? 0 : p.cols - col < 16 ? p.cols - col : 16};
+}
+template <typename T> struct Values { u32x4 r[16 / kVec<T>]; };
+template <typename T> __device__ __forceinline__ Values<T> load_values(const T *x, uint32_t n)
+{
+    Values<T> v;
+#pragma unroll
+    for (int i = 0; i < 16 / kVec<T>; ++i) {
+        const uint32_t left = n > (uint32_t)(i * kVec<T>) ? n - i * kVec<T> : 0;
+        v.r[i] = left >= (uint32_t)kVec<T> ? load16(x + i * kVec<T>) : load_part(x + i * kVec<T>, left);
+    }
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store_values(T *x, const Values<T> &v, uint32_t n)
+{
+#pragma unroll
+    for (int i = 0; i < 16 / kVec<T>; ++i) {
+        const uint32_t left = n > (uint32_t)(i * kVec<T>) ? n - i * kVec<T> : 0;
+        if (left >= (uint32_t)kVec<T>) store16(x + i * kVec<T>, v.r[i]);
+        else store_part(x + i * kVec<T>, v.r[i], left);
+    }
+}
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+__device__ __forceinline__ u32x4 load_bytes(const int8_t *q, uint32_t n)
+{
+    if (n == 16) {
+        const u32x4_any w = *(const TT_GLOBAL u32x4_any *)q;
+        return u32x4{w.x, w.y, w.z, w.w};
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+    for (uint32_t i = 0; i < n; ++i) w[i >> 2] |= (uint32_t)(uint8_t)load1(q + i) << (8 * (i & 3));
+    return u32x4{w[0], w[1], w[2], w[3]};
+}
+
+// Two lanes a block, 16 values each; kUnits blocks of a lane on their way together.
+constexpr int kUnits = 2;
 template <typename T> __global__ __launch_bounds__(kThreads) void pack8_kernel(const PackParams p)
 {
-    const uint64_t u = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    const bool on = u < p.units;
-    const uint64_t blk = (on ? u : p.units - 1) >> 1;
-    const uint32_t half = (uint32_t)u & 1u;
-    const uint32_t row = (uint32_t)(blk / p.bpr), b = (uint32_t)(blk - (uint64_t)row * p.bpr);
-    const uint32_t col = b * kBlock + half * 16;
-    const uint32_t n = !on || col >= p.cols ? 0 : p.cols - col < 16 ? p.cols - col : 16;
-    const size_t at = (size_t)row * p.cols + col;
-    const T *x = static_cast<const T *>(p.X[blockIdx.y]) + at;
-    float f[16];
-    if (n == 16) {
-        constexpr int EV = kVec<T>;
-        u32x4 r[16 / EV];
+    const uint64_t u0 = (uint64_t)blockIdx.x * (kThreads * kUnits) + threadIdx.x;
+    const T *x = static_cast<const T *>(p.X[blockIdx.y]);
+    Half h[kUnits];
+    Values<T> v[kUnits];
 #pragma unroll
-        for (int i = 0; i < 16 / EV; ++i) r[i] = load16(x + i * EV);
+    for (int k = 0; k < kUnits; ++k) {
+        h[k] = half_of(p, u0 + k * kThreads);
+        v[k] = load_values(x + (h[k].n ? h[k].at : 0), h[k].n);
+    }
 #pragma unroll
-        for (int i = 0; i < 16 / EV; ++i) {
-            float g[EV];
-            unpack16(r[i], g, T());
+    for (int k = 0; k < kUnits; ++k) {
+        float f[16];
+        uint32_t top = 0; // magnitudes compare as their bits do, infinities and NaN above all others
 #pragma unroll
-            for (int q = 0; q < EV; ++q) f[i * EV + q] = g[q];
+        for (int i = 0; i < 16 / kVec<T>; ++i) {
+            float g[kVec<T>];
+            unpack16(v[k].r[i], g, T());
+#pragma unroll
+            for (int j = 0; j < kVec<T>; ++j) {
+                const uint32_t m = __float_as_uint(g[j]) & 0x7fffffffu;
+                top = m > top ? m : top;
+                f[i * kVec<T> + j] = g[j];
+            }
         }
-    } else {
+        const uint32_t other = wave::shfl_xor(top, 1);
+        const uint32_t s = scale_byte(other > top ? other : top);
+        if (h[k].n == 0) continue;
+        const float inv = s == 255 ? 0.0f : __uint_as_float((254u - s) << 23);
+        uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = (uint32_t)i < n ? to_float(x[i]) : 0.0f;
+        for (int i = 0; i < 16; ++i) {
+            int q = s == 255 ? 0 : (int)rintf(f[i] * inv);
+            if (q == 0 && s != 255) q = f[i] > 0.0f ? 1 : f[i] < 0.0f ? -1 : 0;
+            w[i >> 2] |= (uint32_t)(q & 255) << (8 * (i & 3));
+        }
+        int8_t *to = p.Q[blockIdx.y] + h[k].at;
+        if (h[k].n == 16) {
+            *(TT_GLOBAL u32x4_any *)to = u32x4_any{w[0], w[1], w[2], w[3]};
+        } else {
+            for (uint32_t i = 0; i < h[k].n; ++i) store1(to + i, (int8_t)(w[i >> 2] >> (8 * (i & 3))));
+        }
+        if ((threadIdx.x & 1u) == 0) store1(p.S[blockIdx.y] + h[k].block, (uint8_t)s);
     }
-    uint32_t top = 0; // magnitudes compare as their bits do, infinities and NaN above all others
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t m = __float_as_uint(f[i]) & 0x7fffffffu;
-        top = m > top ? m : top;
-    }
-    const uint32_t other = wave::shfl_xor(top, 1);
-    top = other > top ? other : top;
-    const uint32_t s = scale_byte(top);
-    if (n == 0) return;
-    const float inv = s == 255 ? 0.0f : __uint_as_float((254u - s) << 23);
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        int q = s == 255 ? 0 : (int)rintf(f[i] * inv);
-        if (q == 0 && s != 255) q = f[i] > 0.0f ? 1 : f[i] < 0.0f ? -1 : 0;
-        w[i >> 2] |= (uint32_t)(q & 255) << (8 * (i & 3));
-    }
-    int8_t *to = p.Q[blockIdx.y] + at;
-    if (n == 16) {
-        typedef uint32_t any __attribute__((ext_vector_type(4), aligned(1)));
-        *reinterpret_cast<any *>(to) = any{w[0], w[1], w[2], w[3]};
-    } else {
-        for (uint32_t i = 0; i < n; ++i) to[i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
-    }
-    if (half == 0) p.S[blockIdx.y][blk] = (uint8_t)s;
 }
 
 __device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255 ? 0x7fc00000u : s << 23); }
+// byte i of a vector, signed
+__device__ __forceinline__ int byte_of(const u32x4 &w, int i) { return (int)(int8_t)(w[i >> 2] >> (8 * (i & 3))); }
 
-// 16 values of a row from 8 bits (to: dense rows like Q's)
+// 16 values of a row from 8 bits
+template <typename T> __device__ __forceinline__ Values<T> values_from(u32x4 q, float scale)
+{
+    Values<T> v;
+#pragma unroll
+    for (int i = 0; i < 16 / kVec<T>; ++i) {
+        float g[kVec<T>];
+#pragma unroll
+        for (int j = 0; j < kVec<T>; ++j) g[j] = (float)byte_of(q, i * kVec<T> + j) * scale;
+        v.r[i] = pack16(g, T());
+    }
+    return v;
+}
+
 template <typename T> __device__ __forceinline__ void unpack_half_block(const PackParams &p, uint32_t shard, uint64_t u)
 {
-    const uint64_t blk = u >> 1;
-    const uint32_t row = (uint32_t)(blk / p.bpr), b = (uint32_t)(blk - (uint64_t)row * p.bpr);
-    const uint32_t col = b * kBlock + ((uint32_t)u & 1u) * 16;
-    if (col >= p.cols) return;
-    const uint32_t n = p.cols - col < 16 ? p.cols - col : 16;
-    const size_t at = (size_t)row * p.cols + col;
-    const int8_t *q = p.Q[shard] + at;
-    T *x = static_cast<T *>(p.X[shard]) + at;
-    const float s = scale_of(p.S[shard][blk]);
-    if (n == 16) {
-        typedef uint32_t any __attribute__((ext_vector_type(4), aligned(1)));
-        const any w = *reinterpret_cast<const any *>(q);
-        constexpr int EV = kVec<T>;
-#pragma unroll
-        for (int i = 0; i < 16 / EV; ++i) {
-            float g[EV];
-#pragma unroll
-            for (int j = 0; j < EV; ++j) g[j] = (float)(int8_t)(w[(i * EV + j) >> 2] >> (8 * (j & 3))) * s;
-            store16(x + i * EV, pack16(g, T()));
-        }
-    } else {
-        for (uint32_t i = 0; i < n; ++i) x[i] = from_float<T>((float)q[i] * s);
-    }
+    const Half h = half_of(p, u);
+    if (h.n == 0) return;
+    const u32x4 q = load_bytes(p.Q[shard] + h.at, h.n);
+    store_values(static_cast<T *>(p.X[shard]) + h.at, values_from<T>(q, scale_of(load1(p.S[shard] + h.block))), h.n);
 }
 
 template <typename T> __global__ __launch_bounds__(kThreads) void unpack8_kernel(const PackParams p)
 {
     const uint64_t u = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (u < p.units) unpack_half_block<T>(p, blockIdx.y, u);
+    unpack_half_block<T>(p, blockIdx.y, u);
+}
+
+// What a layer's backward pass needs of its activations, in one launch: the input unpacked, and the output's gradient where the
+// output's value is above 0 (the output itself is read as its 8 bits and never written out).
+struct GateParams {
+    PackParams x;          // blocks of the input: Q, S, X written
+    const void *dY[kMaxShards];
+    PackParams y;          // blocks of the output: Q, S; X takes the gated gradient
+    uint32_t x_blocks;
+};
+template <typename T> __global__ __launch_bounds__(kThreads) void unpack_gate_kernel(const GateParams p)
+{
+    const uint64_t u = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (blockIdx.y < p.x_blocks) {
+        unpack_half_block<T>(p.x, blockIdx.y, u);
+        return;
+    }
+    const uint32_t b = blockIdx.y - p.x_blocks;
+    const Half h = half_of(p.y, u);
+    if (h.n == 0) return;
+    Values<T> v = load_values(static_cast<const T *>(p.dY[b]) + h.at, h.n);
+    const u32x4 q = load_bytes(p.y.Q[b] + h.at, h.n);
+    const bool number = load1(p.y.S[b] + h.block) != 255;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const bool open = number && byte_of(q, i) > 0;
+        const uint32_t mine = sizeof(T) == 4 ? 0xffffffffu : i & 1 ? 0xffff0000u : 0x0000ffffu;
+        v.r[i / kVec<T>][i % kVec<T> * (int)sizeof(T) / 4] &= open ? 0xffffffffu : ~mine;
+    }
+    store_values(static_cast<T *>(p.y.X[b]) + h.at, v, h.n);
 }
 
 // shard extents and the launch's size; `count` shards
-tt_status pack_geometry(PackParams *p, int64_t srows, int64_t scols, dim3 *grid, int count)
+tt_status pack_geometry(PackParams *p, int64_t srows, int64_t scols, dim3 *grid, int count, uint32_t units_each)
 {
     if (!fits31(srows) || !fits31(scols)) return TT_EUNSUPPORTED;
     p->rows = (uint32_t)srows;
     p->cols = (uint32_t)scols;
-    p->bpr = (uint32_t)((scols + kBlock - 1) / kBlock);
-    p->units = (uint64_t)srows * p->bpr * 2;
-    const uint64_t g = (p->units + kThreads - 1) / kThreads;
+    const uint32_t bpr = (uint32_t)((scols + kBlock - 1) / kBlock);
+    p->by_bpr = divisor(bpr);
+    p->units = (uint64_t)srows * bpr * 2;
+    p->narrow = p->units / 2 + kThreads * kUnits < (uint64_t(1) << 31);
+    const uint64_t each = kThreads * units_each, g = (p->units + each - 1) / each;
     if (g * kThreads >= (uint64_t(1) << 32)) return TT_EUNSUPPORTED;
     *grid = dim3((uint32_t)g, (uint32_t)count);
     return TT_OK;
@@ -158,7 +219,7 @@ tt_status launch_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, c
     PackParams p;
     dim3 grid;
     const int n = 1 << k;
-    const tt_status st = pack_geometry(&p, g.srows, g.scols, &grid, n);
+    const tt_status st = pack_geometry(&p, g.srows, g.scols, &grid, n, pack ? kUnits : 1);
     if (st != TT_OK) return st;
     for (int s = 0; s < kMaxShards; ++s) {
         p.X[s] = s < n ? const_cast<void *>(X[s]) : nullptr;
@@ -166,7 +227,7 @@ tt_status launch_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, c
         p.S[s] = s < n ? static_cast<uint8_t *>(const_cast<void *>(S[s])) : nullptr;
     }
     const uint64_t values = (uint64_t)g.srows * g.scols * n;
-    ProfileScope scope(stream, pack ? TT_K_PACK : TT_K_UNPACK, n, rows, cols, dtype_bytes(dtype), values * (dtype_bytes(dtype) + 1) + (uint64_t)g.srows * p.bpr * n, 0);
+    ProfileScope scope(stream, pack ? TT_K_PACK : TT_K_UNPACK, n, rows, cols, dtype_bytes(dtype), values * (dtype_bytes(dtype) + 1) + (uint64_t)g.srows * p.by_bpr.d * n, 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     if (pack) {
         if (dtype == TT_BF16) hipLaunchKernelGGL((pack8_kernel<uint16_t>), grid, dim3(kThreads), 0, s, p);
@@ -180,29 +241,75 @@ tt_status launch_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, c
 
 template <typename P> const void *const *untyped(P *const *p) { return reinterpret_cast<const void *const *>(p); }
 
-// The workspace of a backward pass from 8 bits: the activations unpacked, one buffer per shard of X and of Y, then what the
-// 16-bit pass asks for.
+// The workspace of a backward pass from 8 bits: the input's blocks unpacked; where the output and its gradient are cut into blocks
+// alike, the gated gradient's blocks, otherwise the output's unpacked; then what the 16-bit pass asks for.  Replicas share a
+// block's buffer: that pass only reads them.
 struct PackedSpace {
-    Grid x, y;
-    size_t x_pitch = 0, y_pitch = 0, inner_at = 0, bytes = 0;
+    BlockTable x, y, dy;
+    bool relu = false, gated = false;
+    tt_layer layer; // of the 16-bit pass
+    size_t x_pitch = 0, y_pitch = 0, y_at = 0, inner_at = 0, bytes = 0;
 };
+uint32_t blocks_of(const BlockTable &b) { return b.nR * b.nC; }
 
 tt_status packed_space(const tt_layer *layer, int64_t batch, int k, int dtype, const tt_tiling &tX, const tt_tiling &tW, const tt_tiling &tY,
                        const tt_tiling &tdY, const tt_tiling &tdX, const uint8_t *fd, const uint8_t *fw, int with_dx, PackedSpace *s)
 {
     size_t inner = 0;
-    const tt_status st = tt_fc_workspace_bytes(layer, batch, k, dtype, TT_OP_DGRAD, tX, tW, tY, tdY, tdX, fd, fw, with_dx, &inner);
+    tt_status st = tt_fc_workspace_bytes(layer, batch, k, dtype, TT_OP_DGRAD, tX, tW, tY, tdY, tdX, fd, fw, with_dx, &inner);
     if (st != TT_OK) return st; // (checks the layer, the types and the tilings)
-    if (!make_grid(tX.cut, k, batch, layer->n_in, &s->x)) return TT_EINFEASIBLE;
+    if (!fits31(batch) || !fits31(layer->n_in) || !fits31(layer->n_out)) return TT_EUNSUPPORTED;
+    s->layer = *layer;
+    s->relu = layer->act == TT_ACT_RELU;
+    if (!make_blocks(nullptr, tX, k, batch, layer->n_in, &s->x) || !make_blocks(nullptr, tdY, k, batch, layer->n_out, &s->dy)) return TT_EINFEASIBLE;
     const size_t e = (size_t)dtype_bytes(dtype);
     s->x_pitch = align_up((size_t)s->x.srows * s->x.scols * e, 256);
-    if (layer->act == TT_ACT_RELU) {
-        if (!make_grid(tY.cut, k, batch, layer->n_out, &s->y)) return TT_EINFEASIBLE;
+    s->y_at = s->inner_at = s->x_pitch * blocks_of(s->x);
+    if (s->relu) {
+        if (!make_blocks(nullptr, tY, k, batch, layer->n_out, &s->y)) return TT_EINFEASIBLE;
+        s->gated = s->y.nR == s->dy.nR && s->y.nC == s->dy.nC;
         s->y_pitch = align_up((size_t)s->y.srows * s->y.scols * e, 256);
+        s->inner_at += s->y_pitch * blocks_of(s->y);
     }
-    s->inner_at = (s->x_pitch + s->y_pitch) << k;
+    if (s->gated) {
+        s->layer.act = TT_ACT_NONE;
+        st = tt_fc_workspace_bytes(&s->layer, batch, k, dtype, TT_OP_DGRAD, tX, tW, tY, tdY, tdX, fd, fw, with_dx, &inner);
+        if (st != TT_OK) return st;
+    }
     s->bytes = s->inner_at + inner;
     return TT_OK;
+}
+
+// one buffer per block: the block a shard holds
+void buffers_of(void **shards, const tt_tiling &t, int k, const BlockTable &b, char *base, size_t pitch)
+{
+    Grid g;
+    if (!make_grid(t.cut, k, (int64_t)b.srows * b.nR, (int64_t)b.scols * b.nC, &g)) return;
+    for (uint32_t s = 0; s < (1u << k); ++s) shards[s] = base + (size_t)(extract(s, g.maskR, k) * b.nC + extract(s, g.maskC, k)) * pitch;
+}
+
+// the blocks of a tensor in 8 bits, one replica of each, and where their values go
+tt_status packed_blocks(PackParams *p, const tt_tiling &t, int k, int64_t rows, int64_t cols, const void *const *Q, const void *const *S, char *to,
+                        size_t pitch, dim3 *grid)
+{
+    BlockTable q, s;
+    if (!make_blocks(Q, t, k, rows, cols, &q) || !make_blocks(S, t, k, rows, cols, &s)) return TT_EINFEASIBLE;
+    const uint32_t n = blocks_of(q);
+    for (uint32_t b = 0; b < (uint32_t)kMaxShards; ++b) {
+        p->X[b] = b < n ? to + b * pitch : nullptr;
+        p->Q[b] = b < n ? static_cast<int8_t *>(q.p[b * q.nrep]) : nullptr;
+        p->S[b] = b < n ? static_cast<uint8_t *>(s.p[b * s.nrep]) : nullptr;
+    }
+    return pack_geometry(p, q.srows, q.scols, grid, (int)n, 1);
+}
+
+template <typename T> void launch_unpack_gate(const GateParams &p, dim3 grid, hipStream_t s)
+{
+    hipLaunchKernelGGL((unpack_gate_kernel<T>), grid, dim3(kThreads), 0, s, p);
+}
+template <typename T> void launch_unpack_blocks(const PackParams &p, dim3 grid, hipStream_t s)
+{
+    hipLaunchKernelGGL((unpack8_kernel<T>), grid, dim3(kThreads), 0, s, p);
 }
 
 } // namespace
@@ -253,12 +360,37 @@ extern "C" tt_status tt_fc_backward_packed(const tt_layer *layer, int64_t batch,
     if (!workspace || ws_bytes < s.bytes || reinterpret_cast<uintptr_t>(workspace) % 256) return TT_EWORKSPACE;
     char *ws = static_cast<char *>(workspace);
     void *X[kMaxShards], *Y[kMaxShards];
-    for (int i = 0; i < (1 << k); ++i) {
-        X[i] = ws + (size_t)i * s.x_pitch;
-        Y[i] = ws + (s.x_pitch << k) + (size_t)i * s.y_pitch;
+    buffers_of(X, tX, k, s.x, ws, s.x_pitch);
+    GateParams p;
+    dim3 gx, gy;
+    if ((st = packed_blocks(&p.x, tX, k, batch, layer->n_in, untyped(XQ), untyped(XS), ws, s.x_pitch, &gx)) != TT_OK) return st;
+    if (s.relu) {
+        if ((st = packed_blocks(&p.y, tY, k, batch, layer->n_out, untyped(YQ), untyped(YS), ws + s.y_at, s.y_pitch, &gy)) != TT_OK) return st;
+        buffers_of(Y, s.gated ? tdY : tY, k, s.gated ? s.dy : s.y, ws + s.y_at, s.y_pitch);
     }
-    if ((st = launch_pack(false, batch, layer->n_in, k, dtype, tX, X, untyped(XQ), untyped(XS), stream)) != TT_OK) return st;
-    if (relu && (st = launch_pack(false, batch, layer->n_out, k, dtype, tY, Y, untyped(YQ), untyped(YS), stream)) != TT_OK) return st;
-    return tt_fc_backward(layer, batch, k, dtype, tX, tW, tY, tdY, tdX, forms_dgrad, forms_wgrad, X, W, relu ? Y : nullptr, dY, dX, dW,
-                          ws + s.inner_at, ws_bytes - s.inner_at, stream);
+    const hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    const bool bf16 = dtype == TT_BF16;
+    const uint64_t nx = (uint64_t)batch * layer->n_in, ny = (uint64_t)batch * layer->n_out;
+    if (s.gated) {
+        BlockTable dy;
+        if (!make_blocks(dY, tdY, k, batch, layer->n_out, &dy)) return TT_EINFEASIBLE;
+        for (uint32_t b = 0; b < (uint32_t)kMaxShards; ++b) p.dY[b] = b < gy.y ? dy.p[b * dy.nrep] : nullptr;
+        p.x_blocks = gx.y;
+        ProfileScope scope(stream, TT_K_UNPACK, 1 << k, batch, layer->n_in + layer->n_out, e, nx * (e + 1) + ny * (2 * e + 1), 0);
+        const dim3 grid(gx.x > gy.x ? gx.x : gy.x, gx.y + gy.y);
+        if (bf16) launch_unpack_gate<uint16_t>(p, grid, hs);
+        else launch_unpack_gate<float>(p, grid, hs);
+    } else {
+        ProfileScope scope(stream, TT_K_UNPACK, 1 << k, batch, layer->n_in, e, nx * (e + 1), 0);
+        if (bf16) launch_unpack_blocks<uint16_t>(p.x, gx, hs);
+        else launch_unpack_blocks<float>(p.x, gx, hs);
+    }
+    if (s.relu && !s.gated) {
+        ProfileScope scope(stream, TT_K_UNPACK, 1 << k, batch, layer->n_out, e, ny * (e + 1), 0);
+        if (bf16) launch_unpack_blocks<uint16_t>(p.y, gy, hs);
+        else launch_unpack_blocks<float>(p.y, gy, hs);
+    }
+    if (hipGetLastError() != hipSuccess) return TT_EDEVICE;
+    return tt_fc_backward(&s.layer, batch, k, dtype, tX, tW, tY, tdY, tdX, forms_dgrad, forms_wgrad, X, W, s.gated ? nullptr : s.relu ? Y : nullptr,
+                          s.gated ? Y : dY, dX, dW, ws + s.inner_at, ws_bytes - s.inner_at, stream);
 }

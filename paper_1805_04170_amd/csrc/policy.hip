@@ -51,24 +51,16 @@ __device__ __forceinline__ Stats joined(Stats a, Stats b)
 }
 __device__ __forceinline__ Stats wave_joined(Stats s)
 {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) s = joined(s, Stats{wave::shfl_xor(s.top, m), wave::shfl_xor(s.sum, m)});
-    return s;
+    const float top = wave_max(s.top);
+    return {top, wave_sum(s.top == -INFINITY ? s.sum : s.sum * wave::exp2_fast(s.top - top))};
 }
-// over a workgroup's waves, in their order; `red`: a Stats per wave
+// over a workgroup's waves, in every thread; `red`: a Stats per wave
 template <int WAVES> __device__ __forceinline__ Stats group_joined(Stats s, Stats *red)
 {
     s = wave_joined(s);
-    if constexpr (WAVES == 1) return s;
     if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    float top = red[0].top;
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, red[i].top);
-    s = {top, 0.0f};
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) s.sum += red[i].sum * (red[i].top == -INFINITY ? 1.0f : wave::exp2_fast(red[i].top - top));
-    return s;
+    return wave_joined((threadIdx.x & 63u) < (uint32_t)WAVES ? red[threadIdx.x & 63u] : Stats{-INFINITY, 0.0f});
 }
 
 template <typename T> __device__ __forceinline__ float max_of(u32x4 v, float m)
@@ -179,7 +171,7 @@ template <typename T> __device__ __forceinline__ void store_unit(const PolicyPar
     const Place to = place_of(p.G, p.s, p.s.b_shift, t, g.q);
     for (uint32_t x = 0; x < p.G.nrep; ++x) {
         T *dst = static_cast<T *>(p.G.p[to.block + x]) + to.at + g.j0 * kVec<T>;
-        store16(dst + (threadIdx.x & 63u) * kVec<T>, v);
+        store16_once(dst + (threadIdx.x & 63u) * kVec<T>, v);
     }
 }
 
@@ -299,13 +291,13 @@ template <typename T> struct RowMap {
     {
         const uint32_t lane = threadIdx.x & 63u;
         if (row) {
-            store16(row + (size_t)u * 64 * kVec<T> + lane * kVec<T>, v);
+            store16_once(row + (size_t)u * 64 * kVec<T> + lane * kVec<T>, v);
             return;
         }
         const Unit g = unit_of(p, u);
         const Place to = place_of(p.G, p.s, p.s.b_shift, t, g.q);
         for (uint32_t x = 0; x < p.G.nrep; ++x)
-            store16(reinterpret_cast<T *>((uintptr_t)uniform(g_table[to.block + x])) + to.at + g.j0 * kVec<T> + lane * kVec<T>, v);
+            store16_once(reinterpret_cast<T *>((uintptr_t)uniform(g_table[to.block + x])) + to.at + g.j0 * kVec<T> + lane * kVec<T>, v);
     }
 };
 
@@ -596,19 +588,25 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(kPartWaves * 64) v
 }
 
 // The rows' losses, added up in 64 bits in an order that depends on their number alone
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 512, kSumLoads = 8;
 __global__ __launch_bounds__(kSumThreads) void sum_losses_kernel(const float *row_loss, uint32_t n, float *loss)
 {
-    __shared__ double part[kSumThreads];
+    __shared__ double part[kSumThreads / 64];
     double s = 0.0;
-    for (uint32_t i = threadIdx.x; i < n; i += kSumThreads) s += (double)row_loss[i];
-    part[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        s = (part[threadIdx.x] + part[threadIdx.x + 64]) + (part[threadIdx.x + 128] + part[threadIdx.x + 192]);
+    for (uint32_t i = threadIdx.x; i < n; i += kSumThreads * kSumLoads) {
+        float f[kSumLoads];
 #pragma unroll
-        for (int m = 32; m > 0; m >>= 1) s += wave::shfl_xor(s, m);
-        if (threadIdx.x == 0) *loss = (float)s;
+        for (int k = 0; k < kSumLoads; ++k) f[k] = i + k * kSumThreads < n ? row_loss[i + k * kSumThreads] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < kSumLoads; ++k) s += (double)f[k];
+    }
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) s += wave::shfl_xor(s, m);
+    if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kSumThreads / 64; ++w) s += part[w];
+        *loss = (float)s;
     }
 }
 
@@ -664,7 +662,9 @@ template <typename T> tt_status launch_policy(PolicyParams &p, hipStream_t s)
         else if (fits(16, 16)) launch_rows<T, 16, 16, true>(p, s);
         else launch_rows<T, 16, 20, true>(p, s);
     } else {
-        if (fits(1, 4)) launch_rows<T, 1, 4, true>(p, s);
+        if (fits(1, 1)) launch_rows<T, 1, 1, true>(p, s);
+        else if (fits(1, 2)) launch_rows<T, 1, 2, true>(p, s);
+        else if (fits(1, 4)) launch_rows<T, 1, 4, true>(p, s);
         else if (fits(1, 8)) launch_rows<T, 1, 8, true>(p, s);
         else if (fits(1, 16)) launch_rows<T, 1, 16, true>(p, s);
         else if (fits(2, 16)) launch_rows<T, 2, 16, true>(p, s);

@@ -41,6 +41,29 @@ __device__ __forceinline__ void forget_uniform(uint32_t &v) { asm volatile("" : 
 // 2^x (1 ulp; what lies below 2^-126 is 0)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// v of the lane that a data-parallel-primitive control names, `other` where it names none
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float v, float other)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(other), (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t other)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)v, CTRL, ROWS, 0xf, false);
+}
+// v combined over the wave, in every lane: up the rows of 16 lanes (shifts by 1, 2, 4, 8), then from row to row (the last lane of
+// a row to the next one, of the lower half to the upper).  No trip through LDS; the order of additions is fixed.
+template <typename V, class F> __device__ __forceinline__ V combined(V v, V none, F &&f)
+{
+    v = f(v, moved<0x111, 0xf>(v, none));
+    v = f(v, moved<0x112, 0xf>(v, none));
+    v = f(v, moved<0x114, 0xf>(v, none));
+    v = f(v, moved<0x118, 0xf>(v, none));
+    v = f(v, moved<0x142, 0xa>(v, none));
+    v = f(v, moved<0x143, 0xc>(v, none));
+    if constexpr (sizeof(V) == 4 && !__is_same(V, uint32_t)) return __uint_as_float(read_lane(__float_as_uint(v), 63));
+    else return read_lane(v, 63);
+}
+
 } // namespace wave
 } // namespace tt
 #endif
@@ -52,24 +75,9 @@ __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__bui
 
 __device__ __forceinline__ uint64_t uniform(uint64_t v) { return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
 
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v = fmaxf(v, wave::shfl_xor(v, m));
-    return v;
-}
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += wave::shfl_xor(v, m);
-    return v;
-}
-__device__ __forceinline__ uint32_t wave_sum(uint32_t v)
-{
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += wave::shfl_xor(v, m);
-    return v;
-}
+__device__ __forceinline__ float wave_max(float v) { return wave::combined(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float v) { return wave::combined(v, 0.0f, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) { return wave::combined(v, 0u, [](uint32_t a, uint32_t b) { return a + b; }); }
 
 // ---- 16-byte vectors that begin at any element: rows of odd length begin anywhere, and the memory system takes a 16-byte
 // access at any address (the compiler splits it where a target does not)
@@ -90,6 +98,11 @@ template <typename T> __device__ __forceinline__ void store16(T *p, u32x4 v)
     *(TT_GLOBAL V *)p = v;
 }
 
+template <typename T> __device__ __forceinline__ void store16_once(T *p, u32x4 v) // (nobody reads it soon: no place in the caches)
+{
+    typedef typename Vec16<sizeof(T)>::type V;
+    __builtin_nontemporal_store((V)v, (TT_GLOBAL V *)p);
+}
 template <typename T> __device__ __forceinline__ T load_scalar(const T *p) { return *(const TT_CONSTANT T *)p; }
 template <typename T> __device__ __forceinline__ T load1(const T *p) { return *(const TT_GLOBAL T *)p; }
 template <typename T> __device__ __forceinline__ void store1(T *p, T v) { *(TT_GLOBAL T *)p = v; }

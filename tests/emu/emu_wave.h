@@ -46,6 +46,11 @@ inline uint64_t ballot(bool p)
     for (int i = 0; i < emu::kWave; ++i) m |= (uint64_t)(w.fb[i] != 0.0f) << i;
     return m;
 }
+template <typename V, class F> inline V combined(V v, V, F &&f)
+{
+    for (int m = 1; m < 64; m <<= 1) v = f(v, shfl_xor(v, m));
+    return v;
+}
 inline void lds_add(uint32_t *p, uint32_t v) { *p += v; }
 inline void fence() { emu::wave_sync(); }
 template <typename V> inline void forget(V &) {}
