@@ -10,7 +10,7 @@
  * Calls with no tokens, rows or columns return TT_OK and write nothing, but for tt_policy_loss's loss (0) and a table
  * gradient without tokens (zeros).  Errors as in tensor_tiling.h: TT_EINVAL (NULL, unknown type or letter, k out of
  * range, negative or misaligned), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 tokens, rows, columns or
- * vocabulary entries, and more), TT_EWORKSPACE, TT_EDEVICE. */
+ * vocabulary entries and more; 2^30 numbers of an embedding; 2^22 tokens of a loss), TT_EWORKSPACE, TT_EDEVICE. */
 #ifndef TENSOR_TILING_TOKENS_H
 #define TENSOR_TILING_TOKENS_H
 
@@ -35,7 +35,8 @@ tt_status tt_embed_forward(int64_t tokens, int64_t vocab, int64_t width, int k, 
 /* dW[v] = scale * sum of dX[t] over the tokens t with ids[t] = v (zeros where there is none), every row written.  The
  * sums are fp32 and run over the tokens sorted by number, in an order that depends on ids alone, so equal calls give equal
  * bits; one rounding to dtype.  dX: tokens x width under tdX;  dW: vocab x width under tdW.
- * Workspace: device memory, 256-byte aligned, at least tt_embed_workspace_bytes; nothing in it needs clearing. */
+ * Workspace: device memory, 256-byte aligned, at least tt_embed_workspace_bytes (may be NULL if 0); nothing in it needs
+ * clearing. */
 tt_status tt_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width, int k, int dtype, tt_tiling tdX, tt_tiling tdW,
                                    size_t *bytes);
 tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t width, int k, int dtype, tt_tiling tdX, tt_tiling tdW,

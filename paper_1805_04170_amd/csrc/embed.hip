@@ -49,9 +49,9 @@ uint64_t groups_of(const Split &w, uint64_t rows)
 
 // a wave's work in the wide form, all of it scalars
 struct WaveWork { uint32_t row, q, j0; };
-__device__ __forceinline__ WaveWork wave_work(const Split &w)
+__device__ __forceinline__ WaveWork wave_work(const Split &w, uint32_t group)
 {
-    const uint32_t g = blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
+    const uint32_t g = group * kWaves + uniform(threadIdx.x >> 6);
     const uint32_t row = quotient(g, w.by_row), rest = g - row * w.by_row.d;
     const uint32_t q = quotient(rest, w.by_segment);
     return {row, q, (rest - q * w.parts) * 64 * kU};
@@ -122,7 +122,7 @@ struct EmbedParams {
 // A wave's part of one token's row, all of it loaded before the first vector is stored.
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_wide_kernel(const EmbedParams p)
 {
-    const WaveWork g = wave_work(p.w);
+    const WaveWork g = wave_work(p.w, blockIdx.x);
     if (g.row >= p.tokens) return;
     const int64_t v = token_scalar<I>(p.ids, g.row);
     const Columns<T> c(p.w.s, g.j0);
@@ -181,11 +181,21 @@ struct SortParams {
 };
 
 constexpr uint32_t kNoToken = ~0u;
-template <typename I> __device__ __forceinline__ uint32_t number_at(const SortParams &p, uint32_t t, uint32_t end)
+// kSortLoads numbers a lane from tb on, kNoToken where there is none (all loads before the first number is looked at)
+template <typename I> __device__ __forceinline__ void load_numbers(uint32_t (&v)[kSortLoads], const SortParams &p, uint32_t tb, uint32_t end)
 {
-    if (t >= end) return kNoToken;
-    const int64_t v = token_at<I>(p.ids, t);
-    return v >= 0 && v < p.vocab ? (uint32_t)v : kNoToken;
+    I raw[kSortLoads];
+    const uint32_t t = tb + (threadIdx.x & 63u);
+#pragma unroll
+    for (int i = 0; i < kSortLoads; ++i) {
+        const uint32_t at = t + i * 64 < end ? t + i * 64 : end - 1;
+        raw[i] = load1(static_cast<const I *>(p.ids) + at);
+    }
+#pragma unroll
+    for (int i = 0; i < kSortLoads; ++i) {
+        const int64_t n = (int64_t)raw[i];
+        v[i] = t + i * 64 < end && n >= 0 && n < p.vocab ? (uint32_t)n : kNoToken;
+    }
 }
 
 template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const SortParams p)
@@ -201,8 +211,7 @@ template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_token
     uint32_t *mine = at + w * range;
     uint32_t below = 0, v[kSortLoads];
     for (uint32_t tb = t0; tb < t1; tb += 64 * kSortLoads) {
-#pragma unroll
-        for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
+        load_numbers<I>(v, p, tb, t1);
 #pragma unroll
         for (int i = 0; i < kSortLoads; ++i) {
             if (v[i] == kNoToken) continue;
@@ -240,10 +249,7 @@ template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_token
     }
     __syncthreads();
     for (uint32_t tb = t0; tb < t1; tb += 64 * kSortLoads) {
-        if (stretch > 64 * kSortLoads) { // (otherwise they are still here)
-#pragma unroll
-            for (int i = 0; i < kSortLoads; ++i) v[i] = number_at<I>(p, tb + i * 64 + lane, t1);
-        }
+        if (stretch > 64 * kSortLoads) load_numbers<I>(v, p, tb, t1); // (otherwise they are still here)
 #pragma unroll
         for (int i = 0; i < kSortLoads; ++i) {
             const bool in = v[i] != kNoToken && (v[i] & (groups - 1)) == me;
@@ -276,7 +282,9 @@ struct EmbedGradParams {
     Places to;
     Divisor by_chunk;
     uint32_t places; // 2^wlog * range
+    uint32_t tokens;
     uint32_t chunk, runs, cols;
+    uint32_t run_groups; // workgroups for runs (wide)
     uint32_t rows, apart; // of the table's gradient per wave, and how far they lie from each other (wide)
     int64_t vocab;
     float scale;
@@ -371,9 +379,6 @@ template <typename I> __device__ __forceinline__ Run run_of(const EmbedGradParam
     return {b, e, (uint32_t)token_at<I>(p.ids, p.order[b]), (uint32_t)token_at<I>(p.ids, p.order[e - 1]), true};
 }
 
-// (2) The first waves take a run each.  The others do p.rows numbers each, 8 lanes to each of them: where their tokens begin comes
-// in one load, and the first 8 tokens of each in another.  The numbers lie p.apart from each other: the frequent ones, which
-// neighbour each other in most vocabularies, go to different waves.
 template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, const EmbedGradParams &p, const Columns<T> &c, uint32_t v, uint32_t q)
 {
     const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, q);
@@ -385,33 +390,41 @@ template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, con
     }
 }
 
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_sums_wide_kernel(const EmbedGradParams p)
+// a run's parts of numbers with many tokens, as partial sums
+template <typename T, typename I> __device__ __forceinline__ void sum_run(const EmbedGradParams &p, const WaveWork &g)
 {
-    const WaveWork g = wave_work(p.w);
+    if (g.row >= p.runs) return;
+    const Run r = run_of<I>(p, g.row);
+    if (!r.any) return;
+    const Columns<T> c(p.w.s, g.j0);
+    const Sources<T> src(p, g);
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+        if (side == 1 && r.last == r.first) break;
+        const uint32_t at = uniform(place(p.to, side == 0 ? r.first : r.last)), vb = load_scalar(p.start + at), ve = load_scalar(p.start + at + 1);
+        if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
+        Sums<T> a;
+        a.clear();
+        add_rows<T, kRunBatch>(a, p, src, c, vb > r.b ? vb : r.b, ve < r.e ? ve : r.e);
+        float *to = partial_of(p, g.row, vb > r.b, g.q);
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+            for (int i = 0; i < kVec<T>; i += 4)
+                store16(to + c.col[u] + i, u32x4{__float_as_uint(a.f[u][i]), __float_as_uint(a.f[u][i + 1]), __float_as_uint(a.f[u][i + 2]), __float_as_uint(a.f[u][i + 3])});
+    }
+}
+
+// p.rows numbers, 8 lanes to each of them: where their tokens begin comes in one load, and the first 8 tokens of each in another.
+// The numbers lie p.apart from each other: the frequent ones, which neighbour each other in most vocabularies, go to
+// different waves.
+template <typename T> __device__ __forceinline__ void sum_rows(const EmbedGradParams &p, const WaveWork &g)
+{
     const uint32_t lane = threadIdx.x & 63u, vocab = (uint32_t)p.vocab;
     const Columns<T> c(p.w.s, g.j0);
     const Sources<T> src(p, g);
     Sums<T> a;
-    if (g.row < p.runs) {
-        const Run r = run_of<I>(p, g.row);
-        if (!r.any) return;
-#pragma unroll 1
-        for (int side = 0; side < 2; ++side) {
-            if (side == 1 && r.last == r.first) break;
-            const uint32_t at = uniform(place(p.to, side == 0 ? r.first : r.last)), vb = load_scalar(p.start + at), ve = load_scalar(p.start + at + 1);
-            if (ve - vb <= p.chunk) continue; // (a number with more tokens than a run holds reaches the run's first or last place)
-            a.clear();
-            add_rows<T, kRunBatch>(a, p, src, c, vb > r.b ? vb : r.b, ve < r.e ? ve : r.e);
-            float *to = partial_of(p, g.row, vb > r.b, g.q);
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int i = 0; i < kVec<T>; i += 4)
-                    store16(to + c.col[u] + i, u32x4{__float_as_uint(a.f[u][i]), __float_as_uint(a.f[u][i + 1]), __float_as_uint(a.f[u][i + 2]), __float_as_uint(a.f[u][i + 3])});
-        }
-        return;
-    }
-    const uint32_t v0 = g.row - p.runs;
+    const uint32_t v0 = g.row;
     if (v0 >= p.apart) return;
     uint32_t begin = 0, end = 0, tokens = 0;
     {
@@ -427,7 +440,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     for (uint32_t k = 0; k < p.rows; ++k) {
         const uint32_t v = v0 + k * p.apart, b = wave::read_lane(begin, (int)k * 8), e = wave::read_lane(end, (int)k * 8);
         if (v >= vocab) break;
-        if (e - b > p.chunk) continue; // (3)
+        if (e - b > p.chunk) continue; // (runs)
         if (e == b) { // most rows
             const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q);
 #pragma unroll
@@ -441,6 +454,68 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
         if (b + 8 < e) add_rows<T, kRowBatch>(a, p, src, c, b + 8, e);
         finish_row(a, p, c, v, g.q);
     }
+}
+
+// The row of a number with many tokens whose first one lies in the run (there is one such number at most, the run's last): the sum
+// over its partial sums.
+struct Long { uint32_t v, last; bool any; };
+template <typename I> __device__ __forceinline__ Long long_of(const EmbedGradParams &p, uint32_t run)
+{
+    const Run r = run_of<I>(p, run);
+    if (!r.any) return {0, 0, false};
+    const uint32_t at = place(p.to, r.last), b = p.start[at], e = p.start[at + 1];
+    return {r.last, quotient(e - 1, p.by_chunk), b >= r.b && e - b > p.chunk};
+}
+// (the first of its partial sums counts as begun inside the run unless it is the run's first place)
+__device__ __forceinline__ const float *partial_in(const EmbedGradParams &p, uint32_t run, uint32_t first_run, bool inside, uint32_t q)
+{
+    return partial_of(p, run, run == first_run && inside, q);
+}
+
+template <typename T, typename I> __device__ __forceinline__ void join_runs(const EmbedGradParams &p, const WaveWork &g)
+{
+    if (g.row >= p.runs) return;
+    const Long w = long_of<I>(p, g.row);
+    if (!w.any) return;
+    const uint32_t v = uniform(w.v), last = uniform(w.last);
+    const bool inside = load_scalar(p.start + place(p.to, v)) > g.row * p.chunk;
+    const Columns<T> c(p.w.s, g.j0);
+    Sums<T> a;
+    a.clear();
+    for (uint32_t run = g.row; run <= last; run += kPartials) {
+        u32x4 r[kPartials][kU][kVec<T> / 4];
+#pragma unroll
+        for (int k = 0; k < kPartials; ++k) {
+            if (run + k > last) break;
+            const float *from = partial_in(p, run + k, g.row, inside, g.q);
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int i = 0; i < kVec<T> / 4; ++i) r[k][u][i] = load16(from + c.col[u] + 4 * i);
+        }
+#pragma unroll
+        for (int k = 0; k < kPartials; ++k) {
+            if (run + k > last) break;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int i = 0; i < kVec<T>; ++i) a.f[u][i] += __uint_as_float(r[k][u][i / 4][i % 4]);
+        }
+    }
+    finish_row(a, p, c, v, g.q);
+}
+
+// (2) The first workgroups' waves take a run each, beside the rows.  (The runs in a launch of their own in front, and the joins in
+// this one: 2 to 3 % faster at 65536 x 8192 and 16384 tokens, 10 % slower at 32000 x 1024 and 8192.)
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_sums_wide_kernel(const EmbedGradParams p)
+{
+    if (blockIdx.x < p.run_groups) sum_run<T, I>(p, wave_work(p.w, blockIdx.x));
+    else sum_rows<T>(p, wave_work(p.w, blockIdx.x - p.run_groups));
+}
+// (3)
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_wide_kernel(const EmbedGradParams p)
+{
+    join_runs<T, I>(p, wave_work(p.w, blockIdx.x));
 }
 
 // the rows of places [b, e) of the sorted list, a vector of each, kRunBatch of them on their way together
@@ -495,56 +570,6 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q), g.j * kVec<T>, n, pack16(s, T()));
 }
 
-// (3) A wave per run and part (a group of lanes per run and segment) looks for a number of many tokens whose first one lies in its
-// run; there is one at most, the run's last.
-struct Long { uint32_t v, last; bool any; };
-template <typename I> __device__ __forceinline__ Long long_of(const EmbedGradParams &p, uint32_t run)
-{
-    const Run r = run_of<I>(p, run);
-    if (!r.any) return {0, 0, false};
-    const uint32_t at = place(p.to, r.last), b = p.start[at], e = p.start[at + 1];
-    return {r.last, quotient(e - 1, p.by_chunk), b >= r.b && e - b > p.chunk};
-}
-// (the first of its partial sums counts as begun inside the run unless it is the run's first place)
-__device__ __forceinline__ const float *partial_in(const EmbedGradParams &p, uint32_t run, uint32_t first_run, bool inside, uint32_t q)
-{
-    return partial_of(p, run, run == first_run && inside, q);
-}
-
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_wide_kernel(const EmbedGradParams p)
-{
-    const WaveWork g = wave_work(p.w);
-    if (g.row >= p.runs) return;
-    const Long w = long_of<I>(p, g.row);
-    if (!w.any) return;
-    const uint32_t v = uniform(w.v), last = uniform(w.last);
-    const bool inside = load_scalar(p.start + place(p.to, v)) > g.row * p.chunk;
-    const Columns<T> c(p.w.s, g.j0);
-    Sums<T> a;
-    a.clear();
-    for (uint32_t run = g.row; run <= last; run += kPartials) {
-        u32x4 r[kPartials][kU][kVec<T> / 4];
-#pragma unroll
-        for (int k = 0; k < kPartials; ++k) {
-            if (run + k > last) break;
-            const float *from = partial_in(p, run + k, g.row, inside, g.q);
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int i = 0; i < kVec<T> / 4; ++i) r[k][u][i] = load16(from + c.col[u] + 4 * i);
-        }
-#pragma unroll
-        for (int k = 0; k < kPartials; ++k) {
-            if (run + k > last) break;
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int i = 0; i < kVec<T>; ++i) a.f[u][i] += __uint_as_float(r[k][u][i / 4][i % 4]);
-        }
-    }
-    finish_row(a, p, c, v, g.q);
-}
-
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_narrow_kernel(const EmbedGradParams p)
 {
     const LaneWork g = lane_work(p.w);
@@ -570,6 +595,126 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
     store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, w.v, g.q), g.j * kVec<T>, n, pack16(s, T()));
+}
+
+// Few tokens: nothing to sort.  Every wave holds all token numbers, 64 to a register, and asks for each of its rows which of them
+// are the row's; one launch.
+constexpr uint32_t kFewTokens = 256, kFewRegisters = kFewTokens / 64;
+struct Found {
+    uint64_t in[kFewRegisters];
+    __device__ __forceinline__ bool any() const
+    {
+        uint64_t m = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kFewRegisters; ++i) m |= in[i];
+        return m != 0;
+    }
+    // takes out the first one
+    __device__ __forceinline__ uint32_t next()
+    {
+        uint32_t t = 0;
+        bool done = false;
+#pragma unroll
+        for (uint32_t i = 0; i < kFewRegisters; ++i) {
+            if (done || in[i] == 0) continue;
+            t = i * 64 + (uint32_t)__builtin_ctzll(in[i]);
+            in[i] &= in[i] - 1;
+            done = true;
+        }
+        return t;
+    }
+};
+template <typename I> struct Few {
+    uint32_t number[kFewRegisters];
+    __device__ __forceinline__ Few(const EmbedGradParams &p)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kFewRegisters; ++i) {
+            const uint32_t t = i * 64 + (threadIdx.x & 63u);
+            const int64_t v = p.tokens ? token_at<I>(p.ids, t < p.tokens ? t : p.tokens - 1) : -1;
+            number[i] = t < p.tokens && v >= 0 && v < p.vocab ? (uint32_t)v : kNoToken;
+        }
+    }
+    // the tokens with numbers in [v, v + n)
+    __device__ __forceinline__ Found of(uint32_t v, uint32_t n) const
+    {
+        Found f;
+#pragma unroll
+        for (uint32_t i = 0; i < kFewRegisters; ++i) f.in[i] = wave::ballot(number[i] != kNoToken && number[i] - v < n);
+        return f;
+    }
+    __device__ __forceinline__ uint32_t number_of(uint32_t t) const
+    {
+        uint32_t v = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kFewRegisters; ++i)
+            if (t / 64 == i) v = wave::read_lane(number[i], (int)(t & 63u));
+        return v;
+    }
+};
+
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_few_wide_kernel(const EmbedGradParams p)
+{
+    const WaveWork g = wave_work(p.w, blockIdx.x);
+    if (g.row >= p.apart) return;
+    const Few<I> few(p);
+    const Columns<T> c(p.w.s, g.j0);
+    const Sources<T> src(p, g);
+#pragma unroll 1
+    for (uint32_t k = 0; k < p.rows; ++k) {
+        const uint32_t v = g.row + k * p.apart;
+        if (v >= (uint32_t)p.vocab) break;
+        Found f = few.of(v, 1);
+        Sums<T> a;
+        a.clear();
+        while (f.any()) {
+            uint32_t t[kRowBatch], n = 0;
+#pragma unroll
+            for (int i = 0; i < kRowBatch; ++i) {
+                n += f.any() ? 1 : 0;
+                t[i] = f.next();
+            }
+            add_batch<T, kRowBatch>(a, p, src, c, n, [&](int i) { return t[i]; });
+        }
+        finish_row(a, p, c, v, g.q);
+    }
+}
+
+template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_few_narrow_kernel(const EmbedGradParams p)
+{
+    const LaneWork g = lane_work(p.w);
+    const uint32_t n = values_of(p.w.s, kVec<T>, g.j), vocab = (uint32_t)p.vocab;
+    const Few<I> few(p);
+    // the wave's rows: those of its first and its last lane, and what lies between
+    const uint32_t v0 = wave::read_lane(g.row, 0), v1 = wave::read_lane(g.row, 63);
+    Found f = few.of(v0, v1 - v0 + 1);
+    float s[kVec<T>] = {};
+    while (f.any()) {
+        uint32_t t[kRowBatch], v[kRowBatch], m = 0;
+        u32x4 r[kRowBatch];
+#pragma unroll
+        for (int i = 0; i < kRowBatch; ++i) {
+            m += f.any() ? 1 : 0;
+            t[i] = f.next();
+            v[i] = few.number_of(t[i]);
+            r[i] = u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < kRowBatch; ++i)
+            if ((uint32_t)i < m && v[i] == g.row && n) r[i] = load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, t[i], g.q) + g.j * kVec<T>, n);
+#pragma unroll
+        for (int i = 0; i < kRowBatch; ++i) {
+            if ((uint32_t)i >= m || v[i] != g.row) continue;
+            float x[kVec<T>];
+            unpack16(r[i], x, T());
+#pragma unroll
+            for (int q = 0; q < kVec<T>; ++q) s[q] += x[q];
+        }
+    }
+    if (g.row >= vocab || n == 0) return;
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
+    store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, g.row, g.q), g.j * kVec<T>, n, pack16(s, T()));
 }
 
 // ----------------------------------------------------------------------------------------------------- host side
@@ -608,11 +753,10 @@ struct GradSpace {
 };
 GradSpace grad_space(int64_t tokens, int64_t vocab, int64_t width)
 {
-    GradSpace s;
+    GradSpace s{0, 0, 0, 0, 0, places_of(vocab)};
+    if (tokens <= (int64_t)kFewTokens) return s; // (nothing is sorted)
     const uint32_t chunk = run_length(tokens);
     s.runs = tokens > chunk ? (uint32_t)((tokens + chunk - 1) / chunk) : 0;
-    s.to = places_of(vocab);
-    s.order = 0;
     s.start = align_up((size_t)tokens * 4, 256);
     s.partial = s.start + align_up((((size_t)s.to.range << s.to.wlog) + 1) * 4, 256);
     s.bytes = s.partial + align_up((size_t)2 * s.runs * (size_t)width * 4, 256);
@@ -676,6 +820,11 @@ namespace {
 template <typename T, typename I>
 tt_status launch_embed_grad(const SortParams &sp, const EmbedGradParams &p, uint32_t run_groups, uint32_t row_groups, hipStream_t s)
 {
+    if (p.tokens <= kFewTokens) {
+        if (p.w.wide) hipLaunchKernelGGL((embed_few_wide_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        else hipLaunchKernelGGL((embed_few_narrow_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        return launched();
+    }
     hipLaunchKernelGGL((sort_tokens_kernel<I>), dim3(1u << sp.to.wlog), dim3(kSortThreads), 0, s, sp);
     if (p.w.wide) {
         hipLaunchKernelGGL((embed_sums_wide_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
@@ -703,7 +852,7 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     if (!make_blocks(dX, tdX, k, tokens, width, &p.G) || !make_blocks(const_cast<const void *const *>(dW), tdW, k, vocab, width, &p.W)) return TT_EINFEASIBLE;
     if (vocab == 0 || width == 0) return TT_OK;
     const GradSpace sp = grad_space(tokens, vocab, width);
-    if (!workspace || ws_bytes < sp.bytes || reinterpret_cast<uintptr_t>(workspace) % 256) return TT_EWORKSPACE;
+    if (sp.bytes && (!workspace || ws_bytes < sp.bytes || reinterpret_cast<uintptr_t>(workspace) % 256)) return TT_EWORKSPACE;
     char *ws = static_cast<char *>(workspace);
     SortParams q;
     q.ids = ids;
@@ -719,6 +868,7 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     p.partial = reinterpret_cast<float *>(ws + sp.partial);
     p.to = sp.to;
     p.places = sp.to.range << sp.to.wlog;
+    p.tokens = (uint32_t)tokens;
     p.chunk = run_length(tokens);
     p.by_chunk = divisor(p.chunk);
     p.runs = sp.runs;
@@ -729,12 +879,13 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     const uint64_t waves = (uint64_t)vocab * p.w.s.nseg * p.w.parts;
     p.rows = waves >= 8 * 8192 ? 8 : waves >= 4 * 8192 ? 4 : waves >= 2 * 8192 ? 2 : 1;
     p.apart = (uint32_t)((vocab + p.rows - 1) / p.rows);
-    const uint64_t run_groups = groups_of(p.w, sp.runs), row_groups = groups_of(p.w, (uint64_t)sp.runs + (p.w.wide ? p.apart : (uint64_t)vocab));
+    const uint64_t run_groups = groups_of(p.w, sp.runs), row_groups = p.w.wide ? run_groups + groups_of(p.w, p.apart) : groups_of(p.w, (uint64_t)sp.runs + (uint64_t)vocab);
     if (run_groups * kThreads >= (uint64_t(1) << 31) || row_groups * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;
     const uint64_t row = (uint64_t)width * e;
     ProfileScope scope(stream, TT_K_EMBED_GRAD, 1 << k, vocab, width, e, (uint64_t)tokens * row + (uint64_t)vocab * row * p.W.nrep, 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const uint32_t rg = (uint32_t)run_groups, wg = (uint32_t)row_groups;
+    p.run_groups = p.w.wide ? rg : 0;
     if (dtype == TT_BF16)
         return id_dtype == TT_I32 ? launch_embed_grad<uint16_t, int32_t>(q, p, rg, wg, s)
                                   : launch_embed_grad<uint16_t, int64_t>(q, p, rg, wg, s);

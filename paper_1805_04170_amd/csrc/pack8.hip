@@ -74,52 +74,120 @@ __device__ __forceinline__ u32x4 load_bytes(const int8_t *q, uint32_t n)
     return u32x4{w[0], w[1], w[2], w[3]};
 }
 
-// Two lanes a block, 16 values each; kUnits blocks of a lane on their way together.
-constexpr int kUnits = 2;
+// The largest magnitude's bits of a vector: magnitudes compare as their bits do, infinities and NaN above all others
+__device__ __forceinline__ uint32_t largest(u32x4 v, float)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t m = v[j] & 0x7fffffffu;
+        top = m > top ? m : top;
+    }
+    return top;
+}
+__device__ __forceinline__ uint32_t largest(u32x4 v, uint16_t)
+{
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t m = v[j] & 0x7fff7fffu;
+        top = __builtin_elementwise_max(top, u16x2{(uint16_t)m, (uint16_t)(m >> 16)});
+    }
+    return (uint32_t)(top.x > top.y ? top.x : top.y) << 16;
+}
+// x / step in whole steps (low byte), ties to even, a step at least where x is not 0: x inv is exact, and 1.5 * 2^23 + n is n in the
+// number's last bits
+__device__ __forceinline__ uint32_t steps_of(float x, float inv)
+{
+    const uint32_t q = __float_as_uint(fmaf(x, inv, 12582912.0f));
+    const int sign = (int)__float_as_uint(x + 0.0f); // (-0 is no step)
+    const uint32_t one = (uint32_t)(sign > 1 ? 1 : sign < -1 ? -1 : sign);
+    return q == 0x4b400000u ? one : q;
+}
+
+__device__ __forceinline__ float inverse_of(uint32_t s) { return s == 255 ? 0.0f : __uint_as_float((254u - s) << 23); }
+// a vector's values as bytes
+template <typename T> struct Bytes { uint32_t w[kVec<T> / 4]; };
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+__device__ __forceinline__ void store_bytes(int8_t *q, const Bytes<uint16_t> &b) { *(TT_GLOBAL u32x2_any *)q = u32x2_any{b.w[0], b.w[1]}; }
+__device__ __forceinline__ void store_bytes(int8_t *q, const Bytes<float> &b) { *(TT_GLOBAL u32_any *)q = b.w[0]; }
+__device__ __forceinline__ void load_bytes(const int8_t *q, Bytes<uint16_t> &b)
+{
+    const u32x2_any w = *(const TT_GLOBAL u32x2_any *)q;
+    b.w[0] = w.x;
+    b.w[1] = w.y;
+}
+__device__ __forceinline__ void load_bytes(const int8_t *q, Bytes<float> &b) { b.w[0] = *(const TT_GLOBAL u32_any *)q; }
+template <typename T> __device__ __forceinline__ Bytes<T> packed(u32x4 v, uint32_t s)
+{
+    const float inv = inverse_of(s);
+    float g[kVec<T>];
+    unpack16(v, g, T());
+    Bytes<T> b;
+#pragma unroll
+    for (int i = 0; i < kVec<T> / 4; ++i) {
+        b.w[i] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b.w[i] |= (steps_of(g[4 * i + j], inv) & 255u) << (8 * j);
+        if (s == 255) b.w[i] = 0;
+    }
+    return b;
+}
+
+// Any width: two lanes a block, 16 values each.
 template <typename T> __global__ __launch_bounds__(kThreads) void pack8_kernel(const PackParams p)
 {
-    const uint64_t u0 = (uint64_t)blockIdx.x * (kThreads * kUnits) + threadIdx.x;
-    const T *x = static_cast<const T *>(p.X[blockIdx.y]);
-    Half h[kUnits];
-    Values<T> v[kUnits];
+    const uint64_t u = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+    const Half h = half_of(p, u);
+    const Values<T> v = load_values(static_cast<const T *>(p.X[blockIdx.y]) + (h.n ? h.at : 0), h.n);
+    uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-        h[k] = half_of(p, u0 + k * kThreads);
-        v[k] = load_values(x + (h[k].n ? h[k].at : 0), h[k].n);
+    for (int i = 0; i < 16 / kVec<T>; ++i) {
+        const uint32_t t = largest(v.r[i], T());
+        top = t > top ? t : top;
+    }
+    const uint32_t other = wave::shfl_xor(top, 1), s = scale_byte(other > top ? other : top);
+    if (h.n == 0) return;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 16 / kVec<T>; ++i) {
+        const Bytes<T> b = packed<T>(v.r[i], s);
+#pragma unroll
+        for (int j = 0; j < kVec<T> / 4; ++j) w[i * kVec<T> / 4 + j] = b.w[j];
+    }
+    int8_t *to = p.Q[blockIdx.y] + h.at;
+    if (h.n == 16) {
+        *(TT_GLOBAL u32x4_any *)to = u32x4_any{w[0], w[1], w[2], w[3]};
+    } else {
+        for (uint32_t i = 0; i < h.n; ++i) store1(to + i, (int8_t)(w[i >> 2] >> (8 * (i & 3))));
+    }
+    if ((threadIdx.x & 1u) == 0) store1(p.S[blockIdx.y] + h.block, (uint8_t)s);
+}
+
+// Rows of whole blocks: a shard is one row of blocks.  A lane takes a vector, 4 (bf16) or 8 lanes a block, so that a wave's loads and
+// stores are one piece of memory each, and kFlat vectors are on their way together.
+constexpr int kFlat = 4;
+template <typename T> __global__ __launch_bounds__(kThreads) void pack8_flat_kernel(const PackParams p)
+{
+    constexpr uint32_t EV = kVec<T>, LANES = kBlock / EV;
+    const uint64_t j0 = (uint64_t)blockIdx.x * (kThreads * kFlat) + threadIdx.x, last = p.units * (16 / EV) - 1;
+    const T *x = static_cast<const T *>(p.X[blockIdx.y]);
+    u32x4 v[kFlat];
+#pragma unroll
+    for (int k = 0; k < kFlat; ++k) {
+        const uint64_t j = j0 + k * kThreads;
+        v[k] = load16(x + (j < last ? j : last) * EV);
     }
 #pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-        float f[16];
-        uint32_t top = 0; // magnitudes compare as their bits do, infinities and NaN above all others
-#pragma unroll
-        for (int i = 0; i < 16 / kVec<T>; ++i) {
-            float g[kVec<T>];
-            unpack16(v[k].r[i], g, T());
-#pragma unroll
-            for (int j = 0; j < kVec<T>; ++j) {
-                const uint32_t m = __float_as_uint(g[j]) & 0x7fffffffu;
-                top = m > top ? m : top;
-                f[i * kVec<T> + j] = g[j];
-            }
-        }
-        const uint32_t other = wave::shfl_xor(top, 1);
-        const uint32_t s = scale_byte(other > top ? other : top);
-        if (h[k].n == 0) continue;
-        const float inv = s == 255 ? 0.0f : __uint_as_float((254u - s) << 23);
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            int q = s == 255 ? 0 : (int)rintf(f[i] * inv);
-            if (q == 0 && s != 255) q = f[i] > 0.0f ? 1 : f[i] < 0.0f ? -1 : 0;
-            w[i >> 2] |= (uint32_t)(q & 255) << (8 * (i & 3));
-        }
-        int8_t *to = p.Q[blockIdx.y] + h[k].at;
-        if (h[k].n == 16) {
-            *(TT_GLOBAL u32x4_any *)to = u32x4_any{w[0], w[1], w[2], w[3]};
-        } else {
-            for (uint32_t i = 0; i < h[k].n; ++i) store1(to + i, (int8_t)(w[i >> 2] >> (8 * (i & 3))));
-        }
-        if ((threadIdx.x & 1u) == 0) store1(p.S[blockIdx.y] + h[k].block, (uint8_t)s);
+    for (int k = 0; k < kFlat; ++k) {
+        const uint64_t j = j0 + k * kThreads;
+        const uint32_t s = scale_byte(wave::group_max<(int)LANES>(largest(v[k], T())));
+        const Bytes<T> b = packed<T>(v[k], s);
+        if (j > last) continue;
+        store_bytes(p.Q[blockIdx.y] + j * EV, b);
+        if (j % LANES == 0) store1(p.S[blockIdx.y] + j / LANES, (uint8_t)s);
     }
 }
 
@@ -155,6 +223,47 @@ template <typename T> __global__ __launch_bounds__(kThreads) void unpack8_kernel
     unpack_half_block<T>(p, blockIdx.y, u);
 }
 
+// ... rows of whole blocks; GATE: what is written is dY where the value is above 0
+template <typename T, bool GATE> __device__ __forceinline__ void unpack_flat(const PackParams &p, uint32_t shard, uint32_t group, const T *dY)
+{
+    constexpr uint32_t EV = kVec<T>, LANES = kBlock / EV;
+    const uint64_t j0 = (uint64_t)group * (kThreads * kFlat) + threadIdx.x, last = p.units * (16 / EV) - 1;
+    Bytes<T> q[kFlat];
+    uint32_t s[kFlat];
+    u32x4 v[kFlat];
+#pragma unroll
+    for (int k = 0; k < kFlat; ++k) {
+        const uint64_t j = j0 + k * kThreads < last ? j0 + k * kThreads : last;
+        load_bytes(p.Q[shard] + j * EV, q[k]);
+        s[k] = load1(p.S[shard] + j / LANES);
+        if constexpr (GATE) v[k] = load16(dY + j * EV);
+    }
+#pragma unroll
+    for (int k = 0; k < kFlat; ++k) {
+        const uint64_t j = j0 + k * kThreads;
+        if (j > last) continue;
+        if constexpr (GATE) {
+#pragma unroll
+            for (uint32_t i = 0; i < EV; ++i) {
+                const bool open = s[k] != 255 && (int8_t)(q[k].w[i / 4] >> (8 * (i & 3))) > 0;
+                const uint32_t mine = sizeof(T) == 4 ? 0xffffffffu : i & 1 ? 0xffff0000u : 0x0000ffffu;
+                v[k][i * sizeof(T) / 4] &= open ? 0xffffffffu : ~mine;
+            }
+        } else {
+            const float scale = scale_of(s[k]);
+            float g[EV];
+#pragma unroll
+            for (uint32_t i = 0; i < EV; ++i) g[i] = (float)(int8_t)(q[k].w[i / 4] >> (8 * (i & 3))) * scale;
+            v[k] = pack16(g, T());
+        }
+        store16(static_cast<T *>(p.X[shard]) + j * EV, v[k]);
+    }
+}
+template <typename T> __global__ __launch_bounds__(kThreads) void unpack8_flat_kernel(const PackParams p)
+{
+    unpack_flat<T, false>(p, blockIdx.y, blockIdx.x, nullptr);
+}
+
 // What a layer's backward pass needs of its activations, in one launch: the input unpacked, and the output's gradient where the
 // output's value is above 0 (the output itself is read as its 8 bits and never written out).
 struct GateParams {
@@ -163,6 +272,12 @@ struct GateParams {
     PackParams y;          // blocks of the output: Q, S; X takes the gated gradient
     uint32_t x_blocks;
 };
+// (both of whole blocks)
+template <typename T> __global__ __launch_bounds__(kThreads) void unpack_gate_flat_kernel(const GateParams p)
+{
+    if (blockIdx.y < p.x_blocks) unpack_flat<T, false>(p.x, blockIdx.y, blockIdx.x, nullptr);
+    else unpack_flat<T, true>(p.y, blockIdx.y - p.x_blocks, blockIdx.x, static_cast<const T *>(p.dY[blockIdx.y - p.x_blocks]));
+}
 template <typename T> __global__ __launch_bounds__(kThreads) void unpack_gate_kernel(const GateParams p)
 {
     const uint64_t u = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -185,8 +300,14 @@ template <typename T> __global__ __launch_bounds__(kThreads) void unpack_gate_ke
     store_values(static_cast<T *>(p.y.X[b]) + h.at, v, h.n);
 }
 
-// shard extents and the launch's size; `count` shards
-tt_status pack_geometry(PackParams *p, int64_t srows, int64_t scols, dim3 *grid, int count, uint32_t units_each)
+// shard extents and how many workgroups a shard takes
+bool flat(const PackParams &p) { return p.cols % kBlock == 0; }
+uint64_t groups_of(const PackParams &p, bool by_vectors, int elem_bytes)
+{
+    const uint64_t each = by_vectors ? (uint64_t)kThreads * kFlat : kThreads, n = by_vectors ? p.units * elem_bytes : p.units; // (16 values: e vectors)
+    return (n + each - 1) / each;
+}
+tt_status pack_geometry(PackParams *p, int64_t srows, int64_t scols)
 {
     if (!fits31(srows) || !fits31(scols)) return TT_EUNSUPPORTED;
     p->rows = (uint32_t)srows;
@@ -194,11 +315,28 @@ tt_status pack_geometry(PackParams *p, int64_t srows, int64_t scols, dim3 *grid,
     const uint32_t bpr = (uint32_t)((scols + kBlock - 1) / kBlock);
     p->by_bpr = divisor(bpr);
     p->units = (uint64_t)srows * bpr * 2;
-    p->narrow = p->units / 2 + kThreads * kUnits < (uint64_t(1) << 31);
-    const uint64_t each = kThreads * units_each, g = (p->units + each - 1) / each;
-    if (g * kThreads >= (uint64_t(1) << 32)) return TT_EUNSUPPORTED;
-    *grid = dim3((uint32_t)g, (uint32_t)count);
-    return TT_OK;
+    p->narrow = p->units / 2 + kThreads < (uint64_t(1) << 31);
+    return p->units >= (uint64_t(1) << 32) - kThreads ? TT_EUNSUPPORTED : TT_OK; // (a launch holds fewer than 2^32 threads)
+}
+template <typename T> void launch_unpack(const PackParams &p, int count, hipStream_t s)
+{
+    const dim3 grid((uint32_t)groups_of(p, flat(p), (int)sizeof(T)), (uint32_t)count);
+    if (flat(p)) hipLaunchKernelGGL((unpack8_flat_kernel<T>), grid, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((unpack8_kernel<T>), grid, dim3(kThreads), 0, s, p);
+}
+template <typename T> void launch_pack(const PackParams &p, int count, hipStream_t s)
+{
+    const dim3 grid((uint32_t)groups_of(p, flat(p), (int)sizeof(T)), (uint32_t)count);
+    if (flat(p)) hipLaunchKernelGGL((pack8_flat_kernel<T>), grid, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((pack8_kernel<T>), grid, dim3(kThreads), 0, s, p);
+}
+template <typename T> void launch_unpack_gate(const GateParams &p, uint32_t y_blocks, hipStream_t s)
+{
+    const bool both = flat(p.x) && flat(p.y);
+    const uint64_t x = groups_of(p.x, both, (int)sizeof(T)), y = groups_of(p.y, both, (int)sizeof(T));
+    const dim3 grid((uint32_t)(x > y ? x : y), p.x_blocks + y_blocks);
+    if (both) hipLaunchKernelGGL((unpack_gate_flat_kernel<T>), grid, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((unpack_gate_kernel<T>), grid, dim3(kThreads), 0, s, p);
 }
 
 bool bytes_fit(const void *const *shards, int k)
@@ -208,7 +346,7 @@ bool bytes_fit(const void *const *shards, int k)
     return true;
 }
 
-tt_status launch_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, const tt_tiling &t, const void *const *X,
+tt_status run_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, const tt_tiling &t, const void *const *X,
                       const void *const *Q, const void *const *S, void *stream)
 {
     if (!valid_k(k) || !valid_tiling(t, k) || !valid_dtype(dtype) || rows < 0 || cols < 0) return TT_EINVAL;
@@ -217,9 +355,8 @@ tt_status launch_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, c
     if (!make_grid(t.cut, k, rows, cols, &g)) return TT_EINFEASIBLE;
     if (rows == 0 || cols == 0) return TT_OK;
     PackParams p;
-    dim3 grid;
     const int n = 1 << k;
-    const tt_status st = pack_geometry(&p, g.srows, g.scols, &grid, n, pack ? kUnits : 1);
+    const tt_status st = pack_geometry(&p, g.srows, g.scols);
     if (st != TT_OK) return st;
     for (int s = 0; s < kMaxShards; ++s) {
         p.X[s] = s < n ? const_cast<void *>(X[s]) : nullptr;
@@ -230,11 +367,11 @@ tt_status launch_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, c
     ProfileScope scope(stream, pack ? TT_K_PACK : TT_K_UNPACK, n, rows, cols, dtype_bytes(dtype), values * (dtype_bytes(dtype) + 1) + (uint64_t)g.srows * p.by_bpr.d * n, 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     if (pack) {
-        if (dtype == TT_BF16) hipLaunchKernelGGL((pack8_kernel<uint16_t>), grid, dim3(kThreads), 0, s, p);
-        else hipLaunchKernelGGL((pack8_kernel<float>), grid, dim3(kThreads), 0, s, p);
+        if (dtype == TT_BF16) launch_pack<uint16_t>(p, n, s);
+        else launch_pack<float>(p, n, s);
     } else {
-        if (dtype == TT_BF16) hipLaunchKernelGGL((unpack8_kernel<uint16_t>), grid, dim3(kThreads), 0, s, p);
-        else hipLaunchKernelGGL((unpack8_kernel<float>), grid, dim3(kThreads), 0, s, p);
+        if (dtype == TT_BF16) launch_unpack<uint16_t>(p, n, s);
+        else launch_unpack<float>(p, n, s);
     }
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }
@@ -290,7 +427,7 @@ void buffers_of(void **shards, const tt_tiling &t, int k, const BlockTable &b, c
 
 // the blocks of a tensor in 8 bits, one replica of each, and where their values go
 tt_status packed_blocks(PackParams *p, const tt_tiling &t, int k, int64_t rows, int64_t cols, const void *const *Q, const void *const *S, char *to,
-                        size_t pitch, dim3 *grid)
+                        size_t pitch)
 {
     BlockTable q, s;
     if (!make_blocks(Q, t, k, rows, cols, &q) || !make_blocks(S, t, k, rows, cols, &s)) return TT_EINFEASIBLE;
@@ -300,16 +437,7 @@ tt_status packed_blocks(PackParams *p, const tt_tiling &t, int k, int64_t rows, 
         p->Q[b] = b < n ? static_cast<int8_t *>(q.p[b * q.nrep]) : nullptr;
         p->S[b] = b < n ? static_cast<uint8_t *>(s.p[b * s.nrep]) : nullptr;
     }
-    return pack_geometry(p, q.srows, q.scols, grid, (int)n, 1);
-}
-
-template <typename T> void launch_unpack_gate(const GateParams &p, dim3 grid, hipStream_t s)
-{
-    hipLaunchKernelGGL((unpack_gate_kernel<T>), grid, dim3(kThreads), 0, s, p);
-}
-template <typename T> void launch_unpack_blocks(const PackParams &p, dim3 grid, hipStream_t s)
-{
-    hipLaunchKernelGGL((unpack8_kernel<T>), grid, dim3(kThreads), 0, s, p);
+    return pack_geometry(p, q.srows, q.scols);
 }
 
 } // namespace
@@ -318,13 +446,13 @@ template <typename T> void launch_unpack_blocks(const PackParams &p, dim3 grid, 
 extern "C" tt_status tt_pack8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling t, const void *const *X, int8_t *const *Q,
                               uint8_t *const *S, void *stream)
 {
-    return tt::launch_pack(true, rows, cols, k, dtype, t, X, tt::untyped(Q), tt::untyped(S), stream);
+    return tt::run_pack(true, rows, cols, k, dtype, t, X, tt::untyped(Q), tt::untyped(S), stream);
 }
 
 extern "C" tt_status tt_unpack8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling t, const int8_t *const *Q, const uint8_t *const *S,
                                 void *const *X, void *stream)
 {
-    return tt::launch_pack(false, rows, cols, k, dtype, t, tt::untyped(X), tt::untyped(Q), tt::untyped(S), stream);
+    return tt::run_pack(false, rows, cols, k, dtype, t, tt::untyped(X), tt::untyped(Q), tt::untyped(S), stream);
 }
 
 extern "C" tt_status tt_fc_packed_workspace_bytes(const tt_layer *layer, int64_t batch, int k, int dtype, tt_tiling tX, tt_tiling tW,
@@ -362,33 +490,32 @@ extern "C" tt_status tt_fc_backward_packed(const tt_layer *layer, int64_t batch,
     void *X[kMaxShards], *Y[kMaxShards];
     buffers_of(X, tX, k, s.x, ws, s.x_pitch);
     GateParams p;
-    dim3 gx, gy;
-    if ((st = packed_blocks(&p.x, tX, k, batch, layer->n_in, untyped(XQ), untyped(XS), ws, s.x_pitch, &gx)) != TT_OK) return st;
+    if ((st = packed_blocks(&p.x, tX, k, batch, layer->n_in, untyped(XQ), untyped(XS), ws, s.x_pitch)) != TT_OK) return st;
     if (s.relu) {
-        if ((st = packed_blocks(&p.y, tY, k, batch, layer->n_out, untyped(YQ), untyped(YS), ws + s.y_at, s.y_pitch, &gy)) != TT_OK) return st;
+        if ((st = packed_blocks(&p.y, tY, k, batch, layer->n_out, untyped(YQ), untyped(YS), ws + s.y_at, s.y_pitch)) != TT_OK) return st;
         buffers_of(Y, s.gated ? tdY : tY, k, s.gated ? s.dy : s.y, ws + s.y_at, s.y_pitch);
     }
     const hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     const bool bf16 = dtype == TT_BF16;
     const uint64_t nx = (uint64_t)batch * layer->n_in, ny = (uint64_t)batch * layer->n_out;
+    p.x_blocks = blocks_of(s.x);
     if (s.gated) {
         BlockTable dy;
         if (!make_blocks(dY, tdY, k, batch, layer->n_out, &dy)) return TT_EINFEASIBLE;
-        for (uint32_t b = 0; b < (uint32_t)kMaxShards; ++b) p.dY[b] = b < gy.y ? dy.p[b * dy.nrep] : nullptr;
-        p.x_blocks = gx.y;
+        const uint32_t n = blocks_of(dy);
+        for (uint32_t b = 0; b < (uint32_t)kMaxShards; ++b) p.dY[b] = b < n ? dy.p[b * dy.nrep] : nullptr;
         ProfileScope scope(stream, TT_K_UNPACK, 1 << k, batch, layer->n_in + layer->n_out, e, nx * (e + 1) + ny * (2 * e + 1), 0);
-        const dim3 grid(gx.x > gy.x ? gx.x : gy.x, gx.y + gy.y);
-        if (bf16) launch_unpack_gate<uint16_t>(p, grid, hs);
-        else launch_unpack_gate<float>(p, grid, hs);
+        if (bf16) launch_unpack_gate<uint16_t>(p, n, hs);
+        else launch_unpack_gate<float>(p, n, hs);
     } else {
         ProfileScope scope(stream, TT_K_UNPACK, 1 << k, batch, layer->n_in, e, nx * (e + 1), 0);
-        if (bf16) launch_unpack_blocks<uint16_t>(p.x, gx, hs);
-        else launch_unpack_blocks<float>(p.x, gx, hs);
+        if (bf16) launch_unpack<uint16_t>(p.x, (int)p.x_blocks, hs);
+        else launch_unpack<float>(p.x, (int)p.x_blocks, hs);
     }
     if (s.relu && !s.gated) {
         ProfileScope scope(stream, TT_K_UNPACK, 1 << k, batch, layer->n_out, e, ny * (e + 1), 0);
-        if (bf16) launch_unpack_blocks<uint16_t>(p.y, gy, hs);
-        else launch_unpack_blocks<float>(p.y, gy, hs);
+        if (bf16) launch_unpack<uint16_t>(p.y, (int)blocks_of(s.y), hs);
+        else launch_unpack<float>(p.y, (int)blocks_of(s.y), hs);
     }
     if (hipGetLastError() != hipSuccess) return TT_EDEVICE;
     return tt_fc_backward(&s.layer, batch, k, dtype, tX, tW, tY, tdY, tdX, forms_dgrad, forms_wgrad, X, W, s.gated ? nullptr : s.relu ? Y : nullptr,

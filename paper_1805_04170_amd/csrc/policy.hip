@@ -28,6 +28,7 @@ struct PolicyParams {
     uint32_t wide_ids, with_dx;
     const float *old_logp, *ref_logp, *advantage, *weight; // weight NULL: log probabilities alone
     float *logp, *row_loss;                                // either may be NULL
+    float *loss;                                           // NULL: log probabilities alone
     Stats *part_stats;                                     // [tokens][parts], where rows are cut
     uint32_t parts;
     Divisor by_parts;
@@ -540,13 +541,43 @@ template <typename T> __global__ __launch_bounds__(kPartWaves * 64) void policy_
     if (threadIdx.x == 0) p.part_stats[blockIdx.x] = s;
 }
 
-// GRAD: a workgroup to a part; otherwise a wave to a token, for the scalars alone
+// The loss of all tokens (no more than the workgroup has threads), each joined from its parts by a thread of its own, added up in
+// their order
+constexpr int kLossTokens = kPartWaves * 64;
+template <typename T> __device__ __forceinline__ void sum_of_parts(const PolicyParams &p, float kk)
+{
+    __shared__ float row_loss[kLossTokens];
+    const uint32_t t = threadIdx.x;
+    if (t < p.tokens) {
+        const int64_t a = p.wide_ids ? token_at<int64_t>(p.actions, t) : token_at<int32_t>(p.actions, t);
+        float loss = 0.0f;
+        if (a >= 0 && a < p.vocab && p.weight[t] != 0.0f) {
+            Stats s{-INFINITY, 0.0f};
+            for (uint32_t i = 0; i < p.parts; ++i) s = joined(s, p.part_stats[(size_t)t * p.parts + i]);
+            const TokenScalars c{p.weight[t], p.old_logp[t], p.policy.kl != 0.0f ? p.ref_logp[t] : 0.0f, p.advantage[t]};
+            loss = row_result(p, c, s, to_float(logit_at<T>(p, t, column_of(p, (uint32_t)a))), kk).loss;
+        }
+        row_loss[t] = loss;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = 0.0;
+        for (uint32_t i = 0; i < p.tokens; ++i) s += (double)row_loss[i];
+        *p.loss = (float)s;
+    }
+}
+
+// GRAD: a workgroup to a part; otherwise a wave to a token, for the scalars alone; one workgroup more for the loss
 template <typename T, bool GRAD> __global__ __launch_bounds__(kPartWaves * 64) void policy_part_result_kernel(const PolicyParams p)
 {
+    const float kk = p.policy.scale * kLog2e;
     const uint32_t t = GRAD ? quotient(blockIdx.x, p.by_parts) : blockIdx.x, part = GRAD ? blockIdx.x - t * p.parts : 0;
+    if (t == p.tokens) {
+        if (part == 0) sum_of_parts<T>(p, kk);
+        return;
+    }
     const uint32_t w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, u0 = part * kPartUnits;
     const int64_t a = action_of(p, t);
-    const float kk = p.policy.scale * kLog2e;
     const u32x4 zero = u32x4{0, 0, 0, 0};
     RowResult res{0.0f, 0.0f, 0.0f, 0.0f, false};
     Stats s{-INFINITY, 0.0f};
@@ -627,10 +658,10 @@ Walk walk_of(const BlockTable &X, const BlockTable &G, int64_t tokens, int64_t v
     return w;
 }
 
-// workgroups that fit the chip at a time: 16 waves of up to 128 registers on each of 256 CUs
+// workgroups that fit the chip at a time: on each of 256 CUs 16 waves of up to 128 registers, or 32 of those that hold a few vectors
 template <typename T, int WAVES, int NC, bool GRAD> void launch_rows(PolicyParams &p, hipStream_t s)
 {
-    const uint32_t most = 256 * (16 / WAVES);
+    const uint32_t most = 256 * (NC <= 4 && WAVES < 16 ? 32 : 16) / WAVES;
     p.groups = p.tokens < most ? p.tokens : most;
     hipLaunchKernelGGL((policy_rows_kernel<T, WAVES, NC, GRAD>), dim3(p.groups), dim3(WAVES * 64), 0, s, p);
 }
@@ -639,10 +670,14 @@ template <typename T> tt_status launch_policy(PolicyParams &p, hipStream_t s)
 {
     const uint32_t u = p.units, q = p.rest ? p.s.nseg : 0; // whole units, and segments with a rest: one at most to a wave, a vector at least
     const auto fits = [&](uint32_t waves, uint32_t nc) { return u <= waves * nc && q <= waves && p.s.seg >= (uint32_t)kVec<T>; };
+    bool summed = !p.loss;
     if (p.parts > 1) {
+        // (a workgroup of the second launch has a thread per token for the loss)
+        const uint32_t one_more = p.loss && p.tokens <= (p.with_dx ? (uint32_t)kLossTokens : 64u) ? 1 : 0;
+        summed = summed || one_more;
         hipLaunchKernelGGL((policy_part_stats_kernel<T>), dim3(p.tokens * p.parts), dim3(kPartWaves * 64), 0, s, p);
-        if (p.with_dx) hipLaunchKernelGGL((policy_part_result_kernel<T, true>), dim3(p.tokens * p.parts), dim3(kPartWaves * 64), 0, s, p);
-        else hipLaunchKernelGGL((policy_part_result_kernel<T, false>), dim3(p.tokens), dim3(64), 0, s, p);
+        if (p.with_dx) hipLaunchKernelGGL((policy_part_result_kernel<T, true>), dim3((p.tokens + one_more) * p.parts), dim3(kPartWaves * 64), 0, s, p);
+        else hipLaunchKernelGGL((policy_part_result_kernel<T, false>), dim3(p.tokens + one_more), dim3(64), 0, s, p);
     } else if (!fits(16, p.with_dx ? 20 : 2)) {
         hipLaunchKernelGGL((policy_stream_kernel<T>), dim3(p.tokens), dim3(kStreamWaves * 64), 0, s, p);
     } else if (!p.with_dx) {
@@ -673,6 +708,7 @@ template <typename T> tt_status launch_policy(PolicyParams &p, hipStream_t s)
         else if (fits(16, 16)) launch_rows<T, 16, 16, true>(p, s);
         else launch_rows<T, 16, 20, true>(p, s);
     }
+    if (!summed) hipLaunchKernelGGL(sum_losses_kernel, dim3(1), dim3(kSumThreads), 0, s, p.row_loss, p.tokens, p.loss);
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }
 
@@ -754,7 +790,8 @@ extern "C" tt_status tt_policy_loss(const tt_policy *policy, int64_t tokens, int
     const uint64_t all = (uint64_t)tokens * (uint64_t)vocab * e;
     ProfileScope scope(stream, TT_K_LOSS, 1 << k, tokens, vocab, e, all * (1 + (dX ? p.G.nrep : 0)), 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (tokens > 0 && (st = launch_policy(p, w, workspace, dtype, id_dtype, s)) != TT_OK) return st;
+    p.loss = loss;
+    if (tokens > 0) return launch_policy(p, w, workspace, dtype, id_dtype, s);
     hipLaunchKernelGGL(sum_losses_kernel, dim3(1), dim3(kSumThreads), 0, s, p.row_loss, p.tokens, loss);
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }
@@ -778,7 +815,7 @@ extern "C" tt_status tt_token_logp(int64_t tokens, int64_t vocab, int k, int dty
     p.actions = ids;
     p.old_logp = p.ref_logp = p.advantage = p.weight = nullptr;
     p.logp = logp;
-    p.row_loss = nullptr;
+    p.row_loss = p.loss = nullptr;
     p.tokens = (uint32_t)tokens;
     p.vocab = vocab;
     p.policy = tt_policy{scale, 0.0f, 0.0f, 0.0f};

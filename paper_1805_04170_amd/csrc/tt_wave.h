@@ -64,6 +64,20 @@ template <typename V, class F> __device__ __forceinline__ V combined(V v, V none
     else return read_lane(v, 63);
 }
 
+// the largest of a group of 4 or 8 neighbouring lanes, in each of them
+template <int LANES> __device__ __forceinline__ uint32_t group_max(uint32_t v)
+{
+    uint32_t o = moved<0xb1, 0xf>(v, v); // lanes 1 0 3 2 of every four
+    v = o > v ? o : v;
+    o = moved<0x4e, 0xf>(v, v); // 2 3 0 1
+    v = o > v ? o : v;
+    if constexpr (LANES == 8) {
+        o = moved<0x141, 0xf>(v, v); // 7 6 5 4 3 2 1 0 of every eight
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
 } // namespace wave
 } // namespace tt
 #endif

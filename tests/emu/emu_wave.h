@@ -51,6 +51,14 @@ template <typename V, class F> inline V combined(V v, V, F &&f)
     for (int m = 1; m < 64; m <<= 1) v = f(v, shfl_xor(v, m));
     return v;
 }
+template <int LANES> inline uint32_t group_max(uint32_t v)
+{
+    for (int m = 1; m < LANES; m <<= 1) {
+        const uint32_t o = shfl_xor(v, m);
+        v = o > v ? o : v;
+    }
+    return v;
+}
 inline void lds_add(uint32_t *p, uint32_t v) { *p += v; }
 inline void fence() { emu::wave_sync(); }
 template <typename V> inline void forget(V &) {}

@@ -163,7 +163,11 @@ def test_embedding_of_wide_rows_tiled(tW, tX, D, dt):
 
 
 def test_embedding_of_large_vocabularies_and_many_tokens():
+    run_embed(256, 1500, 300, "bf16", seed=5, ids=np.arange(256) % 3)
+    run_embed(256, 1500, 30, "bf16", seed=5, ids=np.arange(256) // 100)
     run_embed(3000, 1500, 40, "f32", seed=5)
+    run_embed(3000, 40, 600, "bf16", seed=5)
+    run_embed(2000, 5000, 600, "f32", "RC", "CR", seed=6)
     run_embed(700, 270000, 3, "bf16", seed=6)      # more numbers than 256 workgroups' counters hold
     run_embed(20000, 7, 16, "f32", seed=7)
 
@@ -176,12 +180,18 @@ def test_embedding_tiled(tW, tX, dt, D):
 
 @pytest.mark.parametrize("what", ["one", "none", "two", "huge", "long_runs"])
 def test_embedding_token_patterns(what):
-    T, V = 300, 50
+    for T in (300, 200):
+        run_patterns(T, what)
+
+
+def run_patterns(T, what):
+    V = 50
     rng = np.random.default_rng(4)
     ids = {"one": np.full(T, 49), "none": np.full(T, -1), "two": np.where(np.arange(T) % 2 == 0, 3, 4),
            "huge": np.where(np.arange(T) % 3 == 0, 2 ** 62, np.where(np.arange(T) % 3 == 1, -2 ** 62, V)),
            "long_runs": np.sort(rng.integers(0, 4, T))[::-1].copy()}[what].astype(np.int64)
     run_embed(T, V, 20, "f32", ids=ids)
+    run_embed(T, V, 140, "f32", ids=ids)
 
 
 def test_embedding_skewed_buffers():

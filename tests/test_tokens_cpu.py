@@ -67,12 +67,13 @@ def test_embedding_refusals():
 
 
 def test_embedding_gradient_refusals():
-    need = tt.tt_embed_workspace_bytes(100, 8, 8, 0, "f32", "", "")
-    f = lambda T=100, V=8, D=8, k=0, dt="f32", tX="", tW="", ids=A, dX=P, dW=P, ws=Bytes(need): tt.tt_embed_backward(  # noqa: E731
+    need = tt.tt_embed_workspace_bytes(1000, 8, 8, 0, "f32", "", "")
+    assert need > 0 and tt.tt_embed_workspace_bytes(100, 8, 8, 0, "f32", "", "") == 0      # (few tokens are not sorted)
+    f = lambda T=1000, V=8, D=8, k=0, dt="f32", tX="", tW="", ids=A, dX=P, dW=P, ws=Bytes(need): tt.tt_embed_backward(  # noqa: E731
         T, V, D, k, dt, tX, tW, ids, 1.0, dX, dW, ws, stream=1, id_dtype="i32")
     for bad in (dict(T=-1), dict(k=7), dict(dt=2), dict(ids=None), dict(ids=A + 2), dict(dX=None), dict(dW=[0]), dict(dW=[A + 2])):
         refused("TT_EINVAL", f, **bad)
-    refused("TT_EINFEASIBLE", f, T=101, k=1, tX="R", tW="R", dX=P2, dW=P2)
+    refused("TT_EINFEASIBLE", f, T=1001, k=1, tX="R", tW="R", dX=P2, dW=P2)
     for ws in (None, Bytes(need - 1), Bytes(need, A + 128)):
         refused("TT_EWORKSPACE", f, ws=ws)
     refused("TT_EINVAL", tt.tt_embed_workspace_bytes, 8, 8, -1, 0, "f32", "", "")
