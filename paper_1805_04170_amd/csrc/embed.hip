@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kU = 2;     // vectors per lane of a wave's part of a segment
-constexpr int kRunBatch = 8, kRowBatch = 4, kPartials = 4; // rows, or partial sums, that are on their way together
+constexpr int kRunBatch = 8, kRowBatch = 4, kPartials = 8; // rows, or partial sums, that are on their way together
 
 // How the segments of a row are shared out.  Wide segments (more than 32 vectors): a part of kU vectors per lane to a wave, so
 // that a wave's row, segment and addresses are scalars.  Narrow ones: a vector per lane, a segment to 2^glog lanes.
@@ -875,9 +875,11 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     p.cols = (uint32_t)width;
     p.vocab = vocab;
     p.scale = scale;
-    // as many as leave every CU 32 waves
+    // Rows per wave: as many as leave every CU 32 waves, 4 at most (65536 x 8192, us with 2, 4, 8 of them:
+    // no tokens 178, 190, 192; 16384 tokens 301, 295, 297), 2 where there is nothing to look up first.
     const uint64_t waves = (uint64_t)vocab * p.w.s.nseg * p.w.parts;
-    p.rows = waves >= 8 * 8192 ? 8 : waves >= 4 * 8192 ? 4 : waves >= 2 * 8192 ? 2 : 1;
+    const uint32_t most = tokens <= (int64_t)kFewTokens ? 2 : 4;
+    p.rows = most == 4 && waves >= 4 * 8192 ? 4 : waves >= 2 * 8192 ? 2 : 1;
     p.apart = (uint32_t)((vocab + p.rows - 1) / p.rows);
     const uint64_t run_groups = groups_of(p.w, sp.runs), row_groups = p.w.wide ? run_groups + groups_of(p.w, p.apart) : groups_of(p.w, (uint64_t)sp.runs + (uint64_t)vocab);
     if (run_groups * kThreads >= (uint64_t(1) << 31) || row_groups * kThreads >= (uint64_t(1) << 31)) return TT_EUNSUPPORTED;

@@ -96,14 +96,12 @@ __device__ __forceinline__ uint32_t largest(u32x4 v, uint16_t)
     }
     return (uint32_t)(top.x > top.y ? top.x : top.y) << 16;
 }
-// x / step in whole steps (low byte), ties to even, a step at least where x is not 0: x inv is exact, and 1.5 * 2^23 + n is n in the
-// number's last bits
+// x / step in whole steps (low byte), ties to even, a step at least where x is not 0 (a magnitude of 0.75 rounds to one): x inv is exact,
+// and 1.5 * 2^23 + n is n in the number's last bits.  Comparisons would cost more: each waits for its result.
 __device__ __forceinline__ uint32_t steps_of(float x, float inv)
 {
-    const uint32_t q = __float_as_uint(fmaf(x, inv, 12582912.0f));
-    const int sign = (int)__float_as_uint(x + 0.0f); // (-0 is no step)
-    const uint32_t one = (uint32_t)(sign > 1 ? 1 : sign < -1 ? -1 : sign);
-    return q == 0x4b400000u ? one : q;
+    const float least = fminf(fabsf(ldexpf(x, 160)), 0.75f); // 0 for 0, 0.75 for anything else, the smallest denormal too
+    return __float_as_uint(copysignf(fmaxf(fabsf(x * inv), least), x) + 12582912.0f);
 }
 
 __device__ __forceinline__ float inverse_of(uint32_t s) { return s == 255 ? 0.0f : __uint_as_float((254u - s) << 23); }
@@ -128,9 +126,7 @@ template <typename T> __device__ __forceinline__ Bytes<T> packed(u32x4 v, uint32
     Bytes<T> b;
 #pragma unroll
     for (int i = 0; i < kVec<T> / 4; ++i) {
-        b.w[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b.w[i] |= (steps_of(g[4 * i + j], inv) & 255u) << (8 * j);
+        b.w[i] = wave::low_bytes(steps_of(g[4 * i], inv), steps_of(g[4 * i + 1], inv), steps_of(g[4 * i + 2], inv), steps_of(g[4 * i + 3], inv));
         if (s == 255) b.w[i] = 0;
     }
     return b;

@@ -64,6 +64,11 @@ template <typename V, class F> __device__ __forceinline__ V combined(V v, V none
     else return read_lane(v, 63);
 }
 
+// the low bytes of four words, a's first
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_amdgcn_perm(d, c, 0x0c0c0400u) << 16 | __builtin_amdgcn_perm(b, a, 0x0c0c0400u);
+}
 // the largest of a group of 4 or 8 neighbouring lanes, in each of them
 template <int LANES> __device__ __forceinline__ uint32_t group_max(uint32_t v)
 {

@@ -51,6 +51,7 @@ template <typename V, class F> inline V combined(V v, V, F &&f)
     for (int m = 1; m < 64; m <<= 1) v = f(v, shfl_xor(v, m));
     return v;
 }
+inline uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return (a & 255u) | (b & 255u) << 8 | (c & 255u) << 16 | d << 24; }
 template <int LANES> inline uint32_t group_max(uint32_t v)
 {
     for (int m = 1; m < LANES; m <<= 1) {
