@@ -99,6 +99,54 @@ template <typename T> struct Columns {
     }
 };
 
+// The same for the narrow form's one vector; segments of less than a vector (`tiny`) are loaded value by value.
+template <typename T> struct Column1 {
+    uint32_t col, own;
+    bool tiny;
+    __device__ __forceinline__ Column1(const Pieces &s, uint32_t j) : own(values_of(s, kVec<T>, j)), tiny(s.seg < (uint32_t)kVec<T>)
+    {
+        const uint32_t last = tiny ? 0 : s.seg - kVec<T>;
+        col = j * kVec<T> < last ? j * kVec<T> : last;
+    }
+    __device__ __forceinline__ u32x4 load(const T *segment) const { return tiny ? load_part(segment, own) : load16(segment + col); }
+    __device__ __forceinline__ void store(const BlockTable &b, const Place &to, u32x4 v) const
+    {
+        if (own == 0) return;
+        for (uint32_t x = 0; x < b.nrep; ++x) {
+            T *dst = static_cast<T *>(b.p[to.block + x]) + to.at + col;
+            if (own == (uint32_t)kVec<T>) store16(dst, v);
+            else if (tiny) store_part(dst, v, own);
+            else {
+#pragma unroll
+                for (int i = 1; i < kVec<T>; ++i) {
+                    if ((uint32_t)i < kVec<T> - own) continue;
+                    if constexpr (sizeof(T) == 2) store1(dst + i, (uint16_t)(v[i >> 1] >> (16 * (i & 1))));
+                    else store1(dst + i, __uint_as_float(v[i]));
+                }
+            }
+        }
+    }
+    // fp32 values of the same columns (a short vector's neighbours hold what it has of theirs)
+    __device__ __forceinline__ void load_floats(float (&f)[kVec<T>], const float *segment) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; i += 4) {
+            const u32x4 v = tiny ? load_part(segment + i, own > (uint32_t)i ? own - i < 4 ? own - i : 4 : 0) : load16(segment + col + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[i + k] = __uint_as_float(v[k]);
+        }
+    }
+    __device__ __forceinline__ void store_floats(const float (&f)[kVec<T>], float *segment) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; i += 4) {
+            const u32x4 v = u32x4{__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])};
+            if (tiny) store_part(segment + i, v, own > (uint32_t)i ? own - i < 4 ? own - i : 4 : 0);
+            else store16(segment + col + i, v);
+        }
+    }
+};
+
 template <typename T> __device__ __forceinline__ u32x4 scaled(u32x4 v, float scale)
 {
     float f[kVec<T>];
@@ -144,12 +192,12 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_narrow_kernel(const EmbedParams p)
 {
     const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
-    if (g.row >= p.tokens || n == 0) return;
+    const Column1<T> c(p.w.s, g.j);
+    if (g.row >= p.tokens || c.own == 0) return;
     const int64_t v = token_at<I>(p.ids, g.row);
     u32x4 r = u32x4{0, 0, 0, 0};
-    if (v >= 0 && v < p.vocab) r = scaled<T>(load_vector(source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q) + g.j * kVec<T>, n), p.scale);
-    store_all<T>(p.X, place_of(p.X, p.w.s, p.w.s.b_shift, g.row, g.q), g.j * kVec<T>, n, r);
+    if (v >= 0 && v < p.vocab) r = scaled<T>(c.load(source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q)), p.scale);
+    c.store(p.X, place_of(p.X, p.w.s, p.w.s.b_shift, g.row, g.q), r);
 }
 
 // ------------------------------------------------------------------------------------------------------ backward
@@ -177,7 +225,7 @@ struct SortParams {
     uint32_t tokens;
     Places to;
     int64_t vocab;
-    uint32_t *order, *start;
+    uint32_t *order, *number, *start; // tokens and their numbers in the list's order; where a place's tokens begin
 };
 
 constexpr uint32_t kNoToken = ~0u;
@@ -264,6 +312,7 @@ template <typename I> __global__ __launch_bounds__(kSortThreads) void sort_token
                 if (same) {
                     const uint32_t rank = (uint32_t)__builtin_popcountll(who & ((uint64_t(1) << lane) - 1));
                     p.order[to + rank] = tb + i * 64 + lane;
+                    p.number[to + rank] = v[i];
                     if (rank == 0) mine[n] = to + (uint32_t)__builtin_popcountll(who);
                 }
                 wave::fence();
@@ -277,7 +326,7 @@ struct EmbedGradParams {
     BlockTable G, W; // the rows' gradients, the table's
     Split w;
     const void *ids;
-    const uint32_t *order, *start;
+    const uint32_t *order, *number, *start;
     float *partial; // [2 runs][cols]: run c's part of a number that began before the run, of one that begins inside it
     Places to;
     Divisor by_chunk;
@@ -371,12 +420,12 @@ __device__ __forceinline__ void add_rows(Sums<T> &a, const EmbedGradParams &p, c
 
 // What a run has to do with numbers of many tokens: it may end one at its first place and begin one at its last.
 struct Run { uint32_t b, e, first, last; bool any; };
-template <typename I> __device__ __forceinline__ Run run_of(const EmbedGradParams &p, uint32_t run)
+__device__ __forceinline__ Run run_of(const EmbedGradParams &p, uint32_t run)
 {
-    const uint32_t total = p.start[p.places], b = run * p.chunk;
+    const uint32_t total = load_scalar(p.start + p.places), b = run * p.chunk;
     if (b >= total) return {0, 0, 0, 0, false};
     const uint32_t e = b + p.chunk < total ? b + p.chunk : total;
-    return {b, e, (uint32_t)token_at<I>(p.ids, p.order[b]), (uint32_t)token_at<I>(p.ids, p.order[e - 1]), true};
+    return {b, e, p.number[b], p.number[e - 1], true};
 }
 
 template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, const EmbedGradParams &p, const Columns<T> &c, uint32_t v, uint32_t q)
@@ -391,10 +440,10 @@ template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, con
 }
 
 // a run's parts of numbers with many tokens, as partial sums
-template <typename T, typename I> __device__ __forceinline__ void sum_run(const EmbedGradParams &p, const WaveWork &g)
+template <typename T> __device__ __forceinline__ void sum_run(const EmbedGradParams &p, const WaveWork &g)
 {
     if (g.row >= p.runs) return;
-    const Run r = run_of<I>(p, g.row);
+    const Run r = run_of(p, g.row);
     if (!r.any) return;
     const Columns<T> c(p.w.s, g.j0);
     const Sources<T> src(p, g);
@@ -458,13 +507,13 @@ template <typename T> __device__ __forceinline__ void sum_rows(const EmbedGradPa
 
 // The row of a number with many tokens whose first one lies in the run (there is one such number at most, the run's last): the sum
 // over its partial sums.
-struct Long { uint32_t v, last; bool any; };
-template <typename I> __device__ __forceinline__ Long long_of(const EmbedGradParams &p, uint32_t run)
+struct Long { uint32_t v, b, last; bool any; };
+__device__ __forceinline__ Long long_of(const EmbedGradParams &p, uint32_t run)
 {
-    const Run r = run_of<I>(p, run);
-    if (!r.any) return {0, 0, false};
+    const Run r = run_of(p, run);
+    if (!r.any) return {0, 0, 0, false};
     const uint32_t at = place(p.to, r.last), b = p.start[at], e = p.start[at + 1];
-    return {r.last, quotient(e - 1, p.by_chunk), b >= r.b && e - b > p.chunk};
+    return {r.last, b, quotient(e - 1, p.by_chunk), b >= r.b && e - b > p.chunk};
 }
 // (the first of its partial sums counts as begun inside the run unless it is the run's first place)
 __device__ __forceinline__ const float *partial_in(const EmbedGradParams &p, uint32_t run, uint32_t first_run, bool inside, uint32_t q)
@@ -472,13 +521,13 @@ __device__ __forceinline__ const float *partial_in(const EmbedGradParams &p, uin
     return partial_of(p, run, run == first_run && inside, q);
 }
 
-template <typename T, typename I> __device__ __forceinline__ void join_runs(const EmbedGradParams &p, const WaveWork &g)
+template <typename T> __device__ __forceinline__ void join_runs(const EmbedGradParams &p, const WaveWork &g)
 {
     if (g.row >= p.runs) return;
-    const Long w = long_of<I>(p, g.row);
+    const Long w = long_of(p, g.row);
     if (!w.any) return;
     const uint32_t v = uniform(w.v), last = uniform(w.last);
-    const bool inside = load_scalar(p.start + place(p.to, v)) > g.row * p.chunk;
+    const bool inside = uniform(w.b) > g.row * p.chunk;
     const Columns<T> c(p.w.s, g.j0);
     Sums<T> a;
     a.clear();
@@ -507,19 +556,20 @@ template <typename T, typename I> __device__ __forceinline__ void join_runs(cons
 
 // (2) The first workgroups' waves take a run each, beside the rows.  (The runs in a launch of their own in front, and the joins in
 // this one: 2 to 3 % faster at 65536 x 8192 and 16384 tokens, 10 % slower at 32000 x 1024 and 8192.)
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_sums_wide_kernel(const EmbedGradParams p)
+template <typename T> __global__ __launch_bounds__(kThreads) void embed_sums_wide_kernel(const EmbedGradParams p)
 {
-    if (blockIdx.x < p.run_groups) sum_run<T, I>(p, wave_work(p.w, blockIdx.x));
+    if (blockIdx.x < p.run_groups) sum_run<T>(p, wave_work(p.w, blockIdx.x));
     else sum_rows<T>(p, wave_work(p.w, blockIdx.x - p.run_groups));
 }
 // (3)
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_wide_kernel(const EmbedGradParams p)
+template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_wide_kernel(const EmbedGradParams p)
 {
-    join_runs<T, I>(p, wave_work(p.w, blockIdx.x));
+    join_runs<T>(p, wave_work(p.w, blockIdx.x));
 }
 
 // the rows of places [b, e) of the sorted list, a vector of each, kRunBatch of them on their way together
-template <typename T> __device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, uint32_t n, uint32_t b, uint32_t e)
+template <typename T>
+__device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Column1<T> &c, uint32_t b, uint32_t e)
 {
     for (uint32_t i = b; i < e; i += kRunBatch) {
         uint32_t t[kRunBatch];
@@ -527,7 +577,7 @@ template <typename T> __device__ __forceinline__ void add_vectors(float (&s)[kVe
 #pragma unroll
         for (int k = 0; k < kRunBatch; ++k) t[k] = p.order[i + k < e ? i + k : e - 1];
 #pragma unroll
-        for (int k = 0; k < kRunBatch; ++k) r[k] = load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, t[k], g.q) + g.j * kVec<T>, n);
+        for (int k = 0; k < kRunBatch; ++k) r[k] = c.load(source_of<T>(p.G, p.w.s, p.w.s.a_shift, t[k], g.q));
 #pragma unroll
         for (int k = 0; k < kRunBatch; ++k) {
             float f[kVec<T>];
@@ -537,64 +587,59 @@ template <typename T> __device__ __forceinline__ void add_vectors(float (&s)[kVe
         }
     }
 }
+template <typename T> __device__ __forceinline__ void finish_vector(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Column1<T> &c, uint32_t v)
+{
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
+    c.store(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q), pack16(s, T()));
+}
 
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_sums_narrow_kernel(const EmbedGradParams p)
+template <typename T> __global__ __launch_bounds__(kThreads) void embed_sums_narrow_kernel(const EmbedGradParams p)
 {
     const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
-    if (n == 0) return;
+    const Column1<T> c(p.w.s, g.j);
+    if (c.own == 0) return;
     if (g.row < p.runs) {
-        const Run r = run_of<I>(p, g.row);
+        const Run r = run_of(p, g.row);
         if (!r.any) return;
         for (int side = 0; side < 2; ++side) {
             if (side == 1 && r.last == r.first) break;
             const uint32_t at = place(p.to, side == 0 ? r.first : r.last), vb = p.start[at], ve = p.start[at + 1];
             if (ve - vb <= p.chunk) continue;
             float s[kVec<T>] = {};
-            add_vectors<T>(s, p, g, n, vb > r.b ? vb : r.b, ve < r.e ? ve : r.e);
-            float *to = partial_of(p, g.row, vb > r.b, g.q) + g.j * kVec<T>;
-#pragma unroll
-            for (int i = 0; i < kVec<T>; ++i)
-                if ((uint32_t)i < n) to[i] = s[i];
+            add_vectors<T>(s, p, g, c, vb > r.b ? vb : r.b, ve < r.e ? ve : r.e);
+            c.store_floats(s, partial_of(p, g.row, vb > r.b, g.q));
         }
         return;
     }
     const uint32_t v = g.row - p.runs;
     if ((int64_t)v >= p.vocab) return;
     const uint32_t at = place(p.to, v), b = p.start[at], e = p.start[at + 1];
-    if (e - b > p.chunk) return; // (3)
+    if (e - b > p.chunk) return; // (runs)
     float s[kVec<T>] = {};
-    add_vectors<T>(s, p, g, n, b, e);
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
-    store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q), g.j * kVec<T>, n, pack16(s, T()));
+    add_vectors<T>(s, p, g, c, b, e);
+    finish_vector(s, p, g, c, v);
 }
 
-template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_join_narrow_kernel(const EmbedGradParams p)
+template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_narrow_kernel(const EmbedGradParams p)
 {
     const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j);
-    if (g.row >= p.runs || n == 0) return;
-    const Long w = long_of<I>(p, g.row);
+    const Column1<T> c(p.w.s, g.j);
+    if (g.row >= p.runs || c.own == 0) return;
+    const Long w = long_of(p, g.row);
     if (!w.any) return;
-    const bool inside = p.start[place(p.to, w.v)] > g.row * p.chunk;
+    const bool inside = w.b > g.row * p.chunk;
     float s[kVec<T>] = {};
     for (uint32_t run = g.row; run <= w.last; run += kPartials) {
         float f[kPartials][kVec<T>];
 #pragma unroll
-        for (int k = 0; k < kPartials; ++k) {
-            const float *from = partial_in(p, run + k < w.last ? run + k : w.last, g.row, inside, g.q) + g.j * kVec<T>;
-#pragma unroll
-            for (int i = 0; i < kVec<T>; ++i) f[k][i] = (uint32_t)i < n ? load1(from + i) : 0.0f;
-        }
+        for (int k = 0; k < kPartials; ++k) c.load_floats(f[k], partial_in(p, run + k < w.last ? run + k : w.last, g.row, inside, g.q));
 #pragma unroll
         for (int k = 0; k < kPartials; ++k)
 #pragma unroll
             for (int i = 0; i < kVec<T>; ++i) s[i] = run + k <= w.last ? s[i] + f[k][i] : s[i];
     }
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
-    store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, w.v, g.q), g.j * kVec<T>, n, pack16(s, T()));
+    finish_vector(s, p, g, c, w.v);
 }
 
 // Few tokens: nothing to sort.  Every wave holds all token numbers, 64 to a register, and asks for each of its rows which of them
@@ -683,7 +728,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_few_narrow_kernel(const EmbedGradParams p)
 {
     const LaneWork g = lane_work(p.w);
-    const uint32_t n = values_of(p.w.s, kVec<T>, g.j), vocab = (uint32_t)p.vocab;
+    const Column1<T> c(p.w.s, g.j);
     const Few<I> few(p);
     // the wave's rows: those of its first and its last lane, and what lies between
     const uint32_t v0 = wave::read_lane(g.row, 0), v1 = wave::read_lane(g.row, 63);
@@ -701,7 +746,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
         }
 #pragma unroll
         for (int i = 0; i < kRowBatch; ++i)
-            if ((uint32_t)i < m && v[i] == g.row && n) r[i] = load_vector(source_of<T>(p.G, p.w.s, p.w.s.a_shift, t[i], g.q) + g.j * kVec<T>, n);
+            if ((uint32_t)i < m && v[i] == g.row && c.own) r[i] = c.load(source_of<T>(p.G, p.w.s, p.w.s.a_shift, t[i], g.q));
 #pragma unroll
         for (int i = 0; i < kRowBatch; ++i) {
             if ((uint32_t)i >= m || v[i] != g.row) continue;
@@ -711,10 +756,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
             for (int q = 0; q < kVec<T>; ++q) s[q] += x[q];
         }
     }
-    if (g.row >= vocab || n == 0) return;
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
-    store_all<T>(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, g.row, g.q), g.j * kVec<T>, n, pack16(s, T()));
+    if (g.row < (uint32_t)p.vocab) finish_vector(s, p, g, c, g.row);
 }
 
 // ----------------------------------------------------------------------------------------------------- host side
@@ -747,17 +789,18 @@ Places places_of(int64_t vocab)
 }
 
 struct GradSpace {
-    size_t order, start, partial, bytes;
+    size_t order, number, start, partial, bytes;
     uint32_t runs;
     Places to;
 };
 GradSpace grad_space(int64_t tokens, int64_t vocab, int64_t width)
 {
-    GradSpace s{0, 0, 0, 0, 0, places_of(vocab)};
+    GradSpace s{0, 0, 0, 0, 0, 0, places_of(vocab)};
     if (tokens <= (int64_t)kFewTokens) return s; // (nothing is sorted)
     const uint32_t chunk = run_length(tokens);
     s.runs = tokens > chunk ? (uint32_t)((tokens + chunk - 1) / chunk) : 0;
-    s.start = align_up((size_t)tokens * 4, 256);
+    s.number = align_up((size_t)tokens * 4, 256);
+    s.start = 2 * s.number;
     s.partial = s.start + align_up((((size_t)s.to.range << s.to.wlog) + 1) * 4, 256);
     s.bytes = s.partial + align_up((size_t)2 * s.runs * (size_t)width * 4, 256);
     return s;
@@ -827,11 +870,11 @@ tt_status launch_embed_grad(const SortParams &sp, const EmbedGradParams &p, uint
     }
     hipLaunchKernelGGL((sort_tokens_kernel<I>), dim3(1u << sp.to.wlog), dim3(kSortThreads), 0, s, sp);
     if (p.w.wide) {
-        hipLaunchKernelGGL((embed_sums_wide_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
-        if (run_groups) hipLaunchKernelGGL((embed_join_wide_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_sums_wide_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        if (run_groups) hipLaunchKernelGGL((embed_join_wide_kernel<T>), dim3(run_groups), dim3(kThreads), 0, s, p);
     } else {
-        hipLaunchKernelGGL((embed_sums_narrow_kernel<T, I>), dim3(row_groups), dim3(kThreads), 0, s, p);
-        if (run_groups) hipLaunchKernelGGL((embed_join_narrow_kernel<T, I>), dim3(run_groups), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((embed_sums_narrow_kernel<T>), dim3(row_groups), dim3(kThreads), 0, s, p);
+        if (run_groups) hipLaunchKernelGGL((embed_join_narrow_kernel<T>), dim3(run_groups), dim3(kThreads), 0, s, p);
     }
     return launched();
 }
@@ -860,10 +903,12 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     q.vocab = vocab;
     q.to = sp.to;
     q.order = reinterpret_cast<uint32_t *>(ws + sp.order);
+    q.number = reinterpret_cast<uint32_t *>(ws + sp.number);
     q.start = reinterpret_cast<uint32_t *>(ws + sp.start);
     p.w = split_rows(p.G, p.W, width, 16 / e);
     p.ids = ids;
     p.order = q.order;
+    p.number = q.number;
     p.start = q.start;
     p.partial = reinterpret_cast<float *>(ws + sp.partial);
     p.to = sp.to;

@@ -75,7 +75,6 @@ template <typename T> __device__ __forceinline__ void store_all(const BlockTable
     for (uint32_t x = 0; x < b.nrep; ++x) store_vector(static_cast<T *>(b.p[to.block + x]) + to.at + at, v, n);
 }
 
-template <typename T> __device__ __forceinline__ u32x4 load_vector(const T *p, uint32_t n) { return n == (uint32_t)kVec<T> ? load16(p) : load_part(p, n); }
 
 template <typename I> __device__ __forceinline__ int64_t token_at(const void *ids, size_t i) { return (int64_t)load1(static_cast<const I *>(ids) + i); }
 // ... at an index that all lanes share

@@ -19,7 +19,6 @@
 namespace tt {
 namespace wave {
 
-__device__ __forceinline__ uint32_t lane() { return threadIdx.x & 63u; }
 __device__ __forceinline__ float shfl_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
 __device__ __forceinline__ uint32_t shfl_xor(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask, 64); }
 __device__ __forceinline__ double shfl_xor(double v, int mask) { return __shfl_xor(v, mask, 64); }

@@ -10,8 +10,6 @@ inline uint32_t __umulhi(uint32_t a, uint32_t b) { return (uint32_t)(((uint64_t)
 namespace tt {
 namespace wave {
 
-inline uint32_t lane() { return threadIdx.x & 63u; }
-
 // each lane gives a word and gets the word of lane from(lane)
 template <class F> inline uint32_t exchange(int kind, uint32_t v, F &&from)
 {
