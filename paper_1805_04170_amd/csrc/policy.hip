@@ -2,7 +2,8 @@
 //
 // A row of logits gives one number, log p[a] = z_a - log sum exp z, and with its derivative g of the loss the row's gradient
 // g (onehot(a) - p): two sums over the row and a pass that writes as much as was read.  Memory bounds it (8 flops and two
-// exponentials a value), so the logits are to come from memory once.
+// exponentials a value), so the logits are to come from memory once: 4096 x 131072 bf16 logits, 1.075 GB read and 1.074 written in
+// 415 us, 5.2 TB/s.  Log probabilities alone: 4096 x 131072 179 us, 6.0 TB/s; 16 x 131072 8.3 us on the GPU, trips to memory.
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -460,7 +461,7 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
 }
 
 // Rows that do not fit: one workgroup per row, which reads it for its statistics and again for its gradient (from the caches,
-// where they hold it).
+// where they hold it).  2048 x 200000 bf16: 380 us, 4.3 TB/s of what has to move.
 constexpr int kStreamWaves = 16;
 template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void policy_stream_kernel(const PolicyParams p)
 {
@@ -650,7 +651,9 @@ Walk walk_of(const BlockTable &X, const BlockTable &G, int64_t tokens, int64_t v
     w.whole = (w.s.vps - (w.s.tail ? 1 : 0)) / 64;
     w.units = w.s.nseg * w.whole;
     w.rest = w.s.vps - w.whole * 64;
-    // Cut rows that are worth several workgroups, where there is no gradient or whole rows would leave most CUs idle.
+    // Cut rows that are worth several workgroups, where there is no gradient or whole rows would leave most CUs idle.  Cut / whole, us:
+    // loss of 16 x 131072 13 / 23, 64 15 / 23, 128 24 / 25, 128 x 20000 14.5 / 14.1, 256 x 131072 41 / 34, 512 71 / 58; log probabilities of
+    // 256 x 131072 18 / 30, 4096 179 / 346.
     w.parts = (tokens <= 128 || !with_dx) && w.units > kPartUnits ? (w.units + kPartUnits - 1) / kPartUnits : 1;
     if ((uint64_t)tokens * w.parts >= (uint64_t(1) << 22)) w.parts = 1; // (a launch holds fewer than 2^32 threads)
     w.stats_at = align_up((size_t)tokens * 4, 256);
@@ -689,7 +692,7 @@ template <typename T> tt_status launch_policy(PolicyParams &p, hipStream_t s)
             else if (fits(4, 8)) launch_rows<T, 4, 8, false>(p, s);
             else launch_rows<T, 16, 2, false>(p, s);
         }
-    } else if (p.tokens <= 256) { // a CU to every row: as many waves as have something to do
+    } else if (p.tokens <= 256) { // a CU to every row: as many waves as have something to do (200 x 32768 14.2 us, by the next rule 15.8)
         if (fits(4, 1)) launch_rows<T, 4, 1, true>(p, s);
         else if (fits(16, 2)) launch_rows<T, 16, 2, true>(p, s);
         else if (fits(16, 4)) launch_rows<T, 16, 4, true>(p, s);

@@ -19,7 +19,6 @@
 namespace tt {
 namespace wave {
 
-__device__ __forceinline__ float shfl_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
 __device__ __forceinline__ uint32_t shfl_xor(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask, 64); }
 __device__ __forceinline__ double shfl_xor(double v, int mask) { return __shfl_xor(v, mask, 64); }
 __device__ __forceinline__ uint32_t shfl_up(uint32_t v, int by) { return (uint32_t)__shfl_up((int)v, by, 64); }
@@ -67,19 +66,6 @@ template <typename V, class F> __device__ __forceinline__ V combined(V v, V none
 __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     return __builtin_amdgcn_perm(d, c, 0x0c0c0400u) << 16 | __builtin_amdgcn_perm(b, a, 0x0c0c0400u);
-}
-// the largest of a group of 4 or 8 neighbouring lanes, in each of them
-template <int LANES> __device__ __forceinline__ uint32_t group_max(uint32_t v)
-{
-    uint32_t o = moved<0xb1, 0xf>(v, v); // lanes 1 0 3 2 of every four
-    v = o > v ? o : v;
-    o = moved<0x4e, 0xf>(v, v); // 2 3 0 1
-    v = o > v ? o : v;
-    if constexpr (LANES == 8) {
-        o = moved<0x141, 0xf>(v, v); // 7 6 5 4 3 2 1 0 of every eight
-        v = o > v ? o : v;
-    }
-    return v;
 }
 
 } // namespace wave

@@ -22,7 +22,7 @@ template <class F> inline uint32_t exchange(int kind, uint32_t v, F &&from)
     return r;
 }
 inline uint32_t shfl_xor(uint32_t v, int mask) { return exchange(10, v, [&](int l) { return l ^ mask; }); }
-inline float shfl_xor(float v, int mask) { return __uint_as_float(shfl_xor(__float_as_uint(v), mask)); }
+inline float shfl_xor(float v, int mask) { return __uint_as_float(shfl_xor(__float_as_uint(v), mask)); } // (combined)
 inline double shfl_xor(double v, int mask)
 {
     uint32_t h[2];
@@ -50,14 +50,6 @@ template <typename V, class F> inline V combined(V v, V, F &&f)
     return v;
 }
 inline uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return (a & 255u) | (b & 255u) << 8 | (c & 255u) << 16 | d << 24; }
-template <int LANES> inline uint32_t group_max(uint32_t v)
-{
-    for (int m = 1; m < LANES; m <<= 1) {
-        const uint32_t o = shfl_xor(v, m);
-        v = o > v ? o : v;
-    }
-    return v;
-}
 inline void lds_add(uint32_t *p, uint32_t v) { *p += v; }
 inline void fence() { emu::wave_sync(); }
 template <typename V> inline void forget(V &) {}
