@@ -190,8 +190,8 @@ def run_patterns(T, what):
     ids = {"one": np.full(T, 49), "none": np.full(T, -1), "two": np.where(np.arange(T) % 2 == 0, 3, 4),
            "huge": np.where(np.arange(T) % 3 == 0, 2 ** 62, np.where(np.arange(T) % 3 == 1, -2 ** 62, V)),
            "long_runs": np.sort(rng.integers(0, 4, T))[::-1].copy()}[what].astype(np.int64)
-    run_embed(T, V, 20, "f32", ids=ids)
-    run_embed(T, V, 140, "f32", ids=ids)
+    for D, dt in [(3, "f32"), (5, "bf16"), (20, "f32"), (140, "f32")]:
+        run_embed(T, V, D, dt, ids=ids)
 
 
 def test_embedding_skewed_buffers():
