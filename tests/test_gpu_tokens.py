@@ -194,6 +194,16 @@ def run_patterns(T, what):
         run_embed(T, V, D, dt, ids=ids)
 
 
+@pytest.mark.parametrize("T,V,D,dt", [(257, 1, 33, "bf16"), (256, 2, 40, "f32"), (300, 1, 7, "bf16"), (1024, 31, 9, "f32"), (16385, 3, 8, "bf16"), (258, 257, 1, "f32")])
+def test_embedding_on_either_side_of_what_is_sorted(T, V, D, dt):
+    run_embed(T, V, D, dt, seed=T)
+
+
+@pytest.mark.parametrize("tW,tX,T", [("CCCCCC", "RRRRRR", 64), ("RCRCRC", "CrRrCR", 320), ("rrrrrr", "CCCCCC", 64)])
+def test_embedding_of_six_cuts(tW, tX, T):
+    run_embed(T, 64, 320, "bf16", tW, tX, seed=T)
+
+
 def test_embedding_skewed_buffers():
     run_embed(33, 70, 48, "bf16", seed=8, skew=1)
     run_embed(34, 70, 48, "f32", "C", "R", seed=9, skew=3)
@@ -314,6 +324,11 @@ def test_policy_loss_tiled(tX, tG, dt, V):
     run_policy(24, V, dt, tX, tG, "i32", seed=len(tX), masked=True, scale=0.7)
 
 
+@pytest.mark.parametrize("tX,tG,V", [("CCCCCC", "RRRCCC", 640), ("RCRCRC", "CCCCCC", 4096 + 64), ("rrrrrr", "CrCrCr", 1024), ("CCCCCC", "CCCCCC", 64 * 600)])
+def test_policy_loss_of_six_cuts(tX, tG, V):
+    run_policy(64, V, "bf16", tX, tG, seed=V)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("T,V,kl", [(40, 50, 0.0), (60, 333, 0.05), (30, 1031, 0.3)])
 def test_policy_loss_masked(T, V, kl, dt):
@@ -393,9 +408,9 @@ def test_pack8(rows, cols, dt):
     run_pack(rows, cols, dt, seed=cols)
 
 
-@pytest.mark.parametrize("t", ["R", "C", "r", "RC", "CCr"])
+@pytest.mark.parametrize("t", ["R", "C", "r", "RC", "CCr", "RCRCRC"])
 def test_pack8_tiled(t):
-    run_pack(16, 96, "bf16", t)
+    run_pack(16, 96 if len(t) < 6 else 320, "bf16", t)
     run_pack(16, 88, "f32", t)
 
 
