@@ -15,9 +15,12 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Statistics of a part of a row, in base 2: the sum of 2^(x kk - top) over it, top the largest x kk (rounded: any number serves as
-// long as all use the same).  A part with nothing above -inf has top -inf and a sum of 0, or NaN where it holds one.
+// Statistics of a part of a row, in base 2: the sum of 2^((x - top) kk) over it, top its largest logit as it is stored.  The
+// difference comes first: near the maximum it is exact and for the maximum itself 0, however large the logits are (the rounding
+// of a product x kk would be worth more than a power of 2 from some 1e9 on, and the product infinite for a mask of the type's lowest
+// value).  A part with nothing above -inf has top -inf and a sum of 0, or NaN where it holds one.
 struct Stats { float top, sum; };
+__device__ __forceinline__ float power_of(float x, float top, float kk) { return wave::exp2_fast((x - top) * kk); }
 
 struct PolicyParams {
     BlockTable X, G;
@@ -45,24 +48,27 @@ __device__ __forceinline__ int64_t action_of(const PolicyParams &p, uint32_t t)
 // whether a token counts as far as its weight and action go
 __device__ __forceinline__ bool counts(const PolicyParams &p, uint32_t t, int64_t a) { return a >= 0 && a < p.vocab && !(p.weight && load_scalar(p.weight + t) == 0.0f); }
 
-__device__ __forceinline__ Stats joined(Stats a, Stats b)
+// log2(e) times the logits' factor (finite, so that it is no power at all for the maximum)
+__device__ __forceinline__ float exponent_factor(const PolicyParams &p) { return fminf(p.policy.scale * kLog2e, 3.402823466e38f); }
+
+__device__ __forceinline__ Stats joined(Stats a, Stats b, float kk)
 {
     const float top = fmaxf(a.top, b.top);
-    const float fa = a.top == -INFINITY ? 1.0f : wave::exp2_fast(a.top - top), fb = b.top == -INFINITY ? 1.0f : wave::exp2_fast(b.top - top);
+    const float fa = a.top == -INFINITY ? 1.0f : power_of(a.top, top, kk), fb = b.top == -INFINITY ? 1.0f : power_of(b.top, top, kk);
     return {top, a.sum * fa + b.sum * fb};
 }
-__device__ __forceinline__ Stats wave_joined(Stats s)
+__device__ __forceinline__ Stats wave_joined(Stats s, float kk)
 {
     const float top = wave_max(s.top);
-    return {top, wave_sum(s.top == -INFINITY ? s.sum : s.sum * wave::exp2_fast(s.top - top))};
+    return {top, wave_sum(s.top == -INFINITY ? s.sum : s.sum * power_of(s.top, top, kk))};
 }
 // over a workgroup's waves, in every thread; `red`: a Stats per wave
-template <int WAVES> __device__ __forceinline__ Stats group_joined(Stats s, Stats *red)
+template <int WAVES> __device__ __forceinline__ Stats group_joined(Stats s, Stats *red, float kk)
 {
-    s = wave_joined(s);
+    s = wave_joined(s, kk);
     if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    return wave_joined((threadIdx.x & 63u) < (uint32_t)WAVES ? red[threadIdx.x & 63u] : Stats{-INFINITY, 0.0f});
+    return wave_joined((threadIdx.x & 63u) < (uint32_t)WAVES ? red[threadIdx.x & 63u] : Stats{-INFINITY, 0.0f}, kk);
 }
 
 template <typename T> __device__ __forceinline__ float max_of(u32x4 v, float m)
@@ -73,17 +79,33 @@ template <typename T> __device__ __forceinline__ float max_of(u32x4 v, float m)
     for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, f[i]);
     return m;
 }
-template <typename T> __device__ __forceinline__ float sum_of(u32x4 v, float kk, float top, float s)
+// 2^((x - top) kk) for many x: rest() times the sum of of(x).  fp32: power_of.  bf16, where the arithmetic is what a row waits for,
+// a fused step in place of two (difference first throughout: 1000 x 50021 47.4 us, so 46.4): of(x) = 2^(x kk - c) with c the rounded
+// top kk, rest() what the rounding left out, a power of 2^-4 at most.  Beyond |top| kk = 2^20 a smaller factor keeps c at 2^20: numbers
+// of 8 bits that are not top are 2^-9 of it apart, and have no power then as they had none before.
+template <typename T> struct Powers {
+    float kk, top, c;
+    __device__ __forceinline__ Powers(float k, float t) : kk(k), top(t), c(0.0f)
+    {
+        if constexpr (sizeof(T) == 2) {
+            if (fabsf(top) * kk > 1048576.0f) kk = __uint_as_float((127u + 19u + 127u - ((__float_as_uint(top) >> 23) & 255u)) << 23);
+            c = top * kk;
+        }
+    }
+    __device__ __forceinline__ float rest() const { return sizeof(T) == 2 ? wave::exp2_fast(-fmaf(top, kk, -c)) : 1.0f; }
+    __device__ __forceinline__ float of(float x) const { return sizeof(T) == 2 ? wave::exp2_fast(fmaf(x, kk, -c)) : power_of(x, top, kk); }
+};
+template <typename T, class F> __device__ __forceinline__ float sum_of(u32x4 v, F &&of, float s)
 {
     float f[kVec<T>];
     unpack16(v, f, T());
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) s += wave::exp2_fast(fmaf(f[i], kk, -top));
+    for (int i = 0; i < kVec<T>; ++i) s += of(f[i]);
     return s;
 }
 
 // What a row's statistics come to: its log probability, its part of the loss, the factor of p's numerators in its gradient and
-// what the action's entry has on top.  A few scalars a row, with the differences of near numbers (x_a kk - top, log probabilities)
+// what the action's entry has on top.  A few scalars a row, with log p and its differences from the old and the reference one
 // taken in 64 bits: the loss is a sum of terms of both signs.
 struct RowResult { float logp, loss, coef, at_a; bool live; };
 struct TokenScalars { float weight, old_logp, ref_logp, advantage; };
@@ -97,7 +119,7 @@ __device__ __forceinline__ TokenScalars scalars_of(const PolicyParams &p, uint32
     if (p.policy.kl != 0.0f) c.ref_logp = load_scalar(p.ref_logp + t);
     return c;
 }
-__device__ __forceinline__ RowResult row_result(const PolicyParams &p, const TokenScalars &c, Stats s, float xa, float kk)
+__device__ __forceinline__ RowResult row_result(const PolicyParams &p, const TokenScalars &c, Stats s, float xa)
 {
     RowResult r{0.0f, 0.0f, 0.0f, 0.0f, true};
     if (s.top == -INFINITY && s.sum == 0.0f) { // nothing above -inf
@@ -106,7 +128,7 @@ __device__ __forceinline__ RowResult row_result(const PolicyParams &p, const Tok
     }
     int e = 0;
     const float f = frexpf(s.sum, &e); // log2 of a number next to 1, and a whole number
-    const double lp = ((double)xa * (double)kk - (double)s.top - (double)e - (double)log2f(f)) * 0.6931471805599453;
+    const double lp = ((double)xa - (double)s.top) * (double)p.policy.scale - ((double)e + (double)log2f(f)) * 0.6931471805599453;
     r.logp = (float)lp;
     if (!p.weight) return r;
     const float w = c.weight, adv = c.advantage, lo = 1.0f - p.policy.clip_low, hi = 1.0f + p.policy.clip_high;
@@ -132,27 +154,44 @@ __device__ __forceinline__ void store_scalars(const PolicyParams &p, uint32_t t,
     if (p.row_loss) p.row_loss[t] = r.loss;
 }
 
-// statistics with N more vectors (vectors of -inf add nothing)
-template <typename T, int N> __device__ __forceinline__ Stats with_vectors(Stats s, const u32x4 *r, float kk)
+// statistics with N more vectors (vectors of -inf add nothing); FUSED: by Powers
+template <typename T, int N, bool FUSED = (N > 1)> __device__ __forceinline__ Stats with_vectors(Stats s, const u32x4 *r, float kk)
 {
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < N; ++i) m = max_of<T>(r[i], m);
-    const float top = fmaxf(s.top, m * kk), from = top == -INFINITY ? 0.0f : top;
-    float sum = s.top == -INFINITY ? s.sum : s.sum * wave::exp2_fast(s.top - from);
+    const float top = fmaxf(s.top, m), from = top == -INFINITY ? 0.0f : top;
+    float sum = s.top == -INFINITY ? s.sum : s.sum * power_of(s.top, from, kk);
+    if constexpr (FUSED && sizeof(T) == 2) {
+        const Powers<T> e(kk, from);
+        float more = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum = sum_of<T>(r[i], kk, from, sum);
+        for (int i = 0; i < N; ++i) more = sum_of<T>(r[i], [&](float x) { return e.of(x); }, more);
+        return {top, fmaf(more, e.rest(), sum)};
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum = sum_of<T>(r[i], [&](float x) { return power_of(x, from, kk); }, sum);
     return {top, sum};
 }
 
-template <typename T> __device__ __forceinline__ u32x4 gradient_of(u32x4 v, float kk, float top, float coef)
-{
-    float f[kVec<T>];
-    unpack16(v, f, T());
+// coef 2^((x - top) kk) over a row
+template <typename T> struct Gradient {
+    Powers<T> e;
+    float coef;
+    __device__ __forceinline__ Gradient(float kk, float top, float c) : e(kk, top), coef(c)
+    {
+        coef *= e.rest();
+        e.kk = __uint_as_float(uniform(__float_as_uint(e.kk)));
+    }
+    __device__ __forceinline__ u32x4 of(u32x4 v) const
+    {
+        float f[kVec<T>];
+        unpack16(v, f, T());
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) f[i] = coef * wave::exp2_fast(fmaf(f[i], kk, -top));
-    return pack16(f, T());
-}
+        for (int i = 0; i < kVec<T>; ++i) f[i] = coef * e.of(f[i]);
+        return pack16(f, T());
+    }
+};
 
 // Where whole unit u of a row lies: segment and first vector
 struct Unit { uint32_t q, j0; };
@@ -315,7 +354,7 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
     __shared__ float shared[4]; // top, coef, the action's entry, whether the row counts
     __shared__ uint64_t tables[2][kMaxShards];
     const uint32_t w = uniform(threadIdx.x >> 6);
-    const float kk = p.policy.scale * kLog2e;
+    const float kk = exponent_factor(p);
     const bool has_rest = p.rest && w < p.s.nseg;
     if (p.s.nseg > 1 || p.G.nrep > 1) {
         if (threadIdx.x < (uint32_t)kMaxShards) {
@@ -375,7 +414,7 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
 #pragma unroll
                 for (int k = i; k < i + most; ++k)
                     if (k * WAVES + w >= p.units) r[k] = nothing;
-                s = with_vectors<T, most>(s, r + i, kk);
+                s = with_vectors<T, most, (most > 1 && NC <= 16)>(s, r + i, kk); // (more vectors leave no registers for it: 2048 x 151936 278 us, so 268)
                 if constexpr (!GRAD) { // nobody needs them again
                     if (next_in && p.units) {
 #pragma unroll
@@ -384,7 +423,7 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            s = wave_joined(s);
+            s = wave_joined(s, kk);
             if constexpr (GRAD) {
 #pragma unroll
                 for (int i = 0; i < NC; ++i) wave::forget(r[i]);
@@ -396,12 +435,12 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
             if (w == 0) {
                 if constexpr (WAVES > 1) {
                     const uint32_t lane = threadIdx.x & 63u;
-                    s = wave_joined(lane < (uint32_t)WAVES ? red[lane] : Stats{-INFINITY, 0.0f});
+                    s = wave_joined(lane < (uint32_t)WAVES ? red[lane] : Stats{-INFINITY, 0.0f}, kk);
                 }
                 const float x = to_float(xa);
-                res = row_result(p, c, s, x, kk);
+                res = row_result(p, c, s, x);
                 top = s.top;
-                entry = fmaf(res.coef, wave::exp2_fast(fmaf(x, kk, -top)), res.at_a);
+                entry = fmaf(res.coef, power_of(x, top, kk), res.at_a);
                 if (threadIdx.x == 0) {
                     store_scalars(p, t, res);
                     if constexpr (WAVES > 1 && GRAD) {
@@ -424,19 +463,20 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
         }
         if constexpr (GRAD) {
             T *row = map.g_row(p, t);
+            const Gradient<T> grad(kk, top, res.coef);
             // Everything fetched so far is here and used; said once, or the compiler, which cannot tell for rows that do not
             // count, waits for every store in front of each of the next row's loads.
             __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0)
             const auto emit = [&](auto fetch) {
                 if (has_rest) {
-                    const u32x4 g = res.live ? gradient_of<T>(rest, kk, top, res.coef) : zero;
+                    const u32x4 g = res.live ? grad.of(rest) : zero;
                     if constexpr (decltype(fetch)::value) rest = load_rest<T>(p, next, w);
                     store_rest<T>(p, t, w, g);
                 }
                 if (p.units == 0) return;
 #pragma unroll
                 for (int i = 0; i < NC; ++i) {
-                    const u32x4 g = res.live ? gradient_of<T>(r[i], kk, top, res.coef) : zero;
+                    const u32x4 g = res.live ? grad.of(r[i]) : zero;
                     if constexpr (decltype(fetch)::value) r[i] = map.load(p, next, next_row, slot(i));
                     if (i * WAVES + w < p.units) map.store(p, t, row, i * WAVES + w, g);
                     __builtin_amdgcn_sched_barrier(0);
@@ -469,7 +509,7 @@ template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void polic
     __shared__ Stats red[kStreamWaves];
     const uint32_t t = blockIdx.x, w = uniform(threadIdx.x >> 6);
     const int64_t a = action_of(p, t);
-    const float kk = p.policy.scale * kLog2e;
+    const float kk = exponent_factor(p);
     RowResult res{0.0f, 0.0f, 0.0f, 0.0f, false};
     Stats s{-INFINITY, 0.0f};
     Column ca{0, 0};
@@ -493,11 +533,12 @@ template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void polic
                 const u32x4 r = any_rest<T>(p, t, q);
                 s = with_vectors<T, 1>(s, &r, kk);
             }
-        s = group_joined<kStreamWaves>(s, red);
-        res = row_result(p, scalars_of(p, t), s, xa, kk);
+        s = group_joined<kStreamWaves>(s, red, kk);
+        res = row_result(p, scalars_of(p, t), s, xa);
     }
     if (threadIdx.x == 0) store_scalars(p, t, res);
     if (!p.with_dx) return;
+    const Gradient<T> grad(kk, s.top, res.coef);
     const u32x4 zero = u32x4{0, 0, 0, 0};
     uint32_t u = w;
     for (; u + (U - 1) * kStreamWaves < p.units; u += U * kStreamWaves) {
@@ -505,12 +546,12 @@ template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void polic
 #pragma unroll
         for (int i = 0; i < U; ++i) r[i] = res.live ? load_unit<T>(p, t, u + i * kStreamWaves) : zero;
 #pragma unroll
-        for (int i = 0; i < U; ++i) store_unit<T>(p, t, u + i * kStreamWaves, res.live ? gradient_of<T>(r[i], kk, s.top, res.coef) : zero);
+        for (int i = 0; i < U; ++i) store_unit<T>(p, t, u + i * kStreamWaves, res.live ? grad.of(r[i]) : zero);
     }
-    for (; u < p.units; u += kStreamWaves) store_unit<T>(p, t, u, res.live ? gradient_of<T>(load_unit<T>(p, t, u), kk, s.top, res.coef) : zero);
+    for (; u < p.units; u += kStreamWaves) store_unit<T>(p, t, u, res.live ? grad.of(load_unit<T>(p, t, u)) : zero);
     if (p.rest)
-        for (uint32_t q = w; q < p.s.nseg; q += kStreamWaves) store_any_rest<T>(p, t, q, res.live ? gradient_of<T>(any_rest<T>(p, t, q), kk, s.top, res.coef) : zero);
-    if (res.live) store_action<T, kStreamWaves>(p, t, ca, fmaf(res.coef, wave::exp2_fast(fmaf(xa, kk, -s.top)), res.at_a));
+        for (uint32_t q = w; q < p.s.nseg; q += kStreamWaves) store_any_rest<T>(p, t, q, res.live ? grad.of(any_rest<T>(p, t, q)) : zero);
+    if (res.live) store_action<T, kStreamWaves>(p, t, ca, fmaf(res.coef, power_of(xa, s.top, kk), res.at_a));
 }
 
 // Rows cut into parts of kPartWaves * kPartVectors units, a workgroup to each, in two launches: the parts' statistics, then the rows'
@@ -524,7 +565,7 @@ template <typename T> __global__ __launch_bounds__(kPartWaves * 64) void policy_
     __shared__ Stats red[kPartWaves];
     const uint32_t t = quotient(blockIdx.x, p.by_parts), part = blockIdx.x - t * p.parts, w = uniform(threadIdx.x >> 6), u0 = part * kPartUnits;
     if (!counts(p, t, action_of(p, t))) return;
-    const float kk = p.policy.scale * kLog2e;
+    const float kk = exponent_factor(p);
     u32x4 r[kPartVectors];
 #pragma unroll
     for (int i = 0; i < kPartVectors; ++i) {
@@ -538,7 +579,7 @@ template <typename T> __global__ __launch_bounds__(kPartWaves * 64) void policy_
             const u32x4 v = only_own<T>(p, load_rest<T>(p, t, q));
             s = with_vectors<T, 1>(s, &v, kk);
         }
-    s = group_joined<kPartWaves>(s, red);
+    s = group_joined<kPartWaves>(s, red, kk);
     if (threadIdx.x == 0) p.part_stats[blockIdx.x] = s;
 }
 
@@ -554,9 +595,9 @@ template <typename T> __device__ __forceinline__ void sum_of_parts(const PolicyP
         float loss = 0.0f;
         if (a >= 0 && a < p.vocab && p.weight[t] != 0.0f) {
             Stats s{-INFINITY, 0.0f};
-            for (uint32_t i = 0; i < p.parts; ++i) s = joined(s, p.part_stats[(size_t)t * p.parts + i]);
+            for (uint32_t i = 0; i < p.parts; ++i) s = joined(s, p.part_stats[(size_t)t * p.parts + i], kk);
             const TokenScalars c{p.weight[t], p.old_logp[t], p.policy.kl != 0.0f ? p.ref_logp[t] : 0.0f, p.advantage[t]};
-            loss = row_result(p, c, s, to_float(logit_at<T>(p, t, column_of(p, (uint32_t)a))), kk).loss;
+            loss = row_result(p, c, s, to_float(logit_at<T>(p, t, column_of(p, (uint32_t)a)))).loss;
         }
         row_loss[t] = loss;
     }
@@ -571,7 +612,7 @@ template <typename T> __device__ __forceinline__ void sum_of_parts(const PolicyP
 // GRAD: a workgroup to a part; otherwise a wave to a token, for the scalars alone; one workgroup more for the loss
 template <typename T, bool GRAD> __global__ __launch_bounds__(kPartWaves * 64) void policy_part_result_kernel(const PolicyParams p)
 {
-    const float kk = p.policy.scale * kLog2e;
+    const float kk = exponent_factor(p);
     const uint32_t t = GRAD ? quotient(blockIdx.x, p.by_parts) : blockIdx.x, part = GRAD ? blockIdx.x - t * p.parts : 0;
     if (t == p.tokens) {
         if (part == 0) sum_of_parts<T>(p, kk);
@@ -595,27 +636,28 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(kPartWaves * 64) v
         }
         ca = column_of(p, (uint32_t)a);
         xa = to_float(logit_at<T>(p, t, ca));
-        for (uint32_t i = lane; i < p.parts; i += 64) s = joined(s, p.part_stats[(size_t)t * p.parts + i]);
-        s = wave_joined(s);
-        res = row_result(p, scalars_of(p, t), s, xa, kk);
+        for (uint32_t i = lane; i < p.parts; i += 64) s = joined(s, p.part_stats[(size_t)t * p.parts + i], kk);
+        s = wave_joined(s, kk);
+        res = row_result(p, scalars_of(p, t), s, xa);
     }
     if (part == 0 && threadIdx.x == 0) store_scalars(p, t, res);
     if constexpr (GRAD) {
+        const Gradient<T> grad(kk, s.top, res.coef);
 #pragma unroll
         for (int i = 0; i < kPartVectors; ++i) {
             const uint32_t u = u0 + i * kPartWaves + w;
-            if (u < p.units) store_unit<T>(p, t, u, res.live ? gradient_of<T>(r[i], kk, s.top, res.coef) : zero);
+            if (u < p.units) store_unit<T>(p, t, u, res.live ? grad.of(r[i]) : zero);
         }
         if (p.rest)
             for (uint32_t q = part + w * p.parts; q < p.s.nseg; q += kPartWaves * p.parts)
-                store_rest<T>(p, t, q, res.live ? gradient_of<T>(load_rest<T>(p, t, q), kk, s.top, res.coef) : zero);
+                store_rest<T>(p, t, q, res.live ? grad.of(load_rest<T>(p, t, q)) : zero);
         if (!res.live) return;
         // the action's entry, by the thread that wrote its vector
         const uint32_t j = ca.offset / kVec<T>, unit = ca.q * p.by_ups.d + j / 64;
         const bool whole = j / 64 < p.by_ups.d;
         const uint32_t its_part = whole ? unit / kPartUnits : ca.q % p.parts, wave = whole ? unit % kPartWaves : ca.q / p.parts % kPartWaves;
         if (part != its_part || threadIdx.x != wave * 64 + (j & 63u)) return;
-        store_entry<T>(p, t, ca, fmaf(res.coef, wave::exp2_fast(fmaf(xa, kk, -s.top)), res.at_a));
+        store_entry<T>(p, t, ca, fmaf(res.coef, power_of(xa, s.top, kk), res.at_a));
     }
 }
 

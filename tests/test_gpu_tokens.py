@@ -372,6 +372,141 @@ def test_policy_rows_that_count_show_their_nan():
     assert np.isnan(down(dX[0])[:3]).all() and np.isfinite(down(dX[0])[3]).all()
 
 
+LOWEST = {"bf16": -3.3895313892515355e38, "f32": float(np.finfo(np.float32).min)}
+
+
+def run_policy_of_large_logits(V, dt, mask, scale, tX="", tG="", with_dx=True):
+    """Large finite logits, as masks leave them: rows of nothing but the mask, rows with a masked tail or with one entry left, an action
+    that is ruled out, and rows whose largest logits are near the type's largest value.  No bound beyond run_policy's."""
+    rng, T = np.random.default_rng(V), 8
+    mask = LOWEST[dt] if mask is None else mask
+    x = normal_f32(V, 0, (T, V), 2.0)
+    a = rng.integers(0, max(1, V // 2), T)
+    x[0] = mask
+    x[1, V // 2:] = mask
+    x[2] = mask
+    x[2, a[2]] = 0.5
+    x[3, 1:] = max(mask, -1e30)
+    a[3] = V - 1                                # ruled out, unless it is all there is
+    x[4, a[4]] = 2.5e38
+    x[5] = 2.5e38
+    x[6] = mask
+    x[6, V // 3:] = mask / 2 if mask < -1e35 else mask - 1e4 * abs(mask) * 2.0 ** -8
+    run_policy_of_logits(x, a, dt, scale, tX, tG, with_dx)
+
+
+def run_policy_of_logits(x, a, dt, scale, tX="", tG="", with_dx=True):
+    T, V = x.shape
+    rng, scale, k = np.random.default_rng(V + T), float(np.float32(scale)), len(tX)
+    raw, x = stored(x, dt)
+    logp = tk.token_logp(x, a, scale)
+    old = np.where(np.abs(logp) < 1e3, logp - rng.choice([-0.5, -0.1, 0.05, 0.4], T), 0).astype(np.float32)
+    adv, w = rng.normal(0, 1, T).astype(np.float32), np.full(T, 1.0 / T, dtype=np.float32)
+    p, lo, hi = tt.policy(clip_low=0.2, clip_high=0.25, scale=scale), float(np.float32(0.2)), float(np.float32(0.25))
+    loss, got = empty((1,), torch.float32), empty((T,), torch.float32)
+    dX = outputs(T, V, tG, dt) if with_dx else None
+    Xs, d_a = shards(raw, tX), ids_of(a, "i64")
+    ws = workspace(tt.tt_policy_workspace_bytes(T, V, k, dt, tX, tG if with_dx else None))
+    tt.tt_policy_loss(p, T, V, k, dt, tX, tG, Xs, d_a, up(old), None, up(adv), up(w), loss, got, dX, ws)
+    want_loss, want_logp, want_dX, d = tk.policy_loss(x, a, old.astype(float), old.astype(float), adv.astype(float), w.astype(float), scale, lo, hi, 0.0)
+    lb = logp_bound(want_logp, V)
+
+    def check_logp(got, what):      # (below the type's lowest value stands -inf)
+        with np.errstate(over="ignore"):
+            held = want_logp.astype(np.float32)
+        low = np.isinf(held)
+        assert np.array_equal(down(got)[low], held[low]), what
+        check(down(got)[~low], want_logp[~low], lb[~low], what)
+    check_logp(got, "logp")
+    slope = np.abs(np.exp(want_logp - old) * adv)
+    check(down(loss)[0], want_loss, np.sum(w * slope * (lb + 80 * EPS)), "loss")
+    if with_dx:
+        z = scale * x
+        away = np.max(z, axis=1, keepdims=True) - z
+        prob = np.exp(-away) / np.sum(np.exp(-away), axis=1, keepdims=True)
+        hot = np.zeros((T, V))
+        hot[np.arange(T), a] = 1
+        p_rel = 4 * EPS * (2 * away + 2 * math.log(V + 1) + 160)
+        err = w[:, None] * scale * ((slope * (lb + 16 * EPS))[:, None] * (hot + prob) + np.abs(d)[:, None] * (prob * p_rel + 8 * EPS * hot)) + 1e-37
+        check(full(dX, tG, T, V), want_dX, err + out_eps(dt) * (np.abs(want_dX) + err), "dX")
+    alone = empty((T,), torch.float32)
+    ws = workspace(tt.tt_policy_workspace_bytes(T, V, k, dt, tX))
+    tt.tt_token_logp(T, V, k, dt, tX, scale, Xs, d_a, alone, ws)
+    check_logp(alone, "logp alone")
+
+
+MASKS = [-5e9, -1e10, -1e15, -1e20, -1e30, -1e38, None]
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_policy_loss_of_large_finite_masks(dt, mask):
+    for V, scale in [(40, 1.0), (600, 0.5), (600, 2.0), (4500, 1.0), (40, 4.0), (9, 1e-30)]:
+        run_policy_of_large_logits(V, dt, mask, scale)
+        run_policy_of_large_logits(V, dt, mask, scale, with_dx=False)
+
+
+@pytest.mark.parametrize("mask", [-1e10, -1e30, None])
+@pytest.mark.parametrize("V,dt,tX,tG", [(17000, "bf16", "", ""), (9000, "f32", "", ""), (90000, "f32", "", ""), (170000, "bf16", "", ""), (24, "bf16", "CC", "CC"),
+                                        (4140, "f32", "CC", "RC"), (600, "bf16", "CCC", "RRr")])
+def test_policy_loss_of_large_finite_masks_in_every_form(V, dt, tX, tG, mask):
+    run_policy_of_large_logits(V, dt, mask, 1.0, tX, tG)
+    run_policy_of_large_logits(V, dt, mask, 0.7, tX, tG, with_dx=False)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_policy_loss_of_large_finite_masks_many_rows(dt):
+    """forms that take other kernels for many rows, each row a block of one mask and the rest ordinary"""
+    for T, V in [(300, 40), (300, 2000), (260, 20000)]:
+        x = normal_f32(T, 0, (T, V), 2.0)
+        x[:, V // 2:] = np.array([-1e10, -1e20, LOWEST[dt], -np.inf], np.float32)[np.arange(T) % 4][:, None]
+        whole = np.arange(T) % 7 == 3
+        x[whole] = LOWEST[dt]
+        raw, x = stored(x, dt)
+        a = np.random.default_rng(T).integers(0, V // 2, T)
+        want = tk.token_logp(x, a, 1.0)
+        Xs, d_a, one = shards(raw, ""), ids_of(a, "i32"), np.ones(T, np.float32)
+        for with_dx in (True, False):
+            loss, logp, dX = empty((1,), torch.float32), empty((T,), torch.float32), outputs(T, V, "", dt) if with_dx else None
+            ws = workspace(tt.tt_policy_workspace_bytes(T, V, 0, dt, "", "" if with_dx else None))
+            tt.tt_policy_loss(tt.policy(), T, V, 0, dt, "", "", Xs, d_a, up(want.astype(np.float32)), None, up(one), up(one), loss, logp, dX, ws)
+            check(down(logp), want, logp_bound(want, V), "logp")
+            # all ratios are 1: the loss is -1 a row, the gradient p - onehot
+            check(down(loss)[0], -float(T), T * (np.max(logp_bound(want, V)) + 64 * EPS), "loss")
+            if with_dx:
+                g = down(dX[0])
+                lb = logp_bound(want, V)[:, None]
+                prob = np.exp(x - np.max(x, 1, keepdims=True))
+                prob /= np.sum(prob, 1, keepdims=True)
+                prob[np.arange(T), a] -= 1
+                away = np.minimum(np.max(x, 1, keepdims=True) - x, 200)
+                err = np.abs(prob) * 4 * EPS * (2 * away + 2 * math.log(V + 1) + 160) + 2 * lb * np.abs(prob) + 1e-37
+                err[np.arange(T), a] += 2 * lb[:, 0] + 8 * EPS
+                check(g, prob, err + out_eps(dt) * (np.abs(prob) + err), "dX")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_policy_loss_of_large_logits_a_few_steps_apart(dt):
+    step = 2.0 ** -8 if dt == "bf16" else 2.0 ** -23
+    for V, scale in [(60, 1.0), (700, 0.3)]:
+        base = np.array([1e2, -1e3, 3e4, -1e5, 9e5, -2e6, 5e7, -3e9, 7e12, -1e30, 1e38], np.float64)
+        away = np.random.default_rng(V).integers(0, 6, (len(base), V))
+        x = base[:, None] - np.exp2(np.floor(np.log2(np.abs(base))))[:, None] * step * away
+        x[:, 3] = base
+        run_policy_of_logits(x.astype(np.float32), np.full(len(base), 3), dt, scale)
+
+
+def test_policy_loss_at_the_ends_of_the_scale():
+    """a factor next to the type's largest value: the maximum has probability 1 over its number, everything else none"""
+    x = np.zeros((2, 50), np.float32)
+    x[0, 7] = 1.0
+    raw, x = stored(x, "f32")
+    for scale, want in [(3.4e38, [0.0, -math.log(50)]), (1e-45, [-math.log(50)] * 2)]:
+        out, ws = empty((2,), torch.float32), workspace(tt.tt_policy_workspace_bytes(2, 50, 0, "f32", ""))
+        tt.tt_token_logp(2, 50, 0, "f32", "", scale, shards(raw, ""), ids_of([7, 7], "i64"), out, ws)
+        check(down(out), np.array(want), logp_bound(np.array(want), 50), "logp")
+
+
 def test_policy_loss_of_no_tokens_is_zero():
     loss = empty((1,), torch.float32)
     none = empty((1,), torch.float32)

@@ -88,6 +88,26 @@ def test_policy_special_rows():
     g.test_policy_loss_without_gradient_and_log_probabilities_alone()
 
 
+@pytest.mark.parametrize("mask", [-5e9, -1e10, -1e30, None])
+@pytest.mark.parametrize("V,dt,tX,tG,scale", [(40, "f32", "", "", 1.0), (600, "bf16", "", "", 0.5), (9, "f32", "", "", 1e-30), (24, "bf16", "CC", "CC", 2.0),
+                                              (600, "f32", "CCC", "RRr", 4.0)])
+def test_policy_loss_of_large_finite_masks(V, dt, tX, tG, scale, mask):
+    g.run_policy_of_large_logits(V, dt, mask, scale, tX, tG)
+
+
+def test_policy_loss_of_large_finite_masks_in_cut_rows():
+    g.run_policy_of_large_logits(17000, "bf16", -1e10, 1.0)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_policy_loss_of_large_logits_a_few_steps_apart(dt):
+    g.test_policy_loss_of_large_logits_a_few_steps_apart(dt)
+
+
+def test_policy_loss_at_the_ends_of_the_scale():
+    g.test_policy_loss_at_the_ends_of_the_scale()
+
+
 @pytest.mark.parametrize("T,V,dt,tX", [(1, 1, "f32", ""), (1, 4099, "bf16", ""), (8, 640, "bf16", "CC"), (6, 36, "bf16", "CR")])
 def test_token_logp(T, V, dt, tX):
     g.run_logp(T, V, dt, tX, scale=0.8)
