@@ -79,20 +79,26 @@ template <typename T> __device__ __forceinline__ float max_of(u32x4 v, float m)
     for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, f[i]);
     return m;
 }
-// 2^((x - top) kk) for many x: rest() times the sum of of(x).  fp32: power_of.  bf16, where the arithmetic is what a row waits for,
-// a fused step in place of two (difference first throughout: 1000 x 50021 47.4 us, so 46.4): of(x) = 2^(x kk - c) with c the rounded
-// top kk, rest() what the rounding left out, a power of 2^-4 at most.  Beyond |top| kk = 2^20 a smaller factor keeps c at 2^20: numbers
-// of 8 bits that are not top are 2^-9 of it apart, and have no power then as they had none before.
+// 2^((x - top) kk) for many x: whole() of the sum of of(x).  fp32: power_of.  bf16, where the arithmetic is what a row waits for,
+// a fused step in place of two (difference first throughout: 1000 x 50021 47.4 us, so 46.2): of(x) = 2^(x kk - c) with c the rounded
+// top kk, whole() puts right what the rounding left out, 2^-7 of an exponent at most.  Beyond |top| kk = 2^18 a smaller factor keeps c
+// below it: numbers of 8 bits that are not top are 2^-9 of it apart, 2^8 as an exponent, and have no power then as they had none before.
 template <typename T> struct Powers {
     float kk, top, c;
     __device__ __forceinline__ Powers(float k, float t) : kk(k), top(t), c(0.0f)
     {
         if constexpr (sizeof(T) == 2) {
-            if (fabsf(top) * kk > 1048576.0f) kk = __uint_as_float((127u + 19u + 127u - ((__float_as_uint(top) >> 23) & 255u)) << 23);
+            if (fabsf(top) * kk > 262144.0f) kk = __uint_as_float((127u + 17u + 127u - ((__float_as_uint(top) >> 23) & 255u)) << 23);
             c = top * kk;
         }
     }
-    __device__ __forceinline__ float rest() const { return sizeof(T) == 2 ? wave::exp2_fast(-fmaf(top, kk, -c)) : 1.0f; }
+    // (the exponential's series: a power next to 1 would be rounded to steps as large as what it puts right)
+    __device__ __forceinline__ float whole(float s) const
+    {
+        if (sizeof(T) != 2) return s;
+        const float t = fmaf(top, kk, -c) * 0.693147181f;
+        return fmaf(s * t, fmaf(t, fmaf(t, -1.0f / 6, 0.5f), -1.0f), s);
+    }
     __device__ __forceinline__ float of(float x) const { return sizeof(T) == 2 ? wave::exp2_fast(fmaf(x, kk, -c)) : power_of(x, top, kk); }
 };
 template <typename T, class F> __device__ __forceinline__ float sum_of(u32x4 v, F &&of, float s)
@@ -119,7 +125,7 @@ __device__ __forceinline__ TokenScalars scalars_of(const PolicyParams &p, uint32
     if (p.policy.kl != 0.0f) c.ref_logp = load_scalar(p.ref_logp + t);
     return c;
 }
-__device__ __forceinline__ RowResult row_result(const PolicyParams &p, const TokenScalars &c, Stats s, float xa)
+__device__ __forceinline__ RowResult row_result(const PolicyParams &p, const TokenScalars &c, Stats s, float xa, float kk)
 {
     RowResult r{0.0f, 0.0f, 0.0f, 0.0f, true};
     if (s.top == -INFINITY && s.sum == 0.0f) { // nothing above -inf
@@ -128,7 +134,9 @@ __device__ __forceinline__ RowResult row_result(const PolicyParams &p, const Tok
     }
     int e = 0;
     const float f = frexpf(s.sum, &e); // log2 of a number next to 1, and a whole number
-    const double lp = ((double)xa - (double)s.top) * (double)p.policy.scale - ((double)e + (double)log2f(f)) * 0.6931471805599453;
+    // (by kk, as the sum's powers go: the action's logit and the others are off by the same part of 10^-8, which cancels but for how far
+    // the action lies from the mean of p)
+    const double lp = (((double)xa - (double)s.top) * (double)kk - (double)e - (double)log2f(f)) * 0.6931471805599453;
     r.logp = (float)lp;
     if (!p.weight) return r;
     const float w = c.weight, adv = c.advantage, lo = 1.0f - p.policy.clip_low, hi = 1.0f + p.policy.clip_high;
@@ -167,7 +175,7 @@ template <typename T, int N, bool FUSED = (N > 1)> __device__ __forceinline__ St
         float more = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) more = sum_of<T>(r[i], [&](float x) { return e.of(x); }, more);
-        return {top, fmaf(more, e.rest(), sum)};
+        return {top, sum + e.whole(more)};
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) sum = sum_of<T>(r[i], [&](float x) { return power_of(x, from, kk); }, sum);
@@ -180,7 +188,7 @@ template <typename T> struct Gradient {
     float coef;
     __device__ __forceinline__ Gradient(float kk, float top, float c) : e(kk, top), coef(c)
     {
-        coef *= e.rest();
+        coef = e.whole(coef);
         e.kk = __uint_as_float(uniform(__float_as_uint(e.kk)));
     }
     __device__ __forceinline__ u32x4 of(u32x4 v) const
@@ -438,7 +446,7 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
                     s = wave_joined(lane < (uint32_t)WAVES ? red[lane] : Stats{-INFINITY, 0.0f}, kk);
                 }
                 const float x = to_float(xa);
-                res = row_result(p, c, s, x);
+                res = row_result(p, c, s, x, kk);
                 top = s.top;
                 entry = fmaf(res.coef, power_of(x, top, kk), res.at_a);
                 if (threadIdx.x == 0) {
@@ -534,7 +542,7 @@ template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void polic
                 s = with_vectors<T, 1>(s, &r, kk);
             }
         s = group_joined<kStreamWaves>(s, red, kk);
-        res = row_result(p, scalars_of(p, t), s, xa);
+        res = row_result(p, scalars_of(p, t), s, xa, kk);
     }
     if (threadIdx.x == 0) store_scalars(p, t, res);
     if (!p.with_dx) return;
@@ -597,7 +605,7 @@ template <typename T> __device__ __forceinline__ void sum_of_parts(const PolicyP
             Stats s{-INFINITY, 0.0f};
             for (uint32_t i = 0; i < p.parts; ++i) s = joined(s, p.part_stats[(size_t)t * p.parts + i], kk);
             const TokenScalars c{p.weight[t], p.old_logp[t], p.policy.kl != 0.0f ? p.ref_logp[t] : 0.0f, p.advantage[t]};
-            loss = row_result(p, c, s, to_float(logit_at<T>(p, t, column_of(p, (uint32_t)a)))).loss;
+            loss = row_result(p, c, s, to_float(logit_at<T>(p, t, column_of(p, (uint32_t)a))), kk).loss;
         }
         row_loss[t] = loss;
     }
@@ -638,7 +646,7 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(kPartWaves * 64) v
         xa = to_float(logit_at<T>(p, t, ca));
         for (uint32_t i = lane; i < p.parts; i += 64) s = joined(s, p.part_stats[(size_t)t * p.parts + i], kk);
         s = wave_joined(s, kk);
-        res = row_result(p, scalars_of(p, t), s, xa);
+        res = row_result(p, scalars_of(p, t), s, xa, kk);
     }
     if (part == 0 && threadIdx.x == 0) store_scalars(p, t, res);
     if constexpr (GRAD) {

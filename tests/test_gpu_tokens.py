@@ -507,6 +507,29 @@ def test_policy_loss_at_the_ends_of_the_scale():
         check(down(out), np.array(want), logp_bound(np.array(want), 50), "logp")
 
 
+@pytest.mark.parametrize("V", [8000, 33000])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_log_probabilities_are_off_to_both_sides(dt, V):
+    """No bias: the logits' factor is rounded (to 1.3e-8 of it here), but for the action and for the sum alike.  The mean error of 4096
+    rows is within half a step of fp32 next to 1 (eps / 2 = 3e-8) and four times what roundings of single ones leave of it."""
+    T = 4096
+    x = normal_f32(V, 0, (T, V), 2.5)
+    a = np.random.default_rng(V).integers(0, V, T)
+    x[np.arange(T), a] += 8
+    raw, x = stored(x, dt)
+    z = torch.from_numpy(x).to(DEV)
+    want = (z.gather(1, torch.from_numpy(a).to(DEV)[:, None])[:, 0] - torch.logsumexp(z, 1)).cpu().numpy()
+    one, loss, logp, dX = np.ones(T, np.float32), empty((1,), torch.float32), empty((T,), torch.float32), outputs(T, V, "", dt)
+    Xs, d_a = shards(raw, ""), ids_of(a, "i64")
+    ws = workspace(max(tt.tt_policy_workspace_bytes(T, V, 0, dt, "", ""), tt.tt_policy_workspace_bytes(T, V, 0, dt, "")))
+    tt.tt_policy_loss(tt.policy(), T, V, 0, dt, "", "", Xs, d_a, up(want.astype(np.float32)), None, up(one), up(one), loss, logp, dX, ws)
+    alone = empty((T,), torch.float32)
+    tt.tt_token_logp(T, V, 0, dt, "", 1.0, Xs, d_a, alone, ws)
+    for got in (logp, alone):
+        off = down(got).astype(np.float64) - want
+        assert abs(np.mean(off)) < EPS / 2 + 4 * np.std(off) / math.sqrt(T), np.mean(off)
+
+
 def test_policy_loss_of_no_tokens_is_zero():
     loss = empty((1,), torch.float32)
     none = empty((1,), torch.float32)
