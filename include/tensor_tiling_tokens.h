@@ -36,7 +36,7 @@ tt_status tt_embed_forward(int64_t tokens, int64_t vocab, int64_t width, int k, 
  * sums are fp32 and run over the tokens sorted by number, in an order that depends on ids alone, so equal calls give equal
  * bits; one rounding to dtype.  dX: tokens x width under tdX;  dW: vocab x width under tdW.
  * Workspace: device memory, 256-byte aligned, at least tt_embed_workspace_bytes (may be NULL if 0); nothing in it needs
- * clearing. */
+ * clearing.  What is enough for so many tokens is enough for fewer. */
 tt_status tt_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width, int k, int dtype, tt_tiling tdX, tt_tiling tdW,
                                    size_t *bytes);
 tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t width, int k, int dtype, tt_tiling tdX, tt_tiling tdW,
@@ -65,7 +65,7 @@ typedef struct {
  * statistics and sums fp32, equal calls give equal bits.  actions: id_dtype;  old_logp, ref_logp, advantage, weight, logp
  * (written; may be NULL): fp32, one per token;  loss: one fp32 value (written).
  * Workspace: device memory, 256-byte aligned, at least tt_policy_workspace_bytes (with the same tilings; with_dx = 0 if dX
- * will be NULL). */
+ * will be NULL: the two differ, and neither covers the other).  What is enough for so many tokens is enough for fewer. */
 tt_status tt_policy_workspace_bytes(int64_t tokens, int64_t vocab, int k, int dtype, tt_tiling tX, tt_tiling tdX, int with_dx,
                                     size_t *bytes);
 tt_status tt_policy_loss(const tt_policy *policy, int64_t tokens, int64_t vocab, int k, int dtype, tt_tiling tX, tt_tiling tdX,

@@ -4,6 +4,7 @@
 // g (onehot(a) - p): two sums over the row and a pass that writes as much as was read.  Memory bounds it (8 flops and two
 // exponentials a value), so the logits are to come from memory once: 4096 x 131072 bf16 logits, 1.075 GB read and 1.074 written in
 // 415 us, 5.2 TB/s.  Log probabilities alone: 4096 x 131072 179 us, 6.0 TB/s; 16 x 131072 8.3 us on the GPU, trips to memory.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -694,6 +695,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_losses_kernel(const float *ro
 
 // How rows are walked, and what a launch needs of the workspace: the rows' losses, and the parts' statistics where rows are cut
 struct Walk { Pieces s; uint32_t whole, units, rest, parts; size_t stats_at, bytes; };
+constexpr int64_t kCutRows = 128, kCutParts = (int64_t(1) << 22) - 1; // rows of a gradient, and parts of all rows, up to which rows are cut
 Walk walk_of(const BlockTable &X, const BlockTable &G, int64_t tokens, int64_t vocab, int dtype, bool with_dx)
 {
     Walk w;
@@ -704,11 +706,19 @@ Walk walk_of(const BlockTable &X, const BlockTable &G, int64_t tokens, int64_t v
     // Cut rows that are worth several workgroups, where there is no gradient or whole rows would leave most CUs idle.  Cut / whole, us:
     // loss of 16 x 131072 13 / 23, 64 15 / 23, 128 24 / 25, 128 x 20000 14.5 / 14.1, 256 x 131072 41 / 34, 512 71 / 58; log probabilities of
     // 256 x 131072 18 / 30, 4096 179 / 346.
-    w.parts = (tokens <= 128 || !with_dx) && w.units > kPartUnits ? (w.units + kPartUnits - 1) / kPartUnits : 1;
-    if ((uint64_t)tokens * w.parts >= (uint64_t(1) << 22)) w.parts = 1; // (a launch holds fewer than 2^32 threads)
+    w.parts = (tokens <= kCutRows || !with_dx) && w.units > kPartUnits ? (w.units + kPartUnits - 1) / kPartUnits : 1;
+    if (tokens * w.parts > kCutParts) w.parts = 1; // (a launch holds fewer than 2^32 threads)
     w.stats_at = align_up((size_t)tokens * 4, 256);
     w.bytes = w.stats_at + (w.parts > 1 ? align_up((size_t)tokens * w.parts * sizeof(Stats), 256) : 0);
     return w;
+}
+
+// What covers any smaller number of tokens too: rows are cut where they are few, and need more then.
+size_t room_of(const BlockTable &X, const BlockTable &G, int64_t tokens, int64_t vocab, int dtype, bool with_dx)
+{
+    const Walk w = walk_of(X, G, tokens, vocab, dtype, with_dx);
+    const int64_t parts = (w.units + kPartUnits - 1) / kPartUnits, cut = std::min({tokens, with_dx ? kCutRows : tokens, kCutParts / std::max<int64_t>(parts, 1)});
+    return std::max(w.bytes, walk_of(X, G, cut, vocab, dtype, with_dx).bytes);
 }
 
 // workgroups that fit the chip at a time: on each of 256 CUs 16 waves of up to 128 registers, or 32 of those that hold a few vectors
@@ -802,7 +812,7 @@ extern "C" tt_status tt_policy_workspace_bytes(int64_t tokens, int64_t vocab, in
     if (!make_blocks(nullptr, tX, k, tokens, vocab, &X)) return TT_EINFEASIBLE;
     G = X;
     if (with_dx && !make_blocks(nullptr, tdX, k, tokens, vocab, &G)) return TT_EINFEASIBLE;
-    *bytes = walk_of(X, G, tokens, vocab, dtype, with_dx != 0).bytes;
+    *bytes = room_of(X, G, tokens, vocab, dtype, with_dx != 0);
     return TT_OK;
 }
 

@@ -209,6 +209,25 @@ def test_embedding_skewed_buffers():
     run_embed(34, 70, 48, "f32", "C", "R", seed=9, skew=3)
 
 
+def test_a_workspace_for_many_tokens_covers_fewer():
+    V, D = 40, 24
+    G, dW = [up(normal_f32(3, 1, (16385, D), 0.5))], outputs(V, D, "", "f32")
+    ws = workspace(tt.tt_embed_workspace_bytes(16385, V, D, 0, "f32", "", ""))
+    ids = np.arange(16385) % V
+    for T in (16385, 16384, 257, 100):
+        tt.tt_embed_backward(T, V, D, 0, "f32", "", "", ids_of(ids[:T], "i64"), 1.0, [G[0][:T]], dW, ws)
+        want, mag, n = tk.embed_backward(down(G[0])[:T].astype(float), ids[:T], V, 1.0)
+        check(down(dW[0]), want, (n[:, None] + 1) * EPS * mag, T)
+    T, V = 129, 20000
+    raw, x = stored(normal_f32(4, 0, (T, V), 2.0), "bf16")
+    a, ws = np.arange(T), workspace(tt.tt_policy_workspace_bytes(T, V, 0, "bf16", "", ""))
+    want = tk.token_logp(x, a, 1.0)
+    for n in (129, 128, 3):
+        one, loss, logp, dX = np.ones(n, np.float32), empty((1,), torch.float32), empty((n,), torch.float32), outputs(n, V, "", "bf16")
+        tt.tt_policy_loss(tt.policy(), n, V, 0, "bf16", "", "", [up(raw[:n])], ids_of(a[:n], "i64"), up(want[:n].astype(np.float32)), None, up(one), up(one), loss, logp, dX, ws)
+        check(down(logp), want[:n], logp_bound(want[:n], V), n)
+
+
 def test_embedding_without_tokens_is_a_gradient_of_zeros():
     dW = [empty((6, 5), torch.float32)]
     ws = workspace(tt.tt_embed_workspace_bytes(0, 6, 5, 0, "f32", "", ""))

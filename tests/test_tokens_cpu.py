@@ -146,6 +146,19 @@ def test_packed_backward_refusals():
     assert need > tt.tt_fc_packed_workspace_bytes(tt.layer("fc", "none", 32, 32), 8, 0, "bf16", "", "", "", "", "")
 
 
+def test_a_workspace_for_many_tokens_covers_fewer():
+    counts = [0, 1, 64, 127, 128, 129, 130, 256, 257, 300, 4096, 16383, 16384, 16385, 20000, 32768, 40000, 65535, 65536, 65537, 70000, 131072, 131073, 1 << 20, (1 << 22) - 1]
+    for V, D in [(65536, 8192), (300, 1), (50021, 1500)]:
+        sizes = [tt.tt_embed_workspace_bytes(T, V, D, 0, "bf16", "", "") for T in counts]
+        assert sizes == sorted(sizes), (V, D)
+    for V in (0, 5, 1000, 17000, 131072, 600000, (1 << 31) - 1):
+        for dt in ("bf16", "f32"):
+            for tdX in (None, ""):
+                at = counts + [t + d for p in (1, 2, 3, 8, 37, 64) for t in [((1 << 22) - 1) // p] for d in (-1, 0)]
+                sizes = [tt.tt_policy_workspace_bytes(T, V, 0, dt, "", tdX) for T in sorted(at)]
+                assert sizes == sorted(sizes), (V, dt, tdX)
+
+
 def test_plain_policy_gradient_against_differences():
     rng = np.random.default_rng(5)
     T, V, h = 12, 9, 1e-5
