@@ -7,8 +7,9 @@
  * device buffer whatever the tilings are: they are as small as a row of pointers.  Token numbers are TT_I32 or TT_I64.
  * Shards, and buffers that a call writes, must not overlap any other buffer given to it.
  *
- * Calls with no tokens, rows or columns return TT_OK and write nothing, but for tt_policy_loss's loss (0) and a table
- * gradient without tokens (zeros).  Errors as in tensor_tiling.h: TT_EINVAL (NULL, unknown type or letter, k out of
+ * Calls with no tokens, rows or columns return TT_OK and write nothing, but for tt_policy_loss's loss (0), a table
+ * gradient without tokens (zeros), and log probabilities of an empty vocabulary (0); shards of a tensor without values may be
+ * NULL.  (tt_fc_backward_packed takes a batch of 1 and more, as tt_fc_backward does.)  Errors as in tensor_tiling.h: TT_EINVAL (NULL, unknown type or letter, k out of
  * range, negative or misaligned), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 tokens, rows, columns or
  * vocabulary entries and more; 2^30 numbers of an embedding; 2^22 tokens of a loss), TT_EWORKSPACE, TT_EDEVICE. */
 #ifndef TENSOR_TILING_TOKENS_H

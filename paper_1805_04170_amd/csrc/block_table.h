@@ -44,10 +44,10 @@ inline bool make_blocks(const void *const *shards, const tt_tiling &t, int k, in
     return true;
 }
 
-// every shard is there and aligned to its elements
-inline bool shards_fit(const void *const *shards, int k, int elem_bytes)
+// every shard is there and aligned to its elements (a tensor without values has no buffers)
+inline bool shards_fit(const void *const *shards, int k, int elem_bytes, bool empty = false)
 {
-    if (!shards) return false;
+    if (!shards || empty) return shards != nullptr;
     for (int s = 0; s < (1 << k); ++s)
         if (!shards[s] || reinterpret_cast<uintptr_t>(shards[s]) % (uintptr_t)elem_bytes) return false;
     return true;

@@ -843,7 +843,9 @@ extern "C" tt_status tt_embed_forward(int64_t tokens, int64_t vocab, int64_t wid
     tt_status st = check_sizes(tokens, vocab, width, k, dtype, tW, tX);
     if (st != TT_OK) return st;
     const int e = dtype_bytes(dtype);
-    if (!valid_ids(id_dtype, ids, tokens) || !shards_fit(W, k, e) || !shards_fit(const_cast<const void *const *>(X), k, e)) return TT_EINVAL;
+    if (!valid_ids(id_dtype, ids, tokens) || !shards_fit(W, k, e, vocab == 0 || width == 0) ||
+        !shards_fit(const_cast<const void *const *>(X), k, e, tokens == 0 || width == 0))
+        return TT_EINVAL;
     EmbedParams p;
     if (!make_blocks(W, tW, k, vocab, width, &p.W) || !make_blocks(const_cast<const void *const *>(X), tX, k, tokens, width, &p.X)) return TT_EINFEASIBLE;
     if (tokens == 0 || width == 0) return TT_OK;
@@ -907,7 +909,9 @@ extern "C" tt_status tt_embed_backward(int64_t tokens, int64_t vocab, int64_t wi
     tt_status st = check_sizes(tokens, vocab, width, k, dtype, tdX, tdW);
     if (st != TT_OK) return st;
     const int e = dtype_bytes(dtype);
-    if (!valid_ids(id_dtype, ids, tokens) || !shards_fit(dX, k, e) || !shards_fit(const_cast<const void *const *>(dW), k, e)) return TT_EINVAL;
+    if (!valid_ids(id_dtype, ids, tokens) || !shards_fit(dX, k, e, tokens == 0 || width == 0) ||
+        !shards_fit(const_cast<const void *const *>(dW), k, e, vocab == 0 || width == 0))
+        return TT_EINVAL;
     EmbedGradParams p;
     if (!make_blocks(dX, tdX, k, tokens, width, &p.G) || !make_blocks(const_cast<const void *const *>(dW), tdW, k, vocab, width, &p.W)) return TT_EINFEASIBLE;
     if (vocab == 0 || width == 0) return TT_OK;

@@ -301,9 +301,9 @@ template <typename T> void launch_unpack_gate(const GateParams &p, uint32_t y_bl
     else hipLaunchKernelGGL((unpack_gate_kernel<T>), grid, dim3(kThreads), 0, s, p);
 }
 
-bool bytes_fit(const void *const *shards, int k)
+bool bytes_fit(const void *const *shards, int k, bool empty = false)
 {
-    if (!shards) return false;
+    if (!shards || empty) return shards != nullptr;
     for (int s = 0; s < (1 << k); ++s) if (!shards[s]) return false;
     return true;
 }
@@ -312,10 +312,11 @@ tt_status run_pack(bool pack, int64_t rows, int64_t cols, int k, int dtype, cons
                       const void *const *Q, const void *const *S, void *stream)
 {
     if (!valid_k(k) || !valid_tiling(t, k) || !valid_dtype(dtype) || rows < 0 || cols < 0) return TT_EINVAL;
-    if (!shards_fit(X, k, dtype_bytes(dtype)) || !bytes_fit(Q, k) || !bytes_fit(S, k)) return TT_EINVAL;
+    const bool empty = rows == 0 || cols == 0;
+    if (!shards_fit(X, k, dtype_bytes(dtype), empty) || !bytes_fit(Q, k, empty) || !bytes_fit(S, k, empty)) return TT_EINVAL;
     Grid g;
     if (!make_grid(t.cut, k, rows, cols, &g)) return TT_EINFEASIBLE;
-    if (rows == 0 || cols == 0) return TT_OK;
+    if (empty) return TT_OK;
     PackParams p;
     const int n = 1 << k;
     const tt_status st = pack_geometry(&p, g.srows, g.scols);

@@ -828,7 +828,8 @@ extern "C" tt_status tt_policy_loss(const tt_policy *policy, int64_t tokens, int
         std::isnan(policy->kl) || std::isinf(policy->kl))
         return TT_EINVAL;
     const int e = dtype_bytes(dtype);
-    if (!shards_fit(X, k, e) || (dX && (!valid_tiling(tdX, k) || !shards_fit(const_cast<const void *const *>(dX), k, e)))) return TT_EINVAL;
+    const bool empty = tokens == 0 || vocab == 0;
+    if (!shards_fit(X, k, e, empty) || (dX && (!valid_tiling(tdX, k) || !shards_fit(const_cast<const void *const *>(dX), k, e, empty)))) return TT_EINVAL;
     if ((id_dtype != TT_I32 && id_dtype != TT_I64) || !aligned_to(loss, 4)) return TT_EINVAL;
     if (tokens > 0 && (!aligned_to(actions, id_dtype == TT_I32 ? 4 : 8) || !aligned_to(old_logp, 4) || !aligned_to(advantage, 4) || !aligned_to(weight, 4) ||
                        (policy->kl != 0.0f && !aligned_to(ref_logp, 4)) || (logp && !aligned_to(logp, 4))))
@@ -866,7 +867,7 @@ extern "C" tt_status tt_token_logp(int64_t tokens, int64_t vocab, int k, int dty
     tt_status st = check_sizes(tokens, vocab, k, dtype, tX);
     if (st != TT_OK) return st;
     const int e = dtype_bytes(dtype);
-    if (!(scale > 0.0f) || std::isinf(scale) || !shards_fit(X, k, e) || (id_dtype != TT_I32 && id_dtype != TT_I64)) return TT_EINVAL;
+    if (!(scale > 0.0f) || std::isinf(scale) || !shards_fit(X, k, e, tokens == 0 || vocab == 0) || (id_dtype != TT_I32 && id_dtype != TT_I64)) return TT_EINVAL;
     if (tokens > 0 && (!aligned_to(ids, id_dtype == TT_I32 ? 4 : 8) || !aligned_to(logp, 4))) return TT_EINVAL;
     PolicyParams p;
     if (!make_blocks(X, tX, k, tokens, vocab, &p.X)) return TT_EINFEASIBLE;

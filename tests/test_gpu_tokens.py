@@ -236,6 +236,18 @@ def test_embedding_without_tokens_is_a_gradient_of_zeros():
     assert not down(dW[0]).any()
 
 
+@pytest.mark.parametrize("T,V,D", [(0, 6, 5), (5, 0, 5), (0, 0, 5), (5, 6, 0)])
+def test_embedding_of_tensors_without_values(T, V, D):
+    none = lambda r, c: [torch.empty((r, c), dtype=torch.float32, device=DEV) if r * c == 0 else empty((r, c), torch.float32)]  # noqa: E731
+    X, dW, ids = none(T, D), none(V, D), torch.zeros(T, dtype=torch.int64, device=DEV)
+    tt.tt_embed_forward(T, V, D, 0, "f32", "", "", ids, 1.0, none(V, D), X)
+    tt.tt_embed_backward(T, V, D, 0, "f32", "", "", ids, 1.0, none(T, D), dW, None)
+    if V == 0 and T:
+        assert not down(X[0]).any()
+    if T == 0:
+        assert not down(dW[0]).any()
+
+
 # ------------------------------------------------------------- policy loss
 
 def policy_inputs(T, V, dt, seed, scale, kl, masked):
@@ -554,6 +566,19 @@ def test_policy_loss_of_no_tokens_is_zero():
     none = empty((1,), torch.float32)
     tt.tt_policy_loss(tt.policy(), 0, 40, 0, "f32", "", "", [none], empty((1,), torch.int64), none, None, none, none, loss, none, [none], workspace(256))
     assert down(loss)[0] == 0
+
+
+@pytest.mark.parametrize("T,V", [(0, 40), (3, 0), (0, 0)])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_policy_loss_of_tensors_without_values(T, V, dt):
+    name = "f32" if dt == torch.float32 else "bf16"
+    X, per, a = [torch.empty((T, V), dtype=dt, device=DEV)], torch.ones(T, device=DEV), torch.zeros(T, dtype=torch.int64, device=DEV)
+    loss, logp, dX = empty((1,), torch.float32), empty((T,), torch.float32), [torch.empty((T, V), dtype=dt, device=DEV)]
+    ws = workspace(tt.tt_policy_workspace_bytes(T, V, 0, name, "", ""))
+    tt.tt_policy_loss(tt.policy(kl=0.1), T, V, 0, name, "", "", X, a, per, per, per, per, loss, logp, dX, ws)
+    assert down(loss)[0] == 0 and not down(logp).any()
+    tt.tt_token_logp(T, V, 0, name, "", 1.0, X, a, logp, ws)
+    assert not down(logp).any()
 
 
 # ------------------------------------------------ activations in 8 bits

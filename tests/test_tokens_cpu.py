@@ -146,6 +146,26 @@ def test_packed_backward_refusals():
     assert need > tt.tt_fc_packed_workspace_bytes(tt.layer("fc", "none", 32, 32), 8, 0, "bf16", "", "", "", "", "")
 
 
+def test_tensors_without_values_have_no_buffers():
+    """torch's empty tensors have a NULL address; nothing is launched for them"""
+    none = lambda r, c, dt=torch.float32: [torch.empty((r, c), dtype=dt)]  # noqa: E731
+    ids = torch.empty(0, dtype=torch.int64)
+    assert none(0, 8)[0].data_ptr() == 0
+    for W in (P, none(0, 8)):
+        tt.tt_embed_forward(0, 8 if W is P else 0, 8, 0, "f32", "", "", ids, 1.0, W, none(0, 8), stream=1)
+    tt.tt_embed_forward(8, 8, 0, 0, "f32", "", "", A, 1.0, none(8, 0), none(8, 0), stream=1, id_dtype="i64")
+    tt.tt_embed_backward(8, 0, 8, 0, "f32", "", "", A, 1.0, P, none(0, 8), None, stream=1, id_dtype="i32")
+    tt.tt_embed_backward(0, 8, 0, 0, "f32", "", "", ids, 1.0, none(0, 0), none(8, 0), None, stream=1)
+    tt.tt_token_logp(0, 16, 0, "f32", "", 1.0, none(0, 16), ids, torch.empty(0), None, stream=1)
+    for fn, dts in ((tt.tt_pack8, (torch.float32, torch.int8, torch.uint8)), (tt.tt_unpack8, (torch.int8, torch.uint8, torch.float32))):
+        fn(0, 64, 0, "f32", "", *[none(0, 64, d) for d in dts], stream=1)
+        fn(4, 0, 1, "f32", "R", *[none(2, 0, d) * 2 for d in dts], stream=1)
+        refused("TT_EINVAL", fn, 0, 64, 0, "f32", "", P, None, P, stream=1)
+    refused("TT_EINVAL", tt.tt_embed_forward, 8, 0, 8, 0, "f32", "", "", A, 1.0, none(0, 8), none(0, 8), stream=1, id_dtype="i64")
+    refused("TT_EINVAL", tt.tt_embed_backward, 0, 8, 8, 0, "f32", "", "", ids, 1.0, none(0, 8), none(0, 8), None, stream=1)
+    refused("TT_EINVAL", tt.tt_token_logp, 4, 16, 0, "f32", "", 1.0, none(0, 16), A, A, Bytes(4096), stream=1, id_dtype="i64")
+
+
 def test_a_workspace_for_many_tokens_covers_fewer():
     counts = [0, 1, 64, 127, 128, 129, 130, 256, 257, 300, 4096, 16383, 16384, 16385, 20000, 32768, 40000, 65535, 65536, 65537, 70000, 131072, 131073, 1 << 20, (1 << 22) - 1]
     for V, D in [(65536, 8192), (300, 1), (50021, 1500)]:

@@ -113,6 +113,12 @@ def test_token_logp(T, V, dt, tX):
     g.run_logp(T, V, dt, tX, scale=0.8)
 
 
+@pytest.mark.parametrize("T,V,D", [(0, 6, 5), (5, 0, 5), (0, 0, 5), (5, 6, 0)])
+def test_tensors_without_values(T, V, D):
+    g.test_embedding_of_tensors_without_values(T, V, D)
+    g.test_policy_loss_of_tensors_without_values(T, V if T == 0 else 0, torch.bfloat16)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_pack8(dt):
     for rows, cols in [(1, 1), (3, 31), (5, 33), (2, 200), (9, 47)]:
