@@ -434,13 +434,15 @@ __device__ __forceinline__ Run run_of(const EmbedGradParams &p, uint32_t run)
     return {b, e, p.number[b], p.number[e - 1], true};
 }
 
-template <typename T> __device__ __forceinline__ void finish_row(Sums<T> &a, const EmbedGradParams &p, const Columns<T> &c, uint32_t v, uint32_t q)
+// (scale: p.scale, or 0 for a row without tokens, which is to be 0 whatever p.scale is)
+template <typename T>
+__device__ __forceinline__ void finish_row(Sums<T> &a, const EmbedGradParams &p, const Columns<T> &c, uint32_t v, uint32_t q, float scale)
 {
     const Place to = place_of(p.W, p.w.s, p.w.s.b_shift, v, q);
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
 #pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= p.scale;
+        for (int i = 0; i < kVec<T>; ++i) a.f[u][i] *= scale;
         c.template store<false>(p.W, to, u, pack16(a.f[u], T()));
     }
 }
@@ -507,7 +509,7 @@ template <typename T> __device__ __forceinline__ void sum_rows(const EmbedGradPa
         for (uint32_t i = 0; i < n; i += kRowBatch)
             add_batch<T, kRowBatch>(a, p, src, c, n - i, [&](int j) { return wave::read_lane(tokens, (int)(k * 8 + i) + j); });
         if (b + 8 < e) add_rows<T, kRowBatch>(a, p, src, c, b + 8, e);
-        finish_row(a, p, c, v, g.q);
+        finish_row(a, p, c, v, g.q, p.scale);
     }
 }
 
@@ -557,7 +559,7 @@ template <typename T> __device__ __forceinline__ void join_runs(const EmbedGradP
                 for (int i = 0; i < kVec<T>; ++i) a.f[u][i] += __uint_as_float(r[k][u][i / 4][i % 4]);
         }
     }
-    finish_row(a, p, c, v, g.q);
+    finish_row(a, p, c, v, g.q, p.scale);
 }
 
 // (2) The first workgroups' waves take a run each, beside the rows.  (The runs in a launch of their own in front, and the joins in
@@ -593,10 +595,11 @@ __device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGrad
         }
     }
 }
-template <typename T> __device__ __forceinline__ void finish_vector(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Column1<T> &c, uint32_t v)
+template <typename T>
+__device__ __forceinline__ void finish_vector(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Column1<T> &c, uint32_t v, float scale)
 {
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) s[i] *= p.scale;
+    for (int i = 0; i < kVec<T>; ++i) s[i] *= scale;
     c.store(p.W, place_of(p.W, p.w.s, p.w.s.b_shift, v, g.q), pack16(s, T()));
 }
 
@@ -624,7 +627,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void embed_sums_nar
     if (e - b > p.chunk) return; // (runs)
     float s[kVec<T>] = {};
     add_vectors<T>(s, p, g, c, b, e);
-    finish_vector(s, p, g, c, v);
+    finish_vector(s, p, g, c, v, b < e ? p.scale : 0.0f);
 }
 
 template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_narrow_kernel(const EmbedGradParams p)
@@ -645,7 +648,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_nar
 #pragma unroll
             for (int i = 0; i < kVec<T>; ++i) s[i] = run + k <= w.last ? s[i] + f[k][i] : s[i];
     }
-    finish_vector(s, p, g, c, w.v);
+    finish_vector(s, p, g, c, w.v, p.scale);
 }
 
 // Few tokens: nothing to sort.  Every wave holds all token numbers, 64 to a register, and asks for each of its rows which of them
@@ -717,6 +720,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
         const uint32_t v = g.row + k * p.apart;
         if (v >= (uint32_t)p.vocab) break;
         Found f = few.of(v, 1);
+        const float scale = f.any() ? p.scale : 0.0f;
         Sums<T> a;
         a.clear();
         while (f.any()) {
@@ -728,7 +732,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
             }
             add_batch<T, kRowBatch>(a, p, src, c, n, [&](int i) { return t[i]; });
         }
-        finish_row(a, p, c, v, g.q);
+        finish_row(a, p, c, v, g.q, scale);
     }
 }
 
@@ -740,7 +744,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
     // the wave's rows: those of its first and its last lane, and what lies between
     const uint32_t v0 = wave::read_lane(g.row, 0), v1 = wave::read_lane(g.row, 63);
     Found f = few.of(v0, v1 - v0 + 1);
-    float s[kVec<T>] = {};
+    float s[kVec<T>] = {}, scale = 0.0f;
     while (f.any()) {
         uint32_t t[kRowBatch], v[kRowBatch], m = 0;
         u32x4 r[kRowBatch];
@@ -757,13 +761,14 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 #pragma unroll
         for (int i = 0; i < kRowBatch; ++i) {
             if ((uint32_t)i >= m || v[i] != g.row) continue;
+            scale = p.scale;
             float x[kVec<T>];
             unpack16(r[i], x, T());
 #pragma unroll
             for (int q = 0; q < kVec<T>; ++q) s[q] += x[q];
         }
     }
-    if (g.row < (uint32_t)p.vocab) finish_vector(s, p, g, c, g.row);
+    if (g.row < (uint32_t)p.vocab) finish_vector(s, p, g, c, g.row, scale);
 }
 
 // ----------------------------------------------------------------------------------------------------- host side

@@ -209,6 +209,26 @@ def test_embedding_skewed_buffers():
     run_embed(34, 70, 48, "f32", "C", "R", seed=9, skew=3)
 
 
+@pytest.mark.parametrize("scale", [math.inf, -math.inf, math.nan, -2.0])
+@pytest.mark.parametrize("T", [40, 300])
+def test_table_gradient_rows_without_tokens_are_zeros(T, scale):
+    V = 50
+    ids = np.where(np.arange(T) % 2 == 0, 3, np.arange(T) % 7 + 20)
+    for D, dt in [(3, "f32"), (40, "bf16"), (300, "f32"), (1100, "bf16")]:
+        G, Gf = stored(np.abs(normal_f32(D, 1, (T, D), 0.5)) + 0.25, dt)
+        dW, ws = outputs(V, D, "", dt), workspace(tt.tt_embed_workspace_bytes(T, V, D, 0, dt, "", ""))
+        tt.tt_embed_backward(T, V, D, 0, dt, "", "", ids_of(ids, "i32"), scale, [up(G)], dW, ws)
+        there = np.isin(np.arange(V), ids)
+        assert not dW[0].cpu()[torch.from_numpy(~there)].contiguous().view(torch.uint8).any(), (D, dt)     # (+0)
+        with np.errstate(invalid="ignore"):
+            want, mag, n = tk.embed_backward(Gf, ids, V, scale)
+        if math.isfinite(scale):
+            err = (n[:, None] + 1) * EPS * mag
+            check(down(dW[0]), want, err + out_eps(dt) * (np.abs(want) + err), "dW")
+        else:
+            assert np.array_equal(down(dW[0])[there], want[there], equal_nan=True)
+
+
 def test_a_workspace_for_many_tokens_covers_fewer():
     V, D = 40, 24
     G, dW = [up(normal_f32(3, 1, (16385, D), 0.5))], outputs(V, D, "", "f32")

@@ -113,6 +113,11 @@ def test_token_logp(T, V, dt, tX):
     g.run_logp(T, V, dt, tX, scale=0.8)
 
 
+@pytest.mark.parametrize("T,scale", [(40, float("inf")), (40, -2.0), (300, float("inf")), (300, -2.0)])
+def test_table_gradient_rows_without_tokens_are_zeros(T, scale):
+    g.test_table_gradient_rows_without_tokens_are_zeros(T, scale)
+
+
 @pytest.mark.parametrize("T,V,D", [(0, 6, 5), (5, 0, 5), (0, 0, 5), (5, 6, 0)])
 def test_tensors_without_values(T, V, D):
     g.test_embedding_of_tensors_without_values(T, V, D)
