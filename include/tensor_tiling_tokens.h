@@ -82,7 +82,7 @@ tt_status tt_token_logp(int64_t tokens, int64_t vocab, int k, int dtype, tt_tili
 /* ------------------------------------------------ activations kept in 8 bits
  * The 8-bit form of a rows x cols tensor under a tiling: per shard Q (int8, the shard's shape) and S (uint8, one per block
  * of 32 columns of a row, blocks counted from the shard's first column, the last one short: srows x ceil(scols / 32)).
- * A value is Q * 2^(S - 127).  2^(S - 127) is the smallest power of two (not below 2^-126) that keeps the block's values
+ * A value is Q * 2^(S - 127), for any Q and any S but 255.  2^(S - 127) is, as tt_pack8 makes it, the smallest power of two (not below 2^-126) that keeps the block's values
  * within +-127 steps; Q is the value rounded to the nearest step (ties to even), but one step at least where the value
  * is not 0, so that signs, and with them ReLU's gates, stay as they were.  A block with a NaN or an infinity has S = 255
  * and stands for NaN throughout.  A power of two and eight bits are exact in bf16 and in fp32: unpacking rounds nothing. */

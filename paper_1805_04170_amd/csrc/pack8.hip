@@ -161,7 +161,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void pack8_kernel(c
     if ((threadIdx.x & 1u) == 0) store1(p.S[blockIdx.y] + h.block, (uint8_t)s);
 }
 
-__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255 ? 0x7fc00000u : s << 23); }
+// 2^(s - 127), NaN for 255.  (s = 0, which packing never makes, is a denormal; steps of it are exact in bf16 as well.)
+__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255 ? 0x7fc00000u : s == 0 ? 0x00400000u : s << 23); }
 // byte i of a vector, signed
 __device__ __forceinline__ int byte_of(const u32x4 &w, int i) { return (int)(int8_t)(w[i >> 2] >> (8 * (i & 3))); }
 

@@ -649,6 +649,29 @@ def test_pack8_values_at_the_edges(dt):
     run_pack(len(rows), 40, dt, values=a)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [64, 40])
+def test_unpack8_takes_any_step(cols, dt):
+    """all bytes as Q under all scales, those that packing never makes too; the backward pass's gates go by the same values"""
+    S = np.repeat(np.arange(256, dtype=np.uint8)[:, None], -(-cols // 32), axis=1)
+    Q = np.arange(-128, 128)[(np.arange(256)[:, None] * 7 + np.arange(cols)) % 256].astype(np.int8)
+    X = outputs(256, cols, "", dt)
+    tt.tt_unpack8(256, cols, 0, dt, "", [up(Q)], [up(S)], X)
+    want = tk.unpack8(Q, S)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    assert np.array_equal(down(X[0]), want, equal_nan=True)
+    lay, (W, Wf) = tt.layer("fc", "relu", 16, cols), stored(np.ones((16, cols), np.float32), dt)
+    XQ, XS, (dY, dYf) = np.zeros((256, 16), np.int8), np.full((256, 1), 127, np.uint8), stored(normal_f32(1, 0, (256, cols), 1.0), dt)
+    XQ[np.arange(256), np.arange(256) % 16] = 1
+    dX, dW = outputs(256, 16, "", dt), outputs(16, cols, "", dt)
+    ws = workspace(tt.tt_fc_packed_workspace_bytes(lay, 256, 0, dt, "", "", "", "", ""))
+    tt.tt_fc_backward_packed(lay, 256, 0, dt, "", "", "", "", "", None, None, [up(XQ)], [up(XS)], [up(W)], [up(Q)], [up(S)], [up(dY)], dX, dW, ws)
+    with np.errstate(invalid="ignore"):
+        G = dYf * (want > 0)
+    bound = lambda v, m: (1e-4 if dt == "bf16" else 1e-5) * m + 2 * out_eps(dt) * np.abs(v)  # noqa: E731
+    check(down(dX[0]), G @ Wf.T, bound(G @ Wf.T, ly.abs_product(G, Wf.T)), "dX")
+
+
 def test_pack8_skewed_buffers():
     run_pack(6, 70, "bf16", skew=1)
     run_pack(6, 70, "f32", skew=3)

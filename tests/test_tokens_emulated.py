@@ -133,6 +133,12 @@ def test_pack8(dt):
     g.test_pack8_values_at_the_edges(dt)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [64, 40])
+def test_unpack8_takes_any_step(cols, dt):
+    g.test_unpack8_takes_any_step(cols, dt)
+
+
 @pytest.mark.parametrize("t", [("", "", "", "", ""), ("CC", "RR", "CR", "RC", "Cr")])
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_packed_backward(t, dt):
