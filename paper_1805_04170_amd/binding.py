@@ -161,7 +161,7 @@ def _address(name):
     global _calls
     if _calls is None:      # (the planner and the other ctypes calls do without it)
         from . import _calls as c
-        c.converters(tiling, _padded_forms, _dtype)
+        c.converters(tiling, _padded_forms, _dtype, TilingError)
         _calls = c
     return (_lib or lib()).addresses[name]
 

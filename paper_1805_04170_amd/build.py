@@ -2,6 +2,7 @@
 
     python -m paper_1805_04170_amd.build
 """
+import importlib.util
 import os
 import subprocess
 import sys
@@ -39,8 +40,10 @@ def _compile(src):
 
 def build_calls():
     """the binding's extension module (host code; the library's functions reach it by address)"""
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "python", "calls.cpp"), "-o", CALLS]
+    torch = importlib.util.find_spec("torch")       # (for its DLPack header; without it tensors are asked by their methods)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"]] + \
+          (["-I" + os.path.join(p, "include") for p in torch.submodule_search_locations] if torch else []) + \
+          [os.path.join(CSRC, "python", "calls.cpp"), "-o", CALLS]
     subprocess.check_call(cmd)
     return CALLS
 

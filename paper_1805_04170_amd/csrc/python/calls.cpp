@@ -9,15 +9,75 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <cstring>
+#include <type_traits>
 #include "tensor_tiling.h"
 #include "tensor_tiling_tokens.h"
+#if __has_include(<ATen/dlpack.h>)
+#include <ATen/dlpack.h>
+#endif
+#if defined(DLPACK_MAJOR_VERSION) && (DLPACK_MAJOR_VERSION > 1 || DLPACK_MINOR_VERSION >= 3)
+#define TT_DLPACK_EXCHANGE
+#endif
 
 namespace {
 
 constexpr int kMaxShards = 1 << TT_MAX_K;
 
-PyObject *g_data_ptr, *g_numel, *g_element_size, *g_value; // method and attribute names
+PyObject *g_data_ptr, *g_numel, *g_element_size, *g_value, *g_dtype_name, *g_is_contiguous; // method and attribute names
 PyObject *g_tiling, *g_forms, *g_dtype;                     // the binding's own converters, for the rarer forms
+PyObject *g_error;                                          // its exception: (status, what)
+PyObject *g_float32;                                        // torch.float32, once a tensor was seen
+
+// What a dense tensor is to a call
+struct Described {
+    uint64_t address;
+    int64_t entries;
+    bool fp32, dense;
+};
+#ifdef TT_DLPACK_EXCHANGE
+// A tensor type's DLPack functions: all of the above in one call (a policy loss with seven arrays takes 8.3 us of host time, 9.1
+// by data_ptr(), dtype, numel() and is_contiguous(), and took 8.4 when only the address was asked for).
+PyObject *g_exchange_name, *g_exchange_type, *g_exchange_capsule; // of the type that was seen last
+const DLPackExchangeAPI *g_exchange;
+const DLPackExchangeAPI *exchange_of(PyObject *o)
+{
+    PyObject *type = reinterpret_cast<PyObject *>(Py_TYPE(o));
+    if (type == g_exchange_type) return g_exchange;
+    PyObject *capsule = PyObject_GetAttr(type, g_exchange_name);
+    auto *api = capsule && PyCapsule_IsValid(capsule, "dlpack_exchange_api")
+                    ? static_cast<const DLPackExchangeAPI *>(PyCapsule_GetPointer(capsule, "dlpack_exchange_api")) : nullptr;
+    PyErr_Clear();
+    if (!api || api->header.version.major != DLPACK_MAJOR_VERSION || api->header.version.minor < 3 || !api->dltensor_from_py_object_no_sync) {
+        Py_XDECREF(capsule);
+        return nullptr;
+    }
+    Py_INCREF(type);
+    Py_XSETREF(g_exchange_type, type);
+    Py_XSETREF(g_exchange_capsule, capsule);
+    return g_exchange = api;
+}
+bool described(PyObject *o, Described *d)
+{
+    const DLPackExchangeAPI *api = exchange_of(o);
+    DLTensor t;
+    if (!api) return false;
+    if (api->dltensor_from_py_object_no_sync(o, &t) != 0) {
+        PyErr_Clear(); // (what has no such form is asked by its methods)
+        return false;
+    }
+    d->address = (uint64_t)(uintptr_t)t.data + t.byte_offset;
+    d->fp32 = t.dtype.code == kDLFloat && t.dtype.bits == 32 && t.dtype.lanes == 1;
+    d->entries = 1;
+    d->dense = true;
+    for (int i = t.ndim - 1; i >= 0; --i) {
+        if (t.shape[i] != 1 && t.strides && t.strides[i] != d->entries) d->dense = false;
+        d->entries *= t.shape[i];
+    }
+    return true;
+}
+#else
+bool described(PyObject *, Described *) { return false; }
+#endif
 
 // Arguments of one call.  The first failure leaves a Python exception set and every later step a no-op.
 struct Args {
@@ -72,11 +132,64 @@ struct Args {
         if (v == -1.0 && PyErr_Occurred()) fail();
         return (float)v;
     }
-    // a device buffer: an object with a data_ptr(), an address, or None (NULL)
-    template <typename T = void> T *buffer()
+    void refuse(const char *what, const char *why)
+    {
+        if (PyObject *e = PyObject_CallFunction(g_error, "iN", (int)TT_EINVAL, PyUnicode_FromFormat("%s: %s", what, why))) {
+            PyErr_SetObject(g_error, e);
+            Py_DECREF(e);
+        }
+        fail();
+    }
+    // A per-token array of `count` entries: a dense tensor, an address (anything without a dtype is taken for one), or None (NULL).
+    // These are the tensors that come out of slicing: a strided one, one of another type or a short one would be read as if it
+    // were not.
+    template <typename T = void> T *array(const char *what, int64_t count)
     {
         PyObject *o = next();
-        return !o || o == Py_None ? nullptr : reinterpret_cast<T *>((uintptr_t)pointer_of(o));
+        if (!o || o == Py_None) return nullptr;
+        Described d{0, count, true, true};
+        if (!described(o, &d)) {
+            d.address = pointer_of(o);
+            if (ok && !PyLong_CheckExact(o)) ask(o, &d);
+        }
+        if (ok && count > 0) {
+            if (std::is_same<typename std::remove_const<T>::type, float>::value && !d.fp32) refuse(what, "fp32 values are expected");
+            else if (d.entries < count) refuse(what, "fewer entries than tokens");
+            else if (!d.dense) refuse(what, "a dense tensor is expected");
+        }
+        return reinterpret_cast<T *>((uintptr_t)d.address);
+    }
+    // by an object's methods; left as it is without a dtype
+    void ask(PyObject *o, Described *d)
+    {
+        PyObject *type = PyObject_GetAttr(o, g_dtype_name);
+        if (!type) {
+            if (PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Clear();
+            else fail();
+            return;
+        }
+        d->fp32 = type == g_float32 || is_float32(type);
+        Py_DECREF(type);
+        if (ok) d->entries = (int64_t)method(o, g_numel);
+        if (ok) d->dense = truth(o, g_is_contiguous);
+    }
+    bool is_float32(PyObject *type)
+    {
+        if (!g_float32) {
+            PyObject *torch = PyImport_ImportModule("torch");
+            g_float32 = torch ? PyObject_GetAttrString(torch, "float32") : nullptr;
+            Py_XDECREF(torch);
+            if (!g_float32) return fail();
+        }
+        return type == g_float32;
+    }
+    bool truth(PyObject *o, PyObject *name)
+    {
+        PyObject *x = PyObject_CallMethodNoArgs(o, name);
+        const int v = x ? PyObject_IsTrue(x) : -1;
+        Py_XDECREF(x);
+        if (v < 0) fail();
+        return v > 0;
     }
     // bytes of a ctypes object, valid until the call is over
     const void *bytes_of(PyObject *o, Py_ssize_t least)
@@ -320,7 +433,7 @@ PyObject *embed_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
     const int k = g.i32(), dt = g.dtype();
     const tt_tiling tW = g.tiling(), tX = g.tiling();
     const int idt = g.i32();
-    const void *ids = g.buffer();
+    const void *ids = g.array<const void>("ids", tokens);
     const float scale = g.real();
     void *w[kMaxShards], *x[kMaxShards];
     void **W = g.shards(w), **X = g.shards(x);
@@ -337,7 +450,7 @@ PyObject *embed_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     const int k = g.i32(), dt = g.dtype();
     const tt_tiling tX = g.tiling(), tW = g.tiling();
     const int idt = g.i32();
-    const void *ids = g.buffer();
+    const void *ids = g.array<const void>("ids", tokens);
     const float scale = g.real();
     void *dx[kMaxShards], *dw[kMaxShards];
     void **dX = g.shards(dx), **dW = g.shards(dw);
@@ -360,9 +473,10 @@ PyObject *policy_loss(PyObject *, PyObject *const *args, Py_ssize_t n)
     void *x[kMaxShards], *dx[kMaxShards];
     void **X = g.shards(x);
     const int idt = g.i32();
-    const void *actions = g.buffer();
-    const float *old_logp = g.buffer<float>(), *ref_logp = g.buffer<float>(), *advantage = g.buffer<float>(), *weight = g.buffer<float>();
-    float *loss = g.buffer<float>(), *logp = g.buffer<float>();
+    const void *actions = g.array<const void>("actions", tokens);
+    const float *old_logp = g.array<const float>("old_logp", tokens), *ref_logp = g.array<const float>("ref_logp", tokens);
+    const float *advantage = g.array<const float>("advantage", tokens), *weight = g.array<const float>("weight", tokens);
+    float *loss = g.array<float>("loss", 1), *logp = g.array<float>("logp", tokens);
     void **dX = g.shards(dx);
     size_t bytes;
     void *ws = g.workspace(&bytes), *stream = g.stream();
@@ -383,8 +497,8 @@ PyObject *token_logp(PyObject *, PyObject *const *args, Py_ssize_t n)
     void *x[kMaxShards];
     void **X = g.shards(x);
     const int idt = g.i32();
-    const void *ids = g.buffer();
-    float *logp = g.buffer<float>();
+    const void *ids = g.array<const void>("ids", tokens);
+    float *logp = g.array<float>("logp", tokens);
     size_t bytes;
     void *ws = g.workspace(&bytes), *stream = g.stream();
     return finish(g, [&] { return fn(tokens, vocab, k, dt, tX, scale, in(X), idt, ids, logp, ws, bytes, stream); });
@@ -430,15 +544,15 @@ PyObject *backward_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
-// converters(tiling, forms, dtype): what the binding uses for arguments that are no plain strings
+// converters(tiling, forms, dtype, error): what the binding uses for arguments that are no plain strings, and its exception
 PyObject *converters(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 3) {
-        PyErr_SetString(PyExc_TypeError, "3 arguments expected");
+    if (n != 4) {
+        PyErr_SetString(PyExc_TypeError, "4 arguments expected");
         return nullptr;
     }
-    PyObject **const to[3] = {&g_tiling, &g_forms, &g_dtype};
-    for (int i = 0; i < 3; ++i) {
+    PyObject **const to[4] = {&g_tiling, &g_forms, &g_dtype, &g_error};
+    for (int i = 0; i < 4; ++i) {
         Py_INCREF(args[i]);
         Py_XSETREF(*to[i], args[i]);
     }
@@ -465,6 +579,11 @@ PyMODINIT_FUNC PyInit__calls()
     g_numel = PyUnicode_InternFromString("numel");
     g_element_size = PyUnicode_InternFromString("element_size");
     g_value = PyUnicode_InternFromString("value");
-    if (!g_data_ptr || !g_numel || !g_element_size || !g_value) return nullptr;
+    g_dtype_name = PyUnicode_InternFromString("dtype");
+    g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    if (!g_data_ptr || !g_numel || !g_element_size || !g_value || !g_dtype_name || !g_is_contiguous) return nullptr;
+#ifdef TT_DLPACK_EXCHANGE
+    if (!(g_exchange_name = PyUnicode_InternFromString("__dlpack_c_exchange_api__"))) return nullptr;
+#endif
     return PyModule_Create(&g_module);
 }

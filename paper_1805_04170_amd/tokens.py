@@ -2,8 +2,10 @@
 activations in 8 bits between its passes.  Argument marshalling only, as in binding.py; the calls go through the extension
 module _calls.
 
-Per-token arrays (token numbers, log probabilities, weights) are torch tensors or integer device addresses; the type of token
-numbers is taken from the tensor (torch.int32, torch.int64) or given as id_dtype ("i32", "i64").
+Per-token arrays (token numbers, log probabilities, weights) are dense torch tensors with an entry for every token at least, or
+integer device addresses; the type of token numbers is taken from the tensor (torch.int32, torch.int64) or given as id_dtype ("i32",
+"i64"), all others are torch.float32.  A tensor of another type, a strided one (tokens[:, -1] without .contiguous()) or a short
+one is refused (TT_EINVAL).
 """
 import ctypes
 
@@ -43,12 +45,14 @@ _id_types = {}
 
 def _id_dtype(ids, given):
     if given is not None:
-        return {"i32": TT_I32, "i64": TT_I64}.get(given, given)
+        given = {"i32": TT_I32, "i64": TT_I64}.get(given, given)
+        if not hasattr(ids, "dtype"):       # (an address, or None)
+            return given
     if not _id_types:
         import torch
         _id_types.update({torch.int32: TT_I32, torch.int64: TT_I64})
     t = _id_types.get(getattr(ids, "dtype", None))
-    if t is None:
+    if t is None or given not in (None, t):
         raise TilingError(1, "token numbers of type %s" % (getattr(ids, "dtype", None),))
     return t
 

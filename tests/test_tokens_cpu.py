@@ -40,6 +40,18 @@ class Bytes:
         return 1
 
 
+class Asked:
+    """an object that has a tensor's methods and is none"""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        if name not in ("data_ptr", "dtype", "numel", "is_contiguous"):
+            raise AttributeError(name)
+        return getattr(self.t, name)
+
+
 def test_every_declared_symbol_is_exported_and_bound():
     header = open(os.path.join(ROOT, "include", "tensor_tiling_tokens.h")).read()
     header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
@@ -144,6 +156,47 @@ def test_packed_backward_refusals():
     for ws in (None, Bytes(need - 1), Bytes(need, A + 16)):
         refused("TT_EWORKSPACE", f, ws=ws)
     assert need > tt.tt_fc_packed_workspace_bytes(tt.layer("fc", "none", 32, 32), 8, 0, "bf16", "", "", "", "", "")
+
+
+def test_per_token_arrays_are_dense_and_long_enough():
+    """what slicing leaves is refused before anything is launched: strides, other types, fewer entries than tokens"""
+    T, V, D = 8, 16, 8
+    i64, f32 = torch.zeros(T, dtype=torch.int64), torch.zeros(T)
+    grid, wide = torch.zeros((T, 4), dtype=torch.int64), torch.zeros((T, 4))
+    # a workspace of no bytes: calls whose arrays are accepted end at it, nothing is launched
+    none = Bytes(0)
+    fwd = lambda ids, idt=None: tt.tt_embed_forward(T, V, 0, 0, "f32", "", "", ids, 1.0, P, P, stream=1, id_dtype=idt)  # noqa: E731
+    bwd = lambda ids, idt=None: tt.tt_embed_backward(T, V, 0, 0, "f32", "", "", ids, 1.0, P, P, none, stream=1, id_dtype=idt)  # noqa: E731
+    logp = lambda ids, out=f32, idt=None: tt.tt_token_logp(T, V, 0, "f32", "", 1.0, P, ids, out, none, stream=1, id_dtype=idt)  # noqa: E731
+
+    def loss(actions=i64, old=f32, ref=f32, adv=f32, w=f32, value=torch.zeros(1), lp=f32, idt=None):
+        tt.tt_policy_loss(tt.policy(kl=0.1), T, V, 0, "f32", "", "", P, actions, old, ref, adv, w, value, lp, P, none, stream=1, id_dtype=idt)
+    for fn in (fwd, bwd):
+        for ok in (i64, i64.int(), torch.zeros(T + 3, dtype=torch.int64), grid[:2], grid[0].expand(1, 4).repeat(2, 1)):
+            fn(ok)                          # (no columns: TT_OK, nothing is launched)
+        fn(i64, "i64")
+        fn(A, "i32")
+    plain = Asked(f32)
+    refused("TT_EWORKSPACE", loss, old=plain, adv=torch.nn.Parameter(f32.clone()), w=f32.clone().requires_grad_())
+    for bad in (wide[:, 1], f32.double(), f32[:T - 1]):
+        refused("TT_EINVAL", loss, old=Asked(bad))
+        refused("TT_EINVAL", loss, old=torch.nn.Parameter(bad))
+    for ok in (dict(), dict(actions=i64.int()), dict(ref=None), dict(old=torch.zeros(T + 1)), dict(lp=None), dict(old=A, adv=A)):
+        refused("TT_EWORKSPACE" if ok.get("ref", 0) is not None else "TT_EINVAL", loss, **ok)
+    refused("TT_EWORKSPACE", logp, i64)
+    for bad in (grid[:, -1], grid.int()[:, 0], i64[::2], i64[:T - 1], torch.zeros(1, dtype=torch.int64).expand(T), i64.short(), f32):
+        for fn in (fwd, bwd, logp, loss):
+            refused("TT_EINVAL", fn, bad)
+    for fn in (fwd, bwd, logp):
+        refused("TT_EINVAL", fn, i64.int(), idt="i64")
+        refused("TT_EINVAL", fn, i64, idt="i32")
+    for name in ("old", "ref", "adv", "w", "lp"):
+        for bad in (wide[:, 1], f32.double(), f32.bfloat16(), f32[:T - 1], f32[:1].expand(T), f32.int()):
+            refused("TT_EINVAL", loss, **{name: bad})
+    for bad in (wide[:, 1], f32.double(), f32[1:]):
+        refused("TT_EINVAL", logp, i64, bad)
+    for bad in (torch.zeros(0), torch.zeros(1).double()):
+        refused("TT_EINVAL", loss, value=bad)
 
 
 def test_tensors_without_values_have_no_buffers():
