@@ -21,7 +21,7 @@ constexpr int kU = 2;     // vectors per lane of a wave's part of a segment
 constexpr int kRunBatch = 8, kRowBatch = 4, kPartials = 8; // rows, or partial sums, that are on their way together
 
 // How the segments of a row are shared out.  Wide form: a part of kU vectors per lane to a wave, so that a wave's row, segment and
-// addresses are scalars.  Narrow form: a vector per lane, a segment to 2^glog lanes.  The wide form is the faster one even where it
+// addresses are scalars.  Narrow form: a vector per lane, a segment to 2^glog lanes (one, but for few tokens).  The wide form is the faster one even where it
 // leaves most lanes idle (gradient of a 50000-row table from 8192 tokens, wide / narrow, us: width 8 25 / 35, 64 26 / 35, 192 27 / 42;
 // forward alike), so the narrow one is for segments of less than a vector, and for few tokens, where a wave has nothing to look up and
 // many narrow rows are one store (64 tokens, wide / narrow: width 8 15 / 11, 64 15 / 9, 192 16 / 11).
@@ -69,6 +69,12 @@ __device__ __forceinline__ LaneWork lane_work(const Split &w)
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x, g = i >> w.glog, row = quotient(g, w.by_nseg);
     return {row, g - row * w.s.nseg, i & ((1u << w.glog) - 1)};
 }
+// ... where a segment is less than a vector: all of it
+__device__ __forceinline__ LaneWork small_work(const Split &w)
+{
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = quotient(i, w.by_nseg);
+    return {row, i - row * w.s.nseg, 0};
+}
 
 // A wave's vectors of a segment, one per lane and u.  Every lane loads whole vectors, so that no load depends on a lane: a
 // segment's last vector, where it is short, is the values that end with the segment (those in front of its own are its
@@ -105,7 +111,30 @@ template <typename T> struct Columns {
     }
 };
 
-// The same for the narrow form's one vector; segments of less than a vector (`tiny`) are loaded value by value.
+// Segments of less than a vector: value by value.
+template <typename T> struct Small {
+    uint32_t n;
+    __device__ __forceinline__ explicit Small(const Pieces &s) : n(s.seg) {}
+    __device__ __forceinline__ u32x4 load(const T *segment) const { return load_part(segment, n); }
+    __device__ __forceinline__ void store(const BlockTable &b, const Place &to, u32x4 v) const
+    {
+        for (uint32_t x = 0; x < b.nrep; ++x) store_part(static_cast<T *>(b.p[to.block + x]) + to.at, v, n);
+    }
+    // fp32 values of the same columns
+    __device__ __forceinline__ void load_floats(float (&f)[kVec<T>], const float *segment) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) f[i] = (uint32_t)i < n ? load1(segment + i) : 0.0f;
+    }
+    __device__ __forceinline__ void store_floats(const float (&f)[kVec<T>], float *segment) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i)
+            if ((uint32_t)i < n) store1(segment + i, f[i]);
+    }
+};
+
+// One vector of any segment (few tokens)
 template <typename T> struct Column1 {
     uint32_t col, own;
     bool tiny;
@@ -130,25 +159,6 @@ template <typename T> struct Column1 {
                     else store1(dst + i, __uint_as_float(v[i]));
                 }
             }
-        }
-    }
-    // fp32 values of the same columns (a short vector's neighbours hold what it has of theirs)
-    __device__ __forceinline__ void load_floats(float (&f)[kVec<T>], const float *segment) const
-    {
-#pragma unroll
-        for (int i = 0; i < kVec<T>; i += 4) {
-            const u32x4 v = tiny ? load_part(segment + i, own > (uint32_t)i ? own - i < 4 ? own - i : 4 : 0) : load16(segment + col + i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) f[i + k] = __uint_as_float(v[k]);
-        }
-    }
-    __device__ __forceinline__ void store_floats(const float (&f)[kVec<T>], float *segment) const
-    {
-#pragma unroll
-        for (int i = 0; i < kVec<T>; i += 4) {
-            const u32x4 v = u32x4{__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])};
-            if (tiny) store_part(segment + i, v, own > (uint32_t)i ? own - i < 4 ? own - i : 4 : 0);
-            else store16(segment + col + i, v);
         }
     }
 };
@@ -197,9 +207,9 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
 
 template <typename T, typename I> __global__ __launch_bounds__(kThreads) void embed_narrow_kernel(const EmbedParams p)
 {
-    const LaneWork g = lane_work(p.w);
-    const Column1<T> c(p.w.s, g.j);
-    if (g.row >= p.tokens || c.own == 0) return;
+    const LaneWork g = small_work(p.w);
+    const Small<T> c(p.w.s);
+    if (g.row >= p.tokens) return;
     const int64_t v = token_at<I>(p.ids, g.row);
     u32x4 r = u32x4{0, 0, 0, 0};
     if (v >= 0 && v < p.vocab) r = scaled<T>(c.load(source_of<T>(p.W, p.w.s, p.w.s.a_shift, (uint32_t)v, g.q)), p.scale);
@@ -577,7 +587,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_wid
 
 // the rows of places [b, e) of the sorted list, a vector of each, kRunBatch of them on their way together
 template <typename T>
-__device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Column1<T> &c, uint32_t b, uint32_t e)
+__device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Small<T> &c, uint32_t b, uint32_t e)
 {
     for (uint32_t i = b; i < e; i += kRunBatch) {
         uint32_t t[kRunBatch];
@@ -595,8 +605,8 @@ __device__ __forceinline__ void add_vectors(float (&s)[kVec<T>], const EmbedGrad
         }
     }
 }
-template <typename T>
-__device__ __forceinline__ void finish_vector(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const Column1<T> &c, uint32_t v, float scale)
+template <typename T, class C>
+__device__ __forceinline__ void finish_vector(float (&s)[kVec<T>], const EmbedGradParams &p, const LaneWork &g, const C &c, uint32_t v, float scale)
 {
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) s[i] *= scale;
@@ -605,9 +615,8 @@ __device__ __forceinline__ void finish_vector(float (&s)[kVec<T>], const EmbedGr
 
 template <typename T> __global__ __launch_bounds__(kThreads) void embed_sums_narrow_kernel(const EmbedGradParams p)
 {
-    const LaneWork g = lane_work(p.w);
-    const Column1<T> c(p.w.s, g.j);
-    if (c.own == 0) return;
+    const LaneWork g = small_work(p.w);
+    const Small<T> c(p.w.s);
     if (g.row < p.runs) {
         const Run r = run_of(p, g.row);
         if (!r.any) return;
@@ -627,14 +636,14 @@ template <typename T> __global__ __launch_bounds__(kThreads) void embed_sums_nar
     if (e - b > p.chunk) return; // (runs)
     float s[kVec<T>] = {};
     add_vectors<T>(s, p, g, c, b, e);
-    finish_vector(s, p, g, c, v, b < e ? p.scale : 0.0f);
+    finish_vector<T>(s, p, g, c, v, b < e ? p.scale : 0.0f);
 }
 
 template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_narrow_kernel(const EmbedGradParams p)
 {
-    const LaneWork g = lane_work(p.w);
-    const Column1<T> c(p.w.s, g.j);
-    if (g.row >= p.runs || c.own == 0) return;
+    const LaneWork g = small_work(p.w);
+    const Small<T> c(p.w.s);
+    if (g.row >= p.runs) return;
     const Long w = long_of(p, g.row);
     if (!w.any) return;
     const bool inside = w.b > g.row * p.chunk;
@@ -648,7 +657,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void embed_join_nar
 #pragma unroll
             for (int i = 0; i < kVec<T>; ++i) s[i] = run + k <= w.last ? s[i] + f[k][i] : s[i];
     }
-    finish_vector(s, p, g, c, w.v, p.scale);
+    finish_vector<T>(s, p, g, c, w.v, p.scale);
 }
 
 // Few tokens: nothing to sort.  Every wave holds all token numbers, 64 to a register, and asks for each of its rows which of them
@@ -768,7 +777,7 @@ template <typename T, typename I> __global__ __launch_bounds__(kThreads) void em
             for (int q = 0; q < kVec<T>; ++q) s[q] += x[q];
         }
     }
-    if (g.row < (uint32_t)p.vocab) finish_vector(s, p, g, c, g.row, scale);
+    if (g.row < (uint32_t)p.vocab) finish_vector<T>(s, p, g, c, g.row, scale);
 }
 
 // ----------------------------------------------------------------------------------------------------- host side
