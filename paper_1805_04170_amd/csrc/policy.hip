@@ -163,15 +163,15 @@ __device__ __forceinline__ void store_scalars(const PolicyParams &p, uint32_t t,
     if (p.row_loss) p.row_loss[t] = r.loss;
 }
 
-// statistics with N more vectors (vectors of -inf add nothing); FUSED: by Powers
-template <typename T, int N, bool FUSED = (N > 1)> __device__ __forceinline__ Stats with_vectors(Stats s, const u32x4 *r, float kk)
+// statistics with N more vectors (vectors of -inf add nothing)
+template <typename T, int N> __device__ __forceinline__ Stats with_vectors(Stats s, const u32x4 *r, float kk)
 {
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < N; ++i) m = max_of<T>(r[i], m);
     const float top = fmaxf(s.top, m), from = top == -INFINITY ? 0.0f : top;
     float sum = s.top == -INFINITY ? s.sum : s.sum * power_of(s.top, from, kk);
-    if constexpr (FUSED && sizeof(T) == 2) {
+    if constexpr (N > 1 && sizeof(T) == 2) { // (for one vector what Powers saves is less than what it takes)
         const Powers<T> e(kk, from);
         float more = 0.0f;
 #pragma unroll
@@ -356,7 +356,9 @@ template <typename T> struct RowMap {
 // groups-th row: as a vector's gradient leaves, the next row's vector is fetched into its registers, so that memory always
 // has work while the workgroup computes.  A row's result (a few hundred instructions, logarithms and exponentials to their last
 // bits) is one wave's work.
-constexpr int kTogether = 4; // vectors that are taken into the statistics at a time
+// Vectors that are taken into the statistics at a time: 4, or 2 beside 20 waiting ones, where 4 would leave 32 registers in memory
+// (2048 x 151936 bf16: 267 us, so 259)
+constexpr int together_of(int nc) { return nc > 16 ? 2 : nc < 4 ? nc : 4; }
 template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__(WAVES * 64) void policy_rows_kernel(const PolicyParams p)
 {
     __shared__ Stats red[WAVES];
@@ -418,12 +420,12 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
                 s = with_vectors<T, 1>(s, &rest, kk);
             }
 #pragma unroll
-            for (int i = 0; i < NC; i += kTogether) {
-                constexpr int most = NC < kTogether ? NC : kTogether;
+            for (int i = 0; i < NC; i += together_of(NC)) {
+                constexpr int most = together_of(NC);
 #pragma unroll
                 for (int k = i; k < i + most; ++k)
                     if (k * WAVES + w >= p.units) r[k] = nothing;
-                s = with_vectors<T, most, (most > 1 && NC <= 16)>(s, r + i, kk); // (more vectors leave no registers for it: 2048 x 151936 278 us, so 268)
+                s = with_vectors<T, most>(s, r + i, kk);
                 if constexpr (!GRAD) { // nobody needs them again
                     if (next_in && p.units) {
 #pragma unroll

@@ -42,3 +42,20 @@ def test_kernels_with_loads_in_flight_keep_their_values_in_registers(tmp_path):
                 seen.setdefault(kernel.group(1), []).append((name, int(spilled)))
     assert len(seen) == 9
     assert not [k for ks in seen.values() for k in ks if k[1]]
+
+
+@pytest.mark.skipif(READELF is None or not os.path.exists(binding.LIB_PATH), reason="no llvm-readelf, or the library is not built")
+def test_token_operators_keep_their_values_in_registers(tmp_path):
+    """a row of logits waits in registers while its statistics are joined, and the next row's vectors are on their way"""
+    seen = {}
+    for i, obj in enumerate(code_objects()):
+        path = os.path.join(str(tmp_path), "%d.o" % i)
+        with open(path, "wb") as f:
+            f.write(obj)
+        notes = subprocess.run([READELF, "--notes", path], capture_output=True, text=True, check=True).stdout
+        for name, spilled in re.findall(r"\.symbol:\s+(\S+)\.kd.*?\.vgpr_spill_count:\s+(\d+)", notes, re.S):
+            kernel = re.search(r"(policy_(?:rows|stream|part_stats|part_result)|sum_losses|embed_(?:few_|sums_|join_)?(?:wide|narrow)|sort_tokens|pack8|unpack8|unpack_gate(?:_flat)?)_kernel", name)
+            if kernel:
+                seen.setdefault(kernel.group(1), []).append((name, int(spilled)))
+    assert len(seen) == 5 + 8 + 1 + 4
+    assert not [k for ks in seen.values() for k in ks if k[1]]
