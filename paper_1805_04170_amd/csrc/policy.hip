@@ -3,7 +3,7 @@
 // A row of logits gives one number, log p[a] = z_a - log sum exp z, and with its derivative g of the loss the row's gradient
 // g (onehot(a) - p): two sums over the row and a pass that writes as much as was read.  Memory bounds it (8 flops and two
 // exponentials a value), so the logits are to come from memory once: 4096 x 131072 bf16 logits, 1.075 GB read and 1.074 written in
-// 415 us, 5.2 TB/s.  Log probabilities alone: 4096 x 131072 179 us, 6.0 TB/s; 16 x 131072 8.3 us on the GPU, trips to memory.
+// 417 us, 5.1 TB/s.  Log probabilities alone: 4096 x 131072 177 us, 6.1 TB/s; 16 x 131072 8.2 us on the GPU, trips to memory.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -512,7 +512,7 @@ template <typename T, int WAVES, int NC, bool GRAD> __global__ __launch_bounds__
 }
 
 // Rows that do not fit: one workgroup per row, which reads it for its statistics and again for its gradient (from the caches,
-// where they hold it).  2048 x 200000 bf16: 380 us, 4.3 TB/s of what has to move.
+// where they hold it).  1024 x 200000 bf16: 196 us, 4.2 TB/s of what has to move; 1000 x 100000 fp32: 193, 4.1.
 constexpr int kStreamWaves = 16;
 template <typename T> __global__ __launch_bounds__(kStreamWaves * 64) void policy_stream_kernel(const PolicyParams p)
 {
