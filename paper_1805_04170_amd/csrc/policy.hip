@@ -49,19 +49,26 @@ __device__ __forceinline__ int64_t action_of(const PolicyParams &p, uint32_t t)
 // whether a token counts as far as its weight and action go
 __device__ __forceinline__ bool counts(const PolicyParams &p, uint32_t t, int64_t a) { return a >= 0 && a < p.vocab && !(p.weight && load_scalar(p.weight + t) == 0.0f); }
 
+// power_of with what rounding the product leaves out put right, where statistics are joined: bf16 logits lie at few distances from
+// each other, so that the same roundings would come in every row.
+__device__ __forceinline__ float join_power(float x, float top, float kk)
+{
+    const float d = x - top, e = d * kk;
+    return e > -150.0f ? wave::exp2_fast(e) * fmaf(fmaf(d, kk, -e), 0.693147181f, 1.0f) : 0.0f;
+}
 // log2(e) times the logits' factor (finite, so that it is no power at all for the maximum)
 __device__ __forceinline__ float exponent_factor(const PolicyParams &p) { return fminf(p.policy.scale * kLog2e, 3.402823466e38f); }
 
 __device__ __forceinline__ Stats joined(Stats a, Stats b, float kk)
 {
     const float top = fmaxf(a.top, b.top);
-    const float fa = a.top == -INFINITY ? 1.0f : power_of(a.top, top, kk), fb = b.top == -INFINITY ? 1.0f : power_of(b.top, top, kk);
+    const float fa = a.top == -INFINITY ? 1.0f : join_power(a.top, top, kk), fb = b.top == -INFINITY ? 1.0f : join_power(b.top, top, kk);
     return {top, a.sum * fa + b.sum * fb};
 }
 __device__ __forceinline__ Stats wave_joined(Stats s, float kk)
 {
     const float top = wave_max(s.top);
-    return {top, wave_sum(s.top == -INFINITY ? s.sum : s.sum * power_of(s.top, top, kk))};
+    return {top, wave_sum(s.top == -INFINITY ? s.sum : s.sum * join_power(s.top, top, kk))};
 }
 // over a workgroup's waves, in every thread; `red`: a Stats per wave
 template <int WAVES> __device__ __forceinline__ Stats group_joined(Stats s, Stats *red, float kk)

@@ -581,6 +581,23 @@ def test_log_probabilities_are_off_to_both_sides(dt, V):
         assert abs(np.mean(off)) < EPS / 2 + 4 * np.std(off) / math.sqrt(T), np.mean(off)
 
 
+@pytest.mark.parametrize("dt,V", [("bf16", 8000), ("bf16", 60000), ("f32", 8000)])
+def test_what_rounding_leaves_out_of_joined_sums_is_not_the_same_in_every_row(dt, V):
+    """bf16's largest logits lie at a few distances from each other, whose products with the factor are rounded alike in all rows.  Of
+    16384 rows' mean error an eighth of a step of fp32 is left for what is common to them, and four times what single roundings leave."""
+    T, kind = 16384, torch.bfloat16 if dt == "bf16" else torch.float32
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.empty((T, V), dtype=kind, device=DEV).normal_(0, 2.5, generator=gen)
+    a = torch.randint(0, V, (T,), generator=gen, device=DEV)
+    x[torch.arange(T, device=DEV), a] = torch.empty(T, dtype=kind, device=DEV).normal_(8, 2.5, generator=gen)
+    want = torch.cat([(z.gather(1, i[:, None])[:, 0] - torch.logsumexp(z, 1)) for z, i in ((x[t:t + 1024].double(), a[t:t + 1024]) for t in range(0, T, 1024))])
+    logp, ws = empty((T,), torch.float32), workspace(tt.tt_policy_workspace_bytes(T, V, 0, dt, "", ""))
+    one, loss, dX = torch.ones(T, device=DEV), empty((1,), torch.float32), [torch.empty_like(x)]
+    tt.tt_policy_loss(tt.policy(), T, V, 0, dt, "", "", [x], a, want.float(), None, one, one, loss, logp, dX, ws)
+    off = (logp.double() - want).cpu().numpy()
+    assert abs(np.mean(off)) < EPS / 8 + 4 * np.std(off) / math.sqrt(T), np.mean(off)
+
+
 def test_policy_loss_of_no_tokens_is_zero():
     loss = empty((1,), torch.float32)
     none = empty((1,), torch.float32)
