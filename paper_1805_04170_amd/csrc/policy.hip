@@ -3,7 +3,7 @@
 // A row of logits gives one number, log p[a] = z_a - log sum exp z, and with its derivative g of the loss the row's gradient
 // g (onehot(a) - p): two sums over the row and a pass that writes as much as was read.  Memory bounds it (8 flops and two
 // exponentials a value), so the logits are to come from memory once: 4096 x 131072 bf16 logits, 1.075 GB read and 1.074 written in
-// 417 us, 5.1 TB/s.  Log probabilities alone: 4096 x 131072 177 us, 6.1 TB/s; 16 x 131072 8.2 us on the GPU, trips to memory.
+// 418 us, 5.1 TB/s.  Log probabilities alone: 4096 x 131072 177 us, 6.1 TB/s; 16 x 131072 8.2 us on the GPU, trips to memory.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
