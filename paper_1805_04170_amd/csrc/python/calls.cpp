@@ -474,7 +474,8 @@ PyObject *policy_loss(PyObject *, PyObject *const *args, Py_ssize_t n)
     void **X = g.shards(x);
     const int idt = g.i32();
     const void *actions = g.array<const void>("actions", tokens);
-    const float *old_logp = g.array<const float>("old_logp", tokens), *ref_logp = g.array<const float>("ref_logp", tokens);
+    const float *old_logp = g.array<const float>("old_logp", tokens);
+    const float *ref_logp = g.array<const float>("ref_logp", policy && policy->kl != 0.0f ? tokens : 0); // (not read otherwise)
     const float *advantage = g.array<const float>("advantage", tokens), *weight = g.array<const float>("weight", tokens);
     float *loss = g.array<float>("loss", 1), *logp = g.array<float>("logp", tokens);
     void **dX = g.shards(dx);

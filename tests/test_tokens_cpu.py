@@ -199,6 +199,12 @@ def test_per_token_arrays_are_dense_and_long_enough():
         refused("TT_EINVAL", loss, value=bad)
 
 
+def test_an_array_that_is_not_read_may_be_anything():
+    i64, f32 = torch.zeros(8, dtype=torch.int64), torch.zeros(8)
+    for ref in (None, f32.bfloat16(), f32[:3], torch.zeros((8, 2))[:, 0]):
+        refused("TT_EWORKSPACE", tt.tt_policy_loss, tt.policy(), 8, 16, 0, "f32", "", "", P, i64, f32, ref, f32, f32, torch.zeros(1), f32, P, Bytes(0), stream=1)
+
+
 def test_tensors_without_values_have_no_buffers():
     """torch's empty tensors have a NULL address; nothing is launched for them"""
     none = lambda r, c, dt=torch.float32: [torch.empty((r, c), dtype=dt)]  # noqa: E731
