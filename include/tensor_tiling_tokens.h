@@ -7,11 +7,11 @@
  * device buffer whatever the tilings are: they are as small as a row of pointers.  Token numbers are TT_I32 or TT_I64.
  * Shards, and buffers that a call writes, must not overlap any other buffer given to it.
  *
- * Calls with no tokens, rows or columns return TT_OK and write nothing, but for tt_policy_loss's loss (0), a table
- * gradient without tokens (zeros), and log probabilities of an empty vocabulary (0); shards of a tensor without values may be
- * NULL.  (tt_fc_backward_packed takes a batch of 1 and more, as tt_fc_backward does.)  Errors as in tensor_tiling.h: TT_EINVAL (NULL, unknown type or letter, k out of
- * range, negative or misaligned), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 tokens, rows, columns or
- * vocabulary entries and more; 2^30 numbers of an embedding; 2^22 tokens of a loss), TT_EWORKSPACE, TT_EDEVICE. */
+ * Calls with no tokens, rows or columns return TT_OK and write nothing, but for tt_policy_loss's loss (0), a table gradient
+ * without tokens (zeros), and log probabilities of an empty vocabulary (0); shards of a tensor without values may be NULL.
+ * (tt_fc_backward_packed takes a batch of 1 and more, as tt_fc_backward does.)  Errors as in tensor_tiling.h: TT_EINVAL (NULL,
+ * unknown type or letter, k out of range, negative or misaligned), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 tokens, rows,
+ * columns or vocabulary entries and more; 2^30 numbers of an embedding; 2^22 tokens of a loss), TT_EWORKSPACE, TT_EDEVICE. */
 #ifndef TENSOR_TILING_TOKENS_H
 #define TENSOR_TILING_TOKENS_H
 
@@ -82,10 +82,11 @@ tt_status tt_token_logp(int64_t tokens, int64_t vocab, int k, int dtype, tt_tili
 /* ------------------------------------------------ activations kept in 8 bits
  * The 8-bit form of a rows x cols tensor under a tiling: per shard Q (int8, the shard's shape) and S (uint8, one per block
  * of 32 columns of a row, blocks counted from the shard's first column, the last one short: srows x ceil(scols / 32)).
- * A value is Q * 2^(S - 127), for any Q and any S but 255.  2^(S - 127) is, as tt_pack8 makes it, the smallest power of two (not below 2^-126) that keeps the block's values
- * within +-127 steps; Q is the value rounded to the nearest step (ties to even), but one step at least where the value
- * is not 0, so that signs, and with them ReLU's gates, stay as they were.  A block with a NaN or an infinity has S = 255
- * and stands for NaN throughout.  A power of two and eight bits are exact in bf16 and in fp32: unpacking rounds nothing. */
+ * A value is Q * 2^(S - 127), for any Q and any S but 255.  2^(S - 127) is, as tt_pack8 makes it, the smallest power of two (not
+ * below 2^-126) that keeps the block's values within +-127 steps; Q is the value rounded to the nearest step (ties to even), but one
+ * step at least where the value is not 0, so that signs, and with them ReLU's gates, stay as they were.  A block with a NaN or
+ * an infinity has S = 255 and stands for NaN throughout.  A power of two and eight bits are exact in bf16 and in fp32: unpacking
+ * rounds nothing. */
 enum { TT_PACK8_BLOCK = 32 };
 tt_status tt_pack8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling t, const void *const *X, int8_t *const *Q,
                    uint8_t *const *S, void *stream);

@@ -21,8 +21,8 @@ constexpr int kU = 2;     // vectors per lane of a wave's part of a segment
 constexpr int kRunBatch = 8, kRowBatch = 4, kPartials = 8; // rows, or partial sums, that are on their way together
 
 // How the segments of a row are shared out.  Wide form: a part of kU vectors per lane to a wave, so that a wave's row, segment and
-// addresses are scalars.  Narrow form: a vector per lane, a segment to 2^glog lanes (one, but for few tokens).  The wide form is the faster one even where it
-// leaves most lanes idle (gradient of a 50000-row table from 8192 tokens, wide / narrow, us: width 8 25 / 35, 64 26 / 35, 192 27 / 42;
+// addresses are scalars.  Narrow form: a vector per lane, a segment to 2^glog lanes (one, but for few tokens).  The wide form is the
+// faster one even where it leaves most lanes idle (gradient of a 50000-row table from 8192 tokens, wide / narrow, us: width 8 25 / 35, 64 26 / 35, 192 27 / 42;
 // forward alike), so the narrow one is for segments of less than a vector, and for few tokens, where a wave has nothing to look up and
 // many narrow rows are one store (64 tokens, wide / narrow: width 8 15 / 11, 64 15 / 9, 192 16 / 11).
 struct Split {

@@ -90,7 +90,7 @@ template <typename T> __device__ __forceinline__ float max_of(u32x4 v, float m)
 // 2^((x - top) kk) for many x: whole() of the sum of of(x).  fp32: power_of.  bf16, where the arithmetic is what a row waits for,
 // a fused step in place of two (difference first throughout: 1000 x 50021 47.4 us, so 46.2): of(x) = 2^(x kk - c) with c the rounded
 // top kk, whole() puts right what the rounding left out, 2^-7 of an exponent at most.  Beyond |top| kk = 2^18 a smaller factor keeps c
-// below it: numbers of 8 bits that are not top are 2^-9 of it apart, 2^8 as an exponent, and have no power then as they had none before.
+// below it: numbers of 8 bits that are not top are 2^-8 of it away at least, 2^9 as an exponent, and have no power, as by kk itself.
 template <typename T> struct Powers {
     float kk, top, c;
     __device__ __forceinline__ Powers(float k, float t) : kk(k), top(t), c(0.0f)
