@@ -1,0 +1,106 @@
+/* tensor_tiling_residual.h - what stands between the layers of a residual block, under the conventions of tensor_tiling.h (shards,
+ * tilings, statuses, streams, workspaces): dropout, the residual's addition with a root-mean-square norm behind it and their
+ * gradients, for training; the norm's output in 8 bits and fully-connected layers in 8-bit integers, for answering.
+ *
+ * Per-token values (scales) and per-column values (gains, their gradients, scales of output channels) are whole arrays, one entry
+ * per token or column, dense and in one device buffer whatever the tilings are.  Shards, and buffers that a call writes, must not
+ * overlap any other buffer given to it.  A result does not depend on the tilings, but for the last bits of dgain.
+ *
+ * Calls with no rows or no columns return TT_OK and write nothing, but for a gain's gradient without rows (zeros) and the scales
+ * of rows without columns (0), and a layer of no inputs (zeros); shards of a tensor without values may be NULL.
+ * Errors as in tensor_tiling.h: TT_EINVAL (NULL, unknown type or letter, k out of range, negative, misaligned, parameters out of
+ * range), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 rows or columns and more; 2^37 values of a dropped tensor; sums of
+ * 131072 products of 8-bit integers), TT_EWORKSPACE, TT_EDEVICE. */
+#ifndef TENSOR_TILING_RESIDUAL_H
+#define TENSOR_TILING_RESIDUAL_H
+
+#include "tensor_tiling.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* tt_kernel_record.kernel of these calls' launches: rows = d0, columns = d1, element bytes = d2 (TT_K_FC8: M, N, K) */
+enum { TT_K_DROPOUT = 17, TT_K_NORM = 18, TT_K_NORM_GRAD = 19, TT_K_ROWS8 = 20, TT_K_FC8 = 21 };
+
+/* ----------------------------------------------------------------- dropout
+ * Which values are dropped is computed wherever it is asked for and stored nowhere.  Columns 8 g .. 8 g + 7 of a row take the
+ * eight 16-bit halves (low half first) of the four words of Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers,
+ * as easy as 1, 2, 3; SC 2011) of the counter (g, row, low word, high word of offset + *step) under the key (low word, high word
+ * of seed).  A value is kept where its half is at least P = round(65536 p), and is multiplied by 65536 / (65536 - P) then: the
+ * probability that is applied is P / 65536, and the expectation is exact for it.  Row and column are those of the whole tensor:
+ * the mask is the same under every tiling, and the same in the forward and the backward pass. */
+typedef struct {
+    float p;              /* probability of a value being dropped: 0 or more, P below 65536 */
+    uint64_t seed, offset;
+    const uint64_t *step; /* one number in device memory, read by the kernels when they run (a captured graph's replays may each
+                             find another one there), or NULL: none.  Calls whose masks are to differ differ in offset + *step
+                             (modulo 2^64) or in seed. */
+} tt_drop;
+
+/* Y = X with dropout, X under tX, Y under tY, replicas written once each;  dtype of both TT_F32 | TT_BF16.  What is dropped is 0
+ * whatever X holds there.  The backward pass is the same call on the gradient. */
+tt_status tt_dropout(const tt_drop *drop, int64_t rows, int64_t cols, int k, int dtype, tt_tiling tX, tt_tiling tY,
+                     const void *const *X, void *const *Y, void *stream);
+
+/* -------------------------------------------------- residual sum and its norm
+ *   H = R + dropout(X), rounded to dtype                    (R NULL: no residual;  drop NULL: no dropout)
+ *   Y = gain * H / sqrt(mean over a row of H^2 + eps)
+ * of the sum as it is kept, so that what the backward pass reads is what the forward pass took.  X, R, H: rows x width under tX;
+ * Y: under tY;  H may be NULL;  gain: dtype, one per column, or NULL (ones);  eps: finite, above 0.  Sums fp32 (64 bits in rows
+ * whose squares fp32 does not hold); a row with a NaN or an infinity is NaN throughout. */
+tt_status tt_norm_forward(int64_t rows, int64_t width, int k, int dtype, tt_tiling tX, tt_tiling tY, float eps, const tt_drop *drop,
+                          const void *const *X, const void *const *R, const void *gain, void *const *H, void *const *Y, void *stream);
+
+/* Gradients of the above: with r = 1 / sqrt(mean H^2 + eps), n = r H and c = mean(gain dY n) of a row,
+ *   dS = r (gain dY - c n) + dH      the sum's gradient, and so R's and, without dropout, X's;  dH: what arrives on the sum itself
+ *                                    from later layers, or NULL
+ *   dX = dropout(dS), of the unrounded dS (drop as in the forward call)
+ *   dgain = sum over rows of dY n    fp32
+ * H, dH, dS, dX: rows x width under tX;  dY: under tdY.  dS, dX and dgain may be NULL each; dX needs drop.  Sums fp32; equal calls
+ * give equal bits.  Workspace: device memory, 256-byte aligned, at least tt_norm_workspace_bytes (may be NULL if 0); nothing in it
+ * needs clearing.  What is enough for so many rows is enough for fewer. */
+tt_status tt_norm_workspace_bytes(int64_t rows, int64_t width, int k, int dtype, tt_tiling tX, tt_tiling tdY, size_t *bytes);
+tt_status tt_norm_backward(int64_t rows, int64_t width, int k, int dtype, tt_tiling tX, tt_tiling tdY, float eps, const tt_drop *drop,
+                           const void *const *H, const void *gain, const void *const *dY, const void *const *dH, void *const *dS,
+                           void *const *dX, float *dgain, void *workspace, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------- rows in 8 bits
+ * The 8-bit form of a rows x cols tensor under a tiling: per shard Q (int8, srows rows that begin every tt_pitch8(scols) bytes,
+ * zeros behind a row's values) and, for the whole tensor, S (fp32, one per row).  A value is Q * S.  With m the largest magnitude of
+ * a row, Q = 127 x / m rounded to the nearest whole number (ties to even), exactly, and S = m / 127 in fp32.  A row of zeros has
+ * S = 0; a row with a NaN or an infinity has Q = 0 and S = NaN. */
+enum { TT_ROW8_BYTES = 128 };
+int64_t tt_pitch8(int64_t cols); /* cols rounded up to TT_ROW8_BYTES;  -1: negative, or 2^31 columns and more */
+tt_status tt_rows8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling tX, tt_tiling tQ, const void *const *X, int8_t *const *Q,
+                   float *S, void *stream);
+/* X = Q * S, one fp32 product rounded to dtype; Q and S may hold any values */
+tt_status tt_unrows8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling tQ, tt_tiling tX, const int8_t *const *Q, const float *S,
+                     void *const *X, void *stream);
+/* tt_norm_forward without dropout, Y in 8 bits: Q is taken from gain * H, exactly as above, and S = m r / 127 with m the largest
+ * magnitude of gain * H in a row and r = 1 / sqrt(mean H^2 + eps). */
+tt_status tt_norm_forward8(int64_t rows, int64_t width, int k, int dtype, tt_tiling tX, tt_tiling tQ, float eps, const void *const *X,
+                           const void *const *R, const void *gain, void *const *H, int8_t *const *Q, float *S, void *stream);
+
+/* ------------------------------------------------ fully-connected layer in 8 bits
+ * A weight W (n_in x n_out under tW) in 8 bits, made once: per shard Q is the shard transposed, a row for each of its output
+ * channels (scols rows that begin every tt_pitch8(srows) bytes, zeros behind a row's values), S (fp32, one per output channel) for
+ * the whole weight; steps and scales as above, a column of W for a row.  Workspace as above. */
+tt_status tt_weights8_workspace_bytes(int64_t n_in, int64_t n_out, int k, tt_tiling tW, size_t *bytes);
+tt_status tt_weights8(int64_t n_in, int64_t n_out, int k, int dtype, tt_tiling tW, const void *const *W, int8_t *const *Q, float *S,
+                      void *workspace, size_t ws_bytes, void *stream);
+
+/* Y[t][n] = act(XS[t] WS[n] sum_i XQ[t][i] WQ[n][i]): tt_fc_forward of what the 8-bit forms stand for.  The sum is exact (layer->n_in
+ * up to 131071); it is converted to fp32, multiplied by WS and then by XS, and rounded to dtype once.  XQ (batch x n_in, a row form)
+ * under tX, WQ (a weight's form) under tW, Y: batch x n_out under tY, dtype;  XQ, WQ shards 16-byte aligned.  Q may hold any values; a
+ * row or a channel of scale NaN gives NaN (ReLU keeps it).  Workspace as above, at least tt_fc8_workspace_bytes; batch may be 0. */
+tt_status tt_fc8_workspace_bytes(const tt_layer *layer, int64_t batch, int k, int dtype, tt_tiling tX, tt_tiling tW, tt_tiling tY,
+                                 size_t *bytes);
+tt_status tt_fc_forward8(const tt_layer *layer, int64_t batch, int k, int dtype, tt_tiling tX, tt_tiling tW, tt_tiling tY,
+                         const int8_t *const *XQ, const float *XS, const int8_t *const *WQ, const float *WS, void *const *Y,
+                         void *workspace, size_t ws_bytes, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* TENSOR_TILING_RESIDUAL_H */

@@ -1,0 +1,93 @@
+// Dropout's generator: Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; SC 2011), a
+// bijection of a 128-bit counter under a 64-bit key, so that a value's place in its tensor is all that its random number needs.
+// Sixteen bits a value: eight neighbouring columns of a row share a counter, which is a 16-byte vector of bf16.
+#pragma once
+#include <cmath>
+#include "tensor_tiling_residual.h"
+#include "tt_wave.h"
+
+namespace tt {
+
+struct DropParams {
+    uint32_t k0, k1;      // the key
+    uint32_t at0, at1;    // offset, low and high
+    const uint64_t *step; // added to it, or NULL
+    uint32_t below;       // halves below this are dropped: 1 to 65535 (0: no dropout)
+    float factor;         // of what is kept
+};
+
+// false: parameters out of range
+inline bool make_drop(const tt_drop *d, DropParams *p)
+{
+    *p = {0, 0, 0, 0, nullptr, 0, 1.0f};
+    if (!d) return true;
+    if (!(d->p >= 0.0f && d->p <= 1.0f) || reinterpret_cast<uintptr_t>(d->step) % 8) return false;
+    p->below = (uint32_t)(d->p * 65536.0f + 0.5f);
+    if (p->below >= 65536) return false;
+    p->k0 = (uint32_t)d->seed;
+    p->k1 = (uint32_t)(d->seed >> 32);
+    p->at0 = (uint32_t)d->offset;
+    p->at1 = (uint32_t)(d->offset >> 32);
+    p->step = d->step;
+    p->factor = (float)(65536.0 / (65536 - p->below));
+    return true;
+}
+
+// what all values of a call share
+struct DropState { uint32_t k0, k1, at0, at1, below; float factor; };
+__device__ __forceinline__ DropState drop_state(const DropParams &p)
+{
+    const uint64_t at = ((uint64_t)p.at1 << 32 | p.at0) + (p.step ? load_scalar(p.step) : 0);
+    return {p.k0, p.k1, (uint32_t)at, (uint32_t)(at >> 32), p.below, p.factor};
+}
+
+struct Words4 { uint32_t w[4]; };
+__device__ __forceinline__ Words4 philox(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3, uint32_t k0, uint32_t k1)
+{
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t a = (uint64_t)x0 * 0xD2511F53u, b = (uint64_t)x2 * 0xCD9E8D57u;
+        x0 = (uint32_t)(b >> 32) ^ x1 ^ k0;
+        x2 = (uint32_t)(a >> 32) ^ x3 ^ k1;
+        x1 = (uint32_t)b;
+        x3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return {{x0, x1, x2, x3}};
+}
+
+// bit i: column 8 group + i of the row is kept
+__device__ __forceinline__ uint32_t kept_bits(const DropState &d, uint32_t row, uint32_t group)
+{
+    const Words4 r = philox(group, row, d.at0, d.at1, d.k0, d.k1);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m |= (uint32_t)((i & 1 ? r.w[i >> 1] >> 16 : r.w[i >> 1] & 0xffffu) >= d.below) << i;
+    return m;
+}
+
+// N values (4 or 8) of a row from column `col` on, with dropout
+template <int N> __device__ __forceinline__ void drop_values(const DropState &d, uint32_t row, uint32_t col, float (&f)[N])
+{
+    if ((col & (N - 1)) == 0) { // inside one counter
+        const Words4 r = philox(col >> 3, row, d.at0, d.at1, d.k0, d.k1);
+        const uint32_t below = d.below << 16;
+        [[maybe_unused]] const uint32_t upper = 0u - (col >> 2 & 1);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            // (a high half is compared where it stands: the low one under it changes nothing)
+            uint32_t w = r.w[i >> 1];
+            if constexpr (N == 4) w ^= (w ^ r.w[2 + (i >> 1)]) & upper; // (a choice of addresses would put the words into memory)
+            f[i] = (i & 1 ? w : w << 16) >= below ? f[i] * d.factor : 0.0f;
+        }
+    } else {
+        const uint32_t at = col & 7;
+        uint32_t m = kept_bits(d, row, col >> 3) >> at;
+        if (at + N > 8) m |= kept_bits(d, row, (col >> 3) + 1) << (8 - at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = m >> i & 1 ? f[i] * d.factor : 0.0f;
+    }
+}
+
+} // namespace tt

@@ -1,4 +1,4 @@
-// The layer, flatten, retile and token calls as a Python extension module: arguments go from Python objects straight into the call's
+// The layer, flatten, retile, token and residual calls as a Python extension module: arguments go from Python objects straight into the call's
 // C arguments.  A training step of a small chain is six calls with 27 shard lists between them; through ctypes they took
 // 44 us of host time, as long as the GPU needs for half the kernels, and so 12 us.
 //
@@ -12,6 +12,7 @@
 #include <type_traits>
 #include "tensor_tiling.h"
 #include "tensor_tiling_tokens.h"
+#include "tensor_tiling_residual.h"
 #if __has_include(<ATen/dlpack.h>)
 #include <ATen/dlpack.h>
 #endif
@@ -26,13 +27,13 @@ constexpr int kMaxShards = 1 << TT_MAX_K;
 PyObject *g_data_ptr, *g_numel, *g_element_size, *g_value, *g_dtype_name, *g_is_contiguous; // method and attribute names
 PyObject *g_tiling, *g_forms, *g_dtype;                     // the binding's own converters, for the rarer forms
 PyObject *g_error;                                          // its exception: (status, what)
-PyObject *g_float32;                                        // torch.float32, once a tensor was seen
+PyObject *g_float32, *g_bfloat16;                           // torch.float32 and torch.bfloat16, once they were asked for
 
 // What a dense tensor is to a call
 struct Described {
     uint64_t address;
     int64_t entries;
-    bool fp32, dense;
+    bool fp32, dense, bf16;
 };
 #ifdef TT_DLPACK_EXCHANGE
 // A tensor type's DLPack functions: all of the above in one call (a policy loss with seven arrays takes 8.3 us of host time, 9.1
@@ -67,6 +68,7 @@ bool described(PyObject *o, Described *d)
     }
     d->address = (uint64_t)(uintptr_t)t.data + t.byte_offset;
     d->fp32 = t.dtype.code == kDLFloat && t.dtype.bits == 32 && t.dtype.lanes == 1;
+    d->bf16 = t.dtype.code == kDLBfloat && t.dtype.bits == 16 && t.dtype.lanes == 1;
     d->entries = 1;
     d->dense = true;
     for (int i = t.ndim - 1; i >= 0; --i) {
@@ -147,17 +149,35 @@ struct Args {
     {
         PyObject *o = next();
         if (!o || o == Py_None) return nullptr;
-        Described d{0, count, true, true};
-        if (!described(o, &d)) {
-            d.address = pointer_of(o);
-            if (ok && !PyLong_CheckExact(o)) ask(o, &d);
-        }
+        const Described d = description(o, count);
         if (ok && count > 0) {
             if (std::is_same<typename std::remove_const<T>::type, float>::value && !d.fp32) refuse(what, "fp32 values are expected");
             else if (d.entries < count) refuse(what, "fewer entries than tokens");
             else if (!d.dense) refuse(what, "a dense tensor is expected");
         }
         return reinterpret_cast<T *>((uintptr_t)d.address);
+    }
+    // ... and one of `count` columns whose type is the tensors'
+    const void *columns(const char *what, int64_t count, int dtype)
+    {
+        PyObject *o = next();
+        if (!o || o == Py_None) return nullptr;
+        const Described d = description(o, count);
+        if (ok && count > 0) {
+            if (!(dtype == TT_BF16 ? d.bf16 : d.fp32)) refuse(what, "values of the tensors' type are expected");
+            else if (d.entries < count) refuse(what, "fewer entries than columns");
+            else if (!d.dense) refuse(what, "a dense tensor is expected");
+        }
+        return reinterpret_cast<const void *>((uintptr_t)d.address);
+    }
+    Described description(PyObject *o, int64_t count)
+    {
+        Described d{0, count, true, true, true};
+        if (!described(o, &d)) {
+            d.address = pointer_of(o);
+            if (ok && !PyLong_CheckExact(o)) ask(o, &d);
+        }
+        return d;
     }
     // by an object's methods; left as it is without a dtype
     void ask(PyObject *o, Described *d)
@@ -168,20 +188,21 @@ struct Args {
             else fail();
             return;
         }
-        d->fp32 = type == g_float32 || is_float32(type);
+        d->fp32 = type == g_float32 || is_type(type, &g_float32, "float32");
+        d->bf16 = type == g_bfloat16 || is_type(type, &g_bfloat16, "bfloat16");
         Py_DECREF(type);
         if (ok) d->entries = (int64_t)method(o, g_numel);
         if (ok) d->dense = truth(o, g_is_contiguous);
     }
-    bool is_float32(PyObject *type)
+    bool is_type(PyObject *type, PyObject **known, const char *name)
     {
-        if (!g_float32) {
+        if (!*known) {
             PyObject *torch = PyImport_ImportModule("torch");
-            g_float32 = torch ? PyObject_GetAttrString(torch, "float32") : nullptr;
+            *known = torch ? PyObject_GetAttrString(torch, name) : nullptr;
             Py_XDECREF(torch);
-            if (!g_float32) return fail();
+            if (!*known) return fail();
         }
-        return type == g_float32;
+        return type == *known;
     }
     bool truth(PyObject *o, PyObject *name)
     {
@@ -213,6 +234,11 @@ struct Args {
     {
         PyObject *o = next();
         return o ? static_cast<const tt_layer *>(bytes_of(o, sizeof(tt_layer))) : nullptr;
+    }
+    const tt_drop *drop() // None: no dropout
+    {
+        PyObject *o = next();
+        return !o || o == Py_None ? nullptr : static_cast<const tt_drop *>(bytes_of(o, sizeof(tt_drop)));
     }
     tt_tiling tiling()
     {
@@ -545,6 +571,145 @@ PyObject *backward_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// dropout(address, drop, rows, cols, k, dtype, tX, tY, X, Y, stream): tt_dropout
+PyObject *dropout(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 11);
+    auto fn = g.address<decltype(&tt_dropout)>();
+    const tt_drop *drop = g.drop();
+    const int64_t rows = g.i64(), cols = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tY = g.tiling();
+    void *x[kMaxShards], *y[kMaxShards];
+    void **X = g.shards(x), **Y = g.shards(y);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(drop, rows, cols, k, dt, tX, tY, in(X), Y, stream); });
+}
+
+// norm_forward(address, rows, width, k, dtype, tX, tY, eps, drop, X, R, gain, H, Y, stream): tt_norm_forward
+PyObject *norm_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 15);
+    auto fn = g.address<decltype(&tt_norm_forward)>();
+    const int64_t rows = g.i64(), width = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tY = g.tiling();
+    const float eps = g.real();
+    const tt_drop *drop = g.drop();
+    void *x[kMaxShards], *r[kMaxShards], *h[kMaxShards], *y[kMaxShards];
+    void **X = g.shards(x), **R = g.shards(r);
+    const void *gain = g.columns("gain", width, dt);
+    void **H = g.shards(h), **Y = g.shards(y);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(rows, width, k, dt, tX, tY, eps, drop, in(X), in(R), gain, H, Y, stream); });
+}
+
+// norm_backward(address, rows, width, k, dtype, tX, tdY, eps, drop, H, gain, dY, dH, dS, dX, dgain, workspace, stream): tt_norm_backward
+PyObject *norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 18);
+    auto fn = g.address<decltype(&tt_norm_backward)>();
+    const int64_t rows = g.i64(), width = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tdY = g.tiling();
+    const float eps = g.real();
+    const tt_drop *drop = g.drop();
+    void *h[kMaxShards], *dy[kMaxShards], *dh[kMaxShards], *ds[kMaxShards], *dx[kMaxShards];
+    void **H = g.shards(h);
+    const void *gain = g.columns("gain", width, dt);
+    void **dY = g.shards(dy), **dH = g.shards(dh), **dS = g.shards(ds), **dX = g.shards(dx);
+    float *dgain = g.array<float>("dgain", width);
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    return finish(g, [&] { return fn(rows, width, k, dt, tX, tdY, eps, drop, in(H), gain, in(dY), in(dH), dS, dX, dgain, ws, bytes, stream); });
+}
+
+// norm_forward8(address, rows, width, k, dtype, tX, tQ, eps, X, R, gain, H, Q, S, stream): tt_norm_forward8
+PyObject *norm_forward8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 15);
+    auto fn = g.address<decltype(&tt_norm_forward8)>();
+    const int64_t rows = g.i64(), width = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tQ = g.tiling();
+    const float eps = g.real();
+    void *x[kMaxShards], *r[kMaxShards], *h[kMaxShards], *q[kMaxShards];
+    void **X = g.shards(x), **R = g.shards(r);
+    const void *gain = g.columns("gain", width, dt);
+    void **H = g.shards(h), **Q = g.shards(q);
+    float *S = g.array<float>("S", rows);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(rows, width, k, dt, tX, tQ, eps, in(X), in(R), gain, H, reinterpret_cast<int8_t *const *>(Q), S, stream); });
+}
+
+// rows8(address, rows, cols, k, dtype, tX, tQ, X, Q, S, stream): tt_rows8
+PyObject *rows8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 11);
+    auto fn = g.address<decltype(&tt_rows8)>();
+    const int64_t rows = g.i64(), cols = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tQ = g.tiling();
+    void *x[kMaxShards], *q[kMaxShards];
+    void **X = g.shards(x), **Q = g.shards(q);
+    float *S = g.array<float>("S", rows);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(rows, cols, k, dt, tX, tQ, in(X), reinterpret_cast<int8_t *const *>(Q), S, stream); });
+}
+
+// unrows8(address, rows, cols, k, dtype, tQ, tX, Q, S, X, stream): tt_unrows8
+PyObject *unrows8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 11);
+    auto fn = g.address<decltype(&tt_unrows8)>();
+    const int64_t rows = g.i64(), cols = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tQ = g.tiling(), tX = g.tiling();
+    void *q[kMaxShards], *x[kMaxShards];
+    void **Q = g.shards(q);
+    const float *S = g.array<const float>("S", rows);
+    void **X = g.shards(x);
+    void *stream = g.stream();
+    return finish(g, [&] { return fn(rows, cols, k, dt, tQ, tX, reinterpret_cast<const int8_t *const *>(Q), S, X, stream); });
+}
+
+// weights8(address, n_in, n_out, k, dtype, tW, W, Q, S, workspace, stream): tt_weights8
+PyObject *weights8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 11);
+    auto fn = g.address<decltype(&tt_weights8)>();
+    const int64_t n_in = g.i64(), n_out = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tW = g.tiling();
+    void *w[kMaxShards], *q[kMaxShards];
+    void **W = g.shards(w), **Q = g.shards(q);
+    float *S = g.array<float>("S", n_out);
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    return finish(g, [&] { return fn(n_in, n_out, k, dt, tW, in(W), reinterpret_cast<int8_t *const *>(Q), S, ws, bytes, stream); });
+}
+
+// forward8(address, layer, batch, k, dtype, tX, tW, tY, XQ, XS, WQ, WS, Y, workspace, stream): tt_fc_forward8
+PyObject *forward8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args g(args, n, 15);
+    auto fn = g.address<decltype(&tt_fc_forward8)>();
+    const tt_layer *lay = g.layer();
+    const int64_t batch = g.i64();
+    const int k = g.i32(), dt = g.dtype();
+    const tt_tiling tX = g.tiling(), tW = g.tiling(), tY = g.tiling();
+    void *xq[kMaxShards], *wq[kMaxShards], *y[kMaxShards];
+    void **XQ = g.shards(xq);
+    const float *XS = g.array<const float>("XS", batch);
+    void **WQ = g.shards(wq);
+    const float *WS = g.array<const float>("WS", lay ? lay->n_out : 0);
+    void **Y = g.shards(y);
+    size_t bytes;
+    void *ws = g.workspace(&bytes), *stream = g.stream();
+    const auto i8 = [](void **p) { return reinterpret_cast<const int8_t *const *>(p); };
+    return finish(g, [&] { return fn(lay, batch, k, dt, tX, tW, tY, i8(XQ), XS, i8(WQ), WS, Y, ws, bytes, stream); });
+}
+
 // converters(tiling, forms, dtype, error): what the binding uses for arguments that are no plain strings, and its exception
 PyObject *converters(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -568,7 +733,10 @@ template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)> PyMethodDef
 PyMethodDef g_methods[] = {method_def<forward>("forward"), method_def<forward_static>("forward_static"), method_def<backward>("backward"),
                            method_def<flatten>("flatten"), method_def<retile>("retile"), method_def<embed_forward>("embed_forward"), method_def<embed_backward>("embed_backward"),
                            method_def<policy_loss>("policy_loss"), method_def<token_logp>("token_logp"), method_def<pack8>("pack8"),
-                           method_def<backward_packed>("backward_packed"), method_def<converters>("converters"),
+                           method_def<backward_packed>("backward_packed"), method_def<dropout>("dropout"), method_def<norm_forward>("norm_forward"),
+                           method_def<norm_backward>("norm_backward"), method_def<norm_forward8>("norm_forward8"), method_def<rows8>("rows8"),
+                           method_def<unrows8>("unrows8"), method_def<weights8>("weights8"), method_def<forward8>("forward8"),
+                           method_def<converters>("converters"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

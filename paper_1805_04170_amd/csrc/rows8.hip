@@ -1,0 +1,602 @@
+// Tensors in 8 bits with a scale for each row (tt_rows8, tt_norm_forward8, tt_unrows8) and weights with one for each output channel
+// (tt_weights8).
+//
+// The steps are exact: which whole number 127 x / m is nearest to does not depend on roundings on the way.  That takes little: fp32
+// says it wherever the quotient is not next to the border of two steps, and where it is, once in some thousands, 64 bits do.  For
+// the norm the common factor of a row cancels, so gain * H is what is cut into steps: exact in fp32 where both are bf16, and taken in
+// 64 bits where they are fp32.
+#include <cstdint>
+#include "launch_util.h"
+#include "norm_math.h"
+#include "row_reduce.h"
+#include "tensor_tiling_residual.h"
+
+namespace tt {
+namespace {
+
+struct Rows8Params {
+    BlockTable X, R, H, Q; // (R, H: p[0] NULL where there is none; Q: extents in values, rows begin every `pitch` bytes)
+    const void *gain;
+    float *S;
+    RowShape r;
+    uint32_t pitch;
+    float eps;
+    uint32_t rows, lanes, groups;
+};
+
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+// a vector's steps as bytes
+template <typename T> struct Steps { uint32_t w[kVec<T> / 4]; };
+__device__ __forceinline__ void store_steps(int8_t *p, const Steps<uint16_t> &b) { *(TT_GLOBAL u32x2_any *)p = u32x2_any{b.w[0], b.w[1]}; }
+__device__ __forceinline__ void store_steps(int8_t *p, const Steps<float> &b) { *(TT_GLOBAL u32_any *)p = b.w[0]; }
+__device__ __forceinline__ void load_steps(const int8_t *p, Steps<uint16_t> &b)
+{
+    const u32x2_any w = *(const TT_GLOBAL u32x2_any *)p;
+    b.w[0] = w.x;
+    b.w[1] = w.y;
+}
+__device__ __forceinline__ void load_steps(const int8_t *p, Steps<float> &b) { b.w[0] = *(const TT_GLOBAL u32_any *)p; }
+
+// where a spot's steps lie
+template <bool CUT> __device__ __forceinline__ Lane lane_of8(const BlockTable &b, const Pieces &s, uint32_t shift, uint32_t pitch, uint32_t row, const Spot &v)
+{
+    if constexpr (CUT) {
+        const uint32_t rb = b.nR == 1 ? 0 : quotient(row, b.by_srows), cb = v.q >> shift;
+        return {(rb * b.nC + cb) * b.nrep, (size_t)(row - rb * b.srows) * pitch + (size_t)(v.q - (cb << shift)) * s.seg + v.at};
+    } else {
+        return {0, (size_t)row * pitch + v.at};
+    }
+}
+
+// steps of u, of which |u| <= m, m finite and above 0
+constexpr float kRound = 12582912.0f; // 1.5 * 2^23: a number added to it lies rounded in the sum's last bits
+__device__ __forceinline__ uint32_t step_of(double u, double m) { return (uint32_t)(int)rint(u * 127.0 / m); }
+
+// u = value * gain, and what compares and cuts it: fp32 where that is exact
+template <bool EXACT32> struct Cut8;
+template <> struct Cut8<true> { // u fp32
+    typedef float U;
+    float m, inv;
+    static __device__ __forceinline__ float of(float x, float g) { return x * g; }
+    // Both factors times a power of two.  What that rounds lies far below half a step of the row; a zero has no product with a factor
+    // that leaves fp32.
+    static __device__ __forceinline__ float scaled(float x, float g, float by) { return x == 0.0f || g == 0.0f ? x * g : x * by * (g * by); }
+    __device__ __forceinline__ void init(float most) { m = most; inv = 127.0f / most; }
+    // (the quotient is off by at most 127 * 2^-23)
+    __device__ __forceinline__ uint32_t operator()(float u) const
+    {
+        const float t = u * inv, q = t + kRound;
+        if (fabsf(t - (q - kRound)) > 0.4999f) return step_of(u, m);
+        return __float_as_uint(q);
+    }
+};
+template <> struct Cut8<false> { // u in 64 bits, which hold a product of two fp32 values
+    typedef double U;
+    double m, inv;
+    static __device__ __forceinline__ double of(float x, float g) { return (double)x * g; }
+    static __device__ __forceinline__ double scaled(float x, float g, float) { return of(x, g); } // (64 bits hold any)
+    __device__ __forceinline__ void init(double most) { m = most; inv = 127.0 / most; }
+    __device__ __forceinline__ uint32_t operator()(double u) const
+    {
+        const double t = u * inv, q = rint(t);
+        if (fabs(t - q) > 0.4999999999) return step_of(u, m);
+        return (uint32_t)(int)q;
+    }
+};
+
+__device__ __forceinline__ float magnitude(float u) { return fabsf(u); }
+__device__ __forceinline__ double magnitude(double u) { return fabs(u); }
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ double bits_of(double v) { return v; } // (compared by its bits: Largest)
+__device__ __forceinline__ float value_of(uint32_t v) { return __uint_as_float(v); }
+__device__ __forceinline__ double value_of(double v) { return v; }
+
+// NORM: the sum's norm (else the steps are X's).  A row's vectors lie in registers.
+template <typename T, int V, bool WAVE, int MODE, bool NORM>
+__global__ __launch_bounds__(WAVE ? kWaveBlock : kMostThreads) void rows8_kernel(const Rows8Params p)
+{
+    constexpr uint32_t EV = kVec<T>;
+    constexpr bool CUT = MODE != kPlain, NARROW = MODE == kNarrow, EXACT32 = !NORM || sizeof(T) == 2;
+    constexpr bool AHEAD = V <= 2, KEPT = V <= 2;
+    typedef Cut8<EXACT32> C;
+    typedef typename C::U U;
+    typedef decltype(bits_of(U())) B;
+    __shared__ RowScratch<1> scratch;
+    const uint32_t li = WAVE ? threadIdx.x & (p.lanes - 1) : threadIdx.x;
+    const uint32_t at_once = WAVE ? kWaveBlock / p.lanes : 1, step = p.groups * at_once;
+    const bool res = NORM && p.R.p[0] != nullptr, keep = NORM && p.H.p[0] != nullptr;
+    Spot spots[KEPT ? V : 1];
+    u32x4 gains[KEPT && NORM ? V : 1], x[V], r[V];
+    auto spot = [&](int i) {
+        if constexpr (KEPT) return spots[i];
+        uint32_t j = li + i * p.lanes;
+        wave::forget(j);
+        return spot_of<EV>(p.r, j);
+    };
+    auto gain_of = [&](int i) {
+        if constexpr (!NORM) return ones<T>();
+        else if constexpr (KEPT) return gains[i];
+        else return p.gain ? gain_at<T, MODE>(p.gain, p.r, spot(i)) : ones<T>();
+    };
+    if constexpr (KEPT) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            spots[i] = spot_of<EV>(p.r, li + i * p.lanes);
+            if constexpr (NORM) gains[i] = p.gain ? gain_at<T, MODE>(p.gain, p.r, spots[i]) : ones<T>();
+        }
+    }
+    auto row_of = [&](uint32_t base) { return WAVE ? base + threadIdx.x / p.lanes : base; };
+    auto load = [&](uint32_t base) { // (a row past the end is the last one again)
+        const uint32_t row = row_of(base) < p.rows ? row_of(base) : p.rows - 1;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const Spot v = spot(i);
+            const Lane l = lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row, v);
+            x[i] = load_spot<T, NARROW>(p.X, l, v);
+            if (res) r[i] = load_spot<T, NARROW>(p.R, l, v);
+        }
+    };
+    uint32_t turn = 0;
+    uint32_t base = blockIdx.x * at_once;
+    if constexpr (AHEAD) load(base);
+    for (; base < p.rows; base += step) {
+        const bool live = row_of(base) < p.rows;
+        const uint32_t row = live ? row_of(base) : p.rows - 1;
+        if constexpr (!AHEAD) load(base);
+        u32x4 h[V];
+        // the sum of squares of the values times `by`, and the largest |u| of both factors times `scale`
+        float sum[1];
+        B most[1];
+        auto statistics = [&](float by, float scale) {
+            sum[0] = 0.0f;
+            U top = 0;
+            most[0] = bits_of(top);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const Spot v = spot(i);
+                float f[EV], g[EV];
+                unpack16(h[i], f, T());
+                unpack16(gain_of(i), g, T());
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) {
+                    if constexpr (NORM) sum[0] += v.dup > e ? 0.0f : f[e] * by * (f[e] * by);
+                    most[0] = Largest::of(most[0], bits_of(magnitude(scale == 1.0f ? C::of(f[e], g[e]) : C::scaled(f[e], g[e], scale))));
+                }
+                wave::forget(h[i]); // (unpacked again where it is used next, not kept in 32 bits)
+            }
+            if constexpr (NORM) RowReduce<WAVE, float, Sum>::run(sum, p.lanes, scratch, turn++);
+            RowReduce<WAVE, B, Largest>::run(most, p.lanes, scratch, turn++);
+        };
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const Spot v = spot(i);
+            h[i] = x[i];
+            if (res) h[i] = added<T>(x[i], r[i]);
+            if (v.n == 0) h[i] = u32x4{0, 0, 0, 0};
+            if (keep && live) store_spot<T, CUT, NARROW>(p.H, lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v), v, h[i]);
+        }
+        if constexpr (AHEAD) load(base + step < p.rows ? base + step : base);
+        statistics(1.0f, 1.0f);
+        float mean = NORM ? scaled_mean(sum[0], p.r.cols, p.eps, 1.0f) : 1.0f, factor = 1.0f, scale = 1.0f;
+        U m = value_of(most[0]);
+        // fp32 holds |u| and 127 / |u| well inside (64 bits hold any; a row of zeros has no quotients)
+        const bool inside = EXACT32 ? m >= 0x1p-60f && m <= 0x1p100f : m > 0;
+        const bool fits = fits_fp32(mean) && inside;
+        if (WAVE ? wave::ballot(!fits) != 0 : !fits) {
+            const float by = fits_fp32(mean) ? 1.0f : factor_for(mean), to = !EXACT32 || inside ? 1.0f : m < 1.0f ? 0x1p50f : 0x1p-66f;
+            statistics(by, to);
+            if (!fits) {
+                factor = by;
+                scale = to;
+                m = value_of(most[0]);
+                if constexpr (NORM) mean = scaled_mean(sum[0], p.r.cols, p.eps, by);
+            }
+        }
+        const float root = NORM ? inverse_root(mean) : 1.0f;
+        const bool number = root == root && m <= U(EXACT32 ? 0x1p126 : 0x1p1000), some = number && m > 0;
+        C cut;
+        cut.init(some ? m : U(1));
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            Spot v = spot(i);
+            if (!live) v.n = 0;
+            float f[EV], g[EV];
+            unpack16(h[i], f, T());
+            unpack16(gain_of(i), g, T());
+            uint32_t w[EV];
+            if (scale == 1.0f) {
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) w[e] = cut(C::of(f[e], g[e]));
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) w[e] = cut(C::scaled(f[e], g[e], scale));
+            }
+            Steps<T> b;
+#pragma unroll
+            for (uint32_t e = 0; e < EV; e += 4) b.w[e / 4] = some ? wave::low_bytes(w[e], w[e + 1], w[e + 2], w[e + 3]) : 0u;
+            if (v.n == 0) continue;
+            const Lane l = lane_of8<CUT>(p.Q, p.r.s, p.r.s.b_shift, p.pitch, row, v);
+            for (uint32_t c = 0; c < (CUT ? p.Q.nrep : 1); ++c) {
+                int8_t *to = static_cast<int8_t *>(p.Q.p[l.block + c]) + l.at;
+                if constexpr (NARROW) {
+                    for (uint32_t e = 0; e < v.n; ++e) store1(to + e, (int8_t)(b.w[e >> 2] >> (8 * (e & 3))));
+                } else {
+                    store_steps(to, b);
+                }
+            }
+        }
+        if (!live) continue;
+        // zeros behind the values of each of the row's blocks
+        const uint32_t behind = p.pitch - p.Q.scols, rb = CUT && p.Q.nR > 1 ? quotient(row, p.Q.by_srows) : 0;
+        for (uint32_t j = li; j < behind * p.Q.nC; j += p.lanes) {
+            const uint32_t cb = CUT ? j / behind : 0;
+            for (uint32_t c = 0; c < (CUT ? p.Q.nrep : 1); ++c)
+                store1(static_cast<int8_t *>(p.Q.p[(rb * p.Q.nC + cb) * p.Q.nrep + c]) + (size_t)(row - rb * p.Q.srows) * p.pitch + p.Q.scols + (j - cb * behind), (int8_t)0);
+        }
+        if (li == 0) {
+            const float s = (float)((double)m * root * factor / ((double)scale * scale * 127.0)); // (factors of scaled values: powers of two)
+            store1(p.S + row, number ? s : __builtin_nanf(""));
+        }
+    }
+}
+
+// Rows that registers do not hold: read twice, all in 64 bits.
+template <typename T, bool CUT, bool NORM> __global__ __launch_bounds__(kMostThreads) void rows8_long_kernel(const Rows8Params p)
+{
+    constexpr uint32_t EV = kVec<T>;
+    __shared__ RowScratch<1> scratch;
+    const bool res = NORM && p.R.p[0] != nullptr, keep = NORM && p.H.p[0] != nullptr;
+    uint32_t turn = 0;
+    for (uint32_t row = blockIdx.x; row < p.rows; row += p.groups) {
+        double s[1] = {0.0}, m[1] = {0.0}, root = 1.0;
+        bool number = true;
+        for (int pass = 0; pass < 2; ++pass) {
+            for (uint32_t j = threadIdx.x; j < p.r.units; j += kMostThreads) {
+                const Spot v = spot_of<EV>(p.r, j);
+                const Lane l = lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row, v);
+                u32x4 h = load_spot<T, false>(p.X, l, v);
+                if (res) h = added<T>(h, load_spot<T, false>(p.R, l, v));
+                float f[EV], g[EV];
+                unpack16(h, f, T());
+                unpack16(NORM && p.gain ? gain_at<T, kCut>(p.gain, p.r, v) : ones<T>(), g, T());
+                Steps<T> b;
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) {
+                    const double u = (double)f[e] * g[e];
+                    if (pass == 0) {
+                        s[0] += v.dup > e ? 0.0 : (double)f[e] * f[e];
+                        m[0] = Largest::of(m[0], fabs(u));
+                    } else {
+                        const uint32_t q = number && m[0] > 0 ? step_of(u, m[0]) & 255u : 0u;
+                        b.w[e / 4] = e % 4 == 0 ? q : b.w[e / 4] | q << (8 * (e % 4));
+                    }
+                }
+                if (pass == 0) continue;
+                if (keep) store_spot<T, CUT, false>(p.H, l, v, h);
+                const Lane to = lane_of8<CUT>(p.Q, p.r.s, p.r.s.b_shift, p.pitch, row, v);
+                for (uint32_t c = 0; c < p.Q.nrep; ++c) store_steps(static_cast<int8_t *>(p.Q.p[to.block + c]) + to.at, b);
+            }
+            if (pass) continue;
+            RowReduce<false, double, Largest>::run(m, kMostThreads, scratch, turn++);
+            if constexpr (NORM) {
+                RowReduce<false, double, Sum>::run(s, kMostThreads, scratch, turn++);
+                root = inverse_root_wide(s[0] / p.r.cols + p.eps);
+            }
+            number = root == root && m[0] <= 0x1p1000;
+        }
+        const uint32_t behind = p.pitch - p.Q.scols, rb = p.Q.nR > 1 ? quotient(row, p.Q.by_srows) : 0;
+        for (uint32_t j = threadIdx.x; j < behind * p.Q.nC; j += kMostThreads) {
+            const uint32_t cb = j / behind;
+            for (uint32_t c = 0; c < p.Q.nrep; ++c)
+                store1(static_cast<int8_t *>(p.Q.p[(rb * p.Q.nC + cb) * p.Q.nrep + c]) + (size_t)(row - rb * p.Q.srows) * p.pitch + p.Q.scols + (j - cb * behind), (int8_t)0);
+        }
+        if (threadIdx.x == 0) store1(p.S + row, number ? (float)(m[0] * root / 127.0) : __builtin_nanf(""));
+    }
+}
+
+uint32_t groups_of(const RowLaunch &w, int64_t rows)
+{
+    const int64_t all = (rows + w.at_once - 1) / w.at_once, held = (int64_t)kCUs * (2048 / w.block);
+    return (uint32_t)(all < held ? all : held);
+}
+template <typename T, int MODE, bool NORM> void launch_rows_as(const Rows8Params &p, const RowLaunch &w, hipStream_t s)
+{
+    const dim3 grid(p.groups), block(w.block);
+    if (w.wave) hipLaunchKernelGGL((rows8_kernel<T, 1, true, MODE, NORM>), grid, block, 0, s, p);
+    else if constexpr (MODE != kNarrow) { // (rows of narrow segments have at most 64 vectors)
+        if (w.vectors == 1) hipLaunchKernelGGL((rows8_kernel<T, 1, false, MODE, NORM>), grid, block, 0, s, p);
+        else if (w.vectors == 2) hipLaunchKernelGGL((rows8_kernel<T, 2, false, MODE, NORM>), grid, block, 0, s, p);
+        else if (w.vectors == 4) hipLaunchKernelGGL((rows8_kernel<T, 4, false, MODE, NORM>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((rows8_long_kernel<T, MODE != kPlain, NORM>), grid, block, 0, s, p);
+    }
+}
+template <typename T, bool NORM> void launch_rows(const Rows8Params &p, const RowLaunch &w, hipStream_t s)
+{
+    if (narrow_segments(p.r, kVec<T>)) launch_rows_as<T, kNarrow, NORM>(p, w, s);
+    else if (uncut(p.X) && uncut(p.Q)) launch_rows_as<T, kPlain, NORM>(p, w, s);
+    else launch_rows_as<T, kCut, NORM>(p, w, s);
+}
+
+bool bytes_fit(const void *const *shards, int k, bool empty)
+{
+    if (!shards || empty) return shards != nullptr;
+    for (int s = 0; s < (1 << k); ++s) if (!shards[s]) return false;
+    return true;
+}
+const void *const *untyped(int8_t *const *p) { return reinterpret_cast<const void *const *>(p); }
+const void *const *untyped(const int8_t *const *p) { return reinterpret_cast<const void *const *>(p); }
+const void *const *in(void *const *p) { return const_cast<const void *const *>(p); }
+
+// scales of rows without columns: 0
+__global__ __launch_bounds__(kWaveBlock) void zero_scales_kernel(float *S, uint32_t rows)
+{
+    const uint32_t i = blockIdx.x * kWaveBlock + threadIdx.x;
+    if (i < rows) store1(S + i, 0.0f);
+}
+
+tt_status run_rows8(bool norm, int64_t rows, int64_t cols, int k, int dtype, const tt_tiling &tX, const tt_tiling &tQ, float eps, const void *const *X,
+                    const void *const *R, const void *gain, void *const *H, int8_t *const *Q, float *S, void *stream)
+{
+    if (!valid_k(k) || !valid_tiling(tX, k) || !valid_tiling(tQ, k) || !valid_dtype(dtype) || rows < 0 || cols < 0) return TT_EINVAL;
+    const bool empty = rows == 0 || cols == 0;
+    const int e = dtype_bytes(dtype);
+    if (!shards_fit(X, k, e, empty) || (R && !shards_fit(R, k, e, empty)) || (H && !shards_fit(in(H), k, e, empty)) || !bytes_fit(untyped(Q), k, empty))
+        return TT_EINVAL;
+    if ((gain && !aligned_to(gain, e)) || (rows && !aligned_to(S, 4))) return TT_EINVAL;
+    if (!fits31(rows) || !fits31(cols)) return TT_EUNSUPPORTED;
+    Rows8Params p;
+    if (!make_blocks(X, tX, k, rows, cols, &p.X) || !make_blocks(R, tX, k, rows, cols, &p.R) || !make_blocks(in(H), tX, k, rows, cols, &p.H) ||
+        !make_blocks(untyped(Q), tQ, k, rows, cols, &p.Q))
+        return TT_EINFEASIBLE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (rows == 0) return TT_OK;
+    if (cols == 0) {
+        hipLaunchKernelGGL(zero_scales_kernel, dim3((uint32_t)((rows + kWaveBlock - 1) / kWaveBlock)), dim3(kWaveBlock), 0, s, S, (uint32_t)rows);
+        return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
+    }
+    p.gain = gain;
+    p.S = S;
+    p.eps = eps;
+    p.rows = (uint32_t)rows;
+    p.pitch = (uint32_t)tt_pitch8(p.Q.scols);
+    p.r = row_shape(p.X, p.Q, cols, 16 / e);
+    const RowLaunch w = row_launch(p.r);
+    p.lanes = w.lanes;
+    p.groups = groups_of(w, rows);
+    const uint64_t values = (uint64_t)rows * cols;
+    ProfileScope scope(stream, TT_K_ROWS8, 1 << k, rows, cols, e, values * (e * (1 + (R ? 1 : 0) + (H ? p.H.nrep : 0)) + p.Q.nrep) + 4 * (uint64_t)rows, 0);
+    if (dtype == TT_BF16) norm ? launch_rows<uint16_t, true>(p, w, s) : launch_rows<uint16_t, false>(p, w, s);
+    else norm ? launch_rows<float, true>(p, w, s) : launch_rows<float, false>(p, w, s);
+    return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
+}
+
+// ------------------------------------------------------------ values of 8 bits
+
+constexpr int kThreads = 256, kVectors = 4;
+struct Unrows8Params {
+    BlockTable Q, X;
+    const float *S;
+    RowShape r;
+    uint32_t pitch;
+    uint64_t units;
+    uint32_t small; // they are counted in 31 bits
+    Divisor by_units;
+};
+template <typename T, bool CUT, bool NARROW> __global__ __launch_bounds__(kThreads) void unrows8_kernel(const Unrows8Params p)
+{
+    constexpr uint32_t EV = kVec<T>;
+    const uint64_t first = (uint64_t)blockIdx.x * (kThreads * kVectors);
+    const uint32_t row0 = p.small ? quotient((uint32_t)first, p.by_units) : uniform((uint32_t)(first / p.r.units)), j0 = (uint32_t)(first - (uint64_t)row0 * p.r.units);
+    const uint64_t left = p.units - first;
+    uint32_t row[kVectors];
+    float scale[kVectors];
+    Spot v[kVectors];
+    Steps<T> q[kVectors];
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        const uint32_t u = threadIdx.x + i * kThreads, j = j0 + (u < left ? u : 0); // (past the end: the workgroup's first vector again)
+        const uint32_t over = quotient(j, p.by_units);
+        row[i] = row0 + over;
+        v[i] = spot_of<EV>(p.r, j - over * p.r.units);
+        const Lane l = lane_of8<CUT>(p.Q, p.r.s, p.r.s.a_shift, p.pitch, row[i], v[i]);
+        const int8_t *from = static_cast<const int8_t *>(p.Q.p[l.block]) + l.at;
+        if constexpr (NARROW) {
+            q[i] = Steps<T>();
+            for (uint32_t e = 0; e < v[i].n; ++e) q[i].w[e >> 2] |= (uint32_t)(uint8_t)load1(from + e) << (8 * (e & 3));
+        } else {
+            load_steps(from, q[i]);
+        }
+        scale[i] = load1(p.S + row[i]);
+        if (u >= left) v[i].n = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        float f[EV];
+#pragma unroll
+        for (uint32_t e = 0; e < EV; ++e) f[e] = (float)(int8_t)(q[i].w[e / 4] >> (8 * (e % 4))) * scale[i];
+        store_spot<T, CUT, NARROW>(p.X, lane_of<CUT>(p.X, p.r.s, p.r.s.b_shift, row[i], v[i]), v[i], pack16(f, T()));
+    }
+}
+template <typename T> void launch_unrows(const Unrows8Params &p, hipStream_t s)
+{
+    const dim3 grid((uint32_t)((p.units + kThreads * kVectors - 1) / (kThreads * kVectors))), block(kThreads);
+    if (narrow_segments(p.r, kVec<T>)) hipLaunchKernelGGL((unrows8_kernel<T, true, true>), grid, block, 0, s, p);
+    else if (uncut(p.Q) && uncut(p.X)) hipLaunchKernelGGL((unrows8_kernel<T, false, false>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((unrows8_kernel<T, true, false>), grid, block, 0, s, p);
+}
+
+// ------------------------------------------------------------ weights, once for each
+
+struct Weights8Params {
+    BlockTable W, Q;      // Q[i]: the transposed shard, rows of `pitch` bytes
+    float *S;
+    uint32_t *parts;      // largest magnitudes' bits of each run of rows, by output channel
+    uint32_t n_in, n_out, runs, per_run, pitch, tiles; // (tiles of a block along its output channels)
+    Divisor by_scols;
+};
+template <typename T> __device__ __forceinline__ float weight_at(const Weights8Params &p, uint32_t i, uint32_t n)
+{
+    const uint32_t rb = p.W.nR == 1 ? 0 : quotient(i, p.W.by_srows), cb = p.W.nC == 1 ? 0 : quotient(n, p.by_scols);
+    const T *w = static_cast<const T *>(p.W.p[(rb * p.W.nC + cb) * p.W.nrep]);
+    return to_float(load1(w + (size_t)(i - rb * p.W.srows) * p.W.scols + (n - cb * p.W.scols)));
+}
+template <typename T> __global__ __launch_bounds__(kThreads) void weights8_most_kernel(const Weights8Params p)
+{
+    const uint32_t n = blockIdx.x * kThreads + threadIdx.x;
+    if (n >= p.n_out) return;
+    const uint32_t from = blockIdx.y * p.per_run, to = from + p.per_run < p.n_in ? from + p.per_run : p.n_in;
+    uint32_t top = 0;
+#pragma unroll 4
+    for (uint32_t i = from; i < to; ++i) top = Largest::of(top, __float_as_uint(weight_at<T>(p, i, n)) & 0x7fffffffu);
+    p.parts[(size_t)blockIdx.y * p.n_out + n] = top;
+}
+// 64 output channels x 64 inputs of a block a workgroup; the shard's rows behind its inputs are zeros
+template <typename T> __global__ __launch_bounds__(kThreads) void weights8_kernel(const Weights8Params p)
+{
+    __shared__ int8_t tile[64][64 + 4];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t block = blockIdx.y / p.tiles, rb = block / p.W.nC, cb = block - rb * p.W.nC;
+    const uint32_t i0 = blockIdx.x * 64, n0 = (blockIdx.y - block * p.tiles) * 64, n = n0 + lane;
+    const uint32_t channel = cb * p.W.scols + n;
+    const bool there = n < p.W.scols;
+    uint32_t top = 0;
+    if (there)
+        for (uint32_t r = 0; r < p.runs; ++r) top = Largest::of(top, load1(p.parts + (size_t)r * p.n_out + channel));
+    const float m = __uint_as_float(top);
+    const bool number = top < 0x7f800000u;
+    for (uint32_t i = wave; i < 64; i += kThreads / 64) {
+        uint32_t q = 0;
+        if (there && i0 + i < p.W.srows && number && top) q = step_of(weight_at<T>(p, rb * p.W.srows + i0 + i, channel), m);
+        tile[lane][i] = (int8_t)q;
+    }
+    if (there && wave == 0 && rb == 0 && blockIdx.x == 0) store1(p.S + channel, number ? (float)((double)m / 127.0) : __builtin_nanf(""));
+    __syncthreads();
+    for (uint32_t j = wave; j < 64 && n0 + j < p.W.scols; j += kThreads / 64) {
+        if (i0 + lane >= p.pitch) continue;
+        for (uint32_t c = 0; c < p.W.nrep; ++c)
+            store1(static_cast<int8_t *>(p.Q.p[block * p.W.nrep + c]) + (size_t)(n0 + j) * p.pitch + i0 + lane, tile[j][lane]);
+    }
+}
+
+struct WeightRuns { uint32_t runs, per_run; size_t bytes; };
+WeightRuns weight_runs(int64_t n_in, int64_t n_out)
+{
+    WeightRuns r;
+    r.per_run = (uint32_t)((n_in + 63) / 64);
+    if (r.per_run < 64) r.per_run = 64;
+    r.runs = (uint32_t)((n_in + r.per_run - 1) / r.per_run);
+    r.bytes = align_up((size_t)r.runs * (size_t)n_out * 4, 256);
+    return r;
+}
+tt_status weight_shape(int64_t n_in, int64_t n_out, int k, const tt_tiling &tW, Grid *g)
+{
+    if (!valid_k(k) || !valid_tiling(tW, k) || n_in < 0 || n_out < 0) return TT_EINVAL;
+    // (tiles along the output channels are counted in a launch's second extent, below 2^16)
+    if (!fits31(n_in) || n_out > (int64_t(1) << 21)) return TT_EUNSUPPORTED;
+    return make_grid(tW.cut, k, n_in, n_out, g) ? TT_OK : TT_EINFEASIBLE;
+}
+
+} // namespace
+} // namespace tt
+
+extern "C" int64_t tt_pitch8(int64_t cols)
+{
+    if (cols < 0 || !tt::fits31(cols)) return -1;
+    return (cols + TT_ROW8_BYTES - 1) / TT_ROW8_BYTES * TT_ROW8_BYTES;
+}
+
+extern "C" tt_status tt_rows8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling tX, tt_tiling tQ, const void *const *X, int8_t *const *Q,
+                              float *S, void *stream)
+{
+    return tt::run_rows8(false, rows, cols, k, dtype, tX, tQ, 1.0f, X, nullptr, nullptr, nullptr, Q, S, stream);
+}
+
+extern "C" tt_status tt_norm_forward8(int64_t rows, int64_t width, int k, int dtype, tt_tiling tX, tt_tiling tQ, float eps, const void *const *X,
+                                      const void *const *R, const void *gain, void *const *H, int8_t *const *Q, float *S, void *stream)
+{
+    if (!(eps > 0.0f && eps <= 3.4e38f)) return TT_EINVAL;
+    return tt::run_rows8(true, rows, width, k, dtype, tX, tQ, eps, X, R, gain, H, Q, S, stream);
+}
+
+extern "C" tt_status tt_unrows8(int64_t rows, int64_t cols, int k, int dtype, tt_tiling tQ, tt_tiling tX, const int8_t *const *Q, const float *S,
+                                void *const *X, void *stream)
+{
+    using namespace tt;
+    if (!valid_k(k) || !valid_tiling(tX, k) || !valid_tiling(tQ, k) || !valid_dtype(dtype) || rows < 0 || cols < 0) return TT_EINVAL;
+    const bool empty = rows == 0 || cols == 0;
+    const int e = dtype_bytes(dtype);
+    if (!bytes_fit(untyped(Q), k, empty) || !shards_fit(in(X), k, e, empty) || (!empty && !aligned_to(S, 4))) return TT_EINVAL;
+    if (!fits31(rows) || !fits31(cols)) return TT_EUNSUPPORTED;
+    Unrows8Params p;
+    if (!make_blocks(untyped(Q), tQ, k, rows, cols, &p.Q) || !make_blocks(in(X), tX, k, rows, cols, &p.X)) return TT_EINFEASIBLE;
+    if (empty) return TT_OK;
+    p.S = S;
+    p.pitch = (uint32_t)tt_pitch8(p.Q.scols);
+    p.r = row_shape(p.Q, p.X, cols, 16 / e);
+    p.by_units = divisor(p.r.units);
+    p.units = (uint64_t)rows * p.r.units;
+    p.small = p.units < (uint64_t(1) << 31);
+    if ((uint64_t)rows * (uint64_t)cols >= (uint64_t(1) << 37) || p.units / kVectors >= (uint64_t(1) << 32) - kThreads || p.r.units >= (1u << 31) - kThreads * kVectors)
+        return TT_EUNSUPPORTED; // (a launch holds fewer than 2^32 threads)
+    ProfileScope scope(stream, TT_K_ROWS8, 1 << k, rows, cols, e, (uint64_t)rows * cols * (1 + e * p.X.nrep) + 4 * (uint64_t)rows, 0);
+    if (dtype == TT_BF16) launch_unrows<uint16_t>(p, static_cast<hipStream_t>(stream));
+    else launch_unrows<float>(p, static_cast<hipStream_t>(stream));
+    return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
+}
+
+extern "C" tt_status tt_weights8_workspace_bytes(int64_t n_in, int64_t n_out, int k, tt_tiling tW, size_t *bytes)
+{
+    using namespace tt;
+    Grid g;
+    if (!bytes) return TT_EINVAL;
+    const tt_status st = weight_shape(n_in, n_out, k, tW, &g);
+    if (st != TT_OK) return st;
+    *bytes = n_in == 0 || n_out == 0 ? 0 : weight_runs(n_in, n_out).bytes;
+    return TT_OK;
+}
+
+extern "C" tt_status tt_weights8(int64_t n_in, int64_t n_out, int k, int dtype, tt_tiling tW, const void *const *W, int8_t *const *Q, float *S,
+                                 void *workspace, size_t ws_bytes, void *stream)
+{
+    using namespace tt;
+    Grid g;
+    const tt_status st = weight_shape(n_in, n_out, k, tW, &g);
+    if (st != TT_OK && st != TT_EINFEASIBLE) return st;
+    if (!valid_dtype(dtype)) return TT_EINVAL;
+    const bool empty = n_in == 0 || n_out == 0;
+    const int e = dtype_bytes(dtype);
+    if (!shards_fit(W, k, e, empty) || !bytes_fit(untyped(Q), k, empty) || (n_out && !aligned_to(S, 4))) return TT_EINVAL;
+    if (st != TT_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (n_out == 0) return TT_OK;
+    if (n_in == 0) {
+        hipLaunchKernelGGL(zero_scales_kernel, dim3((uint32_t)((n_out + kWaveBlock - 1) / kWaveBlock)), dim3(kWaveBlock), 0, s, S, (uint32_t)n_out);
+        return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
+    }
+    Weights8Params p;
+    const WeightRuns r = weight_runs(n_in, n_out);
+    if (!workspace || ws_bytes < r.bytes || reinterpret_cast<uintptr_t>(workspace) % 256) return TT_EWORKSPACE;
+    make_blocks(W, tW, k, n_in, n_out, &p.W);
+    make_blocks(untyped(Q), tW, k, n_in, n_out, &p.Q);
+    p.S = S;
+    p.parts = static_cast<uint32_t *>(workspace);
+    p.n_in = (uint32_t)n_in;
+    p.n_out = (uint32_t)n_out;
+    p.runs = r.runs;
+    p.per_run = r.per_run;
+    p.pitch = (uint32_t)tt_pitch8(p.W.srows);
+    p.by_scols = divisor(p.W.scols);
+    ProfileScope scope(stream, TT_K_ROWS8, 1 << k, n_in, n_out, e, (uint64_t)n_in * n_out * (2 * e + p.W.nrep), 0);
+    const dim3 columns((uint32_t)((n_out + kThreads - 1) / kThreads), r.runs), threads(kThreads);
+    p.tiles = (p.W.scols + 63) / 64;
+    const dim3 tiles((p.pitch + 63) / 64, p.tiles * p.W.nR * p.W.nC);
+    if (dtype == TT_BF16) {
+        hipLaunchKernelGGL((weights8_most_kernel<uint16_t>), columns, threads, 0, s, p);
+        hipLaunchKernelGGL((weights8_kernel<uint16_t>), tiles, threads, 0, s, p);
+    } else {
+        hipLaunchKernelGGL((weights8_most_kernel<float>), columns, threads, 0, s, p);
+        hipLaunchKernelGGL((weights8_kernel<float>), tiles, threads, 0, s, p);
+    }
+    return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
+}

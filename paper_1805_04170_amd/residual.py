@@ -1,0 +1,125 @@
+"""Binding of include/tensor_tiling_residual.h, same names: dropout, the residual's addition with a norm behind it and their gradients,
+rows and weights in 8 bits and the layers that multiply them.  Argument marshalling only, as in binding.py; the calls go through the
+extension module _calls.
+
+Scales, gains and their gradients are dense torch tensors with an entry for every row or column at least, or integer device
+addresses: scales and gradients torch.float32, a gain the type of the tensors.  Others are refused (TT_EINVAL).
+"""
+import ctypes
+
+from . import binding as _b
+from .binding import TilingError
+
+TT_ROW8_BYTES = 128
+RESIDUAL_EXPORTS = [
+    "tt_dropout", "tt_norm_forward", "tt_norm_workspace_bytes", "tt_norm_backward", "tt_pitch8", "tt_rows8", "tt_unrows8", "tt_norm_forward8",
+    "tt_weights8_workspace_bytes", "tt_weights8", "tt_fc8_workspace_bytes", "tt_fc_forward8",
+]
+__all__ = RESIDUAL_EXPORTS + ["TT_ROW8_BYTES", "RESIDUAL_EXPORTS", "tt_drop", "drop"]
+
+
+class tt_drop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+def drop(p, seed, offset=0, step=None):
+    """step: a torch.int64 tensor of one number on the device (kept alive with the result), an address, or None; numbers wrap to 64 bits"""
+    at = step
+    if hasattr(step, "data_ptr"):
+        if str(step.dtype) not in ("torch.int64", "torch.uint64") or step.numel() < 1:
+            raise TilingError(1, "step: a number of 64 bits is expected")
+        at = step.data_ptr()
+    d = tt_drop(p, seed & 0xffffffffffffffff, offset & 0xffffffffffffffff, at)
+    d.held = step
+    return d
+
+
+def _fn(name):
+    """the address of a function of the loaded library"""
+    L = _b._lib or _b.lib()
+    try:
+        return L.residual_addresses[name]
+    except AttributeError:
+        L.residual_addresses = {}
+        _b._address("tt_retile")        # (makes the extension module known)
+    except KeyError:
+        pass
+    L.residual_addresses[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
+    return L.residual_addresses[name]
+
+
+def _sized(name, *args):
+    out = ctypes.c_size_t()
+    _b._check(getattr(_b.lib(), name)(*args, ctypes.byref(out)), name)
+    return out.value
+
+
+# ----------------------------------------------------------------- dropout
+
+def tt_dropout(params, rows, cols, k, dtype, tX, tY, X, Y, stream=None):
+    fn = _fn("tt_dropout")
+    _b._check(_b._calls.dropout(fn, params, rows, cols, k, dtype, tX, tY, X, Y, _b._stream(stream)), "tt_dropout")
+
+
+# -------------------------------------------------- residual sum and its norm
+
+def tt_norm_forward(rows, width, k, dtype, tX, tY, eps, X, R, gain, H, Y, params=None, stream=None):
+    """params: the dropout of X, or None"""
+    fn = _fn("tt_norm_forward")
+    _b._check(_b._calls.norm_forward(fn, rows, width, k, dtype, tX, tY, eps, params, X, R, gain, H, Y, _b._stream(stream)), "tt_norm_forward")
+
+
+def tt_norm_workspace_bytes(rows, width, k, dtype, tX, tdY=None):
+    i = ctypes.c_int64
+    return _sized("tt_norm_workspace_bytes", i(rows), i(width), k, _b._dtype(dtype), _b._tiling(tX), _b._t_or(tdY, tX))
+
+
+def tt_norm_backward(rows, width, k, dtype, tX, tdY, eps, H, gain, dY, dH, dS, dX, dgain, workspace=None, params=None, stream=None):
+    fn = _fn("tt_norm_backward")
+    _b._check(_b._calls.norm_backward(fn, rows, width, k, dtype, tX, tdY, eps, params, H, gain, dY, dH, dS, dX, dgain, workspace, _b._stream(stream)),
+              "tt_norm_backward")
+
+
+# ------------------------------------------------------- rows in 8 bits
+
+def tt_pitch8(cols):
+    f = _b.lib().tt_pitch8
+    f.restype, f.argtypes = ctypes.c_int64, [ctypes.c_int64]
+    return f(cols)
+
+
+def tt_rows8(rows, cols, k, dtype, tX, tQ, X, Q, S, stream=None):
+    fn = _fn("tt_rows8")
+    _b._check(_b._calls.rows8(fn, rows, cols, k, dtype, tX, tQ, X, Q, S, _b._stream(stream)), "tt_rows8")
+
+
+def tt_unrows8(rows, cols, k, dtype, tQ, tX, Q, S, X, stream=None):
+    fn = _fn("tt_unrows8")
+    _b._check(_b._calls.unrows8(fn, rows, cols, k, dtype, tQ, tX, Q, S, X, _b._stream(stream)), "tt_unrows8")
+
+
+def tt_norm_forward8(rows, width, k, dtype, tX, tQ, eps, X, R, gain, H, Q, S, stream=None):
+    fn = _fn("tt_norm_forward8")
+    _b._check(_b._calls.norm_forward8(fn, rows, width, k, dtype, tX, tQ, eps, X, R, gain, H, Q, S, _b._stream(stream)), "tt_norm_forward8")
+
+
+# ------------------------------------------------ fully-connected layer in 8 bits
+
+def tt_weights8_workspace_bytes(n_in, n_out, k, tW):
+    i = ctypes.c_int64
+    return _sized("tt_weights8_workspace_bytes", i(n_in), i(n_out), k, _b._tiling(tW))
+
+
+def tt_weights8(n_in, n_out, k, dtype, tW, W, Q, S, workspace=None, stream=None):
+    fn = _fn("tt_weights8")
+    _b._check(_b._calls.weights8(fn, n_in, n_out, k, dtype, tW, W, Q, S, workspace, _b._stream(stream)), "tt_weights8")
+
+
+def tt_fc8_workspace_bytes(lay, batch, k, dtype, tX, tW, tY):
+    t = _b._tiling
+    return _sized("tt_fc8_workspace_bytes", ctypes.byref(lay), ctypes.c_int64(batch), k, _b._dtype(dtype), t(tX), t(tW), t(tY))
+
+
+def tt_fc_forward8(lay, batch, k, dtype, tX, tW, tY, XQ, XS, WQ, WS, Y, workspace=None, stream=None):
+    fn = _fn("tt_fc_forward8")
+    _b._check(_b._calls.forward8(fn, lay, batch, k, dtype, tX, tW, tY, XQ, XS, WQ, WS, Y, workspace, _b._stream(stream)), "tt_fc_forward8")

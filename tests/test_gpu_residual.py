@@ -1,0 +1,521 @@
+"""What stands between the layers of a residual block, against its plain 64-bit forms.
+
+Bounds, from the arithmetic the kernels are said to do (eps = 2^-24, half a step of fp32 next to 1; a bf16 result adds half a step of
+bf16, which has 8 significant bits: 2^-8 of its value):
+  dropout     the factor and one product: 2 eps of the value
+  sum         dropout's product, an addition: 2 eps |dropped| + eps |sum|
+  norm        the sum of squares is one of chains of at most 512 additions of rounded squares and a tree of 10 over them (all terms above 0:
+              its relative error is at most 524 eps, the root's half of that), division, root, and the products: 270 eps of the value
+  gradient    n to 268 eps; c: a sum of such chains over terms of both signs, (526 + 268) eps of the mean of magnitudes; three
+              products and two additions of the parts' magnitudes
+  gain's      each term to 270 eps, a sum of at most `rows` of them: (270 + rows) eps of the sum of magnitudes
+  8 bits      steps exact; scales to 270 eps; values one product
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_1805_04170_amd as tt
+import test_gpu_tokens as base
+from oracle import residual as rs
+from oracle import tiling as tl
+from synthetic import normal_f32
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+NORM_EPS = 1e-5
+
+
+def dt_of(dt):
+    return torch.bfloat16 if dt == "bf16" else torch.float32
+
+
+def rounded(a, dt):
+    """values in the type's precision, round to nearest even"""
+    return base.stored(a, dt)[1]
+
+
+def stored_dt(a, dt):
+    return base.stored(a, dt)
+
+
+def vector(a, dt):
+    return base.up(base.stored(a, dt)[0])
+
+
+def drop_of(p, seed, offset, step):
+    if p is None:
+        return None
+    at = None if step is None else base.up(np.array([step], dtype=np.int64))
+    return tt.drop(p, seed, offset, at)
+
+
+def mask_of(T, D, p, seed, offset, step):
+    return rs.keep_mask(T, D, p, seed, offset + (step or 0))
+
+
+def check_dropped(got, X, p, keep, dt, what):
+    want = rs.dropout(X, p, keep)
+    base.check(got, want, (2 * EPS + base.out_eps(dt)) * (1 + EPS) * np.abs(want), what)
+    assert np.all(got[~keep] == 0), what
+
+
+# ----------------------------------------------------------------- dropout
+
+def run_dropout(T, D, dt, p=0.3, tX="", tY="", seed=0x123456789abcdef0, offset=5, step=None, skew=0, special=False):
+    X = normal_f32(T + D, 0, (T, D), 1.0)
+    if special and X.size:
+        X.reshape(-1)[:: 3] = np.inf
+        X.reshape(-1)[1:: 7] = np.nan
+    X, Xf = stored_dt(X, dt)
+    keep = mask_of(T, D, p, seed, offset, step)
+    Y = base.outputs(T, D, tY, dt, skew)
+    tt.tt_dropout(drop_of(p, seed, offset, step), T, D, len(tX), dt, tX, tY, base.shards(X, tX, skew), Y)
+    got = base.full(Y, tY, T, D)
+    if special:
+        want = rs.dropout(Xf, p, keep)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want)) and np.all(got[~keep] == 0)
+        return got
+    check_dropped(got, Xf, p, keep, dt, "Y")
+    return got
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", [(1, 1), (3, 7), (1, 8), (5, 9), (2, 64), (7, 100), (33, 130), (3, 1031), (2, 4096), (1100, 3)])
+def test_dropout(T, D, dt):
+    run_dropout(T, D, dt, step=T)
+
+
+@pytest.mark.parametrize("tX,tY,D", [("R", "C", 24), ("C", "R", 18), ("CC", "RC", 100), ("rC", "Cr", 50), ("CCC", "rrR", 24), ("RR", "RR", 65), ("CCR", "RCC", 152)])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_dropout_does_not_depend_on_the_tilings(tX, tY, D, dt):
+    got = run_dropout(16, D, dt, 0.4, tX, tY, skew=1)
+    assert np.array_equal(got, run_dropout(16, D, dt, 0.4, "", ""))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_dropout_of_what_is_not_a_number(dt):
+    run_dropout(9, 41, dt, 0.5, special=True)
+
+
+def test_dropout_numbers_of_64_bits():
+    # offset + step wraps; both halves of every 64-bit number count
+    for seed, offset, step in [(1 << 63, (1 << 64) - 1, 2), (0xffffffffffffffff, 1 << 32, -1), (0, 0, None), (1 << 32, 0, (1 << 62) + 3)]:
+        run_dropout(4, 40, "f32", 0.5, seed=seed, offset=offset, step=step)
+
+
+def test_dropout_at_the_ends_of_the_probability():
+    X = run_dropout(4, 40, "f32", 0.0)
+    assert np.all(X != 0)
+    run_dropout(40, 64, "f32", 1.0 / 65536)
+    run_dropout(40, 64, "f32", 65535.0 / 65536)
+    run_dropout(4, 40, "f32", 1.0 / 262144)      # (rounds to nothing)
+
+
+def test_dropout_follows_the_probability_it_is_given():
+    T, D, p = 64, 4096, 0.1
+    X = torch.ones((T, D), device=base.DEV)
+    Y = torch.empty_like(X)
+    for at in range(4):
+        tt.tt_dropout(tt.drop(p, 77, at), T, D, 0, "f32", "", "", [X], [Y])
+        P = rs.dropped_below(p) / 65536.0
+        n = float((Y == 0).sum().item())
+        assert abs(n - T * D * P) < 6 * (T * D * P * (1 - P)) ** 0.5     # (6 standard deviations of the number dropped)
+
+
+# -------------------------------------------------- residual sum and its norm
+
+def norm_inputs(T, D, seed, dt, res, size=1.0):
+    X, Xf = stored_dt(normal_f32(seed, 0, (T, D), size), dt)
+    R, Rf = stored_dt(normal_f32(seed, 1, (T, D), 2.0 * size), dt) if res else (None, np.zeros((T, D)))
+    return X, Xf, R, Rf
+
+
+def gain_of(D, seed, dt, given):
+    if not given:
+        return None, np.ones(D)
+    bits, g = stored_dt(1.0 + normal_f32(seed, 7, (D,), 0.3), dt)
+    return base.up(bits), g
+
+
+def run_norm(T, D, dt, tX="", tY="", p=None, res=True, gain=True, keep_sum=True, seed=3, skew=0, size=1.0, eps=NORM_EPS):
+    X, Xf, R, Rf = norm_inputs(T, D, seed, dt, res, size)
+    g, gf = gain_of(D, seed, dt, gain)
+    Y, H = base.outputs(T, D, tY, dt, skew), base.outputs(T, D, tX, dt, skew) if keep_sum else None
+    keep = mask_of(T, D, p, 99, 1, 2) if p else np.ones((T, D), dtype=bool)
+    tt.tt_norm_forward(T, D, len(tX), dt, tX, tY, eps, base.shards(X, tX, skew), base.shards(R, tX, skew) if res else None, g, H, Y, drop_of(p, 99, 1, 2))
+    dropped = rs.dropout(Xf, p, keep) if p else Xf
+    total = Rf + dropped
+    if keep_sum:
+        held = base.full(H, tX, T, D).astype(np.float64)
+        err = (2 * EPS if p else 0.0) * np.abs(dropped) + EPS * np.abs(total)
+        base.check(held, total, err + base.out_eps(dt) * (np.abs(total) + err), "H")
+    else:
+        held = rounded(total, dt)
+    e32 = float(np.float32(eps))
+    want = rs.norm(held, gf, e32)[0]
+    err = 270 * EPS * np.abs(want)
+    got = base.full(Y, tY, T, D)
+    base.check(got, want, err + base.out_eps(dt) * (np.abs(want) + err) + 2.0 ** -133, "Y")
+    return got
+
+
+WIDTHS = [(1, 1), (2, 5), (3, 8), (37, 40), (5, 64), (9, 100), (6, 512), (3, 520), (4, 1000), (3, 1500), (2, 4096), (2, 8200), (2, 16392), (1, 33000)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", WIDTHS)
+def test_norm(T, D, dt):
+    run_norm(T, D, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("p,res,gain,keep_sum", [(0.3, True, True, True), (0.3, False, False, True), (None, False, True, False), (None, False, False, True), (0.0, True, True, True)])
+def test_norm_forms(p, res, gain, keep_sum, dt):
+    for T, D in [(5, 20), (3, 777), (2, 1031)]:
+        run_norm(T, D, dt, "", "", p, res, gain, keep_sum)
+
+
+TILINGS = [("R", "C", 24), ("C", "R", 18), ("CC", "RC", 1000), ("rC", "Cr", 50), ("CCC", "rrR", 24), ("RR", "RR", 65), ("CCR", "RCC", 4160), ("CCC", "CCR", 16640)]
+
+
+@pytest.mark.parametrize("tX,tY,D", TILINGS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_norm_does_not_depend_on_the_tilings(tX, tY, D, dt):
+    got = run_norm(8, D, dt, tX, tY, 0.25 if D < 5000 else None, skew=1)
+    one = run_norm(8, D, dt, "", "", 0.25 if D < 5000 else None)
+    base.check(got, one, (540 * EPS + 2 * base.out_eps(dt)) * np.abs(one), "tiled")     # (sums run in another order)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-5), (1e-30, 1e-5), (1e-25, 1e-38), (1e36, 1e-38), (1e-12, 1e-24), (1e-37, 1e-12)])
+@pytest.mark.parametrize("D", [40, 1031])
+def test_norm_of_values_whose_squares_leave_fp32(D, size, eps, dt):
+    run_norm(5, D, dt, size=size, eps=eps, res=False)
+
+
+def test_norm_of_zeros_and_of_rows_that_hold_no_numbers():
+    for D in [24, 1000, 40000]:
+        X = normal_f32(1, 0, (4, D), 1.0)
+        X[0] = 0
+        X[1, D // 2] = np.nan
+        X[2, D - 1] = -np.inf
+        Y = base.outputs(4, D, "", "f32")
+        tt.tt_norm_forward(4, D, 0, "f32", "", "", 1e-6, [base.up(X)], None, None, None, Y)
+        got = base.down(Y[0])
+        assert np.all(got[0] == 0) and np.all(np.isnan(got[1:3])) and np.all(np.isfinite(got[3]))
+
+
+# ---------------------------------------------------------------- gradients
+
+def run_norm_backward(T, D, dt, tX="", tY="", p=None, later=True, gain=True, seed=5, skew=0, want_sum=True, want_gain=True, size=1.0, eps=NORM_EPS):
+    H, Hf, dH, dHf = norm_inputs(T, D, seed, dt, later, size)
+    dY, dYf = stored_dt(normal_f32(seed, 4, (T, D), 0.5), dt)
+    if size != 1.0:
+        dHf = np.zeros((T, D))
+        dH = dH if dH is None else np.zeros_like(dH)
+    g, gf = gain_of(D, seed, dt, gain)
+    k = len(tX)
+    dS = base.outputs(T, D, tX, dt, skew) if want_sum else None
+    dX = base.outputs(T, D, tX, dt, skew) if p is not None else None
+    dg = base.empty((D,), torch.float32) if want_gain else None
+    ws = base.workspace(tt.tt_norm_workspace_bytes(T, D, k, dt, tX, tY))
+    args = (base.shards(H, tX, skew), g, base.shards(dY, tY, skew), base.shards(dH, tX, skew) if later else None)
+    tt.tt_norm_backward(T, D, k, dt, tX, tY, eps, *args, dS, dX, dg, ws, drop_of(p, 99, 1, 2))
+    e32 = float(np.float32(eps))
+    want, want_g = rs.norm_backward(Hf, gf, e32, dYf, dHf)
+    r = 1.0 / np.sqrt(np.mean(Hf * Hf, axis=1, keepdims=True) + e32)
+    n = np.abs(Hf * r)
+    mags = r * (np.abs(gf * dYf) + n * np.mean(np.abs(gf * dYf) * n, axis=1, keepdims=True))
+    err = 1100 * EPS * mags + 2 * EPS * (np.abs(dHf) + np.abs(want))
+    if want_sum:
+        base.check(base.full(dS, tX, T, D), want, err + base.out_eps(dt) * (np.abs(want) + err) + 2.0 ** -133, "dS")
+    if p is not None:
+        keep = mask_of(T, D, p, 99, 1, 2)
+        got = base.full(dX, tX, T, D)
+        dropped = rs.dropout(want, p, keep)
+        f = 65536.0 / (65536 - rs.dropped_below(p))
+        bound = f * err + 2 * EPS * np.abs(dropped)
+        base.check(got, dropped, bound + base.out_eps(dt) * (np.abs(dropped) + bound), "dX")
+        assert np.all(got[~keep] == 0)
+    if want_gain:
+        mag = np.sum(np.abs(dYf) * n, axis=0)
+        base.check(base.down(dg), want_g, (270 + T) * EPS * mag + 2.0 ** -149, "dgain")
+        again = base.empty((D,), torch.float32)
+        tt.tt_norm_backward(T, D, k, dt, tX, tY, eps, *args, None, None, again, ws)
+        assert torch.equal(again.view(torch.int32), dg.view(torch.int32))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", WIDTHS)
+def test_norm_backward(T, D, dt):
+    run_norm_backward(T, D, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", [(700, 24), (2600, 8), (600, 520), (300, 2050)])
+def test_norm_backward_of_many_rows(T, D, dt):
+    run_norm_backward(T, D, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("p,later,gain,want_sum,want_gain", [(0.3, True, True, True, True), (0.3, False, False, False, True), (None, False, True, True, False),
+                                                            (None, False, False, False, True), (0.0, True, True, True, True)])
+def test_norm_backward_forms(p, later, gain, want_sum, want_gain, dt):
+    for T, D in [(5, 20), (3, 777), (2, 1031)]:
+        run_norm_backward(T, D, dt, "", "", p, later, gain, want_sum=want_sum, want_gain=want_gain)
+
+
+@pytest.mark.parametrize("tX,tY,D", TILINGS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_norm_backward_tiled(tX, tY, D, dt):
+    run_norm_backward(8, D, dt, tX, tY, 0.25 if D < 5000 else None, skew=1)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-5), (1e-30, 1e-5), (1e-25, 1e-38), (1e36, 1e-38), (1e-12, 1e-24)])
+@pytest.mark.parametrize("D", [40, 1031])
+def test_norm_backward_of_values_whose_squares_leave_fp32(D, size, eps, dt):
+    run_norm_backward(5, D, dt, size=size, eps=eps, later=False)
+
+
+def test_norm_backward_without_rows_is_a_gradient_of_zeros():
+    dg = base.empty((70,), torch.float32)
+    tt.tt_norm_backward(0, 70, 0, "f32", "", "", 1e-5, [0], None, [0], None, None, None, dg, None)
+    assert np.all(base.down(dg) == 0)
+
+
+# ------------------------------------------------------- rows in 8 bits
+
+def empty8(rows, cols, t, skew=0):
+    sr, sc = tl.shard_shape(rows, cols, t)
+    return [base.empty((sr, tt.tt_pitch8(sc)), torch.int8) for _ in range(1 << len(t))]
+
+
+def steps_of(Q, t, rows, cols):
+    """the whole tensor's steps; what lies behind a row's values is zeros"""
+    sc = tl.shard_shape(rows, cols, t)[1]
+    for q in Q:
+        assert not q[:, sc:].any()
+    return tl.untile([q[:, :sc].cpu().contiguous().numpy() for q in Q], t, rows, cols)
+
+
+def check_rows8(Q, S, t, U, root, D, what, bound=270):
+    T = U.shape[0]
+    want_q, most = rs.steps(U)
+    got = steps_of(Q, t, T, D)
+    assert np.array_equal(got, want_q), (what, np.argwhere(got != want_q)[:4])
+    want_s = most * root / 127.0
+    s = base.down(S)
+    assert np.array_equal(np.isnan(s), np.isnan(want_s))
+    fine = np.isfinite(want_s)
+    base.check(s[fine], want_s[fine], bound * EPS * np.abs(want_s[fine]) + 2.0 ** -149, what + " scales")
+
+
+def run_rows8(T, D, dt, tX="", tQ="", seed=11, skew=0, values=None, back=""):
+    X, Xf = stored_dt(normal_f32(seed, 0, (T, D), 1.5) if values is None else values, dt)
+    Q, S = empty8(T, D, tQ), base.empty((T,), torch.float32)
+    tt.tt_rows8(T, D, len(tX), dt, tX, tQ, base.shards(X, tX, skew), Q, S)
+    check_rows8(Q, S, tQ, Xf, np.ones(T), D, "rows", 2)
+    Y = base.outputs(T, D, tX, dt, skew)
+    tt.tt_unrows8(T, D, len(tX), dt, tQ, tX, Q, S, Y)
+    want = steps_of(Q, tQ, T, D).astype(np.float64) * base.down(S).astype(np.float64)[:, None]
+    got = base.full(Y, tX, T, D)
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    base.check(got[fine], want[fine], ((EPS + base.out_eps(dt)) * (1 + EPS) * np.abs(want) + 2.0 ** -133)[fine], "values")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", WIDTHS)
+def test_rows8(T, D, dt):
+    run_rows8(T, D, dt)
+
+
+@pytest.mark.parametrize("tX,tY,D", TILINGS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows8_tiled(tX, tY, D, dt):
+    run_rows8(8, D, dt, tX, tY, skew=1)
+
+
+def border_values(D):
+    """rows whose quotients lie on and beside the border of two steps, and rows of unlike sizes"""
+    rows = []
+    for m in (127.0, 254.0, 1.0, 3.0, 2.0 ** -20, 2.0 ** 100 * 127):
+        j = np.arange(D) % 127
+        x = (j + 0.5) * (m / 127.0)
+        x = np.where(np.arange(D) % 3 == 1, np.nextafter(x.astype(np.float32), np.float32(np.inf)), x)
+        x = np.where(np.arange(D) % 3 == 2, np.nextafter(x.astype(np.float32), np.float32(0)), x)
+        x = np.where(np.arange(D) % 2 == 0, x, -x)
+        x[0] = m
+        rows.append(x)
+    rows += [np.zeros(D), np.full(D, 2.0 ** -126), np.where(np.arange(D) % 2, 3e38, -1.0), np.where(np.arange(D) % 5, 2.0 ** -120, 2.0 ** -118)]
+    bad = np.ones(D)
+    bad[D // 2] = np.nan
+    rows.append(bad)
+    worse = np.ones(D)
+    worse[D - 1] = -np.inf
+    rows.append(worse)
+    return np.array(rows, dtype=np.float32)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [5, 127, 700, 9000, 33000])
+def test_rows8_at_the_borders_of_steps(D, dt):
+    v = border_values(D)
+    run_rows8(v.shape[0], D, dt, values=v)
+
+
+def test_rows8_of_denormal_numbers():
+    x = np.full((2, 40), 2.0 ** -140, dtype=np.float32)
+    x[1, ::2] = 2.0 ** -149
+    run_rows8(2, 40, "f32", values=x)
+
+
+def run_norm8(T, D, dt, tX="", tQ="", res=True, gain=True, keep_sum=True, seed=13, skew=0, size=1.0, eps=NORM_EPS, gains=None):
+    X, Xf, R, Rf = norm_inputs(T, D, seed, dt, res, size)
+    g, gf = gain_of(D, seed, dt, gain)
+    if gains is not None:
+        bits, gf = stored_dt(gains, dt)
+        g = base.up(bits)
+    H = base.outputs(T, D, tX, dt, skew) if keep_sum else None
+    Q, S = empty8(T, D, tQ), base.empty((T,), torch.float32)
+    tt.tt_norm_forward8(T, D, len(tX), dt, tX, tQ, eps, base.shards(X, tX, skew), base.shards(R, tX, skew) if res else None, g, H, Q, S)
+    want_h = rounded((Xf + Rf).astype(np.float32), dt)      # (one addition in fp32, one rounding)
+    if keep_sum:
+        assert np.array_equal(base.full(H, tX, T, D).astype(np.float64), want_h)
+    root = 1.0 / np.sqrt(np.mean(want_h * want_h, axis=1) + float(np.float32(eps)))
+    check_rows8(Q, S, tQ, want_h * gf, root, D, "norm8")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", WIDTHS)
+def test_norm8(T, D, dt):
+    run_norm8(T, D, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("res,gain,keep_sum", [(False, True, True), (True, False, False), (False, False, False)])
+def test_norm8_forms(res, gain, keep_sum, dt):
+    for T, D in [(5, 20), (3, 777), (2, 1031)]:
+        run_norm8(T, D, dt, "", "", res, gain, keep_sum)
+
+
+@pytest.mark.parametrize("tX,tY,D", TILINGS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_norm8_tiled(tX, tY, D, dt):
+    run_norm8(8, D, dt, tX, tY, skew=1)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-5), (1e-30, 1e-5), (1e-25, 1e-38), (1e-12, 1e-24)])
+@pytest.mark.parametrize("D", [40, 1031])
+def test_norm8_of_values_whose_squares_leave_fp32(D, size, eps, dt):
+    run_norm8(5, D, dt, size=size, eps=eps, res=False)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("g", [1e-30, 1e30, 0.0])
+def test_norm8_of_large_and_small_gains(g, dt):
+    for D in [40, 1031]:
+        run_norm8(4, D, dt, gains=(g * (1.0 + np.arange(D) % 5)).astype(np.float32))
+        run_norm8(4, D, dt, gains=np.where(np.arange(D) % 3 == 0, 0.0, g * (1.0 + np.arange(D) % 5)).astype(np.float32), size=1e10, res=False)
+
+
+# ------------------------------------------------ weights in 8 bits
+
+def weights8(W, tW, n_in, n_out, dt, skew=0):
+    sr, sc = tl.shard_shape(n_in, n_out, tW)
+    Q = [base.empty((sc, tt.tt_pitch8(sr)), torch.int8) for _ in range(1 << len(tW))]
+    S = base.empty((n_out,), torch.float32)
+    ws = base.workspace(tt.tt_weights8_workspace_bytes(n_in, n_out, len(tW), tW))
+    tt.tt_weights8(n_in, n_out, len(tW), dt, tW, base.shards(W, tW, skew), Q, S, ws)
+    return Q, S
+
+
+def run_weights8(n_in, n_out, dt, tW="", values=None, skew=0):
+    W, Wf = stored_dt(normal_f32(17, 0, (n_in, n_out), 0.3) if values is None else values, dt)
+    Q, S = weights8(W, tW, n_in, n_out, dt, skew)
+    sr = tl.shard_shape(n_in, n_out, tW)[0]
+    for q in Q:
+        assert not q[:, sr:].any()
+    got = tl.untile([q[:, :sr].T.cpu().contiguous().numpy() for q in Q], tW, n_in, n_out)
+    want, most = rs.steps(np.ascontiguousarray(Wf.T))
+    assert np.array_equal(got, want.T)
+    s = base.down(S)
+    assert np.array_equal(np.isnan(s), np.isnan(most))
+    fine = np.isfinite(most)
+    base.check(s[fine], most[fine] / 127.0, 2 * EPS * most[fine] / 127.0 + 2.0 ** -149, "scales")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n_in,n_out", [(1, 1), (5, 3), (64, 64), (65, 130), (200, 66), (130, 300)])
+def test_weights8(n_in, n_out, dt):
+    run_weights8(n_in, n_out, dt)
+
+
+@pytest.mark.parametrize("tW", ["R", "C", "RC", "CRr", "rrC", "CCR"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_weights8_tiled(tW, dt):
+    run_weights8(72, 136, dt, tW, skew=1)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_weights8_at_the_borders_of_steps(dt):
+    v = np.ascontiguousarray(border_values(150).T)
+    run_weights8(v.shape[0], v.shape[1], dt, values=v)
+
+
+# ------------------------------------------------------------ streams and graphs
+
+def test_a_captured_step_takes_the_number_it_finds():
+    T, D, p = 64, 520, 0.2
+    g = torch.Generator(device=base.DEV)
+    g.manual_seed(5)
+    X, R, dY = (torch.randn(T, D, device=base.DEV, generator=g).bfloat16() for _ in range(3))
+    step = torch.zeros(1, dtype=torch.int64, device=base.DEV)
+    d = tt.drop(p, 1234, 10, step)
+    ws = torch.empty(tt.tt_norm_workspace_bytes(T, D, 0, "bf16", "", ""), dtype=torch.uint8, device=base.DEV)
+
+    def out():
+        return [torch.empty_like(X) for _ in range(4)] + [torch.empty(D, device=base.DEV)]
+
+    def call(o):
+        tt.tt_norm_forward(T, D, 0, "bf16", "", "", 1e-5, [X], [R], None, [o[0]], [o[1]], d)
+        tt.tt_norm_backward(T, D, 0, "bf16", "", "", 1e-5, [o[0]], None, [dY], None, [o[2]], [o[3]], o[4], ws, d)
+    held = out()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(held)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(held)
+    seen = []
+    for at in (3, 1 << 40, 3, 4):
+        step.fill_(at)
+        for o in held:
+            o.fill_(-1)
+        graph.replay()
+        eager = out()
+        call(eager)
+        torch.cuda.synchronize()
+        for a, b in zip(held, eager):
+            assert torch.equal(a, b)
+        seen.append(held[3].clone())
+    assert torch.equal(seen[0], seen[2]) and not torch.equal(seen[0], seen[1]) and not torch.equal(seen[0], seen[3])
+
+
+def test_calls_on_another_stream():
+    T, D = 300, 1500
+    X = torch.randn(T, D, device=base.DEV).bfloat16()
+    Q, S, Y = torch.empty(T, tt.tt_pitch8(D), dtype=torch.int8, device=base.DEV), torch.empty(T, device=base.DEV), torch.empty_like(X)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    tt.tt_rows8(T, D, 0, "bf16", "", "", [X], [Q], S, stream=s)
+    tt.tt_unrows8(T, D, 0, "bf16", "", "", [Q], S, [Y], stream=s)
+    s.synchronize()
+    m = X.double().abs().amax(1, keepdim=True)
+    assert torch.all((Y.double() - X.double()).abs() <= m / 127 * 0.5 + 2.0 ** -8 * X.double().abs() + 2.0 ** -8 * m / 127)

@@ -1,0 +1,152 @@
+"""The kernels between the layers of a residual block on the host, in lock step (tests/emu): the GPU tests' own functions on host
+memory whose neighbouring pages cannot be touched, so that an access outside a buffer ends the run."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+import emu_build
+import paper_1805_04170_amd.binding as binding
+import test_gpu_residual as g
+import test_gpu_tokens as base
+
+pytestmark = pytest.mark.skipif(emu_build.CLANG is None, reason="no host clang++ for the emulation build")
+UNITS = ["emu_lib_dropout.cpp", "emu_lib_norm.cpp", "emu_lib_rows8.cpp"]
+
+
+@pytest.fixture(scope="module")
+def emulated_residual(emulators, tmp_path_factory):
+    """these operators built for the host, linked with the emulated library"""
+    out = str(tmp_path_factory.mktemp("emu_residual"))
+    jobs = []
+    for u in UNITS:
+        o = os.path.join(out, u + ".o")
+        cmd = [emu_build.CLANG] + emu_build.BASE + emu_build.LIBRARY_FLAGS + emu_build.INCLUDES + ["-c", os.path.join(emu_build.EMU, u), "-o", o]
+        jobs.append((o, subprocess.Popen(cmd, stderr=subprocess.PIPE, text=True)))
+    for _, p in jobs:
+        err = p.communicate()[1]
+        assert p.returncode == 0, err[-4000:]
+    lib = emulators.get("library")
+    so = os.path.join(out, "libresidual_emulated.so")
+    subprocess.run([emu_build.CLANG, "-shared", "-o", so] + [o for o, _ in jobs] + [lib, "-Wl,-rpath," + os.path.dirname(lib)], check=True)
+    return so
+
+
+@pytest.fixture(autouse=True, params=["end", "front"])
+def on_host(request, emulated_residual, monkeypatch):
+    monkeypatch.setattr(binding, "LIB_PATH", emulated_residual)
+    monkeypatch.setattr(binding, "_lib", None)
+    monkeypatch.setattr(binding, "_stream", lambda stream: ctypes.c_void_p(0))
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a, **k: None)
+    monkeypatch.setattr(base, "DEV", "cpu")
+    monkeypatch.setattr(base, "GUARD", request.param)
+
+
+SIZES = [(1, 1), (2, 5), (3, 8), (37, 40), (9, 100), (3, 520), (2, 777), (1, 8200)]
+TILINGS = [t for t in g.TILINGS if t[2] <= 1000]
+DTYPES = pytest.mark.parametrize("dt", ["bf16", "f32"])
+
+
+@DTYPES
+def test_dropout(dt):
+    for T, D in [(1, 1), (3, 7), (5, 9), (7, 100), (2, 1031), (300, 3)]:
+        g.run_dropout(T, D, dt, step=T)
+    for tX, tY, D in TILINGS[:-1]:
+        g.run_dropout(8, D, dt, 0.4, tX, tY)
+    g.test_dropout_of_what_is_not_a_number(dt)
+
+
+def test_dropout_numbers():
+    g.test_dropout_numbers_of_64_bits()
+    g.test_dropout_at_the_ends_of_the_probability()
+
+
+@DTYPES
+@pytest.mark.parametrize("T,D", SIZES)
+def test_norm(T, D, dt):
+    g.run_norm(T, D, dt, p=0.2 if D < 1000 else None)
+    g.run_norm_backward(T, D, dt, p=0.2 if D < 1000 else None)
+
+
+@DTYPES
+@pytest.mark.parametrize("tX,tY,D", TILINGS)
+def test_norm_tiled(tX, tY, D, dt):
+    g.run_norm(8, D, dt, tX, tY, 0.25 if D < 100 else None)
+    g.run_norm_backward(8, D, dt, tX, tY, 0.25 if D < 100 else None)
+
+
+@DTYPES
+def test_norm_forms(dt):
+    g.run_norm(4, 20, dt, p=0.3, res=False, gain=False)
+    g.run_norm(3, 777, dt, res=False, keep_sum=False)
+    g.run_norm_backward(4, 20, dt, p=0.3, later=False, gain=False, want_sum=False)
+    g.run_norm_backward(3, 777, dt, later=False, want_gain=False)
+
+
+@DTYPES
+def test_norm_backward_of_many_rows(dt):
+    g.run_norm_backward(600, 24, dt)
+    g.run_norm_backward(300, 520, dt)
+
+
+@DTYPES
+@pytest.mark.parametrize("T,D,tX,tY", [(2, 33000, "", ""), (2, 16640, "CCC", "CCR")])
+def test_norm_of_long_rows(T, D, tX, tY, dt):
+    T = max(T, 1 << max(tX.count("R"), tY.count("R")))
+    g.run_norm(T, D, dt, tX, tY)
+    g.run_norm_backward(T, D, dt, tX, tY)
+    g.run_norm8(T, D, dt, tX, tY)
+    g.run_rows8(T, D, dt, tX, tY)
+
+
+@DTYPES
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-5), (1e-25, 1e-38), (1e36, 1e-38)])
+def test_values_whose_squares_leave_fp32(size, eps, dt):
+    for D in (40, 1031):
+        g.run_norm(3, D, dt, size=size, eps=eps, res=False)
+        g.run_norm_backward(3, D, dt, size=size, eps=eps, later=False)
+        if size < 1e36:
+            g.run_norm8(3, D, dt, size=size, eps=eps, res=False)
+
+
+def test_rows_that_hold_no_numbers():
+    g.test_norm_of_zeros_and_of_rows_that_hold_no_numbers()
+    g.test_norm_backward_without_rows_is_a_gradient_of_zeros()
+
+
+@DTYPES
+@pytest.mark.parametrize("T,D", SIZES)
+def test_rows8(T, D, dt):
+    g.run_rows8(T, D, dt)
+    g.run_norm8(T, D, dt)
+
+
+@DTYPES
+@pytest.mark.parametrize("tX,tY,D", TILINGS)
+def test_rows8_tiled(tX, tY, D, dt):
+    g.run_rows8(8, D, dt, tX, tY)
+    g.run_norm8(8, D, dt, tX, tY)
+
+
+@DTYPES
+def test_rows8_at_the_borders_of_steps(dt):
+    for D in (5, 127, 700):
+        g.test_rows8_at_the_borders_of_steps(D, dt)
+    g.test_rows8_of_denormal_numbers()
+
+
+@DTYPES
+@pytest.mark.parametrize("gain", [1e-30, 1e30, 0.0])
+def test_norm8_of_large_and_small_gains(gain, dt):
+    g.test_norm8_of_large_and_small_gains(gain, dt)
+
+
+@DTYPES
+def test_weights8(dt):
+    for n_in, n_out in [(1, 1), (5, 3), (65, 130), (200, 66)]:
+        g.run_weights8(n_in, n_out, dt)
+    for tW in ["R", "C", "RC", "CRr"]:
+        g.run_weights8(72, 136, dt, tW)
+    g.test_weights8_at_the_borders_of_steps(dt)
