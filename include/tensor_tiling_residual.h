@@ -7,10 +7,11 @@
  * overlap any other buffer given to it.  A result does not depend on the tilings, but for the last bits of dgain.
  *
  * Calls with no rows or no columns return TT_OK and write nothing, but for a gain's gradient without rows (zeros) and the scales
- * of rows without columns (0), and a layer of no inputs (zeros); shards of a tensor without values may be NULL.
+ * of rows without columns (0); shards of a tensor without values may be NULL.  (A layer has inputs and outputs, as for tt_fc_forward.)
  * Errors as in tensor_tiling.h: TT_EINVAL (NULL, unknown type or letter, k out of range, negative, misaligned, parameters out of
- * range), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 rows or columns and more; 2^37 values of a dropped tensor; sums of
- * 131072 products of 8-bit integers), TT_EWORKSPACE, TT_EDEVICE. */
+ * range), TT_EINFEASIBLE (uneven cut), TT_EUNSUPPORTED (2^31 rows or columns and more; 2^37 values of a dropped tensor or of one
+ * that comes from 8 bits; 2^21 output channels of a weight that is brought into 8 bits; a layer of 131072 inputs, 2^24 tokens or 2^36
+ * results), TT_EWORKSPACE, TT_EDEVICE. */
 #ifndef TENSOR_TILING_RESIDUAL_H
 #define TENSOR_TILING_RESIDUAL_H
 

@@ -1,0 +1,467 @@
+// Fully-connected layers in 8-bit integers (tt_fc_forward8).  The operands stay where their shards are: one GPU holds all of them, so a
+// tile of the result reads the blocks that it needs, and a cut of K is a change of address between two K tiles instead of a sum
+// of shards' results.
+//
+// Three forms: few rows (a weight's row goes from memory to a wave's registers once, waves share K); tiles through LDS; tiles whose K
+// is cut into parts, for results of too few tiles for the chip, joined by a second launch.
+#include <cstdint>
+#include "launch_util.h"
+#include "fc8_core.h"
+#include "row_walk.h"
+#include "tensor_tiling_residual.h"
+
+namespace tt {
+namespace {
+
+using namespace fc8;
+
+constexpr uint32_t kCUs = 256, kXcds = 8;
+
+struct Layer8Params {
+    Operand A, B;
+    Steps8 s;
+    BlockTable Y;
+    Divisor y_by_scols;
+    const float *XS, *WS;
+    int32_t *parts;       // sums of a part of K: part, row, channel
+    uint32_t M, N, relu;
+    uint32_t tiles_m, tiles_n, cuts;
+    uint32_t np;          // channels of a row of `parts`
+};
+
+__device__ __forceinline__ float activated(int32_t sum, float ws, float xs, uint32_t relu)
+{
+    const float v = (float)sum * ws * xs;
+    return relu && v < 0.0f ? 0.0f : v; // (NaN stays)
+}
+
+// Result (row, n .. n + count - 1) of one block into every replica; VEC: whole 16-byte vectors
+template <typename T> __device__ __forceinline__ void store_result(const Layer8Params &p, uint32_t row, uint32_t n, u32x4 v, bool vec, uint32_t count)
+{
+    const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows);
+    if (vec) {
+        const uint32_t cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols);
+        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (n - cb * p.Y.scols);
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) store16(static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at, v);
+        return;
+    }
+    for (uint32_t e = 0; e < count; ++e) {
+        const uint32_t c = n + e, cb = p.Y.nC == 1 ? 0 : quotient(c, p.y_by_scols);
+        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (c - cb * p.Y.scols);
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) {
+            T *to = static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at;
+            if constexpr (sizeof(T) == 2) store1(to, (uint16_t)(v[e >> 1] >> (16 * (e & 1))));
+            else store1(to, __uint_as_float(v[e]));
+        }
+    }
+}
+
+extern __shared__ __align__(16) char smem8[];
+
+// T: the result's type, or int32_t: sums of a part of K
+template <int WM, int WN, int TM, int TN, bool ONE, typename T>
+__global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Params p)
+{
+    typedef Tile8<WM, WN, TM, TN, ONE> Tile;
+    // workgroups b, b + 8, .. run on one XCD: they get neighbouring tiles
+    const uint32_t tiles = p.tiles_m * p.tiles_n, total = tiles * p.cuts, per = (total + kXcds - 1) / kXcds;
+    const uint32_t at = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+    if (at >= total) return;
+    const uint32_t cut = at / tiles;
+    int tm, tn;
+    core::grouped_tile((int)(at - cut * tiles), (int)p.tiles_m, (int)p.tiles_n, &tm, &tn);
+    const uint32_t first = (uint32_t)((uint64_t)p.s.all * cut / p.cuts), end = (uint32_t)((uint64_t)p.s.all * (cut + 1) / p.cuts);
+    const uint32_t m0 = (uint32_t)tm * Tile::BM, n0 = (uint32_t)tn * Tile::BN;
+    Tile t;
+    t.run(p.A, p.B, p.s, m0, n0, first, end - first, smem8);
+
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+    const uint32_t row0 = m0 + wave / WN * (TM * 16), col0 = n0 + wave % WN * (TN * 16);
+    if constexpr (sizeof(T) == 4 && !__is_same(T, float)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const uint32_t row = row0 + i * 16 + r, col = col0 + j * 16 + q * 4;
+                if (row < p.M && col < p.N) *(TT_GLOBAL i32x4 *)(p.parts + ((size_t)cut * p.M + row) * p.np + col) = t.acc[i][j];
+            }
+    } else {
+        // rows of 16 TN values turned round through a strip of LDS that is the wave's own
+        constexpr uint32_t W = TN * 16, PITCH = W * sizeof(T) + 16, EV = kVec<T>, VPR = W / EV, NV = 16 * VPR / 64;
+        static_assert(WM * WN * 16 * PITCH <= Tile::kSmem && NV >= 1, "strips");
+        char *strip = smem8 + wave * 16 * PITCH;
+        const bool aligned = p.Y.scols % EV == 0;
+        float ws[TN][4];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t col = col0 + j * 16 + q * 4 + e;
+                ws[j][e] = load1(p.WS + (col < p.N ? col : p.N - 1));
+            }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const uint32_t mine = row0 + i * 16 + r;
+            const float xs = load1(p.XS + (mine < p.M ? mine : p.M - 1));
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = activated(t.acc[i][j][e], ws[j][e], xs, p.relu);
+                char *to = strip + r * PITCH + (j * 16 + q * 4) * sizeof(T);
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<core::u32x2 *>(to) = core::u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                else *reinterpret_cast<u32x4 *>(to) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            }
+            __builtin_amdgcn_wave_barrier(); // (a wave's LDS operations execute in order: the compiler alone needs telling)
+#pragma unroll
+            for (uint32_t n = 0; n < NV; ++n) {
+                const uint32_t idx = lane + 64 * n, lrow = idx / VPR, vc = idx % VPR, row = row0 + i * 16 + lrow, col = col0 + vc * EV;
+                const u32x4 o = *reinterpret_cast<const u32x4 *>(strip + lrow * PITCH + vc * 16);
+                if (row < p.M && col < p.N) {
+                    const uint32_t left = p.N - col;
+                    store_result<T>(p, row, col, o, aligned && left >= EV, left < EV ? left : EV);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// the parts' sums joined: four channels a thread
+constexpr uint32_t kJoin = 256;
+template <typename T> __global__ __launch_bounds__(kJoin) void fc8_join_kernel(const Layer8Params p)
+{
+    const uint32_t per_row = p.np / 4;
+    const uint32_t col = (blockIdx.x * kJoin + threadIdx.x) * 4, row = blockIdx.y;
+    if (col >= per_row * 4) return;
+    i32x4 s = {0, 0, 0, 0};
+    for (uint32_t c = 0; c < p.cuts; ++c) s += *(const TT_GLOBAL i32x4 *)(p.parts + ((size_t)c * p.M + row) * p.np + col);
+    const float xs = load1(p.XS + row);
+    const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows);
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+        const uint32_t n = col + e;
+        if (n >= p.N) break;
+        const uint32_t cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols);
+        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (n - cb * p.Y.scols);
+        const T v = from_float<T>(activated(s[e], load1(p.WS + n), xs, p.relu));
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) store1(static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at, v);
+    }
+}
+
+// Few rows: a workgroup takes 16 TN channels and all of K, its eight waves every eighth K tile each.  A wave's loads of a tile are a whole
+// 128-byte line of each of its rows.
+constexpr uint32_t kFew = 512, kFewWaves = kFew / 64;
+constexpr int kFewAhead = 4; // K tiles that are asked for together
+template <int TM, int TN, typename T> __global__ __launch_bounds__(kFew, 2) void fc8_few_kernel(const Layer8Params p)
+{
+    __shared__ __align__(16) int32_t sums[kFewWaves][TM * 16][TN * 16];
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const uint32_t n0 = blockIdx.x * (TN * 16);
+    i32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    RowAt a[TM], b[TN];
+    auto bind = [&](uint32_t seg) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const uint32_t row = i * 16 + r;
+            a[i] = row_at(p.A, p.s, row < p.M ? row : p.M - 1, seg);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const uint32_t n = n0 + j * 16 + r;
+            b[j] = row_at(p.B, p.s, n < p.N ? n : p.N - 1, seg);
+        }
+    };
+    if (p.s.segments == 1) bind(0);
+    for (uint32_t t0 = wave; t0 < p.s.all; t0 += kFewWaves * kFewAhead) {
+        i32x4 x[kFewAhead][TM][2], w[kFewAhead][TN][2];
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) {
+            const uint32_t t = t0 + u * kFewWaves;
+            const At at = at_tile(p.s, t < p.s.all ? t : t0);
+            if (p.s.segments != 1) bind(at.seg);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t off = at.tile * BK8 + h * 64 + q * 16;
+#pragma unroll
+                for (int j = 0; j < TN; ++j) w[u][j][h] = *(const TT_GLOBAL i32x4 *)(b[j].p + (off < b[j].most ? off : b[j].most));
+#pragma unroll
+                for (int i = 0; i < TM; ++i) x[u][i][h] = *(const TT_GLOBAL i32x4 *)(a[i].p + (off < a[i].most ? off : a[i].most));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) {
+            if (t0 + u * kFewWaves >= p.s.all) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][j][h], x[u][i][h], acc[i][j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4 *>(&sums[wave][i * 16 + r][j * 16 + q * 4]) = acc[i][j];
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < TM * 16 * TN * 16; e += kFew) {
+        const uint32_t row = e / (TN * 16), c = e % (TN * 16), n = n0 + c;
+        if (row >= p.M || n >= p.N) continue;
+        int32_t s = 0;
+#pragma unroll
+        for (uint32_t v = 0; v < kFewWaves; ++v) s += sums[v][row][c];
+        const T y = from_float<T>(activated(s, load1(p.WS + n), load1(p.XS + row), p.relu));
+        const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows), cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols);
+        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (n - cb * p.Y.scols);
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) store1(static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at, y);
+    }
+}
+
+// X's rows gathered under the weight's cuts of K (block by block, rows of `pitch` bytes), where the two cuts meet inside 16 bytes
+constexpr uint32_t kGatherRows = 32768; // of a launch
+struct GatherParams {
+    BlockTable X;
+    Divisor x_by_scols;
+    uint32_t x_pitch, M, seg, pitch, blocks;
+    int8_t *to;
+};
+__global__ __launch_bounds__(256) void fc8_gather_kernel(const GatherParams p)
+{
+    const uint32_t u = blockIdx.x * 256 + threadIdx.x, words = p.pitch / 4; // four values a thread
+    if (u >= words * p.blocks) return;
+    const uint32_t block = u / words, i0 = (u - block * words) * 4;
+    for (uint32_t row = blockIdx.y; row < p.M; row += kGatherRows) {
+        const uint32_t rb = p.X.nR == 1 ? 0 : quotient(row, p.X.by_srows);
+        uint32_t w = 0;
+        for (uint32_t e = 0; e < 4; ++e) {
+            if (i0 + e >= p.seg) break;
+            const uint32_t k = block * p.seg + i0 + e, cb = p.X.nC == 1 ? 0 : quotient(k, p.x_by_scols);
+            const int8_t *x = static_cast<const int8_t *>(p.X.p[(rb * p.X.nC + cb) * p.X.nrep]);
+            w |= (uint32_t)(uint8_t)load1(x + (size_t)(row - rb * p.X.srows) * p.x_pitch + (k - cb * p.X.scols)) << (8 * e);
+        }
+        *(TT_GLOBAL uint32_t *)(p.to + ((size_t)block * p.M + row) * p.pitch + i0) = w;
+    }
+}
+
+// ------------------------------------------------------------------------ launches
+
+
+enum Form { kFewRows, kTiles, kBigTiles };
+struct Plan {
+    Form form;
+    uint32_t tiles_m, tiles_n, cuts;
+    size_t gather_bytes, parts_bytes;
+};
+uint32_t tiles_of(int64_t n, int64_t t) { return (uint32_t)((n + t - 1) / t); }
+
+struct Shape8 {
+    int64_t M, N, K;
+    Grid x, w, y;
+    int64_t seg;     // of K, as the product runs
+    bool gather;     // X is gathered first
+};
+Plan plan_of(const Shape8 &g, int64_t M)
+{
+    Plan p{kFewRows, 1, 1, 1, 0, 0};
+    const uint32_t all = (uint32_t)(g.K / g.seg) * tiles_of(g.seg, BK8);
+    if (g.gather) p.gather_bytes = align_up((size_t)M * (size_t)(g.K / g.seg) * (size_t)tt_pitch8(g.seg), 256);
+    if (M <= 64) return p;
+    const uint64_t big = (uint64_t)tiles_of(M, 256) * tiles_of(g.N, 256);
+    if (big >= kCUs * 3 / 4) {
+        p.form = kBigTiles;
+        p.tiles_m = tiles_of(M, 256);
+        p.tiles_n = tiles_of(g.N, 256);
+        return p;
+    }
+    p.form = kTiles;
+    p.tiles_m = tiles_of(M, 128);
+    p.tiles_n = tiles_of(g.N, 128);
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
+    while (tiles * p.cuts * 2 <= 2 * kCUs && all / (p.cuts * 2) >= 4 && p.cuts < 16) p.cuts *= 2;
+    if (p.cuts > 1) p.parts_bytes = align_up((size_t)p.cuts * (size_t)M * (size_t)((g.N + 3) / 4 * 4) * 4, 256);
+    return p;
+}
+
+tt_status shape_of(const tt_layer *layer, int64_t batch, int k, int dtype, const tt_tiling &tX, const tt_tiling &tW, const tt_tiling &tY, Shape8 *g)
+{
+    if (!layer || layer->kind != TT_FC || batch < 0 || layer->n_in <= 0 || layer->n_out <= 0 || (layer->act != TT_ACT_NONE && layer->act != TT_ACT_RELU))
+        return TT_EINVAL;
+    if (!valid_k(k) || !valid_tiling(tX, k) || !valid_tiling(tW, k) || !valid_tiling(tY, k) || !valid_dtype(dtype)) return TT_EINVAL;
+    g->M = batch;
+    g->N = layer->n_out;
+    g->K = layer->n_in;
+    // (a sum of 131072 products of -128 and -128 leaves 32 bits)
+    if (batch >= (int64_t(1) << 24) || !fits31(g->N) || g->K > 131071) return TT_EUNSUPPORTED;
+    if ((uint64_t)tiles_of(g->M, 128) * tiles_of(g->N, 128) >= (uint64_t(1) << 22)) return TT_EUNSUPPORTED;
+    if (!make_grid(tX.cut, k, g->M, g->K, &g->x) || !make_grid(tW.cut, k, g->K, g->N, &g->w) || !make_grid(tY.cut, k, g->M, g->N, &g->y)) return TT_EINFEASIBLE;
+    g->seg = g->x.scols < g->w.srows ? g->x.scols : g->w.srows;
+    g->gather = g->x.scols != g->w.srows && g->seg % 16 != 0;
+    if (g->gather) g->seg = g->w.srows;
+    return TT_OK;
+}
+
+bool whole_blocks(const Operand &o, const Steps8 &s, uint32_t rows)
+{
+    return (o.row_blocks == 1 || o.srows % rows == 0) && (o.k_shift == 0 || s.seg % BK8 == 0);
+}
+
+template <int WM, int WN, int TM, int TN, bool ONE, typename T> tt_status launch_tiles_as(const Layer8Params &p, hipStream_t s)
+{
+    typedef Tile8<WM, WN, TM, TN, ONE> Tile;
+    auto kernel = fc8_tile_kernel<WM, WN, TM, TN, ONE, T>;
+    const tt_status st = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), Tile::kSmem);
+    if (st != TT_OK) return st;
+    const uint32_t total = p.tiles_m * p.tiles_n * p.cuts;
+    hipLaunchKernelGGL(kernel, dim3((total + kXcds - 1) / kXcds * kXcds), dim3(Tile::NT), Tile::kSmem, s, p);
+    return TT_OK;
+}
+template <typename T> tt_status launch_tiles(const Layer8Params &p, Form form, hipStream_t s)
+{
+    if (form == kBigTiles && whole_blocks(p.A, p.s, 256) && whole_blocks(p.B, p.s, 256)) return launch_tiles_as<2, 4, 8, 4, true, T>(p, s);
+    Layer8Params q = p;
+    q.tiles_m = tiles_of(p.M, 128);
+    q.tiles_n = tiles_of(p.N, 128);
+    if (whole_blocks(p.A, p.s, 128) && whole_blocks(p.B, p.s, 128)) return launch_tiles_as<2, 2, 4, 4, true, T>(q, s);
+    return launch_tiles_as<2, 2, 4, 4, false, T>(q, s);
+}
+template <int TM, typename T> void launch_few_as(const Layer8Params &p, hipStream_t s)
+{
+    if (tiles_of(p.N, 32) >= kCUs) hipLaunchKernelGGL((fc8_few_kernel<TM, 2, T>), dim3(tiles_of(p.N, 32)), dim3(kFew), 0, s, p);
+    else hipLaunchKernelGGL((fc8_few_kernel<TM, 1, T>), dim3(tiles_of(p.N, 16)), dim3(kFew), 0, s, p);
+}
+template <typename T> tt_status launch_layer(const Layer8Params &p, Form form, hipStream_t s)
+{
+    if (form == kFewRows) {
+        if (p.M <= 16) launch_few_as<1, T>(p, s);
+        else if (p.M <= 32) launch_few_as<2, T>(p, s);
+        else launch_few_as<4, T>(p, s);
+        return TT_OK;
+    }
+    if (p.cuts == 1) return launch_tiles<T>(p, form, s);
+    const tt_status st = launch_tiles<int32_t>(p, form, s);
+    if (st != TT_OK) return st;
+    hipLaunchKernelGGL((fc8_join_kernel<T>), dim3((p.np / 4 + kJoin - 1) / kJoin, p.M), dim3(kJoin), 0, s, p);
+    return TT_OK;
+}
+
+bool shards_at(const int8_t *const *shards, int k, bool empty)
+{
+    if (!shards || empty) return shards != nullptr;
+    for (int s = 0; s < (1 << k); ++s)
+        if (!shards[s] || reinterpret_cast<uintptr_t>(shards[s]) % 16) return false;
+    return true;
+}
+const void *const *untyped(const int8_t *const *p) { return reinterpret_cast<const void *const *>(p); }
+const void *const *in(void *const *p) { return const_cast<const void *const *>(p); }
+uint32_t log2_of(int64_t v) { return (uint32_t)__builtin_ctzll((unsigned long long)v); }
+
+} // namespace
+} // namespace tt
+
+extern "C" tt_status tt_fc8_workspace_bytes(const tt_layer *layer, int64_t batch, int k, int dtype, tt_tiling tX, tt_tiling tW, tt_tiling tY, size_t *bytes)
+{
+    using namespace tt;
+    Shape8 g;
+    if (!bytes) return TT_EINVAL;
+    const tt_status st = shape_of(layer, batch, k, dtype, tX, tW, tY, &g);
+    if (st != TT_OK) return st;
+    // enough for fewer rows too: where the rows are fewer, K is cut into more parts
+    *bytes = 0;
+    for (int64_t m = batch; m > 0; m = m > 64 * 1024 ? m / 2 : (m - 1) / 64 * 64) {
+        const Plan p = plan_of(g, m);
+        const size_t need = p.gather_bytes + p.parts_bytes;
+        if (need > *bytes) *bytes = need;
+    }
+    return TT_OK;
+}
+
+extern "C" tt_status tt_fc_forward8(const tt_layer *layer, int64_t batch, int k, int dtype, tt_tiling tX, tt_tiling tW, tt_tiling tY,
+                                    const int8_t *const *XQ, const float *XS, const int8_t *const *WQ, const float *WS, void *const *Y,
+                                    void *workspace, size_t ws_bytes, void *stream)
+{
+    using namespace tt;
+    Shape8 g;
+    const tt_status st = shape_of(layer, batch, k, dtype, tX, tW, tY, &g);
+    if (st != TT_OK && st != TT_EINFEASIBLE) return st;
+    const bool empty = batch == 0;
+    const int e = dtype_bytes(dtype);
+    if (!shards_at(XQ, k, empty) || !shards_at(WQ, k, false) || !shards_fit(in(Y), k, e, empty) || (!empty && !aligned_to(XS, 4)) || !aligned_to(WS, 4)) return TT_EINVAL;
+    if (st != TT_OK) return st;
+    if (empty) return TT_OK;
+    const Plan plan = plan_of(g, g.M);
+    const size_t need = plan.gather_bytes + plan.parts_bytes;
+    if (need && (!workspace || ws_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256)) return TT_EWORKSPACE;
+
+    Layer8Params p;
+    BlockTable X, W;
+    make_blocks(untyped(XQ), tX, k, g.M, g.K, &X);
+    make_blocks(untyped(WQ), tW, k, g.K, g.N, &W);
+    make_blocks(in(Y), tY, k, g.M, g.N, &p.Y);
+    for (int i = 0; i < kMaxShards; ++i) {
+        p.A.p[i] = X.p[i];
+        p.B.p[i] = W.p[i];
+    }
+    p.s.seg = (uint32_t)g.seg;
+    p.s.segments = (uint32_t)(g.K / g.seg);
+    p.s.tiles = tiles_of(g.seg, BK8);
+    p.s.by_tiles = divisor(p.s.tiles);
+    p.s.all = p.s.segments * p.s.tiles;
+    p.A.row_blocks = X.nR;
+    p.A.srows = X.srows;
+    p.A.by_srows = X.by_srows;
+    p.A.row_stride = X.nC * X.nrep;
+    p.A.k_stride = X.nrep;
+    p.A.k_shift = log2_of(X.scols / g.seg > 0 ? X.scols / g.seg : 1);
+    p.A.pitch = (uint32_t)tt_pitch8(X.scols);
+    p.A.rows = (uint32_t)g.M;
+    p.B.row_blocks = W.nC;
+    p.B.srows = W.scols;
+    p.B.by_srows = divisor(W.scols);
+    p.B.row_stride = W.nrep;
+    p.B.k_stride = W.nC * W.nrep;
+    p.B.k_shift = log2_of(W.srows / g.seg);
+    p.B.pitch = (uint32_t)tt_pitch8(W.srows);
+    p.B.rows = (uint32_t)g.N;
+    p.y_by_scols = divisor(p.Y.scols);
+    p.XS = XS;
+    p.WS = WS;
+    p.M = (uint32_t)g.M;
+    p.N = (uint32_t)g.N;
+    p.relu = layer->act == TT_ACT_RELU;
+    p.tiles_m = plan.tiles_m;
+    p.tiles_n = plan.tiles_n;
+    p.cuts = plan.cuts;
+    p.np = (p.N + 3) / 4 * 4;
+    p.parts = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + plan.gather_bytes);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint64_t operands = (uint64_t)g.M * g.K + (uint64_t)g.K * g.N, results = (uint64_t)g.M * g.N;
+    ProfileScope scope(stream, TT_K_FC8, 1 << k, g.M, g.N, g.K, operands + results * e * p.Y.nrep, 2 * results * (uint64_t)g.K);
+    if (g.gather) {
+        GatherParams q;
+        q.X = X;
+        q.x_by_scols = divisor(X.scols);
+        q.x_pitch = p.A.pitch;
+        q.M = p.M;
+        q.seg = p.s.seg;
+        q.pitch = (uint32_t)tt_pitch8(g.seg);
+        q.blocks = p.s.segments;
+        q.to = static_cast<int8_t *>(workspace);
+        for (uint32_t b = 0; b < (uint32_t)kMaxShards; ++b) p.A.p[b] = b < q.blocks ? q.to + (size_t)b * p.M * q.pitch : nullptr;
+        p.A.row_blocks = 1;
+        p.A.srows = p.M;
+        p.A.by_srows = divisor(p.M);
+        p.A.row_stride = 0;
+        p.A.k_stride = 1;
+        p.A.k_shift = 0;
+        p.A.pitch = q.pitch;
+        hipLaunchKernelGGL(fc8_gather_kernel, dim3((q.pitch / 4 * q.blocks + 255) / 256, p.M < kGatherRows ? p.M : kGatherRows), dim3(256), 0, s, q);
+    }
+    const tt_status launched = dtype == TT_BF16 ? launch_layer<uint16_t>(p, plan.form, s) : launch_layer<float>(p, plan.form, s);
+    if (launched != TT_OK) return launched;
+    return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
+}

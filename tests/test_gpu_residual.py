@@ -467,6 +467,128 @@ def test_weights8_at_the_borders_of_steps(dt):
     run_weights8(v.shape[0], v.shape[1], dt, values=v)
 
 
+# ------------------------------------------------ layers in 8 bits
+
+def rows_form(q, t):
+    """8-bit shards of whole numbers (rows x cols)"""
+    out = []
+    for s in tl.tile(q, t):
+        held = np.zeros((s.shape[0], tt.tt_pitch8(s.shape[1])), dtype=np.int8)
+        held[:, :s.shape[1]] = s
+        out.append(base.up(held))
+    return out
+
+
+def weights_form(q, t):
+    return [base.up(np.ascontiguousarray(np.pad(s.T, ((0, 0), (0, tt.tt_pitch8(s.shape[0]) - s.shape[0]))))) for s in tl.tile(q, t)]
+
+
+def run_layer8(M, K, N, dt, tX="", tW="", tY="", relu=True, seed=19, skew=0, whole=False, spare=0):
+    rng = np.random.default_rng(seed + M + 3 * K + 7 * N)
+    xq, wq = rng.integers(-128, 128, (M, K)).astype(np.int8), rng.integers(-128, 128, (K, N)).astype(np.int8)
+    if whole:
+        xq[:], wq[:] = -128, -128
+    xs, ws = (0.01 + rng.random(M)).astype(np.float32), (0.001 + 0.01 * rng.random(N)).astype(np.float32)
+    lay = tt.layer("fc", "relu" if relu else "none", K, N)
+    Y = base.outputs(M, N, tY, dt, skew)
+    need = tt.tt_fc8_workspace_bytes(lay, M + spare, len(tX), dt, tX, tW, tY)
+    space = base.workspace(need)
+    tt.tt_fc_forward8(lay, M, len(tX), dt, tX, tW, tY, rows_form(xq, tX), base.up(xs), weights_form(wq, tW), base.up(ws), Y, space)
+    want = rs.layer8(xq, xs.astype(np.float64), wq, ws.astype(np.float64), relu)
+    base.check(base.full(Y, tY, M, N), want, (3 * EPS + base.out_eps(dt)) * (1 + 4 * EPS) * np.abs(want), "Y")
+
+
+LAYERS = [(1, 1, 1), (1, 5, 3), (3, 128, 16), (16, 200, 40), (17, 64, 33), (40, 130, 70), (64, 1000, 50), (65, 100, 60), (100, 257, 129), (130, 128, 128), (129, 640, 200)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", LAYERS + [(16, 4096, 8200), (300, 3000, 1000), (2049, 256, 4100), (4000, 300, 3001)])
+def test_layer8(M, K, N, dt):
+    run_layer8(M, K, N, dt, relu=M % 2 == 0)
+
+
+CUTS = [("R", "C", "R", 8, 64, 32), ("C", "R", "C", 20, 256, 40), ("C", "R", "r", 70, 36, 40), ("C", "C", "R", 130, 256, 136), ("CC", "RC", "CR", 132, 64, 264), ("CC", "RC", "Cr", 20, 52, 24),
+        ("rr", "RR", "RC", 68, 192, 36), ("RC", "CR", "CC", 72, 96, 72), ("CCC", "RRR", "CCr", 136, 1040, 144), ("CCC", "RRC", "RRR", 16, 72, 40), ("RRR", "CCC", "rrr", 264, 130, 80),
+        ("CCC", "CCR", "RCC", 264, 512, 264)]
+
+
+@pytest.mark.parametrize("tX,tW,tY,M,K,N", CUTS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_layer8_tiled(tX, tW, tY, M, K, N, dt):
+    run_layer8(M, K, N, dt, tX, tW, tY, skew=1)
+
+
+@pytest.mark.parametrize("tX,tW,tY", [("R", "C", "R"), ("C", "R", "C"), ("CR", "RC", "CC")])
+def test_layer8_tiled_large(tX, tW, tY):
+    run_layer8(2048, 512, 6144, "bf16", tX, tW, tY)
+    run_layer8(512, 2048, 1024, "bf16", tX, tW, tY)
+
+
+def test_layer8_of_the_largest_sums():
+    run_layer8(4, 131071, 20, "f32", whole=True)
+    run_layer8(130, 131071, 130, "f32", whole=True)
+
+
+def test_layer8_workspace_covers_fewer_rows():
+    for M in (65, 128, 129, 200, 256):
+        run_layer8(M, 1024, 130, "f32", spare=300 - M)
+
+
+def test_layer8_scales_that_are_not_numbers():
+    for M in (4, 70):
+        q, w = np.ones((M, 64), dtype=np.int8), np.ones((64, 32), dtype=np.int8)
+        xs, ws = np.ones(M, dtype=np.float32), np.ones(32, dtype=np.float32)
+        xs[1], ws[3] = np.nan, np.nan
+        lay = tt.layer("fc", "relu", 64, 32)
+        Y = base.outputs(M, 32, "", "f32")
+        tt.tt_fc_forward8(lay, M, 0, "f32", "", "", "", rows_form(q, ""), base.up(xs), weights_form(w, ""), base.up(ws), Y,
+                          base.workspace(tt.tt_fc8_workspace_bytes(lay, M, 0, "f32", "", "", "")))
+        got = base.down(Y[0])
+        nan = np.zeros((M, 32), dtype=bool)
+        nan[1], nan[:, 3] = True, True
+        assert np.array_equal(np.isnan(got), nan) and np.all(got[~nan] == 64.0)
+
+
+def run_chain8(T, D, F, dt, tX, tW1, tH, tW2, tY):
+    """a block as it answers: the residual's norm in 8 bits, a layer with ReLU, its output in 8 bits, a layer back"""
+    k = len(tX)
+    X, Xf, R, Rf = norm_inputs(T, D, 23, dt, True)
+    g, gf = gain_of(D, 23, dt, True)
+    W1, W1f = stored_dt(normal_f32(23, 5, (D, F), D ** -0.5), dt)
+    W2, W2f = stored_dt(normal_f32(23, 6, (F, D), F ** -0.5), dt)
+    Q1, S1 = weights8(W1, tW1, D, F, dt)
+    Q2, S2 = weights8(W2, tW2, F, D, dt)
+    H, Q, S = base.outputs(T, D, tX, dt), empty8(T, D, tX), base.empty((T,), torch.float32)
+    tt.tt_norm_forward8(T, D, k, dt, tX, tX, NORM_EPS, base.shards(X, tX), base.shards(R, tX), g, H, Q, S)
+    up, down_ = tt.layer("fc", "relu", D, F), tt.layer("fc", "none", F, D)
+    A, Y = base.outputs(T, F, tH, dt), base.outputs(T, D, tY, dt)
+    tt.tt_fc_forward8(up, T, k, dt, tX, tW1, tH, Q, S, Q1, S1, A, base.workspace(tt.tt_fc8_workspace_bytes(up, T, k, dt, tX, tW1, tH)))
+    QA, SA = empty8(T, F, tH), base.empty((T,), torch.float32)
+    tt.tt_rows8(T, F, k, dt, tH, tH, A, QA, SA)
+    tt.tt_fc_forward8(down_, T, k, dt, tH, tW2, tY, QA, SA, Q2, S2, Y, base.workspace(tt.tt_fc8_workspace_bytes(down_, T, k, dt, tH, tW2, tY)))
+    # what the second layer is given is taken as it was computed; each stage is held to its own bound
+    h = base.full(H, tX, T, D).astype(np.float64)
+    n, _ = rs.norm(h, gf, float(np.float32(NORM_EPS)))
+    q1, m1 = rs.steps(np.ascontiguousarray(W1f.T))
+    w1 = (q1 * (m1 / 127.0)[:, None]).T
+    a = np.maximum(n @ w1, 0.0)
+    step = np.max(np.abs(n), axis=1, keepdims=True) / 127.0
+    got = base.full(A, tH, T, F).astype(np.float64)
+    # the norm's values are off by half a step each: sums of D of them by at most half a step of the weights' magnitudes
+    base.check(got, a, 0.5 * step * np.sum(np.abs(w1), axis=0)[None, :] * (1 + 1e-4) + (base.out_eps(dt) + 1e-5) * np.abs(a), "first layer")
+    q2, m2 = rs.steps(np.ascontiguousarray(W2f.T))
+    qa, ma = rs.steps(got)
+    want = rs.layer8(qa, ma / 127.0, q2.T, m2 / 127.0, False)
+    base.check(base.full(Y, tY, T, D), want, (7 * EPS + base.out_eps(dt)) * (1 + 8 * EPS) * np.abs(want), "second layer")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D,F,t", [(3, 72, 200, ("", "", "", "", "")), (72, 264, 520, ("", "", "", "", "")), (16, 64, 128, ("C", "R", "C", "R", "R")),
+                                     (72, 128, 256, ("RC", "CR", "CC", "RR", "rC")), (40, 72, 104, ("CCC", "RRC", "RCC", "CRR", "CCR"))])
+def test_a_block_in_8_bits(T, D, F, t, dt):
+    run_chain8(T, D, F, dt, *t)
+
+
 # ------------------------------------------------------------ streams and graphs
 
 def test_a_captured_step_takes_the_number_it_finds():

@@ -13,7 +13,7 @@ import test_gpu_residual as g
 import test_gpu_tokens as base
 
 pytestmark = pytest.mark.skipif(emu_build.CLANG is None, reason="no host clang++ for the emulation build")
-UNITS = ["emu_lib_dropout.cpp", "emu_lib_norm.cpp", "emu_lib_rows8.cpp"]
+UNITS = ["emu_lib_dropout.cpp", "emu_lib_norm.cpp", "emu_lib_rows8.cpp", "emu_lib_fc8.cpp"]
 
 
 @pytest.fixture(scope="module")
@@ -150,3 +150,33 @@ def test_weights8(dt):
     for tW in ["R", "C", "RC", "CRr"]:
         g.run_weights8(72, 136, dt, tW)
     g.test_weights8_at_the_borders_of_steps(dt)
+
+
+@DTYPES
+@pytest.mark.parametrize("M,K,N", g.LAYERS)
+def test_layer8(M, K, N, dt):
+    g.run_layer8(M, K, N, dt, relu=M % 2 == 0)
+
+
+@pytest.mark.parametrize("tX,tW,tY,M,K,N", [c for c in g.CUTS if c[3] * c[4] * c[5] < 2e7])
+@DTYPES
+def test_layer8_tiled(tX, tW, tY, M, K, N, dt):
+    g.run_layer8(M, K, N, dt, tX, tW, tY)
+
+
+@DTYPES
+def test_layer8_of_many_tiles(dt):
+    g.run_layer8(600, 130, 3100, dt)     # tiles of 128 x 128
+    if dt == "bf16":
+        g.run_layer8(2050, 128, 5400, dt)    # tiles of 256 x 256
+
+
+def test_layer8_in_parts():
+    g.test_layer8_workspace_covers_fewer_rows()
+    g.test_layer8_scales_that_are_not_numbers()
+
+
+@DTYPES
+@pytest.mark.parametrize("T,D,F,t", [(3, 72, 200, ("", "", "", "", "")), (16, 64, 128, ("C", "R", "C", "R", "R")), (40, 72, 104, ("CCC", "RRC", "RCC", "CRR", "CCR"))])
+def test_a_block_in_8_bits(T, D, F, t, dt):
+    g.run_chain8(T, D, F, dt, *t)
