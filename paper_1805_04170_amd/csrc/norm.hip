@@ -574,7 +574,8 @@ extern "C" tt_status tt_norm_backward(int64_t rows, int64_t width, int k, int dt
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 strips((uint32_t)((width + 63) / 64)), threads(kMostThreads);
     if (empty) { // a gradient of zeros: the sum of no rows
-        if (dgain) hipLaunchKernelGGL(norm_gain_kernel, strips, threads, 0, s, static_cast<const float *>(nullptr), 0u, (uint32_t)width, dgain);
+        if (!dgain) return TT_OK;
+        hipLaunchKernelGGL(norm_gain_kernel, strips, threads, 0, s, static_cast<const float *>(nullptr), 0u, (uint32_t)width, dgain);
         return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
     }
     const GradLaunch g = grad_launch(p.r, rows);

@@ -1,0 +1,219 @@
+"""CPU-side checks of the operators between the layers of a residual block: exported symbols, refusals (nothing is launched),
+workspace sizes, the generator's published outputs, and the plain 64-bit forms against differences."""
+import ctypes
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1805_04170_amd as tt
+from oracle import residual as rs
+from test_tokens_cpu import A, Asked, Bytes, P, P2, refused
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+T31 = 1 << 31
+
+
+def test_every_declared_symbol_is_exported_and_bound():
+    header = open(os.path.join(ROOT, "include", "tensor_tiling_residual.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = set(re.findall(r"\b(tt_[a-z0-9_]+)\s*\(", header))
+    assert declared == set(tt.RESIDUAL_EXPORTS)
+    L = ctypes.CDLL(tt.binding.LIB_PATH)
+    for name in declared:
+        assert hasattr(L, name) and hasattr(tt, name), name
+
+
+# ----------------------------------------------------------------- dropout
+
+def test_generator_gives_its_published_outputs():
+    assert rs.philox((0, 0, 0, 0), (0, 0)) == [0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8]
+    assert rs.philox([0xffffffff] * 4, [0xffffffff] * 2) == [0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd]
+    assert rs.philox((0x243f6a88, 0x85a308d3, 0x13198a2e, 0x03707344), (0xa4093822, 0x299f31d0)) == [0xd16cfe09, 0x94fdcceb, 0x5001e420, 0x24126ea1]
+
+
+def test_dropout_refusals():
+    ok = tt.drop(0.5, 1)
+    f = lambda p=ok, T=8, D=8, k=0, dt="f32", tX="", tY="", X=P, Y=P: tt.tt_dropout(p, T, D, k, dt, tX, tY, X, Y, stream=1)  # noqa: E731
+    for bad in (dict(p=None), dict(p=tt.drop(-0.1, 1)), dict(p=tt.drop(1.0, 1)), dict(p=tt.drop(math.nan, 1)), dict(p=tt.drop(65535.5 / 65536, 1)), dict(p=tt.drop(math.inf, 1)),
+                dict(p=tt.drop(0.5, 1, 0, A + 4)), dict(T=-1), dict(D=-1), dict(k=7), dict(k=-1), dict(dt=5), dict(X=None), dict(Y=None), dict(X=[0]), dict(Y=[A + 2]),
+                dict(dt="bf16", X=[A + 1]), dict(k=1, tX="X", tY="R", X=P2, Y=P2), dict(k=1, tX="R", tY="R", X=P2, Y=P)):
+        refused("TT_EINVAL", f, **bad)
+    refused("TT_EINFEASIBLE", f, T=9, k=1, tX="R", tY="r", X=P2, Y=P2)
+    refused("TT_EINFEASIBLE", f, D=9, k=1, tX="r", tY="C", X=P2, Y=P2)
+    for bad in (dict(T=T31), dict(D=T31), dict(T=1 << 20, D=1 << 17), dict(T=T31 - 1, D=64)):
+        refused("TT_EUNSUPPORTED", f, **bad)
+    f(T=0)
+    f(D=0, X=[0], Y=[0])
+    with pytest.raises(tt.TilingError):
+        tt.drop(0.5, 1, 0, torch.zeros(1))          # a step that is no 64-bit number
+    with pytest.raises(tt.TilingError):
+        tt.drop(0.5, 1, 0, torch.zeros(0, dtype=torch.int64))
+    d = tt.drop(0.5, -1, 1 << 64)
+    assert d.seed == (1 << 64) - 1 and d.offset == 0
+
+
+def test_an_oracle_mask_with_a_mistake_is_told_apart():
+    keep = rs.keep_mask(8, 64, 0.5, 7, 9)
+    for other in (rs.keep_mask(8, 64, 0.5, 8, 9), rs.keep_mask(8, 64, 0.5, 7, 10), rs.keep_mask(8, 64, 0.5, 7 + (1 << 32), 9), rs.keep_mask(8, 64, 0.5, 7, 9 + (1 << 32))):
+        assert 0.3 < np.mean(keep != other) < 0.7
+
+
+# -------------------------------------------------- residual sum and its norm
+
+def test_norm_refusals():
+    one = tt.drop(0.5, 1)
+    f = lambda T=8, D=8, k=0, dt="f32", tX="", tY="", eps=1e-5, X=P, R=P, g=A, H=P, Y=P, d=None: tt.tt_norm_forward(  # noqa: E731
+        T, D, k, dt, tX, tY, eps, X, R, g, H, Y, d, stream=1)
+    for bad in (dict(T=-1), dict(D=-1), dict(k=7), dict(dt=3), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(X=None), dict(X=[0]), dict(R=[0]),
+                dict(H=[A + 2]), dict(Y=None), dict(Y=[A + 1]), dict(g=A + 2), dict(dt="bf16", g=A + 1), dict(d=tt.drop(2.0, 1)), dict(k=1, tX="R", tY="q", X=P2, R=P2, H=P2, Y=P2),
+                dict(k=1, tX="R", tY="R", X=P2, R=P, H=P2, Y=P2), dict(g=torch.zeros(8, dtype=torch.bfloat16)), dict(g=torch.zeros(7)), dict(g=torch.zeros(16)[::2]),
+                dict(dt="bf16", g=torch.zeros(8)), dict(dt="bf16", g=Asked(torch.zeros(8))), dict(g=Asked(torch.zeros(8, dtype=torch.bfloat16)))):
+        refused("TT_EINVAL", f, **bad)
+    refused("TT_EINFEASIBLE", f, D=9, k=1, tX="C", tY="R", X=P2, R=P2, H=P2, Y=P2)
+    refused("TT_EINFEASIBLE", f, T=9, k=1, tX="C", tY="R", X=P2, R=P2, H=P2, Y=P2)
+    refused("TT_EUNSUPPORTED", f, T=T31)
+    refused("TT_EUNSUPPORTED", f, D=T31)
+    f(T=0, d=one)
+    f(D=0, X=[0], R=None, g=None, H=None, Y=[0])
+    f(D=0, g=torch.zeros(0, dtype=torch.bfloat16))
+
+
+def test_norm_gradient_refusals():
+    one = tt.drop(0.5, 1)
+    need = tt.tt_norm_workspace_bytes(8, 16, 0, "f32", "", "")
+    assert need > 0
+    f = lambda T=8, D=16, k=0, dt="f32", tX="", tY="", eps=1e-5, H=P, g=A, dY=P, dH=P, dS=P, dX=P, dg=A, ws=Bytes(need), d=one: tt.tt_norm_backward(  # noqa: E731
+        T, D, k, dt, tX, tY, eps, H, g, dY, dH, dS, dX, dg, ws, d, stream=1)
+    for bad in (dict(T=-1), dict(D=-1), dict(k=7), dict(dt=3), dict(eps=0.0), dict(H=None), dict(H=[0]), dict(dY=None), dict(dY=[A + 2]), dict(dH=[0]), dict(dS=[A + 2]), dict(dX=[0]),
+                dict(d=None), dict(d=tt.drop(-1.0, 1)), dict(dg=A + 2), dict(g=A + 2), dict(dg=torch.zeros(15)), dict(dg=torch.zeros(16, dtype=torch.float64)),
+                dict(k=1, tX="R", tY="z", H=P2, dY=P2, dH=P2, dS=P2, dX=P2)):
+        refused("TT_EINVAL", f, **bad)
+    refused("TT_EINFEASIBLE", f, D=9, k=1, tX="C", tY="R", H=P2, dY=P2, dH=P2, dS=P2, dX=P2)
+    refused("TT_EUNSUPPORTED", f, T=T31)
+    for ws in (None, Bytes(need - 1), Bytes(need, A + 128)):
+        refused("TT_EWORKSPACE", f, ws=ws)
+    f(D=0, dg=None)
+    f(T=0, dg=None, ws=None)
+    f(dS=None, dX=None, dg=None)
+    refused("TT_EINVAL", tt.tt_norm_workspace_bytes, 8, 16, 1, "f32", "R", "z")
+    refused("TT_EINFEASIBLE", tt.tt_norm_workspace_bytes, 8, 17, 1, "f32", "R", "C")
+
+
+def test_workspaces_cover_fewer_rows():
+    for D, dt, tX, tY in [(8, "f32", "", ""), (1000, "bf16", "", ""), (4096, "bf16", "C", "r"), (40000, "f32", "", ""), (24, "bf16", "CC", "CC")]:
+        last = 0
+        for T in [0, 1, 2, 8, 64, 200, 256, 1000, 2048, 2056, 4096, 8192, 100000, 1 << 20]:
+            now = tt.tt_norm_workspace_bytes(T, D, len(tX), dt, tX, tY)
+            assert now >= last
+            last = now
+    for K, N in [(128, 64), (4096, 1000), (8192, 8192), (131071, 300)]:
+        lay = tt.layer("fc", "none", K, N)
+        last = 0
+        for M in list(range(0, 700, 13)) + [1000, 1024, 2000, 4096, 10000, 1 << 17, 1 << 20]:
+            now = tt.tt_fc8_workspace_bytes(lay, M, 0, "f32", "", "", "")
+            assert now >= last, (K, N, M)
+            last = now
+
+
+# ------------------------------------------------------- rows, weights and layers in 8 bits
+
+def test_pitch():
+    assert [tt.tt_pitch8(c) for c in (0, 1, 128, 129, 1000, T31 - 1)] == [0, 128, 128, 256, 1024, T31]
+    assert tt.tt_pitch8(-1) == -1 and tt.tt_pitch8(T31) == -1
+
+
+def test_rows8_refusals():
+    f = lambda T=8, D=8, k=0, dt="f32", tX="", tQ="", X=P, Q=P, S=A: tt.tt_rows8(T, D, k, dt, tX, tQ, X, Q, S, stream=1)  # noqa: E731
+    b = lambda T=8, D=8, k=0, dt="f32", tX="", tQ="", X=P, Q=P, S=A: tt.tt_unrows8(T, D, k, dt, tQ, tX, Q, S, X, stream=1)  # noqa: E731
+    n = lambda T=8, D=8, k=0, dt="f32", tX="", tQ="", X=P, Q=P, S=A, R=P, g=A, H=P, eps=1e-5: tt.tt_norm_forward8(  # noqa: E731
+        T, D, k, dt, tX, tQ, eps, X, R, g, H, Q, S, stream=1)
+    for call in (f, b, n):
+        for bad in (dict(T=-1), dict(D=-1), dict(k=7), dict(dt=5), dict(X=None), dict(X=[A + 2]), dict(Q=None), dict(Q=[0]), dict(S=None), dict(S=A + 2), dict(S=torch.zeros(7)),
+                    dict(S=torch.zeros(8).double()), dict(k=1, tX="R", tQ="X", X=P2, Q=P2)):
+            refused("TT_EINVAL", call, **bad)
+        k1 = dict(k=1, X=P2, Q=P2) if call is not n else dict(k=1, X=P2, Q=P2, R=P2, H=P2)
+        refused("TT_EINFEASIBLE", call, D=9, tX="R", tQ="C", **k1)
+        refused("TT_EUNSUPPORTED", call, T=T31)
+        refused("TT_EUNSUPPORTED", call, D=T31)
+        call(T=0, S=None)
+    b(D=0, S=None)
+    refused("TT_EUNSUPPORTED", b, T=1 << 20, D=1 << 17)
+    for bad in (dict(eps=0.0), dict(eps=math.nan), dict(R=[0]), dict(g=A + 1), dict(H=[A + 2]), dict(g=torch.zeros(8).double())):
+        refused("TT_EINVAL", n, **bad)
+
+
+def test_weights8_refusals():
+    need = tt.tt_weights8_workspace_bytes(8, 8, 0, "")
+    f = lambda K=8, N=8, k=0, dt="f32", tW="", W=P, Q=P, S=A, ws=Bytes(need): tt.tt_weights8(K, N, k, dt, tW, W, Q, S, ws, stream=1)  # noqa: E731
+    for bad in (dict(K=-1), dict(N=-1), dict(k=7), dict(dt=5), dict(W=None), dict(W=[A + 2]), dict(Q=None), dict(Q=[0]), dict(S=None), dict(S=A + 2), dict(S=torch.zeros(7)),
+                dict(k=1, tW="X", W=P2, Q=P2)):
+        refused("TT_EINVAL", f, **bad)
+    refused("TT_EINFEASIBLE", f, K=9, k=1, tW="R", W=P2, Q=P2)
+    refused("TT_EUNSUPPORTED", f, K=T31)
+    refused("TT_EUNSUPPORTED", f, N=(1 << 21) + 1)
+    for ws in (None, Bytes(need - 1), Bytes(need, A + 128)):
+        refused("TT_EWORKSPACE", f, ws=ws)
+    f(N=0, S=None, ws=None)
+    refused("TT_EINVAL", tt.tt_weights8_workspace_bytes, 8, 8, 1, "z")
+    refused("TT_EINFEASIBLE", tt.tt_weights8_workspace_bytes, 9, 8, 1, "R")
+
+
+def test_layer8_refusals():
+    lay = tt.layer("fc", "relu", 1024, 256)
+    need = tt.tt_fc8_workspace_bytes(lay, 100, 0, "f32", "", "", "")
+    assert need > 0 and tt.tt_fc8_workspace_bytes(lay, 16, 0, "f32", "", "", "") == 0
+    f = lambda l=lay, M=100, k=0, dt="f32", tX="", tW="", tY="", XQ=P, XS=A, WQ=P, WS=A, Y=P, ws=Bytes(need): tt.tt_fc_forward8(  # noqa: E731
+        l, M, k, dt, tX, tW, tY, XQ, XS, WQ, WS, Y, ws, stream=1)
+    for bad in (dict(l=tt.layer("conv2d", "relu", 8, 8, 4, 4, 3, 3, 1)), dict(l=tt.layer("fc", "relu", 0, 8)), dict(l=tt.layer("fc", "relu", 8, 0)), dict(M=-1), dict(k=7), dict(dt=5), dict(XQ=None),
+                dict(XQ=[A + 8]), dict(WQ=[A + 8]), dict(WQ=None), dict(XS=None), dict(XS=A + 2), dict(WS=None), dict(WS=torch.zeros(255)), dict(XS=torch.zeros(99)), dict(Y=[A + 2]),
+                dict(k=1, tX="R", tW="R", tY="?", XQ=P2, WQ=P2, Y=P2)):
+        refused("TT_EINVAL", f, **bad)
+    refused("TT_EINFEASIBLE", f, M=101, k=1, tX="R", tW="R", tY="C", XQ=P2, WQ=P2, Y=P2)
+    for l in (tt.layer("fc", "none", 131072, 8), tt.layer("fc", "none", 8, T31)):
+        refused("TT_EUNSUPPORTED", f, l=l, WS=A)
+    refused("TT_EUNSUPPORTED", f, M=1 << 24)
+    for ws in (None, Bytes(need - 1), Bytes(need, A + 128)):
+        refused("TT_EWORKSPACE", f, ws=ws)
+    f(M=0, XQ=[0], XS=None, Y=[0], ws=None)
+    # cuts of K that meet inside 16 bytes: X is gathered first
+    small = tt.layer("fc", "none", 72, 8)
+    assert tt.tt_fc8_workspace_bytes(small, 16, 1, "f32", "C", "r", "R") > 0 and tt.tt_fc8_workspace_bytes(small, 16, 1, "f32", "C", "R", "R") == 0
+
+
+# ------------------------------------------------------------ the plain forms
+
+def test_norm_gradients_against_differences():
+    rng = np.random.default_rng(3)
+    T, D, p, eps = 4, 11, 0.3, 1e-3
+    X, R, g, dY, dH = rng.normal(size=(T, D)), rng.normal(size=(T, D)), 1 + 0.3 * rng.normal(size=D), rng.normal(size=(T, D)), rng.normal(size=(T, D))
+    keep = rs.keep_mask(T, D, p, 5, 6)
+
+    def loss(X, R, g):
+        H = R + rs.dropout(X, p, keep)
+        return np.sum(dY * rs.norm(H, g, eps)[0]) + np.sum(dH * H)
+    dS, dg = rs.norm_backward(R + rs.dropout(X, p, keep), g, eps, dY, dH)
+    dX = rs.dropout(dS, p, keep)
+    for a, grad, at in ((X, dX, 0), (R, dS, 1), (g, dg, 2)):
+        for i in np.ndindex(a.shape):
+            args = [[X.copy(), R.copy(), g.copy()] for _ in range(2)]
+            args[0][at][i] += 1e-5
+            args[1][at][i] -= 1e-5
+            # (a central difference of steps 1e-5: third derivatives of order 10 / eps^(1/2) give 1e-8, roundings 1e-10)
+            assert abs((loss(*args[0]) - loss(*args[1])) / 2e-5 - grad[i]) < 1e-6, (at, i)
+
+
+def test_steps_are_the_nearest():
+    from fractions import Fraction
+    rng = np.random.default_rng(4)
+    U = rng.normal(size=(6, 50))
+    U[1, :20] = np.arange(20) + 0.5
+    U[1, 20:] = 127.0
+    Q, most = rs.steps(U)
+    for u, q, m in zip(U, Q, most):
+        for x, n in zip(u, q):
+            exact = Fraction(127) * Fraction(x) / Fraction(m)
+            assert abs(exact - int(n)) <= Fraction(1, 2) and (abs(exact - int(n)) != Fraction(1, 2) or n % 2 == 0)
