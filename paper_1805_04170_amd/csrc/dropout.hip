@@ -2,7 +2,7 @@
 #include <cstdint>
 #include "launch_util.h"
 #include "philox.h"
-#include "row_walk.h"
+#include "row_reduce.h"
 
 namespace tt {
 namespace {
@@ -15,6 +15,7 @@ struct DropoutParams {
     DropParams d;
     uint64_t units;   // vectors of the tensor
     uint32_t small;   // they are counted in 31 bits
+    uint32_t once;    // results are stored past the caches
     Divisor by_units; // vectors of a row
 };
 
@@ -36,14 +37,13 @@ template <typename T, bool CUT, bool NARROW> __global__ __launch_bounds__(kThrea
         row[i] = row0 + over;
         v[i] = spot_of<EV>(p.r, j - over * p.r.units);
         x[i] = load_spot<T, NARROW>(p.X, lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row[i], v[i]), v[i]);
-        if (u >= left) v[i].n = 0;
     }
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
         float f[EV];
         unpack16(x[i], f, T());
         drop_values(d, row[i], v[i].q * p.r.s.seg + v[i].at, f);
-        store_spot<T, CUT, NARROW>(p.Y, lane_of<CUT>(p.Y, p.r.s, p.r.s.b_shift, row[i], v[i]), v[i], pack16(f, T()));
+        store_spot<T, CUT, NARROW>(p.Y, lane_of<CUT>(p.Y, p.r.s, p.r.s.b_shift, row[i], v[i]), v[i], pack16(f, T()), p.once);
     }
 }
 
@@ -75,6 +75,7 @@ extern "C" tt_status tt_dropout(const tt_drop *drop, int64_t rows, int64_t cols,
     p.by_units = divisor(p.r.units);
     p.units = (uint64_t)rows * p.r.units;
     p.small = p.units < (uint64_t(1) << 31);
+    p.once = (uint64_t)rows * cols * e * p.Y.nrep >= kOnceBytes;
     if ((uint64_t)rows * (uint64_t)cols >= (uint64_t(1) << 37) || p.units / kVectors >= (uint64_t(1) << 32) - kThreads || p.r.units >= (1u << 31) - kThreads * kVectors)
         return TT_EUNSUPPORTED; // (a launch holds fewer than 2^32 threads)
     ProfileScope scope(stream, TT_K_DROPOUT, 1 << k, rows, cols, e, (uint64_t)rows * cols * e * (1 + p.Y.nrep), 0);

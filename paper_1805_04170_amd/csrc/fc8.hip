@@ -25,6 +25,7 @@ struct Layer8Params {
     const float *XS, *WS;
     int32_t *parts;       // sums of a part of K: part, row, channel
     uint32_t M, N, relu;
+    uint32_t single;      // Y is one block
     uint32_t tiles_m, tiles_n, cuts;
     uint32_t np;          // channels of a row of `parts`
 };
@@ -35,34 +36,47 @@ __device__ __forceinline__ float activated(int32_t sum, float ws, float xs, uint
     return relu && v < 0.0f ? 0.0f : v; // (NaN stays)
 }
 
-// Result (row, n .. n + count - 1) of one block into every replica; VEC: whole 16-byte vectors
-template <typename T> __device__ __forceinline__ void store_result(const Layer8Params &p, uint32_t row, uint32_t n, u32x4 v, bool vec, uint32_t count)
+// Where results of row `row` from channel n on lie: the block's first replica in the table, and how many channels it has from there
+struct Spot8 { uint32_t block, left; size_t at; };
+__device__ __forceinline__ Spot8 spot8(const Layer8Params &p, uint32_t row, uint32_t n)
 {
-    const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows);
-    if (vec) {
-        const uint32_t cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols);
-        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (n - cb * p.Y.scols);
-        for (uint32_t x = 0; x < p.Y.nrep; ++x) store16(static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at, v);
+    const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows), cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols), c = n - cb * p.Y.scols;
+    return {(rb * p.Y.nC + cb) * p.Y.nrep, p.Y.scols - c, (size_t)(row - rb * p.Y.srows) * p.Y.scols + c};
+}
+template <typename T> __device__ __forceinline__ void store_value(T *to, u32x4 v, uint32_t e)
+{
+    if constexpr (sizeof(T) == 2) store1(to + e, (uint16_t)(v[e >> 1] >> (16 * (e & 1))));
+    else store1(to + e, __uint_as_float(v[e]));
+}
+// A vector of results of a row from channel n on, as far as there are channels: into every replica
+template <typename T> __device__ __forceinline__ void store_results(const Layer8Params &p, uint32_t row, uint32_t n, u32x4 v)
+{
+    constexpr uint32_t EV = kVec<T>;
+    if (p.single) { // (one block: its address is a scalar)
+        T *to = static_cast<T *>(p.Y.p[0]) + (size_t)row * p.N + n;
+        if (p.N - n >= EV) store16(to, v);
+        else
+            for (uint32_t e = 0; e < p.N - n; ++e) store_value<T>(to, v, e);
         return;
     }
-    for (uint32_t e = 0; e < count; ++e) {
-        const uint32_t c = n + e, cb = p.Y.nC == 1 ? 0 : quotient(c, p.y_by_scols);
-        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (c - cb * p.Y.scols);
-        for (uint32_t x = 0; x < p.Y.nrep; ++x) {
-            T *to = static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at;
-            if constexpr (sizeof(T) == 2) store1(to, (uint16_t)(v[e >> 1] >> (16 * (e & 1))));
-            else store1(to, __uint_as_float(v[e]));
-        }
+    const Spot8 s = spot8(p, row, n);
+    if (s.left >= EV) {
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) store16(static_cast<T *>(p.Y.p[s.block + x]) + s.at, v);
+        return;
+    }
+    for (uint32_t e = 0; e < EV && n + e < p.N; ++e) {
+        const Spot8 t = spot8(p, row, n + e);
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) store_value<T>(static_cast<T *>(p.Y.p[t.block + x]) + t.at - e, v, e);
     }
 }
 
 extern __shared__ __align__(16) char smem8[];
 
 // T: the result's type, or int32_t: sums of a part of K
-template <int WM, int WN, int TM, int TN, bool ONE, typename T>
+template <int WM, int WN, int TM, int TN, int NS, bool ONE, typename T>
 __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Params p)
 {
-    typedef Tile8<WM, WN, TM, TN, ONE> Tile;
+    typedef Tile8<WM, WN, TM, TN, NS, ONE> Tile;
     // workgroups b, b + 8, .. run on one XCD: they get neighbouring tiles
     const uint32_t tiles = p.tiles_m * p.tiles_n, total = tiles * p.cuts, per = (total + kXcds - 1) / kXcds;
     const uint32_t at = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
@@ -70,10 +84,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
     const uint32_t cut = at / tiles;
     int tm, tn;
     core::grouped_tile((int)(at - cut * tiles), (int)p.tiles_m, (int)p.tiles_n, &tm, &tn);
-    const uint32_t first = (uint32_t)((uint64_t)p.s.all * cut / p.cuts), end = (uint32_t)((uint64_t)p.s.all * (cut + 1) / p.cuts);
+    // the parts take K tiles in turn: what they read at a time lies side by side in memory
     const uint32_t m0 = (uint32_t)tm * Tile::BM, n0 = (uint32_t)tn * Tile::BN;
     Tile t;
-    t.run(p.A, p.B, p.s, m0, n0, first, end - first, smem8);
+    t.run(p.A, p.B, p.s, m0, n0, cut, p.cuts, (p.s.all - cut + p.cuts - 1) / p.cuts, smem8);
 
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
     const uint32_t row0 = m0 + wave / WN * (TM * 16), col0 = n0 + wave % WN * (TN * 16);
@@ -90,7 +104,6 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
         constexpr uint32_t W = TN * 16, PITCH = W * sizeof(T) + 16, EV = kVec<T>, VPR = W / EV, NV = 16 * VPR / 64;
         static_assert(WM * WN * 16 * PITCH <= Tile::kSmem && NV >= 1, "strips");
         char *strip = smem8 + wave * 16 * PITCH;
-        const bool aligned = p.Y.scols % EV == 0;
         float ws[TN][4];
 #pragma unroll
         for (int j = 0; j < TN; ++j)
@@ -117,36 +130,42 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
             for (uint32_t n = 0; n < NV; ++n) {
                 const uint32_t idx = lane + 64 * n, lrow = idx / VPR, vc = idx % VPR, row = row0 + i * 16 + lrow, col = col0 + vc * EV;
                 const u32x4 o = *reinterpret_cast<const u32x4 *>(strip + lrow * PITCH + vc * 16);
-                if (row < p.M && col < p.N) {
-                    const uint32_t left = p.N - col;
-                    store_result<T>(p, row, col, o, aligned && left >= EV, left < EV ? left : EV);
-                }
+                if (row < p.M && col < p.N) store_results<T>(p, row, col, o);
             }
             __builtin_amdgcn_wave_barrier();
         }
     }
 }
 
-// the parts' sums joined: four channels a thread
+// the parts' sums joined: a vector of results a thread
 constexpr uint32_t kJoin = 256;
 template <typename T> __global__ __launch_bounds__(kJoin) void fc8_join_kernel(const Layer8Params p)
 {
-    const uint32_t per_row = p.np / 4;
-    const uint32_t col = (blockIdx.x * kJoin + threadIdx.x) * 4, row = blockIdx.y;
-    if (col >= per_row * 4) return;
-    i32x4 s = {0, 0, 0, 0};
-    for (uint32_t c = 0; c < p.cuts; ++c) s += *(const TT_GLOBAL i32x4 *)(p.parts + ((size_t)c * p.M + row) * p.np + col);
-    const float xs = load1(p.XS + row);
-    const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows);
+    constexpr uint32_t EV = kVec<T>, Q = EV / 4;
+    const uint32_t col = (blockIdx.x * kJoin + threadIdx.x) * EV, row = blockIdx.y;
+    if (col >= p.N) return;
+    i32x4 s[Q];
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t n = col + e;
-        if (n >= p.N) break;
-        const uint32_t cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols);
-        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (n - cb * p.Y.scols);
-        const T v = from_float<T>(activated(s[e], load1(p.WS + n), xs, p.relu));
-        for (uint32_t x = 0; x < p.Y.nrep; ++x) store1(static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at, v);
+    for (uint32_t q = 0; q < Q; ++q) s[q] = i32x4{0, 0, 0, 0};
+    // (four parts at a time, past the last one that one again and without weight: loads that wait for nothing)
+    for (uint32_t c = 0; c < p.cuts; c += 4) {
+        i32x4 part[4][Q];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+            for (uint32_t q = 0; q < Q; ++q)
+                part[u][q] = *(const TT_GLOBAL i32x4 *)(p.parts + ((size_t)(c + u < p.cuts ? c + u : p.cuts - 1) * p.M + row) * p.np + col + 4 * q);
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+            for (uint32_t q = 0; q < Q; ++q)
+                if (c + u < p.cuts) s[q] += part[u][q];
     }
+    const float xs = load1(p.XS + row);
+    float v[EV];
+#pragma unroll
+    for (uint32_t e = 0; e < EV; ++e) v[e] = activated(s[e / 4][e % 4], load1(p.WS + (col + e < p.N ? col + e : p.N - 1)), xs, p.relu);
+    store_results<T>(p, row, col, pack16(v, T()));
 }
 
 // Few rows: a workgroup takes 16 TN channels and all of K, its eight waves every eighth K tile each.  A wave's loads of a tile are a whole
@@ -216,9 +235,12 @@ template <int TM, int TN, typename T> __global__ __launch_bounds__(kFew, 2) void
 #pragma unroll
         for (uint32_t v = 0; v < kFewWaves; ++v) s += sums[v][row][c];
         const T y = from_float<T>(activated(s, load1(p.WS + n), load1(p.XS + row), p.relu));
-        const uint32_t rb = p.Y.nR == 1 ? 0 : quotient(row, p.Y.by_srows), cb = p.Y.nC == 1 ? 0 : quotient(n, p.y_by_scols);
-        const size_t at = (size_t)(row - rb * p.Y.srows) * p.Y.scols + (n - cb * p.Y.scols);
-        for (uint32_t x = 0; x < p.Y.nrep; ++x) store1(static_cast<T *>(p.Y.p[(rb * p.Y.nC + cb) * p.Y.nrep + x]) + at, y);
+        if (p.single) {
+            store1(static_cast<T *>(p.Y.p[0]) + (size_t)row * p.N + n, y);
+            continue;
+        }
+        const Spot8 t = spot8(p, row, n);
+        for (uint32_t x = 0; x < p.Y.nrep; ++x) store1(static_cast<T *>(p.Y.p[t.block + x]) + t.at, y);
     }
 }
 
@@ -251,7 +273,8 @@ __global__ __launch_bounds__(256) void fc8_gather_kernel(const GatherParams p)
 // ------------------------------------------------------------------------ launches
 
 
-enum Form { kFewRows, kTiles, kBigTiles };
+enum Form { kFewRows, kSmallTiles, kMiddleTiles, kBigTiles };
+constexpr int64_t kTileM[] = {0, 128, 256, 256}, kTileN[] = {0, 128, 128, 256};
 struct Plan {
     Form form;
     uint32_t tiles_m, tiles_n, cuts;
@@ -271,19 +294,31 @@ Plan plan_of(const Shape8 &g, int64_t M)
     const uint32_t all = (uint32_t)(g.K / g.seg) * tiles_of(g.seg, BK8);
     if (g.gather) p.gather_bytes = align_up((size_t)M * (size_t)(g.K / g.seg) * (size_t)tt_pitch8(g.seg), 256);
     if (M <= 64) return p;
-    const uint64_t big = (uint64_t)tiles_of(M, 256) * tiles_of(g.N, 256);
-    if (big >= kCUs * 3 / 4) {
-        p.form = kBigTiles;
-        p.tiles_m = tiles_of(M, 256);
-        p.tiles_n = tiles_of(g.N, 256);
-        return p;
+    // What a form costs, in hundredths of a microsecond: rounds of workgroups over the CUs, each a start, its K tiles and its results;
+    // parts of K are written and read again, by one more launch.
+    const uint64_t tile_cost[] = {0, 35, 60, 115}, start = 400;
+    uint64_t best = ~(uint64_t)0;
+    for (int form = kSmallTiles; form <= kBigTiles; ++form) {
+        const uint64_t tm = tiles_of(M, kTileM[form]), tn = tiles_of(g.N, kTileN[form]);
+        for (uint32_t cuts = 1; cuts <= 16 && cuts * 4 <= (all > 4 ? all : 4); ++cuts) {
+            if (form == kBigTiles && cuts > 1) break;
+            const uint64_t rounds = (tm * tn * cuts + kCUs - 1) / kCUs;
+            const uint64_t cost = rounds * (start + tile_cost[form] * ((all + cuts - 1) / cuts)) + (cuts > 1 ? 450 + cuts * (uint64_t)M * (uint64_t)g.N / 5000 : 0);
+            if (cost >= best) continue;
+            best = cost;
+            p.form = (Form)form;
+            p.tiles_m = (uint32_t)tm;
+            p.tiles_n = (uint32_t)tn;
+            p.cuts = cuts;
+        }
     }
-    p.form = kTiles;
-    p.tiles_m = tiles_of(M, 128);
-    p.tiles_n = tiles_of(g.N, 128);
-    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
-    while (tiles * p.cuts * 2 <= 2 * kCUs && all / (p.cuts * 2) >= 4 && p.cuts < 16) p.cuts *= 2;
-    if (p.cuts > 1) p.parts_bytes = align_up((size_t)p.cuts * (size_t)M * (size_t)((g.N + 3) / 4 * 4) * 4, 256);
+    if (const int f = tuning_int("TT_FC8_FORM", 0)) {
+        p.form = (Form)f;
+        p.tiles_m = tiles_of(M, kTileM[f]);
+        p.tiles_n = tiles_of(g.N, kTileN[f]);
+        p.cuts = (uint32_t)tuning_int("TT_FC8_CUTS", 1);
+    }
+    if (p.cuts > 1) p.parts_bytes = align_up((size_t)p.cuts * (size_t)M * (size_t)((g.N + 7) / 8 * 8) * 4, 256);
     return p;
 }
 
@@ -310,10 +345,10 @@ bool whole_blocks(const Operand &o, const Steps8 &s, uint32_t rows)
     return (o.row_blocks == 1 || o.srows % rows == 0) && (o.k_shift == 0 || s.seg % BK8 == 0);
 }
 
-template <int WM, int WN, int TM, int TN, bool ONE, typename T> tt_status launch_tiles_as(const Layer8Params &p, hipStream_t s)
+template <int WM, int WN, int TM, int TN, int NS, bool ONE, typename T> tt_status launch_tiles_as(const Layer8Params &p, hipStream_t s)
 {
-    typedef Tile8<WM, WN, TM, TN, ONE> Tile;
-    auto kernel = fc8_tile_kernel<WM, WN, TM, TN, ONE, T>;
+    typedef Tile8<WM, WN, TM, TN, NS, ONE> Tile;
+    auto kernel = fc8_tile_kernel<WM, WN, TM, TN, NS, ONE, T>;
     const tt_status st = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), Tile::kSmem);
     if (st != TT_OK) return st;
     const uint32_t total = p.tiles_m * p.tiles_n * p.cuts;
@@ -322,12 +357,14 @@ template <int WM, int WN, int TM, int TN, bool ONE, typename T> tt_status launch
 }
 template <typename T> tt_status launch_tiles(const Layer8Params &p, Form form, hipStream_t s)
 {
-    if (form == kBigTiles && whole_blocks(p.A, p.s, 256) && whole_blocks(p.B, p.s, 256)) return launch_tiles_as<2, 4, 8, 4, true, T>(p, s);
+    const auto whole = [&](Form f) { return whole_blocks(p.A, p.s, (uint32_t)kTileM[f]) && whole_blocks(p.B, p.s, (uint32_t)kTileN[f]); };
+    if (form == kBigTiles && whole(form)) return launch_tiles_as<2, 4, 8, 4, 2, true, T>(p, s);
+    if (form == kMiddleTiles && whole(form)) return launch_tiles_as<2, 2, 8, 4, 3, true, T>(p, s);
     Layer8Params q = p;
     q.tiles_m = tiles_of(p.M, 128);
     q.tiles_n = tiles_of(p.N, 128);
-    if (whole_blocks(p.A, p.s, 128) && whole_blocks(p.B, p.s, 128)) return launch_tiles_as<2, 2, 4, 4, true, T>(q, s);
-    return launch_tiles_as<2, 2, 4, 4, false, T>(q, s);
+    if (whole(kSmallTiles)) return launch_tiles_as<2, 2, 4, 4, 4, true, T>(q, s);
+    return launch_tiles_as<2, 2, 4, 4, 2, false, T>(q, s);
 }
 template <int TM, typename T> void launch_few_as(const Layer8Params &p, hipStream_t s)
 {
@@ -345,7 +382,7 @@ template <typename T> tt_status launch_layer(const Layer8Params &p, Form form, h
     if (p.cuts == 1) return launch_tiles<T>(p, form, s);
     const tt_status st = launch_tiles<int32_t>(p, form, s);
     if (st != TT_OK) return st;
-    hipLaunchKernelGGL((fc8_join_kernel<T>), dim3((p.np / 4 + kJoin - 1) / kJoin, p.M), dim3(kJoin), 0, s, p);
+    hipLaunchKernelGGL((fc8_join_kernel<T>), dim3((p.np / kVec<T> + kJoin - 1) / kJoin, p.M), dim3(kJoin), 0, s, p);
     return TT_OK;
 }
 
@@ -436,7 +473,8 @@ extern "C" tt_status tt_fc_forward8(const tt_layer *layer, int64_t batch, int k,
     p.tiles_m = plan.tiles_m;
     p.tiles_n = plan.tiles_n;
     p.cuts = plan.cuts;
-    p.np = (p.N + 3) / 4 * 4;
+    p.np = (p.N + 7) / 8 * 8;
+    p.single = uncut(p.Y);
     p.parts = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + plan.gather_bytes);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t operands = (uint64_t)g.M * g.K + (uint64_t)g.K * g.N, results = (uint64_t)g.M * g.N;

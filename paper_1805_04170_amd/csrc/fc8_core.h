@@ -65,7 +65,7 @@ template <int ROWS, int NT, bool ONE> struct Feed {
     uint32_t voff[ONE ? NL : 1];
     uint64_t base;
     const char *row[ONE ? 1 : NL];
-    uint32_t most, row0, kc;
+    uint32_t most, row0, kc, tile;
     At at;
     __device__ __forceinline__ void bind(const Operand &o, const Steps8 &s)
     {
@@ -81,9 +81,10 @@ template <int ROWS, int NT, bool ONE> struct Feed {
             }
         }
     }
-    __device__ __forceinline__ void begin(const Operand &o, const Steps8 &s, uint32_t first_row, uint32_t tile)
+    __device__ __forceinline__ void begin(const Operand &o, const Steps8 &s, uint32_t first_row, uint32_t first)
     {
         row0 = first_row;
+        tile = first;
         at = at_tile(s, tile);
         kc = ((threadIdx.x & 7) ^ ((threadIdx.x >> 4) & 7)) * 16;
         if constexpr (ONE) {
@@ -95,12 +96,15 @@ template <int ROWS, int NT, bool ONE> struct Feed {
         }
         bind(o, s);
     }
-    __device__ __forceinline__ void next(const Operand &o, const Steps8 &s)
+    // `by` K tiles further
+    __device__ __forceinline__ void next(const Operand &o, const Steps8 &s, uint32_t by)
     {
-        if (++at.tile < s.tiles) {
-            if constexpr (ONE) base += BK8;
+        tile += by;
+        at.tile += by;
+        if (at.tile < s.tiles) {
+            if constexpr (ONE) base += by * BK8;
         } else {
-            at = {at.seg + 1, 0};
+            at = at_tile(s, tile);
             bind(o, s);
         }
     }
@@ -152,17 +156,19 @@ __device__ __forceinline__ void k_step8(i32x4 (&acc)[TM][TN], const Frags8<TM, T
     }
 }
 
-// Sums over K tiles first .. first + count - 1 (count above 0) of rows m0 .. and channels n0 .. of the result.  WM x WN waves, each
-// 16 TM x 16 TN; two LDS stages.  A lane ends up with row lane % 16 and four consecutive channels 4 (lane / 16) .. of every block.
-template <int WM, int WN, int TM, int TN, bool ONE> struct Tile8 {
+// Sums over `count` K tiles (more than 0), first, first + by, .., of rows m0 .. and channels n0 .. of the result.  WM x WN waves, each
+// 16 TM x 16 TN; NS LDS stages, so that NS - 1 K tiles are on their way or being multiplied.  A lane ends up with row lane % 16 and
+// four consecutive channels 4 (lane / 16) .. of every block.
+template <int WM, int WN, int TM, int TN, int NS, bool ONE> struct Tile8 {
     static constexpr int NT = WM * WN * 64, BM = WM * TM * 16, BN = WN * TN * 16;
     static constexpr int kA = BM * BK8, kB = BN * BK8, kStage = kA + kB;
-    static constexpr size_t kSmem = 2 * (size_t)kStage;
+    static constexpr size_t kSmem = NS * (size_t)kStage;
     typedef Feed<BM, NT, ONE> FA;
     typedef Feed<BN, NT, ONE> FB;
     static constexpr int LPS = FA::NL + FB::NL;
+    static_assert(NS >= 2 && (NS - 1) * LPS < 64, "loads that a wait can count");
     i32x4 acc[TM][TN];
-    __device__ __forceinline__ void run(const Operand &A, const Operand &B, const Steps8 &s, uint32_t m0, uint32_t n0, uint32_t first, uint32_t count, char *smem)
+    __device__ __forceinline__ void run(const Operand &A, const Operand &B, const Steps8 &s, uint32_t m0, uint32_t n0, uint32_t first, uint32_t by, uint32_t count, char *smem)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const uint32_t lds0 = dev::lds_addr(smem);
@@ -177,13 +183,13 @@ template <int WM, int WN, int TM, int TN, bool ONE> struct Tile8 {
         };
         auto advance = [&]() {
             if (left > 0) {
-                fa.next(A, s);
-                fb.next(B, s);
+                fa.next(A, s, by);
+                fb.next(B, s, by);
                 --left;
             }
         };
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
+        for (int st = 0; st < NS; ++st) {
 #pragma unroll
             for (int i = 0; i < LPS; ++i) issue(i, lds0 + (uint32_t)st * kStage);
             advance();
@@ -197,7 +203,7 @@ template <int WM, int WN, int TM, int TN, bool ONE> struct Tile8 {
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-        __builtin_amdgcn_s_waitcnt(mma::waitcnt_vm(LPS)); // this wave's chunks of the first tile have landed
+        __builtin_amdgcn_s_waitcnt(mma::waitcnt_vm((NS - 1) * LPS)); // this wave's chunks of the first tile have landed
         __syncthreads();                                  // everyone's have
 #pragma unroll
         for (int j = 0; j < TN; ++j) f0.b[j] = rb.read(smem + kA, 0, j);
@@ -208,10 +214,10 @@ template <int WM, int WN, int TM, int TN, bool ONE> struct Tile8 {
             const char *At = smem + cur * kStage;
             k_step8<0>(acc, f0, f1, ra, rb, At, At + kA, 1, [](int) {});
             // this wave has read the tile, and its chunks of the next one have landed; then everyone's
-            __builtin_amdgcn_s_waitcnt(mma::waitcnt_vm_lds(0));
+            __builtin_amdgcn_s_waitcnt(mma::waitcnt_vm_lds((NS - 2) * LPS));
             __syncthreads();
             const uint32_t lds_free = lds0 + cur * kStage;
-            cur ^= 1;
+            cur = cur + 1 == NS ? 0 : cur + 1;
             const char *nA = smem + cur * kStage;
             k_step8<LPS>(acc, f1, f0, ra, rb, nA, nA + kA, 0, [&](int i) { issue(i, lds_free); });
             advance();

@@ -14,10 +14,9 @@ namespace {
 struct NormParams {
     BlockTable X, R, H, Y; // (R, H: p[0] NULL where there is none)
     const void *gain;
-    RowShape r;
+    RowWalk w;
     DropParams d;
-    float eps;
-    uint32_t rows, lanes, groups;
+    float eps, per_col; // 1 / columns
 };
 
 // the sum as it is kept: R + dropout(X) in the tensors' type
@@ -36,102 +35,81 @@ template <typename T> __device__ __forceinline__ u32x4 sum_of(u32x4 x, u32x4 r, 
     return pack16(f, T());
 }
 
-template <typename T, int V, bool WAVE, int MODE>
-__global__ __launch_bounds__(WAVE ? kWaveBlock : kMostThreads) void norm_forward_kernel(const NormParams p)
+enum { kResidual = 1, kKeepSum = 2 };
+template <typename T, class Walk, uint32_t MOST, int FLAGS> __global__ __launch_bounds__(MOST) void norm_forward_kernel(const NormParams p)
 {
     constexpr uint32_t EV = kVec<T>;
-    constexpr bool CUT = MODE != kPlain, NARROW = MODE == kNarrow;
-    constexpr bool AHEAD = V <= 2, KEPT = V <= 2; // more vectors than that: nothing is asked for ahead, places and gains are worked out and read again
+    constexpr int V = Walk::V;
+    constexpr bool AHEAD = V <= 2; // the next row's vectors are asked for while this one's sums are joined
     __shared__ RowScratch<1> scratch;
     const DropState d = drop_state(p.d);
-    const uint32_t li = WAVE ? threadIdx.x & (p.lanes - 1) : threadIdx.x;
-    const uint32_t at_once = WAVE ? kWaveBlock / p.lanes : 1, step = p.groups * at_once;
-    const bool res = p.R.p[0] != nullptr, keep = p.H.p[0] != nullptr;
-    Spot spots[KEPT ? V : 1];
-    u32x4 gains[KEPT ? V : 1], x[V], r[V];
-    auto spot = [&](int i) {
-        if constexpr (KEPT) return spots[i];
-        uint32_t j = li + i * p.lanes;
-        wave::forget(j);
-        return spot_of<EV>(p.r, j);
-    };
-    auto gain_of = [&](int i) {
-        if constexpr (KEPT) return gains[i];
-        return p.gain ? gain_at<T, MODE>(p.gain, p.r, spot(i)) : ones<T>();
-    };
-    if constexpr (KEPT) {
+    const bool res = has<FLAGS>(p.w.flags, kResidual), keep = has<FLAGS>(p.w.flags, kKeepSum);
+    Walk walk;
+    walk.init(p.w);
+    const uint32_t at_once = walk.at_once(p.w), step = p.w.groups * at_once;
+    u32x4 x[V], r[V], gain[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) gain[i] = p.gain ? walk.by_column(p.w, p.gain, i) : ones<T>();
+    auto load = [&](uint32_t base) {
+        const uint32_t row = walk.row(p.w, base) < p.w.rows ? walk.row(p.w, base) : p.w.rows - 1;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            spots[i] = spot_of<EV>(p.r, li + i * p.lanes);
-            gains[i] = p.gain ? gain_at<T, MODE>(p.gain, p.r, spots[i]) : ones<T>();
-        }
-    }
-    auto row_of = [&](uint32_t base) { return WAVE ? base + threadIdx.x / p.lanes : base; };
-    auto load = [&](uint32_t base) { // (a row past the end is the last one again)
-        const uint32_t row = row_of(base) < p.rows ? row_of(base) : p.rows - 1;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const Spot v = spot(i);
-            const Lane l = lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row, v);
-            x[i] = load_spot<T, NARROW>(p.X, l, v);
-            if (res) r[i] = load_spot<T, NARROW>(p.R, l, v);
+            const Spot v = walk.spot(p.w, i);
+            const Place at = walk.template place<true>(p.w, p.X, row, i);
+            x[i] = walk.load(p.X, at, v);
+            if (res) r[i] = walk.load(p.R, at, v);
         }
     };
-    uint32_t turn = 0;
-    uint32_t base = blockIdx.x * at_once;
+    uint32_t turn = 0, base = blockIdx.x * at_once;
     if constexpr (AHEAD) load(base);
-    for (; base < p.rows; base += step) {
-        const bool live = row_of(base) < p.rows;
-        const uint32_t row = live ? row_of(base) : p.rows - 1;
+    for (; base < p.w.rows; base += step) {
+        const uint32_t row = walk.row(p.w, base) < p.w.rows ? walk.row(p.w, base) : p.w.rows - 1; // (a row past the end is the last one again)
         if constexpr (!AHEAD) load(base);
         u32x4 h[V];
         float sum[1] = {0.0f};
+        auto add = [&](int i, float by) {
+            float f[EV];
+            unpack16(walk.counted(p.w, i, h[i]), f, T());
+#pragma unroll
+            for (uint32_t e = 0; e < EV; ++e) sum[0] += f[e] * by * (f[e] * by);
+            wave::forget(h[i]); // (unpacked again where it is used next, not kept in 32 bits)
+        };
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const Spot v = spot(i);
-            h[i] = sum_of<T>(x[i], r[i], res, d, row, v.q * p.r.s.seg + v.at);
-            if (v.n == 0) h[i] = u32x4{0, 0, 0, 0};
-            float f[EV];
-            unpack16(h[i], f, T());
-#pragma unroll
-            for (uint32_t e = 0; e < EV; ++e) sum[0] += v.dup > e ? 0.0f : f[e] * f[e];
-            wave::forget(h[i]);
+            const Spot v = walk.spot(p.w, i);
+            h[i] = sum_of<T>(x[i], r[i], res, d, row, v.q * p.w.r.s.seg + v.at);
+            add(i, 1.0f);
         }
-        if constexpr (AHEAD) load(base + step < p.rows ? base + step : base);
-        RowReduce<WAVE, float, Sum>::run(sum, p.lanes, scratch, turn++);
-        float mean = scaled_mean(sum[0], p.r.cols, p.eps, 1.0f), factor = 1.0f;
-        const bool fits = fits_fp32(mean);
-        if (WAVE ? wave::ballot(!fits) != 0 : !fits) {
+        if constexpr (AHEAD) load(base + step < p.w.rows ? base + step : base);
+        walk.template reduce<float, Sum>(p.w, sum, scratch, turn++);
+        float mean = scaled_mean(sum[0], p.per_col, p.eps, 1.0f), factor = 1.0f;
+        const bool fits = fits_fp32(mean), others = Walk::any(!fits);
+        if (others) {
             const float by = factor_for(mean);
             sum[0] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                wave::forget(h[i]); // (unpacked again: the values are not kept in 32 bits over the sum)
-                const Spot v = spot(i);
-                float f[EV];
-                unpack16(h[i], f, T());
-#pragma unroll
-                for (uint32_t e = 0; e < EV; ++e) sum[0] += v.dup > e ? 0.0f : f[e] * by * (f[e] * by);
-            }
-            RowReduce<WAVE, float, Sum>::run(sum, p.lanes, scratch, turn++);
+            for (int i = 0; i < V; ++i) add(i, by);
+            walk.template reduce<float, Sum>(p.w, sum, scratch, turn++);
             if (!fits) {
                 factor = by;
-                mean = scaled_mean(sum[0], p.r.cols, p.eps, by);
+                mean = scaled_mean(sum[0], p.per_col, p.eps, by);
             }
         }
         const float root = inverse_root(mean);
-        const uint32_t keep_n = live ? ~0u : 0u;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            Spot v = spot(i);
-            v.n &= keep_n;
             float f[EV], g[EV];
             unpack16(h[i], f, T());
-            unpack16(gain_of(i), g, T());
+            unpack16(gain[i], g, T());
+            if (others) {
 #pragma unroll
-            for (uint32_t e = 0; e < EV; ++e) f[e] = f[e] * factor * root * g[e];
-            if (keep) store_spot<T, CUT, NARROW>(p.H, lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v), v, h[i]);
-            store_spot<T, CUT, NARROW>(p.Y, lane_of<CUT>(p.Y, p.r.s, p.r.s.b_shift, row, v), v, pack16(f, T()));
+                for (uint32_t e = 0; e < EV; ++e) f[e] *= factor;
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < EV; ++e) f[e] = f[e] * root * g[e];
+            const Spot v = walk.spot(p.w, i);
+            if (keep) walk.store(p.H, walk.template place<true>(p.w, p.H, row, i), v, h[i], p.w.once);
+            walk.store(p.Y, walk.template place<false>(p.w, p.Y, row, i), v, pack16(f, T()), p.w.once);
         }
     }
 }
@@ -144,58 +122,55 @@ template <typename T, bool CUT> __global__ __launch_bounds__(kMostThreads) void 
     const DropState d = drop_state(p.d);
     const bool res = p.R.p[0] != nullptr, keep = p.H.p[0] != nullptr;
     uint32_t turn = 0;
-    for (uint32_t row = blockIdx.x; row < p.rows; row += p.groups) {
+    for (uint32_t row = blockIdx.x; row < p.w.rows; row += p.w.groups) {
         double s[1] = {0.0}, root = 0.0;
         for (int pass = 0; pass < 2; ++pass) {
-            for (uint32_t j = threadIdx.x; j < p.r.units; j += kMostThreads) {
-                const Spot v = spot_of<EV>(p.r, j);
-                const Lane l = lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row, v);
+            for (uint32_t j = threadIdx.x; j < p.w.r.units; j += kMostThreads) {
+                const Spot v = spot_of<EV>(p.w.r, j);
+                const Lane l = lane_of<CUT>(p.X, p.w.r.s, p.w.r.s.a_shift, row, v);
                 const u32x4 x = load_spot<T, false>(p.X, l, v), r = res ? load_spot<T, false>(p.R, l, v) : x;
-                const u32x4 h = sum_of<T>(x, r, res, d, row, v.q * p.r.s.seg + v.at);
+                const u32x4 h = sum_of<T>(x, r, res, d, row, v.q * p.w.r.s.seg + v.at);
                 float f[EV], g[EV];
                 unpack16(h, f, T());
                 if (pass == 0) {
 #pragma unroll
                     for (uint32_t e = 0; e < EV; ++e) s[0] += v.dup > e ? 0.0 : (double)f[e] * f[e];
                 } else {
-                    unpack16(p.gain ? gain_at<T, kCut>(p.gain, p.r, v) : ones<T>(), g, T());
+                    unpack16(p.gain ? load16(static_cast<const T *>(p.gain) + v.q * p.w.r.s.seg + v.at) : ones<T>(), g, T());
 #pragma unroll
                     for (uint32_t e = 0; e < EV; ++e) f[e] = (float)(f[e] * root * g[e]);
                     if (keep) store_spot<T, CUT, false>(p.H, l, v, h);
-                    store_spot<T, CUT, false>(p.Y, lane_of<CUT>(p.Y, p.r.s, p.r.s.b_shift, row, v), v, pack16(f, T()));
+                    store_spot<T, CUT, false>(p.Y, lane_of<CUT>(p.Y, p.w.r.s, p.w.r.s.b_shift, row, v), v, pack16(f, T()));
                 }
             }
             if (pass == 0) {
-                RowReduce<false, double, Sum>::run(s, kMostThreads, scratch, turn++);
-                root = inverse_root_wide(s[0] / p.r.cols + p.eps);
+                over_workgroup<double, Sum>(s, kMostWaves, scratch, turn++);
+                root = inverse_root_wide(s[0] / p.w.r.cols + p.eps);
             }
         }
     }
 }
 
-// workgroups of a launch whose workgroups walk over rows: what the CUs hold at a time
-uint32_t groups_of(const RowLaunch &w, int64_t rows)
-{
-    const int64_t all = (rows + w.at_once - 1) / w.at_once, held = (int64_t)kCUs * (2048 / w.block);
-    return (uint32_t)(all < held ? all : held);
-}
-
-template <typename T, int MODE> void launch_forward_as(const NormParams &p, const RowLaunch &w, hipStream_t s)
-{
-    const dim3 grid(p.groups), block(w.block);
-    if (w.wave) hipLaunchKernelGGL((norm_forward_kernel<T, 1, true, MODE>), grid, block, 0, s, p);
-    else if constexpr (MODE != kNarrow) { // (rows of narrow segments have at most 64 vectors)
-        if (w.vectors == 1) hipLaunchKernelGGL((norm_forward_kernel<T, 1, false, MODE>), grid, block, 0, s, p);
-        else if (w.vectors == 2) hipLaunchKernelGGL((norm_forward_kernel<T, 2, false, MODE>), grid, block, 0, s, p);
-        else if (w.vectors == 4) hipLaunchKernelGGL((norm_forward_kernel<T, 4, false, MODE>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((norm_forward_long_kernel<T, MODE != kPlain>), grid, block, 0, s, p);
+template <typename T> struct ForwardLaunch {
+    const NormParams &p;
+    const RowLaunch &l;
+    hipStream_t s;
+    template <class Walk, uint32_t MOST, int FLAGS> void as() { hipLaunchKernelGGL((norm_forward_kernel<T, Walk, MOST, FLAGS>), dim3(p.w.groups), dim3(l.block), 0, s, p); }
+    template <class Walk, uint32_t MOST> void run()
+    {
+        if constexpr (MOST == kWaveBlock) as<Walk, MOST, kAsGiven>();
+        else if (p.w.flags == kResidual + kKeepSum) as<Walk, MOST, kResidual + kKeepSum>();
+        else if (p.w.flags == kResidual) as<Walk, MOST, kResidual>();
+        else if (p.w.flags == kKeepSum) as<Walk, MOST, kKeepSum>();
+        else as<Walk, MOST, 0>();
     }
-}
-template <typename T> void launch_forward(const NormParams &p, const RowLaunch &w, hipStream_t s)
+};
+template <typename T> void launch_forward(const NormParams &p, const RowLaunch &l, hipStream_t s)
 {
-    if (narrow_segments(p.r, kVec<T>)) launch_forward_as<T, kNarrow>(p, w, s);
-    else if (uncut(p.X) && uncut(p.Y)) launch_forward_as<T, kPlain>(p, w, s);
-    else launch_forward_as<T, kCut>(p, w, s);
+    const bool cut = !(uncut(p.X) && uncut(p.Y));
+    if (with_walk<T>(p.w, l, cut, ForwardLaunch<T>{p, l, s})) return;
+    if (cut) hipLaunchKernelGGL((norm_forward_long_kernel<T, true>), dim3(p.w.groups), dim3(l.block), 0, s, p);
+    else hipLaunchKernelGGL((norm_forward_long_kernel<T, false>), dim3(p.w.groups), dim3(l.block), 0, s, p);
 }
 
 // ---------------------------------------------------------------- gradients
@@ -203,156 +178,172 @@ template <typename T> void launch_forward(const NormParams &p, const RowLaunch &
 struct GradParams {
     BlockTable H, dY, dH, dS, dX; // (dH, dS, dX: p[0] NULL where there is none)
     const void *gain;
-    float *parts;                 // a row of sums by column for each wave (WAVE) or workgroup, or NULL
+    float *parts;                 // a row of sums by column for each workgroup, or NULL
     double *stats;                // (long rows) 1 / root and c of each row
-    RowShape r;
+    RowWalk w;
     DropParams d;
-    float eps;
-    uint32_t rows, lanes, groups;
+    float eps, per_col;
 };
 
-// Sums by column over the rows that a group of lanes walks over stay in registers, and leave as one row of partial sums in the end;
+// Sums by column over the rows that a wave walks over stay in registers, and leave as one row of partial sums a workgroup in the end;
 // norm_gain_kernel adds these up, in an order that the launch's shape alone sets.
-template <typename T, int V, bool WAVE, int MODE>
-__global__ __launch_bounds__(WAVE ? kWaveBlock : kMostThreads) void norm_backward_kernel(const GradParams p)
+enum { kLater = 1, kSum = 2, kBranch = 4 };
+template <typename T, class Walk, uint32_t MOST, int FLAGS> __global__ __launch_bounds__(MOST) void norm_backward_kernel(const GradParams p)
 {
     constexpr uint32_t EV = kVec<T>;
-    constexpr bool CUT = MODE != kPlain, NARROW = MODE == kNarrow;
-    constexpr bool AHEAD = V == 1, KEPT = V == 1;
+    constexpr int V = Walk::V;
+    constexpr bool AHEAD = V <= 2, GROUPS = MOST == kWaveBlock, KEPT = V <= 2; // KEPT: the gain stays in registers
+
     __shared__ RowScratch<2> scratch;
     const DropState d = drop_state(p.d);
-    const uint32_t li = WAVE ? threadIdx.x & (p.lanes - 1) : threadIdx.x;
-    const uint32_t at_once = WAVE ? kWaveBlock / p.lanes : 1, step = p.groups * at_once;
-    const bool later = p.dH.p[0] != nullptr, sums = p.dS.p[0] != nullptr, branch = p.dX.p[0] != nullptr;
-    Spot spots[KEPT ? V : 1];
-    u32x4 gains[KEPT ? V : 1], h[V], y[V], g[V];
-    float by_col[V][EV];
-    auto spot = [&](int i) {
-        if constexpr (KEPT) return spots[i];
-        uint32_t j = li + i * p.lanes;
-        wave::forget(j);
-        return spot_of<EV>(p.r, j);
-    };
+    const bool later = has<FLAGS>(p.w.flags, kLater), sums = has<FLAGS>(p.w.flags, kSum), branch = has<FLAGS>(p.w.flags, kBranch);
+    Walk walk;
+    walk.init(p.w);
+    const uint32_t at_once = walk.at_once(p.w), step = p.w.groups * at_once;
+    u32x4 h[V], y[V], gain[KEPT ? V : 1];
     auto gain_of = [&](int i) {
-        if constexpr (KEPT) return gains[i];
-        return p.gain ? gain_at<T, MODE>(p.gain, p.r, spot(i)) : ones<T>();
+        if constexpr (KEPT) return gain[i];
+        return p.gain ? walk.by_column(p.w, p.gain, i) : ones<T>();
     };
+    float by_col[V][EV];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        if constexpr (KEPT) {
-            spots[i] = spot_of<EV>(p.r, li + i * p.lanes);
-            gains[i] = p.gain ? gain_at<T, MODE>(p.gain, p.r, spots[i]) : ones<T>();
-        }
+        if constexpr (KEPT) gain[i] = p.gain ? walk.by_column(p.w, p.gain, i) : ones<T>();
 #pragma unroll
         for (uint32_t e = 0; e < EV; ++e) by_col[i][e] = 0.0f;
     }
-    auto row_of = [&](uint32_t base) { return WAVE ? base + threadIdx.x / p.lanes : base; };
     auto load = [&](uint32_t base) {
-        const uint32_t row = row_of(base) < p.rows ? row_of(base) : p.rows - 1;
+        const uint32_t row = walk.row(p.w, base) < p.w.rows ? walk.row(p.w, base) : p.w.rows - 1;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const Spot v = spot(i);
-            const Lane l = lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v);
-            h[i] = load_spot<T, NARROW>(p.H, l, v);
-            y[i] = load_spot<T, NARROW>(p.dY, lane_of<CUT>(p.dY, p.r.s, p.r.s.b_shift, row, v), v);
-            if (later) g[i] = load_spot<T, NARROW>(p.dH, l, v);
+            const Spot v = walk.spot(p.w, i);
+            const Place at = walk.template place<true>(p.w, p.H, row, i);
+            h[i] = walk.load(p.H, at, v);
+            y[i] = walk.load(p.dY, walk.template place<false>(p.w, p.dY, row, i), v);
         }
     };
-    uint32_t turn = 0;
-    uint32_t base = blockIdx.x * at_once;
-    if constexpr (AHEAD) load(base < p.rows ? base : 0);
-    for (; base < p.rows; base += step) {
-        const bool live = row_of(base) < p.rows;
-        const uint32_t row = live ? row_of(base) : p.rows - 1;
+    uint32_t turn = 0, base = blockIdx.x * at_once;
+    if constexpr (AHEAD) load(base);
+    for (; base < p.w.rows; base += step) {
+        const bool live = walk.row(p.w, base) < p.w.rows;
+        const uint32_t row = live ? walk.row(p.w, base) : p.w.rows - 1;
         if constexpr (!AHEAD) load(base);
-        u32x4 hc[V], yc[V], gc[V];
+        u32x4 hc[V], yc[V], g[V];
+        if (later) { // (not needed before the row's sums are joined)
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = walk.load(p.dH, walk.template place<true>(p.w, p.H, row, i), walk.spot(p.w, i));
+        }
         float sum[2] = {0.0f, 0.0f}; // of squares, and of gain dY H
         auto add = [&](int i, float by) {
-            const Spot v = spot(i);
             float f[EV], dy[EV], gn[EV];
-            unpack16(hc[i], f, T());
+            unpack16(walk.counted(p.w, i, hc[i]), f, T());
             unpack16(yc[i], dy, T());
             unpack16(gain_of(i), gn, T());
 #pragma unroll
             for (uint32_t e = 0; e < EV; ++e) {
-                const float x = v.dup > e ? 0.0f : f[e] * by;
+                const float x = f[e] * by;
                 sum[0] += x * x;
-                sum[1] += v.dup > e ? 0.0f : gn[e] * dy[e] * x;
+                sum[1] += gn[e] * dy[e] * x;
             }
+            wave::forget(hc[i]);
+            wave::forget(yc[i]);
         };
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const bool none = spot(i).n == 0 || !live;
-            hc[i] = none ? u32x4{0, 0, 0, 0} : h[i];
-            yc[i] = none ? u32x4{0, 0, 0, 0} : y[i];
-            if (later) gc[i] = g[i];
+            hc[i] = h[i];
+            yc[i] = y[i];
             add(i, 1.0f);
-            wave::forget(hc[i]);
-            wave::forget(yc[i]);
         }
-        if constexpr (AHEAD) load(base + step < p.rows ? base + step : base);
-        RowReduce<WAVE, float, Sum, Sum>::run(sum, p.lanes, scratch, turn++);
-        float mean = scaled_mean(sum[0], p.r.cols, p.eps, 1.0f), factor = 1.0f, dot = sum[1];
-        const bool fits = fits_fp32(mean);
-        if (WAVE ? wave::ballot(!fits) != 0 : !fits) {
+        if constexpr (AHEAD) load(base + step < p.w.rows ? base + step : base);
+        walk.template reduce<float, Sum, Sum>(p.w, sum, scratch, turn++);
+        float mean = scaled_mean(sum[0], p.per_col, p.eps, 1.0f), factor = 1.0f, dot = sum[1];
+        const bool fits = fits_fp32(mean), others = Walk::any(!fits);
+        if (others) {
             const float by = factor_for(mean);
             sum[0] = sum[1] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                add(i, by);
-                wave::forget(hc[i]);
-                wave::forget(yc[i]);
-            }
-            RowReduce<WAVE, float, Sum, Sum>::run(sum, p.lanes, scratch, turn++);
+            for (int i = 0; i < V; ++i) add(i, by);
+            walk.template reduce<float, Sum, Sum>(p.w, sum, scratch, turn++);
             if (!fits) {
                 factor = by;
-                mean = scaled_mean(sum[0], p.r.cols, p.eps, by);
+                mean = scaled_mean(sum[0], p.per_col, p.eps, by);
                 dot = sum[1];
             }
         }
-        const float root = inverse_root(mean), c = root * dot / (float)p.r.cols;
-        const uint32_t keep_n = live ? ~0u : 0u;
+        const float root = inverse_root(mean), c = root * dot * p.per_col;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            Spot v = spot(i);
-            v.n &= keep_n;
             float f[EV], dy[EV], gn[EV], at[EV];
             unpack16(hc[i], f, T());
             unpack16(yc[i], dy, T());
             unpack16(gain_of(i), gn, T());
-            if (later) unpack16(gc[i], at, T());
+            if (others) {
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) f[e] *= factor;
+            }
 #pragma unroll
             for (uint32_t e = 0; e < EV; ++e) {
-                const float n = f[e] * factor * root;
+                const float n = f[e] * root;
                 if (live) by_col[i][e] += dy[e] * n;
-                const float ds = (gn[e] * dy[e] - c * n) * root * factor;
-                f[e] = later ? ds + at[e] : ds;
+                f[e] = (gn[e] * dy[e] - c * n) * root;
             }
-            const Lane l = lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v);
-            if (sums) store_spot<T, CUT, NARROW>(p.dS, l, v, pack16(f, T()));
+            if (others) {
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) f[e] *= factor;
+            }
+            if (later) {
+                unpack16(g[i], at, T());
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) f[e] += at[e];
+            }
+            const Spot v = walk.spot(p.w, i);
+            const Place to = walk.template place<true>(p.w, p.H, row, i);
+            if (sums) walk.store(p.dS, to, v, pack16(f, T()), p.w.once);
             if (branch) {
-                drop_values(d, row, v.q * p.r.s.seg + v.at, f);
-                store_spot<T, CUT, NARROW>(p.dX, l, v, pack16(f, T()));
+                drop_values(d, row, v.q * p.w.r.s.seg + v.at, f);
+                walk.store(p.dX, to, v, pack16(f, T()), p.w.once);
             }
         }
     }
     if (!p.parts) return;
-    // groups of a wave that hold the same columns are joined first
-    if constexpr (WAVE) {
-        for (uint32_t m = p.lanes; m < 64; m <<= 1) {
+    float *to = p.parts + (size_t)blockIdx.x * p.w.r.cols;
+    auto out = [&](int i, const float (&v)[EV]) {
+        const Spot s = walk.spot(p.w, i);
+        const uint32_t col = walk.column(p.w, i);
+        if (s.n == EV && s.dup == 0) {
+#pragma unroll
+            for (uint32_t e = 0; e < EV; e += 4) store16(to + col + e, u32x4{__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])});
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < EV; ++e)
+                if (e >= s.dup && e < s.n) store1(to + col + e, v[e]);
+        }
+    };
+    // rows that a workgroup holds at a time are joined first: groups of a wave with the same columns, then the waves
+    if constexpr (GROUPS) {
+        for (uint32_t m = p.w.lanes; m < 64; m <<= 1) {
 #pragma unroll
             for (uint32_t e = 0; e < EV; ++e) by_col[0][e] += lane_xor(by_col[0][e], m);
         }
-        if ((threadIdx.x & 63) >= p.lanes) return;
     }
-    float *to = p.parts + (size_t)(WAVE ? blockIdx.x * (kWaveBlock / 64) + (threadIdx.x >> 6) : blockIdx.x) * p.r.cols;
+    if (GROUPS || p.w.waves == 1) {
+        __shared__ float joined[kWaveBlock / 64][GROUPS ? 1 : V][GROUPS ? 64 : 64][EV];
+        const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const Spot v = spot(i);
+        for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (uint32_t e = 0; e < EV; ++e)
-            if (e >= v.dup && e < v.n) store1(to + v.q * p.r.s.seg + v.at + e, by_col[i][e]);
+            for (uint32_t e = 0; e < EV; ++e) joined[wave][i][lane][e] = by_col[i][e];
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (uint32_t e = 0; e < EV; ++e)
+                for (uint32_t o = 1; o < kWaveBlock / 64; ++o) by_col[i][e] += joined[o][i][lane][e];
+        if (GROUPS && lane >= p.w.lanes) return;
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) out(i, by_col[i]);
 }
 
 // dgain from `count` rows of partial sums: 64 columns a workgroup, a wave takes every 16th row
@@ -380,25 +371,25 @@ template <typename T, bool CUT> __global__ __launch_bounds__(kMostThreads) void 
     constexpr uint32_t EV = kVec<T>;
     __shared__ RowScratch<2> scratch;
     uint32_t turn = 0;
-    for (uint32_t row = blockIdx.x; row < p.rows; row += kLongGroups) {
+    for (uint32_t row = blockIdx.x; row < p.w.rows; row += kLongGroups) {
         double s[2] = {0.0, 0.0};
-        for (uint32_t j = threadIdx.x; j < p.r.units; j += kMostThreads) {
-            const Spot v = spot_of<EV>(p.r, j);
+        for (uint32_t j = threadIdx.x; j < p.w.r.units; j += kMostThreads) {
+            const Spot v = spot_of<EV>(p.w.r, j);
             float f[EV], dy[EV], gn[EV];
-            unpack16(load_spot<T, false>(p.H, lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v), v), f, T());
-            unpack16(load_spot<T, false>(p.dY, lane_of<CUT>(p.dY, p.r.s, p.r.s.b_shift, row, v), v), dy, T());
-            unpack16(p.gain ? gain_at<T, kCut>(p.gain, p.r, v) : ones<T>(), gn, T());
+            unpack16(load_spot<T, false>(p.H, lane_of<CUT>(p.H, p.w.r.s, p.w.r.s.a_shift, row, v), v), f, T());
+            unpack16(load_spot<T, false>(p.dY, lane_of<CUT>(p.dY, p.w.r.s, p.w.r.s.b_shift, row, v), v), dy, T());
+            unpack16(p.gain ? load16(static_cast<const T *>(p.gain) + v.q * p.w.r.s.seg + v.at) : ones<T>(), gn, T());
 #pragma unroll
             for (uint32_t e = 0; e < EV; ++e) {
                 s[0] += v.dup > e ? 0.0 : (double)f[e] * f[e];
                 s[1] += v.dup > e ? 0.0 : (double)gn[e] * dy[e] * f[e];
             }
         }
-        RowReduce<false, double, Sum, Sum>::run(s, kMostThreads, scratch, turn++);
+        over_workgroup<double, Sum, Sum>(s, kMostWaves, scratch, turn++);
         if (threadIdx.x == 0) {
-            const double root = inverse_root_wide(s[0] / p.r.cols + p.eps);
+            const double root = inverse_root_wide(s[0] / p.w.r.cols + p.eps);
             p.stats[2 * (size_t)row] = root;
-            p.stats[2 * (size_t)row + 1] = root * s[1] / p.r.cols;
+            p.stats[2 * (size_t)row + 1] = root * s[1] / p.w.r.cols;
         }
     }
 }
@@ -407,19 +398,19 @@ template <typename T, bool CUT> __global__ __launch_bounds__(kWaveBlock) void no
     constexpr uint32_t EV = kVec<T>;
     const DropState d = drop_state(p.d);
     const bool later = p.dH.p[0] != nullptr, sums = p.dS.p[0] != nullptr, branch = p.dX.p[0] != nullptr;
-    const Spot v = spot_of<EV>(p.r, blockIdx.x * kWaveBlock + threadIdx.x);
+    const Spot v = spot_of<EV>(p.w.r, blockIdx.x * kWaveBlock + threadIdx.x);
     if (v.n == 0) return;
     float gn[EV];
     double by_col[EV];
-    unpack16(p.gain ? gain_at<T, kCut>(p.gain, p.r, v) : ones<T>(), gn, T());
+    unpack16(p.gain ? load16(static_cast<const T *>(p.gain) + v.q * p.w.r.s.seg + v.at) : ones<T>(), gn, T());
 #pragma unroll
     for (uint32_t e = 0; e < EV; ++e) by_col[e] = 0.0;
-    for (uint32_t row = blockIdx.y; row < p.rows; row += p.groups) {
+    for (uint32_t row = blockIdx.y; row < p.w.rows; row += p.w.groups) {
         const double root = load1(p.stats + 2 * (size_t)row), c = load1(p.stats + 2 * (size_t)row + 1);
-        const Lane l = lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v);
+        const Lane l = lane_of<CUT>(p.H, p.w.r.s, p.w.r.s.a_shift, row, v);
         float f[EV], dy[EV], at[EV];
         unpack16(load_spot<T, false>(p.H, l, v), f, T());
-        unpack16(load_spot<T, false>(p.dY, lane_of<CUT>(p.dY, p.r.s, p.r.s.b_shift, row, v), v), dy, T());
+        unpack16(load_spot<T, false>(p.dY, lane_of<CUT>(p.dY, p.w.r.s, p.w.r.s.b_shift, row, v), v), dy, T());
         if (later) unpack16(load_spot<T, false>(p.dH, l, v), at, T());
 #pragma unroll
         for (uint32_t e = 0; e < EV; ++e) {
@@ -429,66 +420,74 @@ template <typename T, bool CUT> __global__ __launch_bounds__(kWaveBlock) void no
         }
         if (sums) store_spot<T, CUT, false>(p.dS, l, v, pack16(f, T()));
         if (branch) {
-            drop_values(d, row, v.q * p.r.s.seg + v.at, f);
+            drop_values(d, row, v.q * p.w.r.s.seg + v.at, f);
             store_spot<T, CUT, false>(p.dX, l, v, pack16(f, T()));
         }
     }
     if (!p.parts) return;
-    float *to = p.parts + (size_t)blockIdx.y * p.r.cols + v.q * p.r.s.seg + v.at;
+    float *to = p.parts + (size_t)blockIdx.y * p.w.r.cols + v.q * p.w.r.s.seg + v.at;
 #pragma unroll
     for (uint32_t e = 0; e < EV; ++e)
         if (e >= v.dup) store1(to + e, (float)by_col[e]);
 }
 
-// What a backward launch of so many rows takes: workgroups, and rows of partial sums
+// vectors of a lane that registers hold beside their sums by column
+template <typename T> constexpr int kGradLimit = sizeof(T) == 2 ? 3 : 4;
+
+// What a backward launch of so many rows takes: workgroups, each with a row of partial sums
 struct GradLaunch {
-    RowLaunch w;
-    uint32_t groups, parts;
+    RowLaunch l;
+    uint32_t groups;
     size_t stats_bytes, bytes;
 };
-// Eight rows a group of lanes where there are many: partial sums are a thirty-second of what is read and written then, and less.
-GradLaunch grad_launch(const RowShape &r, int64_t rows)
+// Four rows a wave or more: partial sums are a sixteenth of what is read and written then, and less.
+GradLaunch grad_launch(RowWalk *w, int64_t rows, int ev)
 {
     GradLaunch g;
-    g.w = row_launch(r);
+    g.l = row_launch(w, ev, 1, ev == 8 ? kGradLimit<uint16_t> : kGradLimit<float>); // (more vectors a lane leave too few waves)
     g.stats_bytes = 0;
-    if (g.w.vectors == 0) {
+    if (g.l.kind == kLong) {
         g.groups = (uint32_t)(rows < 64 ? rows : 64); // (of each strip)
-        g.parts = g.groups;
         g.stats_bytes = align_up((size_t)rows * 2 * sizeof(double), 256);
     } else {
-        const int64_t most = (int64_t)kCUs * (2048 / g.w.block), walks = (rows + g.w.at_once - 1) / g.w.at_once;
-        int64_t n = walks / 8;
-        if (n < kCUs) n = kCUs;
-        if (n > walks) n = walks;
-        if (n > most) n = most;
-        g.groups = (uint32_t)n;
-        g.parts = g.groups * (g.w.wave ? kWaveBlock / 64 : 1);
+        const int64_t most = row_groups(g.l, rows, kMostThreads), walks = (rows + g.l.at_once - 1) / g.l.at_once;
+        int64_t n = walks / 4;
+        if (n < 1) n = 1;
+        g.groups = (uint32_t)(n < most ? n : most);
     }
-    g.bytes = rows == 0 || r.cols == 0 ? 0 : g.stats_bytes + align_up((size_t)g.parts * r.cols * sizeof(float), 256);
+    g.bytes = rows == 0 || w->r.cols == 0 ? 0 : g.stats_bytes + align_up((size_t)g.groups * w->r.cols * sizeof(float), 256);
     return g;
 }
 
-template <typename T, int MODE> void launch_backward_as(const GradParams &p, const GradLaunch &g, hipStream_t s)
-{
-    const dim3 grid(p.groups), block(g.w.block);
-    if (g.w.wave) hipLaunchKernelGGL((norm_backward_kernel<T, 1, true, MODE>), grid, block, 0, s, p);
-    else if constexpr (MODE != kNarrow) {
-        if (g.w.vectors == 1) hipLaunchKernelGGL((norm_backward_kernel<T, 1, false, MODE>), grid, block, 0, s, p);
-        else if (g.w.vectors == 2) hipLaunchKernelGGL((norm_backward_kernel<T, 2, false, MODE>), grid, block, 0, s, p);
-        else if (g.w.vectors == 4) hipLaunchKernelGGL((norm_backward_kernel<T, 4, false, MODE>), grid, block, 0, s, p);
-        else {
-            const dim3 rows(p.rows < kLongGroups ? p.rows : kLongGroups), strips((p.r.units + kWaveBlock - 1) / kWaveBlock, g.groups), lanes(kWaveBlock);
-            hipLaunchKernelGGL((norm_stats_long_kernel<T, MODE != kPlain>), rows, block, 0, s, p);
-            hipLaunchKernelGGL((norm_backward_long_kernel<T, MODE != kPlain>), strips, lanes, 0, s, p);
-        }
+template <typename T> struct BackwardLaunch {
+    const GradParams &p;
+    const RowLaunch &l;
+    hipStream_t s;
+    template <class Walk, uint32_t MOST, int FLAGS> void as() { hipLaunchKernelGGL((norm_backward_kernel<T, Walk, MOST, FLAGS>), dim3(p.w.groups), dim3(l.block), 0, s, p); }
+    // (the forms of a training step; a gain's gradient alone, and one branch's without the sum's, go by the parameters)
+    template <class Walk, uint32_t MOST> void run()
+    {
+        const uint32_t f = p.w.flags;
+        if constexpr (MOST == kWaveBlock) as<Walk, MOST, kAsGiven>();
+        else if (f == kSum) as<Walk, MOST, kSum>();
+        else if (f == kSum + kLater) as<Walk, MOST, kSum + kLater>();
+        else if (f == kSum + kBranch) as<Walk, MOST, kSum + kBranch>();
+        else if (f == kSum + kBranch + kLater) as<Walk, MOST, kSum + kBranch + kLater>();
+        else as<Walk, MOST, kAsGiven>();
     }
-}
-template <typename T> void launch_backward(const GradParams &p, const GradLaunch &g, hipStream_t s)
+};
+template <typename T, bool CUT> void launch_backward_long(const GradParams &p, hipStream_t s)
 {
-    if (narrow_segments(p.r, kVec<T>)) launch_backward_as<T, kNarrow>(p, g, s);
-    else if (uncut(p.H) && uncut(p.dY)) launch_backward_as<T, kPlain>(p, g, s);
-    else launch_backward_as<T, kCut>(p, g, s);
+    const dim3 rows(p.w.rows < kLongGroups ? p.w.rows : kLongGroups), strips((p.w.r.units + kWaveBlock - 1) / kWaveBlock, p.w.groups);
+    hipLaunchKernelGGL((norm_stats_long_kernel<T, CUT>), rows, dim3(kMostThreads), 0, s, p);
+    hipLaunchKernelGGL((norm_backward_long_kernel<T, CUT>), strips, dim3(kWaveBlock), 0, s, p);
+}
+template <typename T> void launch_backward(const GradParams &p, const RowLaunch &l, hipStream_t s)
+{
+    const bool cut = !(uncut(p.H) && uncut(p.dY));
+    if (with_walk<T, kGradLimit<T>>(p.w, l, cut, BackwardLaunch<T>{p, l, s})) return;
+    if (cut) launch_backward_long<T, true>(p, s);
+    else launch_backward_long<T, false>(p, s);
 }
 
 // the geometry of a backward call (shard lists may be NULL)
@@ -498,9 +497,8 @@ tt_status grad_shape(int64_t rows, int64_t width, int k, int dtype, const tt_til
     if (!valid_k(k) || !valid_tiling(tX, k) || !valid_tiling(tdY, k) || !valid_dtype(dtype) || rows < 0 || width < 0) return TT_EINVAL;
     if (!fits31(rows) || !fits31(width)) return TT_EUNSUPPORTED;
     if (!make_blocks(H, tX, k, rows, width, &p->H) || !make_blocks(dY, tdY, k, rows, width, &p->dY)) return TT_EINFEASIBLE;
-    p->rows = (uint32_t)rows;
-    if (width == 0) p->r = RowShape{};
-    else p->r = row_shape(p->H, p->dY, width, 16 / dtype_bytes(dtype));
+    if (width == 0) p->w = RowWalk{};
+    else p->w = row_walk(p->H, p->dY, rows, width, 16 / dtype_bytes(dtype));
     return TT_OK;
 }
 
@@ -529,14 +527,15 @@ extern "C" tt_status tt_norm_forward(int64_t rows, int64_t width, int k, int dty
     if (empty) return TT_OK;
     p.gain = gain;
     p.eps = eps;
-    p.rows = (uint32_t)rows;
-    p.r = row_shape(p.X, p.Y, width, 16 / e);
-    const RowLaunch w = row_launch(p.r);
-    p.lanes = w.lanes;
-    p.groups = groups_of(w, rows);
+    p.per_col = (float)(1.0 / (double)width);
+    p.w = row_walk(p.X, p.Y, rows, width, 16 / e);
+    const RowLaunch l = row_launch(&p.w, 16 / e, 1);
+    p.w.groups = row_groups(l, rows);
+    p.w.flags = (R ? kResidual : 0) + (H ? kKeepSum : 0);
+    p.w.once = (uint64_t)rows * width * e * ((H ? p.H.nrep : 0) + p.Y.nrep) >= kOnceBytes;
     ProfileScope scope(stream, TT_K_NORM, 1 << k, rows, width, e, (uint64_t)rows * width * e * (1 + (R ? 1 : 0) + (H ? p.H.nrep : 0) + p.Y.nrep), 0);
-    if (dtype == TT_BF16) launch_forward<uint16_t>(p, w, static_cast<hipStream_t>(stream));
-    else launch_forward<float>(p, w, static_cast<hipStream_t>(stream));
+    if (dtype == TT_BF16) launch_forward<uint16_t>(p, l, static_cast<hipStream_t>(stream));
+    else launch_forward<float>(p, l, static_cast<hipStream_t>(stream));
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }
 
@@ -547,7 +546,7 @@ extern "C" tt_status tt_norm_workspace_bytes(int64_t rows, int64_t width, int k,
     if (!bytes) return TT_EINVAL;
     const tt_status st = grad_shape(rows, width, k, dtype, tX, tdY, nullptr, nullptr, &p);
     if (st != TT_OK) return st;
-    *bytes = rows == 0 || width == 0 ? 0 : grad_launch(p.r, rows).bytes;
+    *bytes = rows == 0 || width == 0 ? 0 : grad_launch(&p.w, rows, 16 / dtype_bytes(dtype)).bytes;
     return TT_OK;
 }
 
@@ -578,25 +577,27 @@ extern "C" tt_status tt_norm_backward(int64_t rows, int64_t width, int k, int dt
         hipLaunchKernelGGL(norm_gain_kernel, strips, threads, 0, s, static_cast<const float *>(nullptr), 0u, (uint32_t)width, dgain);
         return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
     }
-    const GradLaunch g = grad_launch(p.r, rows);
+    const GradLaunch g = grad_launch(&p.w, rows, 16 / e);
     if (!workspace || ws_bytes < g.bytes || reinterpret_cast<uintptr_t>(workspace) % 256) return TT_EWORKSPACE;
     if (!dS && !dX && !dgain) return TT_OK;
     p.gain = gain;
     p.eps = eps;
-    p.lanes = g.w.lanes;
-    p.groups = g.groups;
+    p.per_col = (float)(1.0 / (double)width);
+    p.w.groups = g.groups;
+    p.w.flags = (dH ? kLater : 0) + (dS ? kSum : 0) + (dX ? kBranch : 0);
+    p.w.once = (uint64_t)rows * width * e * ((dS ? 1 : 0) + (dX ? 1 : 0)) * p.H.nrep >= kOnceBytes;
     p.stats = static_cast<double *>(workspace);
     float *parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + g.stats_bytes);
     p.parts = dgain ? parts : nullptr;
     const uint64_t values = (uint64_t)rows * width * e;
     {
         ProfileScope scope(stream, TT_K_NORM_GRAD, 1 << k, rows, width, e, values * (2 + (dH ? 1 : 0) + ((dS ? 1 : 0) + (dX ? 1 : 0)) * p.H.nrep), 0);
-        if (dtype == TT_BF16) launch_backward<uint16_t>(p, g, s);
-        else launch_backward<float>(p, g, s);
+        if (dtype == TT_BF16) launch_backward<uint16_t>(p, g.l, s);
+        else launch_backward<float>(p, g.l, s);
     }
     if (dgain) {
-        ProfileScope scope(stream, TT_K_NORM_GRAD, 1, g.parts, width, 4, (uint64_t)g.parts * width * 4, 0);
-        hipLaunchKernelGGL(norm_gain_kernel, strips, threads, 0, s, const_cast<const float *>(parts), g.parts, (uint32_t)width, dgain);
+        ProfileScope scope(stream, TT_K_NORM_GRAD, 1, g.groups, width, 4, (uint64_t)g.groups * width * 4, 0);
+        hipLaunchKernelGGL(norm_gain_kernel, strips, threads, 0, s, const_cast<const float *>(parts), g.groups, (uint32_t)width, dgain);
     }
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }

@@ -1,5 +1,6 @@
 // What the kernels that take a row's root mean square share.
 #pragma once
+#include <cmath>
 #include "row_reduce.h"
 
 namespace tt {
@@ -8,24 +9,20 @@ namespace tt {
 // a mean of 2^-80 does not notice) are summed again as values times a power of two, which rounds nothing.
 __device__ __forceinline__ bool fits_fp32(float mean) { return mean >= 0x1p-80f && mean < 0x1p90f; }
 __device__ __forceinline__ float factor_for(float mean) { return mean < 1.0f ? 0x1p80f : 0x1p-80f; }
-__device__ __forceinline__ float scaled_mean(float sum, uint32_t cols, float eps, float factor) { return sum / (float)cols + eps * factor * factor; }
-// 1 / sqrt(mean); NaN where the row held an infinity
-__device__ __forceinline__ float inverse_root(float mean) { return mean < __builtin_inff() ? 1.0f / sqrtf(mean) : __builtin_nanf(""); }
-
+__device__ __forceinline__ float scaled_mean(float sum, float per_col, float eps, float factor) { return sum * per_col + eps * factor * factor; }
+// 1 / sqrt(mean) (1 ulp); NaN where the row held an infinity
+__device__ __forceinline__ float inverse_root(float mean)
+{
+#ifdef TT_HOST_EMULATION
+    const float r = 1.0f / sqrtf(mean);
+#else
+    const float r = __builtin_amdgcn_rsqf(mean);
+#endif
+    return mean < __builtin_inff() ? r : __builtin_nanf("");
+}
 __device__ __forceinline__ double inverse_root_wide(double mean) // (finite values of fp32 have a finite sum in 64 bits)
 {
     return mean <= 0x1p300 ? 1.0 / sqrt(mean) : (double)__builtin_nanf("");
-}
-
-template <typename T, int MODE> __device__ __forceinline__ u32x4 gain_at(const void *gain, const RowShape &r, const Spot &v)
-{
-    const T *g = static_cast<const T *>(gain) + v.q * r.s.seg + v.at;
-    if constexpr (MODE == kNarrow) return load_part(g, v.n);
-    else return load16(g);
-}
-template <typename T> __device__ __forceinline__ u32x4 ones()
-{
-    return sizeof(T) == 2 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u} : u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
 }
 
 // R + X in the tensors' type

@@ -76,10 +76,11 @@ template <int N> __device__ __forceinline__ void drop_values(const DropState &d,
         [[maybe_unused]] const uint32_t upper = 0u - (col >> 2 & 1);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            // (a high half is compared where it stands: the low one under it changes nothing)
             uint32_t w = r.w[i >> 1];
             if constexpr (N == 4) w ^= (w ^ r.w[2 + (i >> 1)]) & upper; // (a choice of addresses would put the words into memory)
-            f[i] = (i & 1 ? w : w << 16) >= below ? f[i] * d.factor : 0.0f;
+            // (a high half is compared where it stands: the low one under it changes nothing)
+            const bool keep = i & 1 ? w >= below : (uint16_t)w >= (uint16_t)d.below;
+            f[i] = keep ? f[i] * d.factor : 0.0f;
         }
     } else {
         const uint32_t at = col & 7;

@@ -18,10 +18,9 @@ struct Rows8Params {
     BlockTable X, R, H, Q; // (R, H: p[0] NULL where there is none; Q: extents in values, rows begin every `pitch` bytes)
     const void *gain;
     float *S;
-    RowShape r;
+    RowWalk w;
     uint32_t pitch;
-    float eps;
-    uint32_t rows, lanes, groups;
+    float eps, per_col;
 };
 
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
@@ -53,9 +52,9 @@ template <bool CUT> __device__ __forceinline__ Lane lane_of8(const BlockTable &b
 constexpr float kRound = 12582912.0f; // 1.5 * 2^23: a number added to it lies rounded in the sum's last bits
 __device__ __forceinline__ uint32_t step_of(double u, double m) { return (uint32_t)(int)rint(u * 127.0 / m); }
 
-// u = value * gain, and what compares and cuts it: fp32 where that is exact
-template <bool EXACT32> struct Cut8;
-template <> struct Cut8<true> { // u fp32
+// u = value * gain, and what compares and cuts it: fp32 where that is exact.  BITS: of u, 24 at most.
+template <bool EXACT32, int BITS> struct Cut8;
+template <int BITS> struct Cut8<true, BITS> { // u fp32
     typedef float U;
     float m, inv;
     static __device__ __forceinline__ float of(float x, float g) { return x * g; }
@@ -63,26 +62,41 @@ template <> struct Cut8<true> { // u fp32
     // that leaves fp32.
     static __device__ __forceinline__ float scaled(float x, float g, float by) { return x == 0.0f || g == 0.0f ? x * g : x * by * (g * by); }
     __device__ __forceinline__ void init(float most) { m = most; inv = 127.0f / most; }
-    // (the quotient is off by at most 127 * 2^-23)
-    __device__ __forceinline__ uint32_t operator()(float u) const
+    // The quotient is off by at most 127 * 2^-23.  `far`: the largest distance of a quotient from its step; near_border() says whether
+    // one's has to be looked at again.
+    typedef float Far;
+    __device__ __forceinline__ uint32_t operator()(float u, float &far) const
     {
         const float t = u * inv, q = t + kRound;
-        if (fabsf(t - (q - kRound)) > 0.4999f) return step_of(u, m);
+        far = fmaxf(far, fabsf(t - (q - kRound)));
         return __float_as_uint(q);
     }
+    static __device__ __forceinline__ bool near_border(float far) { return far > 0.4999f; }
+    // the step of a u whose quotient is near a border j + 1/2: 127 u against (j + 1/2) m, products that fp32 holds where u has up to
+    // 16 bits (of two bf16 values)
+    __device__ __forceinline__ uint32_t exactly(float u) const
+    {
+        if constexpr (BITS > 16) return step_of(u, m);
+        const float j = floorf(fabsf(u * inv)), mine = 127.0f * fabsf(u), border = (j + 0.5f) * m;
+        const int q = (int)j, up = mine > border || (mine == border && (q & 1)) ? 1 : 0;
+        return (uint32_t)(u < 0.0f ? -(q + up) : q + up);
+    }
 };
-template <> struct Cut8<false> { // u in 64 bits, which hold a product of two fp32 values
+template <int BITS> struct Cut8<false, BITS> { // u in 64 bits, which hold a product of two fp32 values
     typedef double U;
     double m, inv;
     static __device__ __forceinline__ double of(float x, float g) { return (double)x * g; }
     static __device__ __forceinline__ double scaled(float x, float g, float) { return of(x, g); } // (64 bits hold any)
     __device__ __forceinline__ void init(double most) { m = most; inv = 127.0 / most; }
-    __device__ __forceinline__ uint32_t operator()(double u) const
+    typedef double Far;
+    __device__ __forceinline__ uint32_t operator()(double u, double &far) const
     {
         const double t = u * inv, q = rint(t);
-        if (fabs(t - q) > 0.4999999999) return step_of(u, m);
+        far = fmax(far, fabs(t - q));
         return (uint32_t)(int)q;
     }
+    static __device__ __forceinline__ bool near_border(double far) { return far > 0.4999999999; }
+    __device__ __forceinline__ uint32_t exactly(double u) const { return step_of(u, m); }
 };
 
 __device__ __forceinline__ float magnitude(float u) { return fabsf(u); }
@@ -92,105 +106,110 @@ __device__ __forceinline__ double bits_of(double v) { return v; } // (compared b
 __device__ __forceinline__ float value_of(uint32_t v) { return __uint_as_float(v); }
 __device__ __forceinline__ double value_of(double v) { return v; }
 
+// where a walk's vector lies in the 8-bit form
+template <class Walk> __device__ __forceinline__ Lane lane8(const Walk &walk, const RowWalk &w, const BlockTable &b, uint32_t pitch, uint32_t row, const Spot &v)
+{
+    return lane_of8<Walk::CUT>(b, w.r.s, w.r.s.b_shift, pitch, row, v);
+}
+
 // NORM: the sum's norm (else the steps are X's).  A row's vectors lie in registers.
-template <typename T, int V, bool WAVE, int MODE, bool NORM>
-__global__ __launch_bounds__(WAVE ? kWaveBlock : kMostThreads) void rows8_kernel(const Rows8Params p)
+enum { kResidual = 1, kKeepSum = 2 };
+template <typename T, class Walk, bool NORM, uint32_t MOST, int FLAGS> __global__ __launch_bounds__(MOST) void rows8_kernel(const Rows8Params p)
 {
     constexpr uint32_t EV = kVec<T>;
-    constexpr bool CUT = MODE != kPlain, NARROW = MODE == kNarrow, EXACT32 = !NORM || sizeof(T) == 2;
-    constexpr bool AHEAD = V <= 2, KEPT = V <= 2;
-    typedef Cut8<EXACT32> C;
+    constexpr int V = Walk::V;
+    constexpr bool CUT = Walk::CUT, NARROW = Walk::NARROW, EXACT32 = !NORM || sizeof(T) == 2, AHEAD = V <= 2, KEPT = V <= 2; // KEPT: the gain stays in registers
+    typedef Cut8<EXACT32, sizeof(T) == 2 ? (NORM ? 16 : 8) : 24> C;
     typedef typename C::U U;
     typedef decltype(bits_of(U())) B;
-    __shared__ RowScratch<1> scratch;
-    const uint32_t li = WAVE ? threadIdx.x & (p.lanes - 1) : threadIdx.x;
-    const uint32_t at_once = WAVE ? kWaveBlock / p.lanes : 1, step = p.groups * at_once;
-    const bool res = NORM && p.R.p[0] != nullptr, keep = NORM && p.H.p[0] != nullptr;
-    Spot spots[KEPT ? V : 1];
-    u32x4 gains[KEPT && NORM ? V : 1], x[V], r[V];
-    auto spot = [&](int i) {
-        if constexpr (KEPT) return spots[i];
-        uint32_t j = li + i * p.lanes;
-        wave::forget(j);
-        return spot_of<EV>(p.r, j);
-    };
+    __shared__ RowScratch<2> scratch;
+    const bool res = NORM && has<FLAGS>(p.w.flags, kResidual), keep = NORM && has<FLAGS>(p.w.flags, kKeepSum);
+    Walk walk;
+    walk.init(p.w);
+    const uint32_t at_once = walk.at_once(p.w), step = p.w.groups * at_once;
+    u32x4 x[V], r[V], gain[NORM && KEPT ? V : 1];
+    if constexpr (NORM && KEPT) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) gain[i] = p.gain ? walk.by_column(p.w, p.gain, i) : ones<T>();
+    }
     auto gain_of = [&](int i) {
         if constexpr (!NORM) return ones<T>();
-        else if constexpr (KEPT) return gains[i];
-        else return p.gain ? gain_at<T, MODE>(p.gain, p.r, spot(i)) : ones<T>();
+        else if constexpr (KEPT) return gain[i];
+        else return p.gain ? walk.by_column(p.w, p.gain, i) : ones<T>();
     };
-    if constexpr (KEPT) {
+    auto load = [&](uint32_t base) {
+        const uint32_t row = walk.row(p.w, base) < p.w.rows ? walk.row(p.w, base) : p.w.rows - 1;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            spots[i] = spot_of<EV>(p.r, li + i * p.lanes);
-            if constexpr (NORM) gains[i] = p.gain ? gain_at<T, MODE>(p.gain, p.r, spots[i]) : ones<T>();
-        }
-    }
-    auto row_of = [&](uint32_t base) { return WAVE ? base + threadIdx.x / p.lanes : base; };
-    auto load = [&](uint32_t base) { // (a row past the end is the last one again)
-        const uint32_t row = row_of(base) < p.rows ? row_of(base) : p.rows - 1;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const Spot v = spot(i);
-            const Lane l = lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row, v);
-            x[i] = load_spot<T, NARROW>(p.X, l, v);
-            if (res) r[i] = load_spot<T, NARROW>(p.R, l, v);
+            const Spot v = walk.spot(p.w, i);
+            const Place at = walk.template place<true>(p.w, p.X, row, i);
+            x[i] = walk.load(p.X, at, v);
+            if (res) r[i] = walk.load(p.R, at, v);
         }
     };
-    uint32_t turn = 0;
-    uint32_t base = blockIdx.x * at_once;
+    uint32_t turn = 0, base = blockIdx.x * at_once;
     if constexpr (AHEAD) load(base);
-    for (; base < p.rows; base += step) {
-        const bool live = row_of(base) < p.rows;
-        const uint32_t row = live ? row_of(base) : p.rows - 1;
+    for (; base < p.w.rows; base += step) {
+        const uint32_t row = walk.row(p.w, base) < p.w.rows ? walk.row(p.w, base) : p.w.rows - 1; // (a row past the end is the last one again)
         if constexpr (!AHEAD) load(base);
         u32x4 h[V];
-        // the sum of squares of the values times `by`, and the largest |u| of both factors times `scale`
         float sum[1];
         B most[1];
+        // u of a vector, both factors times `scale`
+        auto each_u = [&](int i, float scale, auto &&use) {
+            float f[EV], g[EV];
+            unpack16(h[i], f, T());
+            unpack16(gain_of(i), g, T());
+            if (scale == 1.0f) {
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) use(e, NORM ? C::of(f[e], g[e]) : (U)f[e]);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < EV; ++e) use(e, C::scaled(f[e], g[e], scale));
+            }
+        };
+        // the sum of squares of the values times `by`, and the largest |u|
         auto statistics = [&](float by, float scale) {
             sum[0] = 0.0f;
-            U top = 0;
-            most[0] = bits_of(top);
+            most[0] = bits_of(U(0));
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const Spot v = spot(i);
-                float f[EV], g[EV];
-                unpack16(h[i], f, T());
-                unpack16(gain_of(i), g, T());
+                if constexpr (NORM) {
+                    float f[EV];
+                    unpack16(walk.counted(p.w, i, h[i]), f, T());
 #pragma unroll
-                for (uint32_t e = 0; e < EV; ++e) {
-                    if constexpr (NORM) sum[0] += v.dup > e ? 0.0f : f[e] * by * (f[e] * by);
-                    most[0] = Largest::of(most[0], bits_of(magnitude(scale == 1.0f ? C::of(f[e], g[e]) : C::scaled(f[e], g[e], scale))));
+                    for (uint32_t e = 0; e < EV; ++e) sum[0] += f[e] * by * (f[e] * by);
                 }
+                each_u(i, scale, [&](uint32_t, U u) { most[0] = Largest::of(most[0], bits_of(magnitude(u))); });
                 wave::forget(h[i]); // (unpacked again where it is used next, not kept in 32 bits)
             }
-            if constexpr (NORM) RowReduce<WAVE, float, Sum>::run(sum, p.lanes, scratch, turn++);
-            RowReduce<WAVE, B, Largest>::run(most, p.lanes, scratch, turn++);
+            if constexpr (NORM && sizeof(B) == 4) {
+                uint32_t both[2] = {__float_as_uint(sum[0]), most[0]};
+                walk.template reduce<uint32_t, SumBits, Largest>(p.w, both, scratch, turn++);
+                sum[0] = __uint_as_float(both[0]);
+                most[0] = both[1];
+            } else {
+                if constexpr (NORM) walk.template reduce<float, Sum>(p.w, sum, scratch, turn++);
+                walk.template reduce<B, Largest>(p.w, most, scratch, turn++);
+            }
         };
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const Spot v = spot(i);
-            h[i] = x[i];
-            if (res) h[i] = added<T>(x[i], r[i]);
-            if (v.n == 0) h[i] = u32x4{0, 0, 0, 0};
-            if (keep && live) store_spot<T, CUT, NARROW>(p.H, lane_of<CUT>(p.H, p.r.s, p.r.s.a_shift, row, v), v, h[i]);
-        }
-        if constexpr (AHEAD) load(base + step < p.rows ? base + step : base);
+        for (int i = 0; i < V; ++i) h[i] = res ? added<T>(x[i], r[i]) : x[i];
+        if constexpr (AHEAD) load(base + step < p.w.rows ? base + step : base);
         statistics(1.0f, 1.0f);
-        float mean = NORM ? scaled_mean(sum[0], p.r.cols, p.eps, 1.0f) : 1.0f, factor = 1.0f, scale = 1.0f;
+        float mean = NORM ? scaled_mean(sum[0], p.per_col, p.eps, 1.0f) : 1.0f, factor = 1.0f, scale = 1.0f;
         U m = value_of(most[0]);
         // fp32 holds |u| and 127 / |u| well inside (64 bits hold any; a row of zeros has no quotients)
         const bool inside = EXACT32 ? m >= 0x1p-60f && m <= 0x1p100f : m > 0;
         const bool fits = fits_fp32(mean) && inside;
-        if (WAVE ? wave::ballot(!fits) != 0 : !fits) {
-            const float by = fits_fp32(mean) ? 1.0f : factor_for(mean), to = !EXACT32 || inside ? 1.0f : m < 1.0f ? 0x1p50f : 0x1p-66f;
+        if (Walk::any(!fits)) {
+            const float by = fits_fp32(mean) ? 1.0f : factor_for(mean), to = !EXACT32 || inside ? 1.0f : m < 1.0f ? 0x1p50f : 0x1p-70f;
             statistics(by, to);
             if (!fits) {
                 factor = by;
                 scale = to;
                 m = value_of(most[0]);
-                if constexpr (NORM) mean = scaled_mean(sum[0], p.r.cols, p.eps, by);
+                if constexpr (NORM) mean = scaled_mean(sum[0], p.per_col, p.eps, by);
             }
         }
         const float root = NORM ? inverse_root(mean) : 1.0f;
@@ -199,42 +218,46 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMostThreads) void rows8_kernel
         cut.init(some ? m : U(1));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            Spot v = spot(i);
-            if (!live) v.n = 0;
-            float f[EV], g[EV];
-            unpack16(h[i], f, T());
-            unpack16(gain_of(i), g, T());
+            const Spot v = walk.spot(p.w, i);
+            if (keep) walk.store(p.H, walk.template place<true>(p.w, p.H, row, i), v, h[i], p.w.once);
             uint32_t w[EV];
-            if (scale == 1.0f) {
-#pragma unroll
-                for (uint32_t e = 0; e < EV; ++e) w[e] = cut(C::of(f[e], g[e]));
-            } else {
-#pragma unroll
-                for (uint32_t e = 0; e < EV; ++e) w[e] = cut(C::scaled(f[e], g[e], scale));
+            typename C::Far far = 0;
+            each_u(i, scale, [&](uint32_t e, U u) { w[e] = cut(u, far); });
+            if (C::near_border(far)) { // (one vector in some hundreds)
+                each_u(i, scale, [&](uint32_t e, U u) {
+                    typename C::Far mine = 0;
+                    cut(u, mine);
+                    if (C::near_border(mine)) w[e] = cut.exactly(u);
+                });
             }
             Steps<T> b;
 #pragma unroll
             for (uint32_t e = 0; e < EV; e += 4) b.w[e / 4] = some ? wave::low_bytes(w[e], w[e + 1], w[e + 2], w[e + 3]) : 0u;
-            if (v.n == 0) continue;
-            const Lane l = lane_of8<CUT>(p.Q, p.r.s, p.r.s.b_shift, p.pitch, row, v);
-            for (uint32_t c = 0; c < (CUT ? p.Q.nrep : 1); ++c) {
+            const Lane l = lane8(walk, p.w, p.Q, p.pitch, row, v);
+            auto one = [&](uint32_t c) {
                 int8_t *to = static_cast<int8_t *>(p.Q.p[l.block + c]) + l.at;
                 if constexpr (NARROW) {
                     for (uint32_t e = 0; e < v.n; ++e) store1(to + e, (int8_t)(b.w[e >> 2] >> (8 * (e & 3))));
                 } else {
                     store_steps(to, b);
                 }
+            };
+            one(0);
+            if constexpr (CUT) {
+                for (uint32_t c = 1; c < p.Q.nrep; ++c) one(c);
             }
         }
-        if (!live) continue;
         // zeros behind the values of each of the row's blocks
-        const uint32_t behind = p.pitch - p.Q.scols, rb = CUT && p.Q.nR > 1 ? quotient(row, p.Q.by_srows) : 0;
-        for (uint32_t j = li; j < behind * p.Q.nC; j += p.lanes) {
-            const uint32_t cb = CUT ? j / behind : 0;
-            for (uint32_t c = 0; c < (CUT ? p.Q.nrep : 1); ++c)
-                store1(static_cast<int8_t *>(p.Q.p[(rb * p.Q.nC + cb) * p.Q.nrep + c]) + (size_t)(row - rb * p.Q.srows) * p.pitch + p.Q.scols + (j - cb * behind), (int8_t)0);
+        const uint32_t behind = p.pitch - p.Q.scols;
+        if (behind) {
+            const uint32_t rb = CUT && p.Q.nR > 1 ? quotient(row, p.Q.by_srows) : 0;
+            for (uint32_t j = walk.number(p.w); j < behind * p.Q.nC; j += walk.count(p.w)) {
+                const uint32_t cb = CUT ? j / behind : 0;
+                for (uint32_t c = 0; c < (CUT ? p.Q.nrep : 1); ++c)
+                    store1(static_cast<int8_t *>(p.Q.p[(rb * p.Q.nC + cb) * p.Q.nrep + c]) + (size_t)(row - rb * p.Q.srows) * p.pitch + p.Q.scols + (j - cb * behind), (int8_t)0);
+            }
         }
-        if (li == 0) {
+        if (walk.number(p.w) == 0) {
             const float s = (float)((double)m * root * factor / ((double)scale * scale * 127.0)); // (factors of scaled values: powers of two)
             store1(p.S + row, number ? s : __builtin_nanf(""));
         }
@@ -248,18 +271,18 @@ template <typename T, bool CUT, bool NORM> __global__ __launch_bounds__(kMostThr
     __shared__ RowScratch<1> scratch;
     const bool res = NORM && p.R.p[0] != nullptr, keep = NORM && p.H.p[0] != nullptr;
     uint32_t turn = 0;
-    for (uint32_t row = blockIdx.x; row < p.rows; row += p.groups) {
+    for (uint32_t row = blockIdx.x; row < p.w.rows; row += p.w.groups) {
         double s[1] = {0.0}, m[1] = {0.0}, root = 1.0;
         bool number = true;
         for (int pass = 0; pass < 2; ++pass) {
-            for (uint32_t j = threadIdx.x; j < p.r.units; j += kMostThreads) {
-                const Spot v = spot_of<EV>(p.r, j);
-                const Lane l = lane_of<CUT>(p.X, p.r.s, p.r.s.a_shift, row, v);
+            for (uint32_t j = threadIdx.x; j < p.w.r.units; j += kMostThreads) {
+                const Spot v = spot_of<EV>(p.w.r, j);
+                const Lane l = lane_of<CUT>(p.X, p.w.r.s, p.w.r.s.a_shift, row, v);
                 u32x4 h = load_spot<T, false>(p.X, l, v);
                 if (res) h = added<T>(h, load_spot<T, false>(p.R, l, v));
                 float f[EV], g[EV];
                 unpack16(h, f, T());
-                unpack16(NORM && p.gain ? gain_at<T, kCut>(p.gain, p.r, v) : ones<T>(), g, T());
+                unpack16(NORM && p.gain ? load16(static_cast<const T *>(p.gain) + v.q * p.w.r.s.seg + v.at) : ones<T>(), g, T());
                 Steps<T> b;
 #pragma unroll
                 for (uint32_t e = 0; e < EV; ++e) {
@@ -274,14 +297,14 @@ template <typename T, bool CUT, bool NORM> __global__ __launch_bounds__(kMostThr
                 }
                 if (pass == 0) continue;
                 if (keep) store_spot<T, CUT, false>(p.H, l, v, h);
-                const Lane to = lane_of8<CUT>(p.Q, p.r.s, p.r.s.b_shift, p.pitch, row, v);
+                const Lane to = lane_of8<CUT>(p.Q, p.w.r.s, p.w.r.s.b_shift, p.pitch, row, v);
                 for (uint32_t c = 0; c < p.Q.nrep; ++c) store_steps(static_cast<int8_t *>(p.Q.p[to.block + c]) + to.at, b);
             }
             if (pass) continue;
-            RowReduce<false, double, Largest>::run(m, kMostThreads, scratch, turn++);
+            over_workgroup<double, Largest>(m, kMostWaves, scratch, turn++);
             if constexpr (NORM) {
-                RowReduce<false, double, Sum>::run(s, kMostThreads, scratch, turn++);
-                root = inverse_root_wide(s[0] / p.r.cols + p.eps);
+                over_workgroup<double, Sum>(s, kMostWaves, scratch, turn++);
+                root = inverse_root_wide(s[0] / p.w.r.cols + p.eps);
             }
             number = root == root && m[0] <= 0x1p1000;
         }
@@ -295,27 +318,24 @@ template <typename T, bool CUT, bool NORM> __global__ __launch_bounds__(kMostThr
     }
 }
 
-uint32_t groups_of(const RowLaunch &w, int64_t rows)
-{
-    const int64_t all = (rows + w.at_once - 1) / w.at_once, held = (int64_t)kCUs * (2048 / w.block);
-    return (uint32_t)(all < held ? all : held);
-}
-template <typename T, int MODE, bool NORM> void launch_rows_as(const Rows8Params &p, const RowLaunch &w, hipStream_t s)
-{
-    const dim3 grid(p.groups), block(w.block);
-    if (w.wave) hipLaunchKernelGGL((rows8_kernel<T, 1, true, MODE, NORM>), grid, block, 0, s, p);
-    else if constexpr (MODE != kNarrow) { // (rows of narrow segments have at most 64 vectors)
-        if (w.vectors == 1) hipLaunchKernelGGL((rows8_kernel<T, 1, false, MODE, NORM>), grid, block, 0, s, p);
-        else if (w.vectors == 2) hipLaunchKernelGGL((rows8_kernel<T, 2, false, MODE, NORM>), grid, block, 0, s, p);
-        else if (w.vectors == 4) hipLaunchKernelGGL((rows8_kernel<T, 4, false, MODE, NORM>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((rows8_long_kernel<T, MODE != kPlain, NORM>), grid, block, 0, s, p);
+template <typename T, bool NORM> struct RowsLaunch {
+    const Rows8Params &p;
+    const RowLaunch &l;
+    hipStream_t s;
+    template <class Walk, uint32_t MOST, int FLAGS> void as() { hipLaunchKernelGGL((rows8_kernel<T, Walk, NORM, MOST, FLAGS>), dim3(p.w.groups), dim3(l.block), 0, s, p); }
+    template <class Walk, uint32_t MOST> void run()
+    {
+        if constexpr (MOST == kWaveBlock || !NORM) as<Walk, MOST, NORM ? kAsGiven : 0>();
+        else if (p.w.flags == kResidual + kKeepSum) as<Walk, MOST, kResidual + kKeepSum>();
+        else as<Walk, MOST, kAsGiven>();
     }
-}
-template <typename T, bool NORM> void launch_rows(const Rows8Params &p, const RowLaunch &w, hipStream_t s)
+};
+template <typename T, bool NORM> void launch_rows(const Rows8Params &p, const RowLaunch &l, hipStream_t s)
 {
-    if (narrow_segments(p.r, kVec<T>)) launch_rows_as<T, kNarrow, NORM>(p, w, s);
-    else if (uncut(p.X) && uncut(p.Q)) launch_rows_as<T, kPlain, NORM>(p, w, s);
-    else launch_rows_as<T, kCut, NORM>(p, w, s);
+    const bool cut = !(uncut(p.X) && uncut(p.Q));
+    if (with_walk<T>(p.w, l, cut, RowsLaunch<T, NORM>{p, l, s})) return;
+    if (cut) hipLaunchKernelGGL((rows8_long_kernel<T, true, NORM>), dim3(p.w.groups), dim3(l.block), 0, s, p);
+    else hipLaunchKernelGGL((rows8_long_kernel<T, false, NORM>), dim3(p.w.groups), dim3(l.block), 0, s, p);
 }
 
 bool bytes_fit(const void *const *shards, int k, bool empty)
@@ -358,22 +378,23 @@ tt_status run_rows8(bool norm, int64_t rows, int64_t cols, int k, int dtype, con
     p.gain = gain;
     p.S = S;
     p.eps = eps;
-    p.rows = (uint32_t)rows;
+    p.per_col = (float)(1.0 / (double)cols);
     p.pitch = (uint32_t)tt_pitch8(p.Q.scols);
-    p.r = row_shape(p.X, p.Q, cols, 16 / e);
-    const RowLaunch w = row_launch(p.r);
-    p.lanes = w.lanes;
-    p.groups = groups_of(w, rows);
+    p.w = row_walk(p.X, p.Q, rows, cols, 16 / e);
+    const RowLaunch l = row_launch(&p.w, 16 / e, 2);
+    p.w.groups = row_groups(l, rows);
+    p.w.flags = (R ? kResidual : 0) + (H ? kKeepSum : 0);
+    p.w.once = H && (uint64_t)rows * cols * e * p.H.nrep >= kOnceBytes;
     const uint64_t values = (uint64_t)rows * cols;
     ProfileScope scope(stream, TT_K_ROWS8, 1 << k, rows, cols, e, values * (e * (1 + (R ? 1 : 0) + (H ? p.H.nrep : 0)) + p.Q.nrep) + 4 * (uint64_t)rows, 0);
-    if (dtype == TT_BF16) norm ? launch_rows<uint16_t, true>(p, w, s) : launch_rows<uint16_t, false>(p, w, s);
-    else norm ? launch_rows<float, true>(p, w, s) : launch_rows<float, false>(p, w, s);
+    if (dtype == TT_BF16) norm ? launch_rows<uint16_t, true>(p, l, s) : launch_rows<uint16_t, false>(p, l, s);
+    else norm ? launch_rows<float, true>(p, l, s) : launch_rows<float, false>(p, l, s);
     return hipGetLastError() == hipSuccess ? TT_OK : TT_EDEVICE;
 }
 
 // ------------------------------------------------------------ values of 8 bits
 
-constexpr int kThreads = 256, kVectors = 4;
+constexpr int kThreads = 256, kVectors = 8;
 struct Unrows8Params {
     BlockTable Q, X;
     const float *S;
@@ -408,7 +429,6 @@ template <typename T, bool CUT, bool NARROW> __global__ __launch_bounds__(kThrea
             load_steps(from, q[i]);
         }
         scale[i] = load1(p.S + row[i]);
-        if (u >= left) v[i].n = 0;
     }
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
