@@ -84,9 +84,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
     const uint32_t cut = at / tiles;
     int tm, tn;
     core::grouped_tile((int)(at - cut * tiles), (int)p.tiles_m, (int)p.tiles_n, &tm, &tn);
-    // the parts take K tiles in turn: what they read at a time lies side by side in memory
     const uint32_t m0 = (uint32_t)tm * Tile::BM, n0 = (uint32_t)tn * Tile::BN;
     Tile t;
+    // the parts take K tiles in turn: what they read at a time lies side by side in memory
     t.run(p.A, p.B, p.s, m0, n0, cut, p.cuts, (p.s.all - cut + p.cuts - 1) / p.cuts, smem8);
 
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
@@ -273,8 +273,8 @@ __global__ __launch_bounds__(256) void fc8_gather_kernel(const GatherParams p)
 // ------------------------------------------------------------------------ launches
 
 
-enum Form { kFewRows, kSmallTiles, kMiddleTiles, kBigTiles };
-constexpr int64_t kTileM[] = {0, 128, 256, 256}, kTileN[] = {0, 128, 128, 256};
+enum Form { kFewRows, kTinyTiles, kSmallTiles, kMiddleTiles, kBigTiles };
+constexpr int64_t kTileM[] = {0, 64, 128, 256, 256}, kTileN[] = {0, 64, 128, 128, 256};
 struct Plan {
     Form form;
     uint32_t tiles_m, tiles_n, cuts;
@@ -296,14 +296,14 @@ Plan plan_of(const Shape8 &g, int64_t M)
     if (M <= 64) return p;
     // What a form costs, in hundredths of a microsecond: rounds of workgroups over the CUs, each a start, its K tiles and its results;
     // parts of K are written and read again, by one more launch.
-    const uint64_t tile_cost[] = {0, 35, 60, 115}, start = 400;
+    const uint64_t tile_cost[] = {0, 36, 49, 75, 112}, start[] = {0, 570, 720, 1050, 1000};
     uint64_t best = ~(uint64_t)0;
-    for (int form = kSmallTiles; form <= kBigTiles; ++form) {
+    for (int form = kTinyTiles; form <= kBigTiles; ++form) {
         const uint64_t tm = tiles_of(M, kTileM[form]), tn = tiles_of(g.N, kTileN[form]);
         for (uint32_t cuts = 1; cuts <= 16 && cuts * 4 <= (all > 4 ? all : 4); ++cuts) {
             if (form == kBigTiles && cuts > 1) break;
-            const uint64_t rounds = (tm * tn * cuts + kCUs - 1) / kCUs;
-            const uint64_t cost = rounds * (start + tile_cost[form] * ((all + cuts - 1) / cuts)) + (cuts > 1 ? 450 + cuts * (uint64_t)M * (uint64_t)g.N / 5000 : 0);
+            const uint64_t held = form == kTinyTiles ? 2 * kCUs : kCUs, rounds = (tm * tn * cuts + held - 1) / held;
+            const uint64_t cost = rounds * (start[form] + tile_cost[form] * ((all + cuts - 1) / cuts)) + (cuts > 1 ? 450 + cuts * (uint64_t)M * (uint64_t)g.N / 5000 : 0);
             if (cost >= best) continue;
             best = cost;
             p.form = (Form)form;
@@ -360,15 +360,19 @@ template <typename T> tt_status launch_tiles(const Layer8Params &p, Form form, h
     const auto whole = [&](Form f) { return whole_blocks(p.A, p.s, (uint32_t)kTileM[f]) && whole_blocks(p.B, p.s, (uint32_t)kTileN[f]); };
     if (form == kBigTiles && whole(form)) return launch_tiles_as<2, 4, 8, 4, 2, true, T>(p, s);
     if (form == kMiddleTiles && whole(form)) return launch_tiles_as<2, 2, 8, 4, 3, true, T>(p, s);
+    if (form == kTinyTiles && whole(form)) return launch_tiles_as<2, 2, 2, 2, 4, true, T>(p, s);
     Layer8Params q = p;
     q.tiles_m = tiles_of(p.M, 128);
     q.tiles_n = tiles_of(p.N, 128);
     if (whole(kSmallTiles)) return launch_tiles_as<2, 2, 4, 4, 4, true, T>(q, s);
     return launch_tiles_as<2, 2, 4, 4, 2, false, T>(q, s);
 }
+// The more channels a workgroup takes, the less often X is read; a workgroup for every CU comes first.
 template <int TM, typename T> void launch_few_as(const Layer8Params &p, hipStream_t s)
 {
-    if (tiles_of(p.N, 32) >= kCUs) hipLaunchKernelGGL((fc8_few_kernel<TM, 2, T>), dim3(tiles_of(p.N, 32)), dim3(kFew), 0, s, p);
+    constexpr int MOST = TM == 1 ? 4 : 2;
+    if (MOST == 4 && tiles_of(p.N, 64) >= kCUs) hipLaunchKernelGGL((fc8_few_kernel<TM, MOST, T>), dim3(tiles_of(p.N, 64)), dim3(kFew), 0, s, p);
+    else if (tiles_of(p.N, 32) >= kCUs) hipLaunchKernelGGL((fc8_few_kernel<TM, 2, T>), dim3(tiles_of(p.N, 32)), dim3(kFew), 0, s, p);
     else hipLaunchKernelGGL((fc8_few_kernel<TM, 1, T>), dim3(tiles_of(p.N, 16)), dim3(kFew), 0, s, p);
 }
 template <typename T> tt_status launch_layer(const Layer8Params &p, Form form, hipStream_t s)

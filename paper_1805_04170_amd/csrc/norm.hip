@@ -346,19 +346,28 @@ template <typename T, class Walk, uint32_t MOST, int FLAGS> __global__ __launch_
     for (int i = 0; i < V; ++i) out(i, by_col[i]);
 }
 
-// dgain from `count` rows of partial sums: 64 columns a workgroup, a wave takes every 16th row
+// dgain from `count` rows of partial sums: 16 columns a workgroup, a group of 16 lanes takes every 64th row
+constexpr uint32_t kGainColumns = 16, kGainRows = kMostThreads / kGainColumns;
 __global__ __launch_bounds__(kMostThreads) void norm_gain_kernel(const float *parts, uint32_t count, uint32_t cols, float *dgain)
 {
-    __shared__ float of_wave[kMostWaves][64];
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane;
+    __shared__ float of_wave[kMostWaves][kGainColumns];
+    const uint32_t lane = threadIdx.x % kGainColumns, first = threadIdx.x / kGainColumns, col = blockIdx.x * kGainColumns + lane;
+    const uint32_t from = col < cols ? col : 0;
     float s = 0.0f;
-    if (col < cols) {
-#pragma unroll 8
-        for (uint32_t i = wave; i < count; i += kMostWaves) s += load1(parts + (size_t)i * cols + col);
+    // eight rows at a time, past the last one that one again and without weight: loads that wait for nothing
+    for (uint32_t i = first; i < count; i += 8 * kGainRows) {
+        float v[8];
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) v[u] = load1(parts + (size_t)(i + u * kGainRows < count ? i + u * kGainRows : i) * cols + from);
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) s += i + u * kGainRows < count ? v[u] : 0.0f;
     }
-    of_wave[wave][lane] = s;
+    s += lane_xor(s, 16);
+    s += lane_xor(s, 32);
+    if ((threadIdx.x & 63) < kGainColumns) of_wave[threadIdx.x >> 6][lane] = s;
     __syncthreads();
-    if (wave || col >= cols) return;
+    if (threadIdx.x >= kGainColumns || col >= cols) return;
+    s = of_wave[0][lane];
     for (int w = 1; w < kMostWaves; ++w) s += of_wave[w][lane];
     store1(dgain + col, s);
 }
@@ -451,7 +460,10 @@ GradLaunch grad_launch(RowWalk *w, int64_t rows, int ev)
         g.stats_bytes = align_up((size_t)rows * 2 * sizeof(double), 256);
     } else {
         const int64_t most = row_groups(g.l, rows, kMostThreads), walks = (rows + g.l.at_once - 1) / g.l.at_once;
-        int64_t n = walks / 4;
+        const int64_t waves = g.l.block / 64, least = tuning_int("TT_GRAD_LEAST", 2);
+        int64_t n = walks / 4, few = 16 * kCUs / waves;
+        if (few > (walks + least - 1) / least) few = (walks + least - 1) / least;
+        if (n < few) n = few;
         if (n < 1) n = 1;
         g.groups = (uint32_t)(n < most ? n : most);
     }
@@ -571,7 +583,7 @@ extern "C" tt_status tt_norm_backward(int64_t rows, int64_t width, int k, int dt
     make_blocks(in(dX), tX, k, rows, width, &p.dX);
     if (width == 0) return TT_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 strips((uint32_t)((width + 63) / 64)), threads(kMostThreads);
+    const dim3 strips((uint32_t)((width + kGainColumns - 1) / kGainColumns)), threads(kMostThreads);
     if (empty) { // a gradient of zeros: the sum of no rows
         if (!dgain) return TT_OK;
         hipLaunchKernelGGL(norm_gain_kernel, strips, threads, 0, s, static_cast<const float *>(nullptr), 0u, (uint32_t)width, dgain);

@@ -62,13 +62,13 @@ template <int BITS> struct Cut8<true, BITS> { // u fp32
     // that leaves fp32.
     static __device__ __forceinline__ float scaled(float x, float g, float by) { return x == 0.0f || g == 0.0f ? x * g : x * by * (g * by); }
     __device__ __forceinline__ void init(float most) { m = most; inv = 127.0f / most; }
-    // The quotient is off by at most 127 * 2^-23.  `far`: the largest distance of a quotient from its step; near_border() says whether
+    // The quotient is off by at most 127 * 2^-24.  `far`: the largest distance of a quotient from its step; near_border() says whether
     // one's has to be looked at again.
     typedef float Far;
     __device__ __forceinline__ uint32_t operator()(float u, float &far) const
     {
-        const float t = u * inv, q = t + kRound;
-        far = fmaxf(far, fabsf(t - (q - kRound)));
+        const float q = fmaf(u, inv, kRound);
+        far = fmaxf(far, fabsf(fmaf(u, inv, kRound - q)));
         return __float_as_uint(q);
     }
     static __device__ __forceinline__ bool near_border(float far) { return far > 0.4999f; }
@@ -99,6 +99,18 @@ template <int BITS> struct Cut8<false, BITS> { // u in 64 bits, which hold a pro
     __device__ __forceinline__ uint32_t exactly(double u) const { return step_of(u, m); }
 };
 
+// the largest magnitude's bits of a vector of bf16: magnitudes compare as their bits do
+__device__ __forceinline__ uint32_t largest_of(u32x4 v)
+{
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t m = v[j] & 0x7fff7fffu;
+        top = __builtin_elementwise_max(top, u16x2{(uint16_t)m, (uint16_t)(m >> 16)});
+    }
+    return (uint32_t)(top.x > top.y ? top.x : top.y) << 16;
+}
 __device__ __forceinline__ float magnitude(float u) { return fabsf(u); }
 __device__ __forceinline__ double magnitude(double u) { return fabs(u); }
 __device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
@@ -137,6 +149,19 @@ template <typename T, class Walk, bool NORM, uint32_t MOST, int FLAGS> __global_
         else if constexpr (KEPT) return gain[i];
         else return p.gain ? walk.by_column(p.w, p.gain, i) : ones<T>();
     };
+    // A maximum of fp32 values passes a NaN by.  One in H shows in the sum of squares; a gain that is not finite is looked for here, and
+    // shows in every row.
+    constexpr bool FLOATS = NORM && KEPT && EXACT32;
+    uint32_t bad = 0;
+    if constexpr (FLOATS) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float g[EV];
+            unpack16(gain[i], g, T());
+#pragma unroll
+            for (uint32_t e = 0; e < EV; ++e) bad |= fabsf(g[e]) < __builtin_inff() ? 0u : 0x7fc00000u;
+        }
+    }
     auto load = [&](uint32_t base) {
         const uint32_t row = walk.row(p.w, base) < p.w.rows ? walk.row(p.w, base) : p.w.rows - 1;
 #pragma unroll
@@ -180,7 +205,16 @@ template <typename T, class Walk, bool NORM, uint32_t MOST, int FLAGS> __global_
 #pragma unroll
                     for (uint32_t e = 0; e < EV; ++e) sum[0] += f[e] * by * (f[e] * by);
                 }
-                each_u(i, scale, [&](uint32_t, U u) { most[0] = Largest::of(most[0], bits_of(magnitude(u))); });
+                if constexpr (FLOATS) {
+                    float top = 0.0f;
+                    each_u(i, scale, [&](uint32_t, float u) { top = fmaxf(top, fabsf(u)); });
+                    most[0] = Largest::of(most[0], __float_as_uint(top) | bad);
+                } else if constexpr (!NORM && sizeof(T) == 2) {
+                    if (scale == 1.0f) most[0] = Largest::of(most[0], largest_of(h[i]));
+                    else each_u(i, scale, [&](uint32_t, U u) { most[0] = Largest::of(most[0], bits_of(magnitude(u))); });
+                } else {
+                    each_u(i, scale, [&](uint32_t, U u) { most[0] = Largest::of(most[0], bits_of(magnitude(u))); });
+                }
                 wave::forget(h[i]); // (unpacked again where it is used next, not kept in 32 bits)
             }
             if constexpr (NORM && sizeof(B) == 4) {
@@ -402,6 +436,7 @@ struct Unrows8Params {
     uint32_t pitch;
     uint64_t units;
     uint32_t small; // they are counted in 31 bits
+    uint32_t once;  // results are stored past the caches
     Divisor by_units;
 };
 template <typename T, bool CUT, bool NARROW> __global__ __launch_bounds__(kThreads) void unrows8_kernel(const Unrows8Params p)
@@ -435,7 +470,7 @@ template <typename T, bool CUT, bool NARROW> __global__ __launch_bounds__(kThrea
         float f[EV];
 #pragma unroll
         for (uint32_t e = 0; e < EV; ++e) f[e] = (float)(int8_t)(q[i].w[e / 4] >> (8 * (e % 4))) * scale[i];
-        store_spot<T, CUT, NARROW>(p.X, lane_of<CUT>(p.X, p.r.s, p.r.s.b_shift, row[i], v[i]), v[i], pack16(f, T()));
+        store_spot<T, CUT, NARROW>(p.X, lane_of<CUT>(p.X, p.r.s, p.r.s.b_shift, row[i], v[i]), v[i], pack16(f, T()), p.once);
     }
 }
 template <typename T> void launch_unrows(const Unrows8Params &p, hipStream_t s)
@@ -557,6 +592,7 @@ extern "C" tt_status tt_unrows8(int64_t rows, int64_t cols, int k, int dtype, tt
     p.by_units = divisor(p.r.units);
     p.units = (uint64_t)rows * p.r.units;
     p.small = p.units < (uint64_t(1) << 31);
+    p.once = (uint64_t)rows * cols * e * p.X.nrep >= kOnceBytes;
     if ((uint64_t)rows * (uint64_t)cols >= (uint64_t(1) << 37) || p.units / kVectors >= (uint64_t(1) << 32) - kThreads || p.r.units >= (1u << 31) - kThreads * kVectors)
         return TT_EUNSUPPORTED; // (a launch holds fewer than 2^32 threads)
     ProfileScope scope(stream, TT_K_ROWS8, 1 << k, rows, cols, e, (uint64_t)rows * cols * (1 + e * p.X.nrep) + 4 * (uint64_t)rows, 0);
