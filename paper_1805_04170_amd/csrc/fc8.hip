@@ -27,6 +27,8 @@ struct Layer8Params {
     uint32_t M, N, relu;
     uint32_t single;      // Y is one block
     uint32_t tiles_m, tiles_n, cuts;
+    uint32_t run_m, run_n;           // rows and channels that tiles are laid over together: all of them, or those of a block
+    Divisor by_run_m, by_run_n;      // tiles of such a run
     uint32_t np;          // channels of a row of `parts`
 };
 
@@ -48,26 +50,35 @@ template <typename T> __device__ __forceinline__ void store_value(T *to, u32x4 v
     if constexpr (sizeof(T) == 2) store1(to + e, (uint16_t)(v[e >> 1] >> (16 * (e & 1))));
     else store1(to + e, __uint_as_float(v[e]));
 }
-// A vector of results of a row from channel n on, as far as there are channels: into every replica
-template <typename T> __device__ __forceinline__ void store_results(const Layer8Params &p, uint32_t row, uint32_t n, u32x4 v)
+// A vector of results of a row from channel n on, up to channel `end`: into every replica
+template <typename T> __device__ __forceinline__ void store_results(const Layer8Params &p, uint32_t row, uint32_t n, uint32_t end, u32x4 v)
 {
     constexpr uint32_t EV = kVec<T>;
     if (p.single) { // (one block: its address is a scalar)
         T *to = static_cast<T *>(p.Y.p[0]) + (size_t)row * p.N + n;
-        if (p.N - n >= EV) store16(to, v);
+        if (end - n >= EV) store16(to, v);
         else
-            for (uint32_t e = 0; e < p.N - n; ++e) store_value<T>(to, v, e);
+            for (uint32_t e = 0; e < end - n; ++e) store_value<T>(to, v, e);
         return;
     }
     const Spot8 s = spot8(p, row, n);
-    if (s.left >= EV) {
+    if (s.left >= EV && end - n >= EV) {
         for (uint32_t x = 0; x < p.Y.nrep; ++x) store16(static_cast<T *>(p.Y.p[s.block + x]) + s.at, v);
         return;
     }
-    for (uint32_t e = 0; e < EV && n + e < p.N; ++e) {
+    for (uint32_t e = 0; e < EV && n + e < end; ++e) {
         const Spot8 t = spot8(p, row, n + e);
         for (uint32_t x = 0; x < p.Y.nrep; ++x) store_value<T>(static_cast<T *>(p.Y.p[t.block + x]) + t.at - e, v, e);
     }
+}
+
+// four sums of a part, as far as the tile's channels go
+__device__ __forceinline__ void store_sums(int32_t *to, i32x4 v, uint32_t left)
+{
+    typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= 4) *(TT_GLOBAL i32x4_any *)to = v;
+    else
+        for (uint32_t e = 0; e < left; ++e) store1(to + e, v[e]);
 }
 
 extern __shared__ __align__(16) char smem8[];
@@ -84,10 +95,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
     const uint32_t cut = at / tiles;
     int tm, tn;
     core::grouped_tile((int)(at - cut * tiles), (int)p.tiles_m, (int)p.tiles_n, &tm, &tn);
-    const uint32_t m0 = (uint32_t)tm * Tile::BM, n0 = (uint32_t)tn * Tile::BN;
+    const uint32_t rm = quotient((uint32_t)tm, p.by_run_m), rn = quotient((uint32_t)tn, p.by_run_n);
+    const uint32_t m0 = rm * p.run_m + ((uint32_t)tm - rm * p.by_run_m.d) * Tile::BM, n0 = rn * p.run_n + ((uint32_t)tn - rn * p.by_run_n.d) * Tile::BN;
+    const uint32_t m1 = (rm + 1) * p.run_m, n1 = (rn + 1) * p.run_n;
     Tile t;
     // the parts take K tiles in turn: what they read at a time lies side by side in memory
-    t.run(p.A, p.B, p.s, m0, n0, cut, p.cuts, (p.s.all - cut + p.cuts - 1) / p.cuts, smem8);
+    t.run(p.A, p.B, p.s, m0, m1, n0, n1, cut, p.cuts, (p.s.all - cut + p.cuts - 1) / p.cuts, smem8);
 
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
     const uint32_t row0 = m0 + wave / WN * (TM * 16), col0 = n0 + wave % WN * (TN * 16);
@@ -97,7 +110,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const uint32_t row = row0 + i * 16 + r, col = col0 + j * 16 + q * 4;
-                if (row < p.M && col < p.N) *(TT_GLOBAL i32x4 *)(p.parts + ((size_t)cut * p.M + row) * p.np + col) = t.acc[i][j];
+                if (row < m1 && col < n1) store_sums(p.parts + ((size_t)cut * p.M + row) * p.np + col, t.acc[i][j], n1 - col);
             }
     } else {
         // rows of 16 TN values turned round through a strip of LDS that is the wave's own
@@ -110,12 +123,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t col = col0 + j * 16 + q * 4 + e;
-                ws[j][e] = load1(p.WS + (col < p.N ? col : p.N - 1));
+                ws[j][e] = load1(p.WS + (col < n1 ? col : n1 - 1));
             }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const uint32_t mine = row0 + i * 16 + r;
-            const float xs = load1(p.XS + (mine < p.M ? mine : p.M - 1));
+            const float xs = load1(p.XS + (mine < m1 ? mine : m1 - 1));
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 float v[4];
@@ -130,7 +143,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Pa
             for (uint32_t n = 0; n < NV; ++n) {
                 const uint32_t idx = lane + 64 * n, lrow = idx / VPR, vc = idx % VPR, row = row0 + i * 16 + lrow, col = col0 + vc * EV;
                 const u32x4 o = *reinterpret_cast<const u32x4 *>(strip + lrow * PITCH + vc * 16);
-                if (row < p.M && col < p.N) store_results<T>(p, row, col, o);
+                if (row < m1 && col < n1) store_results<T>(p, row, col, n1, o);
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -165,7 +178,7 @@ template <typename T> __global__ __launch_bounds__(kJoin) void fc8_join_kernel(c
     float v[EV];
 #pragma unroll
     for (uint32_t e = 0; e < EV; ++e) v[e] = activated(s[e / 4][e % 4], load1(p.WS + (col + e < p.N ? col + e : p.N - 1)), xs, p.relu);
-    store_results<T>(p, row, col, pack16(v, T()));
+    store_results<T>(p, row, col, p.N, pack16(v, T()));
 }
 
 // Few rows: a workgroup takes 16 TN channels and all of K, its eight waves every eighth K tile each.  A wave's loads of a tile are a whole
@@ -340,9 +353,17 @@ tt_status shape_of(const tt_layer *layer, int64_t batch, int k, int dtype, const
     return TT_OK;
 }
 
-bool whole_blocks(const Operand &o, const Steps8 &s, uint32_t rows)
+// How tiles of `size` are laid over an operand's rows: over all of them where tiles end where blocks do or there is one block; over
+// each block by itself where that takes at most a quarter more tiles.  one: a tile's rows lie in one block then, and no K tile passes a
+// row's end.
+struct Laid { uint32_t run, tiles; bool one; };
+Laid laid_over(const Operand &o, const Steps8 &s, uint32_t size)
 {
-    return (o.row_blocks == 1 || o.srows % rows == 0) && (o.k_shift == 0 || s.seg % BK8 == 0);
+    const bool ends = o.k_shift == 0 || s.seg % BK8 == 0;
+    const uint32_t all = tiles_of(o.rows, size), by_block = tiles_of(o.srows, size) * o.row_blocks;
+    if (o.row_blocks == 1 || o.srows % size == 0) return {o.rows, all, ends};
+    if (ends && by_block <= all + all / 4) return {o.srows, by_block, true};
+    return {o.rows, all, false};
 }
 
 template <int WM, int WN, int TM, int TN, int NS, bool ONE, typename T> tt_status launch_tiles_as(const Layer8Params &p, hipStream_t s)
@@ -355,17 +376,31 @@ template <int WM, int WN, int TM, int TN, int NS, bool ONE, typename T> tt_statu
     hipLaunchKernelGGL(kernel, dim3((total + kXcds - 1) / kXcds * kXcds), dim3(Tile::NT), Tile::kSmem, s, p);
     return TT_OK;
 }
-template <typename T> tt_status launch_tiles(const Layer8Params &p, Form form, hipStream_t s)
+template <typename T> tt_status launch_tiles(const Layer8Params &given, Form form, hipStream_t s)
 {
-    const auto whole = [&](Form f) { return whole_blocks(p.A, p.s, (uint32_t)kTileM[f]) && whole_blocks(p.B, p.s, (uint32_t)kTileN[f]); };
-    if (form == kBigTiles && whole(form)) return launch_tiles_as<2, 4, 8, 4, 2, true, T>(p, s);
-    if (form == kMiddleTiles && whole(form)) return launch_tiles_as<2, 2, 8, 4, 3, true, T>(p, s);
-    if (form == kTinyTiles && whole(form)) return launch_tiles_as<2, 2, 2, 2, 4, true, T>(p, s);
-    Layer8Params q = p;
-    q.tiles_m = tiles_of(p.M, 128);
-    q.tiles_n = tiles_of(p.N, 128);
-    if (whole(kSmallTiles)) return launch_tiles_as<2, 2, 4, 4, 4, true, T>(q, s);
-    return launch_tiles_as<2, 2, 4, 4, 2, false, T>(q, s);
+    Layer8Params p = given;
+    // (a form whose tiles do not fit the blocks gives way to one of smaller tiles, in the end to one that looks every row's block up)
+    for (; form >= kTinyTiles; form = form > kSmallTiles ? kSmallTiles : kFewRows) {
+        const Laid m = laid_over(p.A, p.s, (uint32_t)kTileM[form]), n = laid_over(p.B, p.s, (uint32_t)kTileN[form]);
+        p.run_m = m.run;
+        p.run_n = n.run;
+        p.tiles_m = m.tiles;
+        p.tiles_n = n.tiles;
+        p.by_run_m = divisor(tiles_of(m.run, kTileM[form]));
+        p.by_run_n = divisor(tiles_of(n.run, kTileN[form]));
+        if (!m.one || !n.one) continue;
+        if (form == kBigTiles) return launch_tiles_as<2, 4, 8, 4, 2, true, T>(p, s);
+        if (form == kMiddleTiles) return launch_tiles_as<2, 2, 8, 4, 3, true, T>(p, s);
+        if (form == kSmallTiles) return launch_tiles_as<2, 2, 4, 4, 4, true, T>(p, s);
+        return launch_tiles_as<2, 2, 2, 2, 4, true, T>(p, s);
+    }
+    p.run_m = p.M;
+    p.run_n = p.N;
+    p.tiles_m = tiles_of(p.M, 128);
+    p.tiles_n = tiles_of(p.N, 128);
+    p.by_run_m = divisor(p.tiles_m);
+    p.by_run_n = divisor(p.tiles_n);
+    return launch_tiles_as<2, 2, 4, 4, 2, false, T>(p, s);
 }
 // The more channels a workgroup takes, the less often X is read; a workgroup for every CU comes first.
 template <int TM, typename T> void launch_few_as(const Layer8Params &p, hipStream_t s)

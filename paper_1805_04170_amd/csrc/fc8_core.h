@@ -57,7 +57,7 @@ __device__ __forceinline__ RowAt row_at(const Operand &o, const Steps8 &s, uint3
 }
 
 // The K tiles of ROWS rows of an operand on their way into LDS, by NT threads: chunk c = tid + NT i of a tile is row c / 8, position
-// c % 8, and holds the row's chunk position ^ ((row >> 1) & 7).  Rows past the end are the last row again: they feed results that are
+// c % 8, and holds the row's chunk position ^ ((row >> 1) & 7).  Rows from `end` on are the last row again: they feed results that are
 // never stored.  ONE: the rows lie in one block and no K tile passes a row's end, so the address is a scalar and an offset.
 template <int ROWS, int NT, bool ONE> struct Feed {
     static constexpr int NL = ROWS * 8 / NT;
@@ -65,7 +65,7 @@ template <int ROWS, int NT, bool ONE> struct Feed {
     uint32_t voff[ONE ? NL : 1];
     uint64_t base;
     const char *row[ONE ? 1 : NL];
-    uint32_t most, row0, kc, tile;
+    uint32_t most, row0, end, kc, tile;
     At at;
     __device__ __forceinline__ void bind(const Operand &o, const Steps8 &s)
     {
@@ -75,15 +75,16 @@ template <int ROWS, int NT, bool ONE> struct Feed {
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 const uint32_t r = row0 + (threadIdx.x >> 3) + NT / 8 * i;
-                const RowAt x = row_at(o, s, r < o.rows ? r : o.rows - 1, at.seg);
+                const RowAt x = row_at(o, s, r < end ? r : end - 1, at.seg);
                 row[i] = x.p;
                 most = x.most;
             }
         }
     }
-    __device__ __forceinline__ void begin(const Operand &o, const Steps8 &s, uint32_t first_row, uint32_t first)
+    __device__ __forceinline__ void begin(const Operand &o, const Steps8 &s, uint32_t first_row, uint32_t end_row, uint32_t first)
     {
         row0 = first_row;
+        end = end_row;
         tile = first;
         at = at_tile(s, tile);
         kc = ((threadIdx.x & 7) ^ ((threadIdx.x >> 4) & 7)) * 16;
@@ -91,7 +92,7 @@ template <int ROWS, int NT, bool ONE> struct Feed {
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 const uint32_t r = row0 + (threadIdx.x >> 3) + NT / 8 * i;
-                voff[i] = ((r < o.rows ? r : o.rows - 1) - row0) * o.pitch + kc;
+                voff[i] = ((r < end ? r : end - 1) - row0) * o.pitch + kc;
             }
         }
         bind(o, s);
@@ -156,7 +157,8 @@ __device__ __forceinline__ void k_step8(i32x4 (&acc)[TM][TN], const Frags8<TM, T
     }
 }
 
-// Sums over `count` K tiles (more than 0), first, first + by, .., of rows m0 .. and channels n0 .. of the result.  WM x WN waves, each
+// Sums over `count` K tiles (more than 0), first, first + by, .., of rows m0 .. m1 - 1 and channels n0 .. n1 - 1 of the
+// result (of the tile from m0, n0 on).  WM x WN waves, each
 // 16 TM x 16 TN; NS LDS stages, so that NS - 1 K tiles are on their way or being multiplied.  A lane ends up with row lane % 16 and
 // four consecutive channels 4 (lane / 16) .. of every block.
 template <int WM, int WN, int TM, int TN, int NS, bool ONE> struct Tile8 {
@@ -168,14 +170,14 @@ template <int WM, int WN, int TM, int TN, int NS, bool ONE> struct Tile8 {
     static constexpr int LPS = FA::NL + FB::NL;
     static_assert(NS >= 2 && (NS - 1) * LPS < 64, "loads that a wait can count");
     i32x4 acc[TM][TN];
-    __device__ __forceinline__ void run(const Operand &A, const Operand &B, const Steps8 &s, uint32_t m0, uint32_t n0, uint32_t first, uint32_t by, uint32_t count, char *smem)
+    __device__ __forceinline__ void run(const Operand &A, const Operand &B, const Steps8 &s, uint32_t m0, uint32_t m1, uint32_t n0, uint32_t n1, uint32_t first, uint32_t by, uint32_t count, char *smem)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const uint32_t lds0 = dev::lds_addr(smem);
         FA fa;
         FB fb;
-        fa.begin(A, s, m0, first);
-        fb.begin(B, s, n0, first);
+        fa.begin(A, s, m0, m1, first);
+        fb.begin(B, s, n0, n1, first);
         uint32_t left = count - 1; // K tiles behind the one that is fetched next; past the end the last one is fetched again
         auto issue = [&](int i, uint32_t stage) {
             if (i < FA::NL) fa.issue(i, stage);

@@ -1,7 +1,8 @@
 // How kernels walk over the rows of tiled tensors with a row in registers: which lanes hold what of it, loads, stores, and sums and
 // maxima over it.
 //
-//   GroupWalk   rows of up to 32 vectors, and rows of segments of less than a vector: a power of two of lanes a row, a vector each
+//   GroupWalk   rows of up to 32 vectors, of up to 64 in several segments, and of segments of less than a vector: a power of two of
+//               lanes a row, a vector each
 //   SlotWalk    others: one wave or several a row.  A segment (row_walk.h) is dealt out in slots of 64 vectors, so that what a wave loads
 //               at a time lies in one block: row, block and address are scalars, and a lane adds its place in the slot.
 #pragma once
@@ -106,7 +107,8 @@ inline RowWalk row_walk(const BlockTable &a, const BlockTable &b, int64_t rows, 
 inline RowLaunch row_launch(RowWalk *w, int ev, uint32_t most = 4, uint32_t limit = 4)
 {
     RowLaunch l{kLong, 0, 64, kMostWaves, kMostThreads, 1};
-    if (w->r.units <= 32 || narrow_segments(w->r, ev)) { // (a row of narrow segments has at most 64 vectors)
+    // rows of up to 32 vectors, or 64 in segments that would leave half of the slots empty (a row of narrow segments has at most 64)
+    if (w->r.units <= 32 || (w->r.units <= 64 && w->slots > 1) || narrow_segments(w->r, ev)) {
         uint32_t lanes = 1;
         while (lanes < w->r.units) lanes <<= 1;
         l = {kGroups, 1, lanes, 0, kWaveBlock, kWaveBlock / lanes};

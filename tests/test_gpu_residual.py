@@ -509,7 +509,7 @@ def test_layer8(M, K, N, dt):
 
 CUTS = [("R", "C", "R", 8, 64, 32), ("C", "R", "C", 20, 256, 40), ("C", "R", "r", 70, 36, 40), ("C", "C", "R", 130, 256, 136), ("CC", "RC", "CR", 132, 64, 264), ("CC", "RC", "Cr", 20, 52, 24),
         ("rr", "RR", "RC", 68, 192, 36), ("RC", "CR", "CC", 72, 96, 72), ("CCC", "RRR", "CCr", 136, 1040, 144), ("CCC", "RRC", "RRR", 16, 72, 40), ("RRR", "CCC", "rrr", 264, 130, 80),
-        ("CCC", "CCR", "RCC", 264, 512, 264)]
+        ("CCC", "CCR", "RCC", 264, 512, 264), ("RR", "CC", "CR", 400, 128, 400), ("R", "C", "C", 1000, 256, 1036), ("RC", "RC", "RR", 600, 384, 300), ("RR", "RR", "rC", 1024, 320, 72)]
 
 
 @pytest.mark.parametrize("tX,tW,tY,M,K,N", CUTS)
