@@ -73,6 +73,6 @@ def steps(U):
 
 def layer8(XQ, XS, WQ, WS, relu):
     """XQ: tokens x inputs, WQ: inputs x outputs, whole numbers; scales in 64 bits"""
-    total = XQ.astype(np.int64) @ WQ.astype(np.int64)
-    Y = total.astype(np.float64) * WS[None, :] * XS[:, None]
+    total = XQ.astype(np.float64) @ WQ.astype(np.float64)      # (whole numbers below 2^53: exact in any order)
+    Y = total * WS[None, :] * XS[:, None]
     return np.where(Y < 0, 0.0, Y) if relu else Y

@@ -84,7 +84,7 @@ __device__ __forceinline__ void store_sums(int32_t *to, i32x4 v, uint32_t left)
 extern __shared__ __align__(16) char smem8[];
 
 // T: the result's type, or int32_t: sums of a part of K
-template <int WM, int WN, int TM, int TN, int NS, bool ONE, typename T>
+template <int WM, int WN, int TM, int TN, int NS, int ONE, typename T>
 __global__ __launch_bounds__(WM *WN * 64, 2) void fc8_tile_kernel(const Layer8Params p)
 {
     typedef Tile8<WM, WN, TM, TN, NS, ONE> Tile;
@@ -184,7 +184,7 @@ template <typename T> __global__ __launch_bounds__(kJoin) void fc8_join_kernel(c
 // Few rows: a workgroup takes 16 TN channels and all of K, its eight waves every eighth K tile each.  A wave's loads of a tile are a whole
 // 128-byte line of each of its rows.
 constexpr uint32_t kFew = 512, kFewWaves = kFew / 64;
-constexpr int kFewAhead = 4; // K tiles that are asked for together
+constexpr int kFewAhead = 4; // K tiles that are asked for together (two, and the next two on their way meanwhile: 18.8 us instead of 14.9)
 template <int TM, int TN, typename T> __global__ __launch_bounds__(kFew, 2) void fc8_few_kernel(const Layer8Params p)
 {
     __shared__ __align__(16) int32_t sums[kFewWaves][TM * 16][TN * 16];
@@ -214,7 +214,7 @@ template <int TM, int TN, typename T> __global__ __launch_bounds__(kFew, 2) void
 #pragma unroll
         for (int u = 0; u < kFewAhead; ++u) {
             const uint32_t t = t0 + u * kFewWaves;
-            const At at = at_tile(p.s, t < p.s.all ? t : t0);
+            const At at = at_tile(p.s, t < p.s.all ? t : t0); // (past the end the first one again, which is not multiplied)
             if (p.s.segments != 1) bind(at.seg);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -306,7 +306,10 @@ Plan plan_of(const Shape8 &g, int64_t M)
     Plan p{kFewRows, 1, 1, 1, 0, 0};
     const uint32_t all = (uint32_t)(g.K / g.seg) * tiles_of(g.seg, BK8);
     if (g.gather) p.gather_bytes = align_up((size_t)M * (size_t)(g.K / g.seg) * (size_t)tt_pitch8(g.seg), 256);
-    if (M <= 64) return p;
+    // Few rows straight from memory while a wave asks for all of its K tiles at once: 16 x 4096 x 4096 9.0 us, in tiles 10.9; 32 x 2048 x 2048
+    // 8.1 and 9.0.  Not beyond: 16 x 8192 x 8192 20 us, in tiles 17; 16 x 16384 x 1024 19 and 11; 64 x 2048 x 2048 12 and 9.
+    if ((M <= 16 && all <= kFewWaves * kFewAhead) || (M <= 32 && all <= kFewWaves * kFewAhead / 2)) return p;
+    M = (M + 63) / 64 * 64; // (one choice, and one size of a workspace, for all rows that the smallest tile holds)
     // What a form costs, in hundredths of a microsecond: rounds of workgroups over the CUs, each a start, its K tiles and its results;
     // parts of K are written and read again, by one more launch.
     const uint64_t tile_cost[] = {0, 36, 49, 75, 112}, start[] = {0, 570, 720, 1050, 1000};
@@ -354,19 +357,18 @@ tt_status shape_of(const tt_layer *layer, int64_t batch, int k, int dtype, const
 }
 
 // How tiles of `size` are laid over an operand's rows: over all of them where tiles end where blocks do or there is one block; over
-// each block by itself where that takes at most a quarter more tiles.  one: a tile's rows lie in one block then, and no K tile passes a
-// row's end.
-struct Laid { uint32_t run, tiles; bool one; };
+// each block by itself where that takes at most a quarter more tiles.
+struct Laid { uint32_t run, tiles; int one; };
 Laid laid_over(const Operand &o, const Steps8 &s, uint32_t size)
 {
-    const bool ends = o.k_shift == 0 || s.seg % BK8 == 0;
+    const int one = o.k_shift == 0 || s.seg % BK8 == 0 ? kInside : kToTheEnd;
     const uint32_t all = tiles_of(o.rows, size), by_block = tiles_of(o.srows, size) * o.row_blocks;
-    if (o.row_blocks == 1 || o.srows % size == 0) return {o.rows, all, ends};
-    if (ends && by_block <= all + all / 4) return {o.srows, by_block, true};
-    return {o.rows, all, false};
+    if (o.row_blocks == 1 || o.srows % size == 0) return {o.rows, all, one};
+    if (by_block <= all + all / 4) return {o.srows, by_block, one};
+    return {o.rows, all, kAnywhere};
 }
 
-template <int WM, int WN, int TM, int TN, int NS, bool ONE, typename T> tt_status launch_tiles_as(const Layer8Params &p, hipStream_t s)
+template <int WM, int WN, int TM, int TN, int NS, int ONE, typename T> tt_status launch_tiles_as(const Layer8Params &p, hipStream_t s)
 {
     typedef Tile8<WM, WN, TM, TN, NS, ONE> Tile;
     auto kernel = fc8_tile_kernel<WM, WN, TM, TN, NS, ONE, T>;
@@ -380,7 +382,7 @@ template <typename T> tt_status launch_tiles(const Layer8Params &given, Form for
 {
     Layer8Params p = given;
     // (a form whose tiles do not fit the blocks gives way to one of smaller tiles, in the end to one that looks every row's block up)
-    for (; form >= kTinyTiles; form = form > kSmallTiles ? kSmallTiles : kFewRows) {
+    for (; form >= kTinyTiles; form = form == kSmallTiles ? kFewRows : kSmallTiles) {
         const Laid m = laid_over(p.A, p.s, (uint32_t)kTileM[form]), n = laid_over(p.B, p.s, (uint32_t)kTileN[form]);
         p.run_m = m.run;
         p.run_n = n.run;
@@ -388,11 +390,13 @@ template <typename T> tt_status launch_tiles(const Layer8Params &given, Form for
         p.tiles_n = n.tiles;
         p.by_run_m = divisor(tiles_of(m.run, kTileM[form]));
         p.by_run_n = divisor(tiles_of(n.run, kTileN[form]));
-        if (!m.one || !n.one) continue;
-        if (form == kBigTiles) return launch_tiles_as<2, 4, 8, 4, 2, true, T>(p, s);
-        if (form == kMiddleTiles) return launch_tiles_as<2, 2, 8, 4, 3, true, T>(p, s);
-        if (form == kSmallTiles) return launch_tiles_as<2, 2, 4, 4, 4, true, T>(p, s);
-        return launch_tiles_as<2, 2, 2, 2, 4, true, T>(p, s);
+        const int one = m.one < n.one ? m.one : n.one;
+        if (one == kAnywhere || (one == kToTheEnd && form != kSmallTiles)) continue;
+        if (form == kBigTiles) return launch_tiles_as<2, 4, 8, 4, 2, kInside, T>(p, s);
+        if (form == kMiddleTiles) return launch_tiles_as<2, 2, 8, 4, 3, kInside, T>(p, s);
+        if (form == kTinyTiles) return launch_tiles_as<2, 2, 2, 2, 4, kInside, T>(p, s);
+        if (one == kInside) return launch_tiles_as<2, 2, 4, 4, 4, kInside, T>(p, s);
+        return launch_tiles_as<2, 2, 4, 4, 4, kToTheEnd, T>(p, s);
     }
     p.run_m = p.M;
     p.run_n = p.N;
@@ -400,7 +404,7 @@ template <typename T> tt_status launch_tiles(const Layer8Params &given, Form for
     p.tiles_n = tiles_of(p.N, 128);
     p.by_run_m = divisor(p.tiles_m);
     p.by_run_n = divisor(p.tiles_n);
-    return launch_tiles_as<2, 2, 4, 4, 2, false, T>(p, s);
+    return launch_tiles_as<2, 2, 4, 4, 2, kAnywhere, T>(p, s);
 }
 // The more channels a workgroup takes, the less often X is read; a workgroup for every CU comes first.
 template <int TM, typename T> void launch_few_as(const Layer8Params &p, hipStream_t s)
@@ -414,8 +418,7 @@ template <typename T> tt_status launch_layer(const Layer8Params &p, Form form, h
 {
     if (form == kFewRows) {
         if (p.M <= 16) launch_few_as<1, T>(p, s);
-        else if (p.M <= 32) launch_few_as<2, T>(p, s);
-        else launch_few_as<4, T>(p, s);
+        else launch_few_as<2, T>(p, s);
         return TT_OK;
     }
     if (p.cuts == 1) return launch_tiles<T>(p, form, s);
@@ -446,7 +449,7 @@ extern "C" tt_status tt_fc8_workspace_bytes(const tt_layer *layer, int64_t batch
     if (!bytes) return TT_EINVAL;
     const tt_status st = shape_of(layer, batch, k, dtype, tX, tW, tY, &g);
     if (st != TT_OK) return st;
-    // enough for fewer rows too: where the rows are fewer, K is cut into more parts
+    // enough for fewer rows too: where the rows are fewer, K is cut into more parts (plan_of() goes by multiples of 64)
     *bytes = 0;
     for (int64_t m = batch; m > 0; m = m > 64 * 1024 ? m / 2 : (m - 1) / 64 * 64) {
         const Plan p = plan_of(g, m);

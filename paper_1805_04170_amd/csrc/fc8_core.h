@@ -58,8 +58,12 @@ __device__ __forceinline__ RowAt row_at(const Operand &o, const Steps8 &s, uint3
 
 // The K tiles of ROWS rows of an operand on their way into LDS, by NT threads: chunk c = tid + NT i of a tile is row c / 8, position
 // c % 8, and holds the row's chunk position ^ ((row >> 1) & 7).  Rows from `end` on are the last row again: they feed results that are
-// never stored.  ONE: the rows lie in one block and no K tile passes a row's end, so the address is a scalar and an offset.
-template <int ROWS, int NT, bool ONE> struct Feed {
+// never stored.
+//   kInside     the rows lie in one block and no K tile passes a row's end, so the address is a scalar and an offset
+//   kToTheEnd   ... but K tiles may pass the row's end: lanes behind it fetch the tile's first bytes instead
+//   kAnywhere   rows of any block
+enum { kAnywhere = 0, kToTheEnd = 1, kInside = 2 };
+template <int ROWS, int NT, int ONE> struct Feed {
     static constexpr int NL = ROWS * 8 / NT;
     static_assert(NL >= 1 && (NT / 8) % 16 == 0, "the swizzle is the same for all of a thread's chunks");
     uint32_t voff[ONE ? NL : 1];
@@ -70,7 +74,9 @@ template <int ROWS, int NT, bool ONE> struct Feed {
     __device__ __forceinline__ void bind(const Operand &o, const Steps8 &s)
     {
         if constexpr (ONE) {
-            base = core2::uniform64(row_at(o, s, row0, at.seg).p) + (uint64_t)at.tile * BK8;
+            const RowAt x = row_at(o, s, row0, at.seg);
+            base = core2::uniform64(x.p) + (uint64_t)at.tile * BK8;
+            most = uniform(x.most);
         } else {
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
@@ -112,8 +118,10 @@ template <int ROWS, int NT, bool ONE> struct Feed {
     __device__ __forceinline__ void issue(int i, uint32_t lds) const
     {
         const uint32_t to = lds + core2::wave2() * 1024u + (uint32_t)i * (NT * 16u);
-        if constexpr (ONE) {
+        if constexpr (ONE == kInside) {
             dev::lds_dma16(voff[i], base, to);
+        } else if constexpr (ONE == kToTheEnd) {
+            dev::lds_dma16(at.tile * BK8 + kc <= most ? voff[i] : voff[i] - kc, base, to);
         } else {
             const uint32_t off = at.tile * BK8 + kc;
             dev::lds_dma16(row[i] + (off < most ? off : most), to);
@@ -161,7 +169,7 @@ __device__ __forceinline__ void k_step8(i32x4 (&acc)[TM][TN], const Frags8<TM, T
 // result (of the tile from m0, n0 on).  WM x WN waves, each
 // 16 TM x 16 TN; NS LDS stages, so that NS - 1 K tiles are on their way or being multiplied.  A lane ends up with row lane % 16 and
 // four consecutive channels 4 (lane / 16) .. of every block.
-template <int WM, int WN, int TM, int TN, int NS, bool ONE> struct Tile8 {
+template <int WM, int WN, int TM, int TN, int NS, int ONE> struct Tile8 {
     static constexpr int NT = WM * WN * 64, BM = WM * TM * 16, BN = WN * TN * 16;
     static constexpr int kA = BM * BK8, kB = BN * BK8, kStage = kA + kB;
     static constexpr size_t kSmem = NS * (size_t)kStage;

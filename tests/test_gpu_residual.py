@@ -502,7 +502,8 @@ LAYERS = [(1, 1, 1), (1, 5, 3), (3, 128, 16), (16, 200, 40), (17, 64, 33), (40, 
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-@pytest.mark.parametrize("M,K,N", LAYERS + [(16, 4096, 8200), (300, 3000, 1000), (2049, 256, 4100), (4000, 300, 3001)])
+@pytest.mark.parametrize("M,K,N", LAYERS + [(16, 4096, 8200), (32, 2048, 500), (9, 4300, 70), (300, 3000, 1000), (2049, 256, 4100), (4000, 300, 3001),
+                                            (989, 141, 4118), (5470, 67, 381), (5541, 12596, 147), (6565, 7442, 65)])
 def test_layer8(M, K, N, dt):
     run_layer8(M, K, N, dt, relu=M % 2 == 0)
 
@@ -530,8 +531,8 @@ def test_layer8_of_the_largest_sums():
 
 
 def test_layer8_workspace_covers_fewer_rows():
-    for M in (65, 128, 129, 200, 256):
-        run_layer8(M, 1024, 130, "f32", spare=300 - M)
+    for M in (1, 17, 64, 65, 128, 129, 200):
+        run_layer8(M, 4224, 130, "f32", spare=300 - M)
 
 
 def test_layer8_scales_that_are_not_numbers():
@@ -589,6 +590,57 @@ def test_a_block_in_8_bits(T, D, F, t, dt):
     run_chain8(T, D, F, dt, *t)
 
 
+# ------------------------------------------------ a block as it is trained
+
+def run_block_step(T, D, F, dt, p, tX, tY, tW, tZ, seed=29):
+    """Y = norm(R + dropout(X)), Z = relu(Y W); back through the layer, the norm and the dropout.  Each stage is held to its bound on what
+    the stage before it left."""
+    k = len(tX)
+    X, Xf, R, Rf = norm_inputs(T, D, seed, dt, True)
+    g, gf = gain_of(D, seed, dt, True)
+    W, Wf = stored_dt(normal_f32(seed, 5, (D, F), D ** -0.5), dt)
+    dZ, dZf = stored_dt(normal_f32(seed, 6, (T, F), 0.1), dt)
+    dL, dLf = stored_dt(normal_f32(seed, 8, (T, D), 0.1), dt)      # what arrives on the sum from the layers behind the block
+    drop = drop_of(p, 41, 3, 9)
+    keep = mask_of(T, D, p, 41, 3, 9)
+    H, Y = base.outputs(T, D, tX, dt), base.outputs(T, D, tY, dt)
+    tt.tt_norm_forward(T, D, k, dt, tX, tY, NORM_EPS, base.shards(X, tX), base.shards(R, tX), g, H, Y, drop)
+    lay = tt.layer("fc", "relu", D, F)
+    Z, Ws = base.outputs(T, F, tZ, dt), base.shards(W, tW)
+    tt.tt_fc_forward(lay, T, k, dt, tY, tW, tZ, None, Y, Ws, Z, base.workspace(tt.tt_fc_workspace_bytes(lay, T, k, dt, tt.TT_OP_FWD, tY, tW, tZ)))
+    dY, dW = base.outputs(T, D, tY, dt), base.outputs(D, F, tW, dt)
+    ws = base.workspace(tt.tt_fc_workspace_bytes(lay, T, k, dt, tt.TT_OP_DGRAD, tY, tW, tZ, tZ, tY))
+    tt.tt_fc_backward(lay, T, k, dt, tY, tW, tZ, tZ, tY, None, None, Y, Ws, Z, base.shards(dZ, tZ), dY, dW, ws)
+    dS, dX, dg = base.outputs(T, D, tX, dt), base.outputs(T, D, tX, dt), base.empty((D,), torch.float32)
+    ws = base.workspace(tt.tt_norm_workspace_bytes(T, D, k, dt, tX, tY))
+    tt.tt_norm_backward(T, D, k, dt, tX, tY, NORM_EPS, H, g, dY, base.shards(dL, tX), dS, dX, dg, ws, drop)
+    h, y, z, dy = (base.full(a, t, T, n).astype(np.float64) for a, t, n in ((H, tX, D), (Y, tY, D), (Z, tZ, F), (dY, tY, D)))
+    e32, eo = float(np.float32(NORM_EPS)), base.out_eps(dt)
+    total = Rf + rs.dropout(Xf, p, keep)
+    base.check(h, total, (3 * EPS + eo) * (np.abs(total) + np.abs(total - Rf)), "H")
+    want = rs.norm(h, gf, e32)[0]
+    base.check(y, want, (270 * EPS + eo) * (1 + 2.0 ** -8) * np.abs(want), "Y")
+    G = dZf * (z > 0)
+    # (a product of K terms: chains of fp32 additions, K eps of the sum of magnitudes at most)
+    base.check(z, np.maximum(y @ Wf, 0), D * EPS * (np.abs(y) @ np.abs(Wf)) + eo * np.abs(y @ Wf) * (1 + 2.0 ** -8) + eo * D * EPS, "Z")
+    base.check(dy, G @ Wf.T, (F * EPS + eo) * (np.abs(G) @ np.abs(Wf.T)), "dY")
+    want, want_g = rs.norm_backward(h, gf, e32, dy, dLf)
+    r = 1.0 / np.sqrt(np.mean(h * h, axis=1, keepdims=True) + e32)
+    n = np.abs(h * r)
+    err = 1100 * EPS * r * (np.abs(gf * dy) + n * np.mean(np.abs(gf * dy) * n, axis=1, keepdims=True)) + 2 * EPS * (np.abs(dLf) + np.abs(want))
+    base.check(base.full(dS, tX, T, D), want, err + eo * (np.abs(want) + err), "dS")
+    f = 65536.0 / (65536 - rs.dropped_below(p))
+    bound = f * err + 2 * EPS * f * np.abs(want)
+    base.check(base.full(dX, tX, T, D), rs.dropout(want, p, keep), bound + eo * (f * np.abs(want) + bound), "dX")
+    base.check(base.down(dg), want_g, (270 + T) * EPS * np.sum(np.abs(dy) * n, axis=0), "dgain")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D,F,t", [(24, 72, 96, ("", "", "", "")), (64, 256, 128, ("C", "R", "C", "C")), (32, 128, 256, ("RC", "RR", "rr", "RR")), (64, 64, 64, ("CCC", "rRR", "RCC", "CRC"))])
+def test_a_block_trained(T, D, F, t, dt):
+    run_block_step(T, D, F, dt, 0.2, *t)
+
+
 # ------------------------------------------------------------ streams and graphs
 
 def test_a_captured_step_takes_the_number_it_finds():
@@ -641,3 +693,74 @@ def test_calls_on_another_stream():
     s.synchronize()
     m = X.double().abs().amax(1, keepdim=True)
     assert torch.all((Y.double() - X.double()).abs() <= m / 127 * 0.5 + 2.0 ** -8 * X.double().abs() + 2.0 ** -8 * m / 127)
+
+
+def test_a_block_in_8_bits_captured_and_replayed():
+    T, D, F = 96, 520, 4104
+    dev = base.DEV
+    g = torch.Generator(device=dev)
+    g.manual_seed(7)
+    X, R = (torch.randn(T, D, device=dev, generator=g).bfloat16() for _ in range(2))
+    W = (torch.randn(D, F, device=dev, generator=g) * D ** -0.5).bfloat16()
+    WQ, WS = torch.empty(F, tt.tt_pitch8(D), dtype=torch.int8, device=dev), torch.empty(F, device=dev)
+    tt.tt_weights8(D, F, 0, "bf16", "", [W], [WQ], WS, torch.empty(tt.tt_weights8_workspace_bytes(D, F, 0, ""), dtype=torch.uint8, device=dev))
+    lay = tt.layer("fc", "relu", D, F)
+    ws = torch.empty(max(256, tt.tt_fc8_workspace_bytes(lay, T, 0, "bf16", "", "", "")), dtype=torch.uint8, device=dev)
+
+    def out():
+        return [torch.empty_like(X), torch.empty(T, tt.tt_pitch8(D), dtype=torch.int8, device=dev), torch.empty(T, device=dev), torch.empty(T, F, dtype=torch.bfloat16, device=dev)]
+
+    def call(o):
+        tt.tt_norm_forward8(T, D, 0, "bf16", "", "", 1e-5, [X], [R], None, [o[0]], [o[1]], o[2])
+        tt.tt_fc_forward8(lay, T, 0, "bf16", "", "", "", [o[1]], o[2], [WQ], WS, [o[3]], ws)
+    held = out()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(held)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(held)
+    for step in range(3):
+        X.normal_(generator=g)
+        for o in held:
+            o.fill_(1)
+        graph.replay()
+        eager = out()
+        call(eager)
+        torch.cuda.synchronize()
+        for a, b in zip(held, eager):
+            assert torch.equal(a, b), step
+
+
+def test_rows_and_layers_beyond_32_bit_offsets():
+    """tensors of more than 2^31 values: what lies behind them is reached, and what lies in front stays apart"""
+    dev = base.DEV
+    T, D = 270000, 8192
+    X = torch.zeros(T, D, dtype=torch.bfloat16, device=dev)
+    X[-3:] = torch.randn(3, D, device=dev).bfloat16()
+    X[:2] = 3.0
+    Q, S = torch.empty(T, D, dtype=torch.int8, device=dev), torch.empty(T, device=dev)
+    tt.tt_rows8(T, D, 0, "bf16", "", "", [X], [Q], S)
+    Y = torch.empty_like(X)
+    tt.tt_unrows8(T, D, 0, "bf16", "", "", [Q], S, [Y])
+    m = X[-3:].double().abs().amax(1, keepdim=True)
+    want = torch.round(X[-3:].double() * 127.0 / m)
+    assert torch.equal(Q[-3:].double(), want) and torch.all(Q[:2] == 127) and not Q[2:-3].any()
+    assert torch.all((Y[-3:].double() - X[-3:].double()).abs() <= m / 254 + 2.0 ** -7 * X[-3:].double().abs() + 2.0 ** -8 * m / 127)
+    tt.tt_norm_forward(T, D, 0, "bf16", "", "", 1e-5, [X], None, None, None, [Y])
+    r = torch.rsqrt(X[-3:].double().square().mean(1, keepdim=True) + 1e-5)
+    assert torch.all((Y[-3:].double() - X[-3:].double() * r).abs() <= 2.0 ** -7 * (X[-3:].double() * r).abs()) and not Y[2:-3].any()
+    tt.tt_dropout(tt.drop(0.5, 3), T, D, 0, "bf16", "", "", [X], [Y])
+    part = torch.empty(4, D, dtype=torch.bfloat16, device=dev)
+    tt.tt_dropout(tt.drop(0.5, 3), 4, D, 0, "bf16", "", "", [X[:4]], [part])
+    assert torch.equal(Y[:4], part) and 0.4 < float((Y[-3:] == 0).float().mean()) < 0.6
+    # a layer whose input has more than 2^31 bytes
+    lay = tt.layer("fc", "none", D, 16)
+    W, WS = torch.ones(16, D, dtype=torch.int8, device=dev), torch.ones(16, device=dev)
+    Z = torch.empty(T, 16, device=dev)
+    ws = torch.empty(max(256, tt.tt_fc8_workspace_bytes(lay, T, 0, "f32", "", "", "")), dtype=torch.uint8, device=dev)
+    tt.tt_fc_forward8(lay, T, 0, "f32", "", "", "", [Q], S, [W], WS, [Z], ws)
+    want = Q[-3:].double().sum(1, keepdim=True) * S[-3:].double()[:, None]
+    assert torch.all((Z[-3:].double() - want).abs() <= 3 * EPS * want.abs()) and not Z[2:-3].any()

@@ -113,7 +113,7 @@ def test_workspaces_cover_fewer_rows():
     for K, N in [(128, 64), (4096, 1000), (8192, 8192), (131071, 300)]:
         lay = tt.layer("fc", "none", K, N)
         last = 0
-        for M in list(range(0, 700, 13)) + [1000, 1024, 2000, 4096, 10000, 1 << 17, 1 << 20]:
+        for M in list(range(0, 700, 7)) + [1000, 1024, 2000, 4096, 10000, 1 << 17, 1 << 20]:
             now = tt.tt_fc8_workspace_bytes(lay, M, 0, "f32", "", "", "")
             assert now >= last, (K, N, M)
             last = now
@@ -163,9 +163,9 @@ def test_weights8_refusals():
 
 
 def test_layer8_refusals():
-    lay = tt.layer("fc", "relu", 1024, 256)
+    lay = tt.layer("fc", "relu", 16384, 256)
     need = tt.tt_fc8_workspace_bytes(lay, 100, 0, "f32", "", "", "")
-    assert need > 0 and tt.tt_fc8_workspace_bytes(lay, 16, 0, "f32", "", "", "") == 0
+    assert need > 0 and tt.tt_fc8_workspace_bytes(tt.layer("fc", "relu", 4096, 256), 16, 0, "f32", "", "", "") == 0
     f = lambda l=lay, M=100, k=0, dt="f32", tX="", tW="", tY="", XQ=P, XS=A, WQ=P, WS=A, Y=P, ws=Bytes(need): tt.tt_fc_forward8(  # noqa: E731
         l, M, k, dt, tX, tW, tY, XQ, XS, WQ, WS, Y, ws, stream=1)
     for bad in (dict(l=tt.layer("conv2d", "relu", 8, 8, 4, 4, 3, 3, 1)), dict(l=tt.layer("fc", "relu", 0, 8)), dict(l=tt.layer("fc", "relu", 8, 0)), dict(M=-1), dict(k=7), dict(dt=5), dict(XQ=None),

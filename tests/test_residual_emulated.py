@@ -164,11 +164,22 @@ def test_layer8_tiled(tX, tW, tY, M, K, N, dt):
     g.run_layer8(M, K, N, dt, tX, tW, tY)
 
 
-@DTYPES
-def test_layer8_of_many_tiles(dt):
-    g.run_layer8(600, 130, 3100, dt)     # tiles of 128 x 128
-    if dt == "bf16":
-        g.run_layer8(2050, 128, 5400, dt)    # tiles of 256 x 256
+# the forms of a product by the launch code's environment overrides, which the product build does not have: tiles of 64 x 64, 128 x 128,
+# 256 x 128 and 256 x 256; K in parts; blocks of rows and of K that tiles end in, pass, or lie across
+@pytest.mark.parametrize("form,parts", [(1, 1), (1, 3), (2, 1), (2, 2), (3, 1), (3, 2), (4, 1)])
+def test_layer8_forms(form, parts, monkeypatch):
+    monkeypatch.setenv("TT_FC8_FORM", str(form))
+    monkeypatch.setenv("TT_FC8_CUTS", str(parts))
+    g.run_layer8(130, 700, 270, "bf16", relu=False)
+    g.run_layer8(132, 576, 136, "f32", "R", "C", "C")
+
+
+@pytest.mark.parametrize("tX,tW,tY,M,K,N", [("r", "R", "r", 70, 288, 40), ("C", "r", "R", 70, 288, 40), ("RC", "Cr", "CR", 140, 544, 264), ("RR", "RR", "CC", 520, 576, 72),
+                                            ("rr", "CC", "RC", 70, 200, 520), ("RR", "CC", "rr", 72, 130, 72)])
+def test_layer8_where_blocks_end_inside_tiles(tX, tW, tY, M, K, N, monkeypatch):
+    monkeypatch.setenv("TT_FC8_FORM", "2")
+    monkeypatch.setenv("TT_FC8_CUTS", "1")
+    g.run_layer8(M, K, N, "bf16", tX, tW, tY)
 
 
 def test_layer8_in_parts():
@@ -180,3 +191,9 @@ def test_layer8_in_parts():
 @pytest.mark.parametrize("T,D,F,t", [(3, 72, 200, ("", "", "", "", "")), (16, 64, 128, ("C", "R", "C", "R", "R")), (40, 72, 104, ("CCC", "RRC", "RCC", "CRR", "CCR"))])
 def test_a_block_in_8_bits(T, D, F, t, dt):
     g.run_chain8(T, D, F, dt, *t)
+
+
+@DTYPES
+@pytest.mark.parametrize("t", [("", "", "", ""), ("RC", "RR", "rr", "RR")])
+def test_a_block_trained(t, dt):
+    g.run_block_step(16, 64, 32, dt, 0.2, *t)
