@@ -449,25 +449,36 @@ struct GradLaunch {
     uint32_t groups;
     size_t stats_bytes, bytes;
 };
-// Four rows a wave or more: partial sums are a sixteenth of what is read and written then, and less.
+// Four rows a workgroup or more where there are many, so that partial sums are a sixteenth of what is read and written, and less; two
+// where workgroups of four would leave the chip fewer than 16 waves a CU.
+uint32_t grad_groups(const RowLaunch &l, int64_t rows)
+{
+    const int64_t most = row_groups(l, rows, kMostThreads), walks = (rows + l.at_once - 1) / l.at_once;
+    int64_t n = walks / 4, few = 16 * kCUs / (l.block / 64);
+    if (few > (walks + 1) / 2) few = (walks + 1) / 2;
+    if (n < few) n = few;
+    return (uint32_t)(n < most ? n : most);
+}
 GradLaunch grad_launch(RowWalk *w, int64_t rows, int ev)
 {
     GradLaunch g;
-    g.l = row_launch(w, ev, 1, ev == 8 ? kGradLimit<uint16_t> : kGradLimit<float>); // (more vectors a lane leave too few waves)
+    // A vector a lane, whose sums by column leave room for the next row's: rows of 2048 bf16 59 us, with two a lane 62 (16384 of them); of
+    // 4096 105 and 111.  Two where that makes a row one wave's, without a barrier: 1024 bf16 60 and 56 us (32768 rows).
+    g.l = row_launch(w, ev, w->slots == 2 ? 2 : 1, ev == 8 ? kGradLimit<uint16_t> : kGradLimit<float>);
     g.stats_bytes = 0;
     if (g.l.kind == kLong) {
         g.groups = (uint32_t)(rows < 64 ? rows : 64); // (of each strip)
         g.stats_bytes = align_up((size_t)rows * 2 * sizeof(double), 256);
     } else {
-        const int64_t most = row_groups(g.l, rows, kMostThreads), walks = (rows + g.l.at_once - 1) / g.l.at_once;
-        const int64_t waves = g.l.block / 64, least = tuning_int("TT_GRAD_LEAST", 2);
-        int64_t n = walks / 4, few = 16 * kCUs / waves;
-        if (few > (walks + least - 1) / least) few = (walks + least - 1) / least;
-        if (n < few) n = few;
-        if (n < 1) n = 1;
-        g.groups = (uint32_t)(n < most ? n : most);
+        g.groups = grad_groups(g.l, rows);
     }
-    g.bytes = rows == 0 || w->r.cols == 0 ? 0 : g.stats_bytes + align_up((size_t)g.groups * w->r.cols * sizeof(float), 256);
+    // (what is enough for so many rows is enough for fewer, which may have two waves a row instead of one, and more workgroups)
+    uint32_t parts = g.groups;
+    if (w->slots == 2) {
+        const uint32_t two = grad_groups({kSlots, 1, 64, 2, 128, 1}, rows);
+        parts = parts > two ? parts : two;
+    }
+    g.bytes = rows == 0 || w->r.cols == 0 ? 0 : g.stats_bytes + align_up((size_t)parts * w->r.cols * sizeof(float), 256);
     return g;
 }
 
@@ -541,7 +552,7 @@ extern "C" tt_status tt_norm_forward(int64_t rows, int64_t width, int k, int dty
     p.eps = eps;
     p.per_col = (float)(1.0 / (double)width);
     p.w = row_walk(p.X, p.Y, rows, width, 16 / e);
-    const RowLaunch l = row_launch(&p.w, 16 / e, 1);
+    const RowLaunch l = row_launch(&p.w, 16 / e);
     p.w.groups = row_groups(l, rows);
     p.w.flags = (R ? kResidual : 0) + (H ? kKeepSum : 0);
     p.w.once = (uint64_t)rows * width * e * ((H ? p.H.nrep : 0) + p.Y.nrep) >= kOnceBytes;

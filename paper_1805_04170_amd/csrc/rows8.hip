@@ -71,7 +71,7 @@ template <int BITS> struct Cut8<true, BITS> { // u fp32
         far = fmaxf(far, fabsf(fmaf(u, inv, kRound - q)));
         return __float_as_uint(q);
     }
-    static __device__ __forceinline__ bool near_border(float far) { return far > 0.4999f; }
+    static __device__ __forceinline__ bool near_border(float far) { return far > 0.49998f; }
     // the step of a u whose quotient is near a border j + 1/2: 127 u against (j + 1/2) m, products that fp32 holds where u has up to
     // 16 bits (of two bf16 values)
     __device__ __forceinline__ uint32_t exactly(float u) const
