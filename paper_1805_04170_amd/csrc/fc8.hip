@@ -2,8 +2,14 @@
 // tile of the result reads the blocks that it needs, and a cut of K is a change of address between two K tiles instead of a sum
 // of shards' results.
 //
-// Three forms: few rows (a weight's row goes from memory to a wave's registers once, waves share K); tiles through LDS; tiles whose K
-// is cut into parts, for results of too few tiles for the chip, joined by a second launch.
+// Forms: few rows (a weight's row goes from memory to a wave's registers once, waves share K); tiles through LDS, of 64 x 64 to 256 x 256;
+// tiles whose K is cut into parts, for results of too few tiles for the chip, joined by a second launch.
+//
+// What bounds them.  A K tile of 128 values costs a workgroup, from the slope over K: 256 x 256 1.12 us where its products alone take 0.85,
+// 256 x 128 0.75 and 0.43, 128 x 128 0.49 and 0.21: the smaller ones wait for LDS and for the barrier between two K tiles.
+// 4096 x 8192 x 8192: 213 us, 2.6 PFLOP/s, slower than that slope says (the library's own 8-bit product reaches 2.1 at 8192^3).
+// 256 x 25088 x 4096 in four parts: 41 us, 2.5 TB/s of its weights, and 7 for joining the parts; with pairs of K tiles fetched at once
+// and a ring half as deep it was slower.  16 x 4096 x 16384 by few rows: 14.5 us, 4.6 TB/s.
 #include <cstdint>
 #include "launch_util.h"
 #include "fc8_core.h"

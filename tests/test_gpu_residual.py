@@ -461,6 +461,11 @@ def test_weights8_tiled(tW, dt):
     run_weights8(72, 136, dt, tW, skew=1)
 
 
+def test_weights8_of_more_blocks_than_a_grid_has_rows():
+    """8 blocks of rows, each of 8194 tiles: 65552 together, a grid's second dimension ends at 65535"""
+    run_weights8(8, 64 * 8194, "bf16", "RRR")
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_weights8_at_the_borders_of_steps(dt):
     v = np.ascontiguousarray(border_values(150).T)
