@@ -7,7 +7,7 @@
 // tell how many stores lie between a load and its use it waits for all of them.  So lanes past a row's end load and store what
 // another lane does (no access depends on a lane), the first replica is stored outside of the loop over replicas, and what a call
 // has is a template argument: gradients of 16384 x 8192 bf16 over 8 shards, with dropout, 293 -> 246 us.
-// Figures: sum, dropout and norm of 16384 x 4096 bf16 102 to 106 us, 5.1 to 5.3 TB/s (an elementwise sum of two such tensors, three
+// Figures: sum, dropout and norm of 16384 x 4096 bf16 102 to 106 us (by the card), 5.1 to 5.3 TB/s (an elementwise sum of two such tensors, three
 // streams instead of four, 5.8); the gradients above 250 us, 5.4 TB/s; 8192 x 4096 fp32 100 and 124 us, 5.4 TB/s.
 #include <cstdint>
 #include "launch_util.h"
